@@ -67,10 +67,12 @@ typedef enum {
     FSD_ERR_WORKSPACE = -5, /* workspace NULL, misaligned or too small */
     FSD_ERR_MODE = -6,      /* mode is not an fsd_mode */
     FSD_ERR_LAUNCH = -7,    /* the HIP runtime refused a launch */
-    FSD_ERR_TOO_LARGE = -8  /* fsd_verify_chain_static: sizes beyond its fixed scratch buffer */
+    FSD_ERR_TOO_LARGE = -8, /* fsd_verify_chain_static: sizes beyond its fixed scratch buffer */
+    FSD_ERR_LAYOUT = -9     /* a stride, an alignment or an overlap that the call does not take */
 } fsd_status;
 
-typedef enum { FSD_F32 = 0, FSD_BF16 = 1 } fsd_dtype;
+/* (FSD_F16: queries, keys and values of fsd_attend_* and fsd_cache_append only; logits are FSD_F32 or FSD_BF16.) */
+typedef enum { FSD_F32 = 0, FSD_BF16 = 1, FSD_F16 = 2 } fsd_dtype;
 
 /* Divergence between the target distribution p and the draft distribution q
  * (paper App. C): KL is KL(p || q) (C.1), JS the Jensen-Shannon divergence
@@ -89,7 +91,8 @@ enum {
     FSD_ROW_BAD_PARENT = 2, /* tree: parent[j] outside [-1, j) */
     FSD_ROW_TOO_DEEP = 4,   /* tree: a node deeper than max_depth */
     FSD_ROW_BAD_TOKEN = 8,  /* strict SD: candidate token id outside [0, V) */
-    FSD_ROW_INTERNAL = 16   /* a bounded device-side wait expired (never expected) */
+    FSD_ROW_INTERNAL = 16,  /* a bounded device-side wait expired (never expected) */
+    FSD_ROW_BAD_CACHE = 32  /* cache calls: a length, block number, path node or position outside its range */
 };
 
 /* Limits: 1 <= V <= fsd_max_vocab(dtype) (524288 for both dtypes); 1 <= K, N,
@@ -294,6 +297,187 @@ int rfsd_verify_chain(const void* target_logits, const void* draft_logits, const
 size_t fsd_calibrate_workspace_bytes(int B, int K);
 int fsd_calibrate_threshold(const float* divergences, int B, int K, float target_fraction, float* T_out,
                             float* fraction_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Around a verify call: the operators that make its logits and that use its
+ * outputs.  A serving step is, per layer of the target model, fsd_attend_* over
+ * the candidates; then, on the logits, fsd_condition_*; then a verify call; then
+ * fsd_cache_append with the verify call's accept_len (path_len, path_nodes).
+ *
+ * These calls keep the conventions above (device pointers, asynchronous on
+ * hip_stream, argument errors before anything is launched, nothing allocated),
+ * and may be recorded into HIP graphs.  Their workgroups never wait for one
+ * another: they can share the GPU with any other work.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Penalties for repeated tokens, biases and a grammar's mask on the logits of
+ * a verify call.  Every row is conditioned on the tokens of its OWN context: the
+ * history, and the candidates on the way to it.  With z the logit of entry v,
+ *
+ *   seen(v)    v occurs in the history or on the way
+ *   count(v)   how often it occurs in the generated part of the history (from
+ *              prompt_len on) and on the way
+ *   z1 = z / r where seen(v) and z > 0, z * r where seen(v) and z <= 0, else z
+ *   z2 = z1 - frequency * count(v) - (count(v) > 0 ? presence : 0)
+ *   z3 = z2 + bias(v);  -inf where the mask does not allow v
+ *
+ * in binary32 in this order, rounded once to the logits' type; an entry that
+ * none of this touches keeps its bits.  A masked entry is -inf whatever it held
+ * (NaN as well); a mask that allows nothing leaves a row of -inf, which a verify
+ * call reports (FSD_ROW_NONFINITE).
+ *
+ * All members may be NULL / 0: what is missing does not apply.
+ */
+typedef struct {
+    const int32_t* history;      /* [B, history_stride] token ids, in order; ids outside [0, V) are passed over */
+    const int32_t* history_len;  /* [B] how many count (taken as within [0, history_stride]); NULL: all */
+    const int32_t* prompt_len;   /* [B] how many of them are the prompt; NULL: none */
+    int history_stride;
+    int bias_count;
+    const int32_t* bias_tokens;  /* [B, bias_count]; ids outside [0, V) are passed over; of equal ids the last counts */
+    const float* bias_values;    /* [B, bias_count] */
+    const float* repetition;     /* [B] r, > 0; NULL: 1 */
+    const float* presence;       /* [B] */
+    const float* frequency;      /* [B] */
+    const uint32_t* allowed;     /* [B, allowed_contexts, ceil(V / 32)] bit v % 32 of word v / 32: v is allowed */
+    int allowed_contexts;        /* 1: one mask a sequence; contexts of the call: one mask for each; 0 with allowed NULL */
+} fsd_conditions;
+
+/*
+ *   logits      [B, rows, V]  rows = K+1: the target rows of fsd_verify_chain; rows = K: its draft
+ *                             rows.  Row i stands behind candidates 0 .. i-1 (both kinds).
+ *   cand_tokens [B, K]        candidate token ids (0 <= K <= 2048; may be NULL when K is 0: a
+ *                             step without candidates); ids outside [0, V) are passed over
+ *   out         [B, rows, V]  out; may be logits itself (in place), else must not overlap it
+ * A mask per context has K+1 of them, also for draft rows: context i stands behind candidates 0 .. i-1.
+ */
+int fsd_condition_chain(const void* logits, const int32_t* cand_tokens, int B, int K, int rows, int V, int dtype,
+                        const fsd_conditions* conditions, void* out, void* hip_stream);
+
+/*
+ * The same for a token tree.  rows = N+1: the target rows of fsd_verify_tree (row 0: the root's
+ * context, row j+1: the context that ends with node j); rows = N: its draft rows (row j: the
+ * context of node j's parent).  A mask per context has N+1 of them, numbered like the target rows.
+ * A parent outside [-1, j) is taken as -1 (the verify call flags it).  1 <= N <= 2048.
+ */
+int fsd_condition_tree(const void* logits, const int32_t* node_tokens, const int32_t* parent, int B, int N, int rows,
+                       int V, int dtype, const fsd_conditions* conditions, void* out, void* hip_stream);
+
+/*
+ * A paged cache of keys and values in 8 bits (OCP e4m3), in blocks of
+ * FSD_CACHE_BLOCK tokens, with one scale for each block and head:
+ *
+ *   k_codes [layers, num_blocks, kv_heads, 64, head_dim]       a key of a token is head_dim bytes in a row
+ *   v_codes [layers, num_blocks, kv_heads, 4, head_dim, 16]    token t of a block: group t / 16, place t % 16
+ *   k_scale, v_scale [layers, num_blocks, kv_heads]            value = code * scale, scale > 0
+ *   block_table [B, max_blocks]   token t of sequence b is token t % 64 of block block_table[b][t / 64]
+ *   cache_len   [B]               tokens of sequence b in the cache
+ *
+ * (Values lie by groups of 16 tokens because the attention's matrix instruction takes them with
+ * the token index running fastest: 16 bytes of one head dimension are then one load, and a token that is
+ * appended still touches 2 KB at head_dim 128, not the whole block.)
+ * head_dim is 64, 128 or 256.  What lies behind a sequence's last token in its last block is never
+ * used: it may hold anything.  Blocks may be shared by sequences as long as nothing is appended to
+ * them.  Code and scale arrays start on 16-byte boundaries.
+ */
+#define FSD_CACHE_BLOCK 64
+typedef struct {
+    void* k_codes;
+    void* v_codes;
+    float* k_scale;
+    float* v_scale;
+    const int32_t* block_table;
+    const int32_t* cache_len;
+    int layers, num_blocks, kv_heads, head_dim, max_blocks;
+} fsd_cache;
+
+/*
+ * Rotation by position (of queries and keys): of the first `dim` elements of a head, pairs are turned by the
+ * angle of their position, the rest is left alone.  FSD_ROPE_HALVES pairs elements i and i + dim/2,
+ * FSD_ROPE_PAIRS 2i and 2i+1, i < dim/2:  a' = a cos - b sin,  b' = b cos + a sin  (binary32).
+ *
+ *   table [rows, dim] binary32, 16-byte aligned: row p holds the dim/2 cosines, then the dim/2 sines of
+ *         position p.  dim: a multiple of 16, at most head_dim.
+ */
+typedef enum { FSD_ROPE_HALVES = 0, FSD_ROPE_PAIRS = 1 } fsd_rope;
+typedef struct {
+    const float* table;
+    int rows, dim, style;
+} fsd_rotation;
+
+/*
+ * Appends keys and values to the cache: of every sequence row 0 (the token emitted last, whose key
+ * and value the cache does not hold yet) and the accepted candidates behind it.
+ *
+ *   k, v  [layers, B, R, kv_heads, head_dim]  rows as in fsd_attend_*: row 0, then row j+1 for
+ *         candidate (node) j; FSD_F32, FSD_BF16 or FSD_F16.  token_stride: elements from one token's
+ *         keys to the next one's (>= kv_heads * head_dim, a multiple of 8); sequences are R, layers B * R tokens apart.
+ *   accept_len [B]             as the verify calls give it (path_len): accept_len + 1 rows are
+ *                              appended; -1: none.  For a prompt of n tokens: n - 1.
+ *   path_nodes [B, max_depth]  as fsd_verify_tree gives them; NULL for a chain (rows 0 .. accept_len)
+ *   rotation                   of the keys, at positions cache_len, cache_len + 1, ...; NULL: none
+ *   cache_len_out [B]          out  optional: cache_len + accept_len + 1.  Not cache_len itself (other
+ *                              workgroups of the call still read that): copy it over afterwards.
+ *   row_status [B]             out  optional
+ *
+ * A block's scale is the smallest power of two s with |x| <= 448 s for every (finite) x appended to it, but
+ * at least 2^-100 and at least the scale the block has if it holds tokens of the sequence already: those are rounded again
+ * to the new scale if it is larger (exact but for codes that leave the normal range, as s is a power of two).
+ * Codes are the nearest e4m3 value of x / s, ties to even; a value that is not finite is held as NaN.
+ *
+ * Nothing of a sequence is appended, its cache_len_out is its cache_len and FSD_ROW_BAD_CACHE is
+ * set, if accept_len is outside [-1, R) (or over max_depth), a path node outside [0, R-1), cache_len or the new length
+ * outside [0, 64 * max_blocks], a block to be written outside [0, num_blocks) or a position outside the rotation's table.
+ * Two sequences that append to one block in one call race on it.
+ * R <= 2^20, B <= 65535, layers * B * kv_heads * blocks a sequence < 2^31.
+ */
+int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, int R, int dtype,
+                     const int32_t* accept_len, const int32_t* path_nodes, int max_depth,
+                     const fsd_rotation* rotation, const fsd_cache* cache, int32_t* cache_len_out,
+                     int32_t* row_status, void* hip_stream);
+
+/*
+ * Attention of a step's rows over the cache and over one another: what the target model does in the
+ * pass that verifies the candidates (or, with R = 1, in a step without candidates, or with a larger R on a piece of a
+ * prompt).  Row 0 is the token emitted last, row i+1 candidate i; none of them is in the cache yet.
+ * Row r sees all cache_len tokens of its sequence and, of the rows, 0 .. r.
+ *
+ *   q        [B, R, heads, head_dim]      FSD_BF16 or FSD_F16; heads a multiple of kv_heads: query head i
+ *                                         reads key head i / (heads / kv_heads)
+ *   k, v     [B, R, kv_heads, head_dim]   same type
+ *   q_stride, kv_stride                   elements from one token to the next (multiples of 8;
+ *                                         sequences are R tokens apart); q, k, v are 16-byte aligned
+ *   row_count [B]  optional: rows of the sequence (taken as within [0, R]); what lies behind them is neither read nor written
+ *   scale          of the products before the softmax (any finite number)
+ *   rotation       of q and k, at position cache_len + (number of rows before it that the row sees); NULL: none
+ *   layer          which of the cache's layers
+ *   out      [B, R, heads, head_dim] dense, out, 16-byte aligned
+ *   row_status [B] out optional: FSD_ROW_BAD_CACHE where cache_len is outside [0, 64 * max_blocks], a
+ *                  block outside [0, num_blocks), row_count outside [0, R] or a position outside the rotation's table (the call then
+ *                  takes the nearest length and position, and leaves such blocks out)
+ *   workspace      fsd_attend_workspace_bytes(...) bytes, 256-byte aligned
+ *
+ * Products of 16-bit operands are summed in binary32; the rotated queries and keys and the softmax's weights
+ * enter them with the 11 significant bits of binary16 (scaled so that they stay in its range), the codes exactly; statistics are
+ * binary32, the result is rounded once.  A NaN among the keys, values or codes a row sees makes its outputs NaN.
+ * 1 <= R <= 2049, 1 <= heads / kv_heads <= 64, heads <= 1024, B <= 65535, B * R < 2^24.
+ */
+size_t fsd_attend_workspace_bytes(int B, int R, int heads, int kv_heads, int head_dim);
+int fsd_attend_chain(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, int B, int R,
+                     int heads, int dtype, const int32_t* row_count, float scale, const fsd_rotation* rotation,
+                     const fsd_cache* cache, int layer, void* out, int32_t* row_status, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The same over a token tree: R = N+1 rows, row j+1 for node j, parent [B, N] as in fsd_verify_tree.
+ * Row j+1 sees the cache, row 0 and the rows of the nodes on the way to node j, itself included.  A parent outside
+ * [-1, j) is taken as -1 and flagged (FSD_ROW_BAD_PARENT).
+ */
+int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
+                    const int32_t* parent, int B, int R, int heads, int dtype, const int32_t* row_count, float scale,
+                    const fsd_rotation* rotation, const fsd_cache* cache, int layer, void* out, int32_t* row_status,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------------------
  * Everything below is for tests, tuning and benchmarks, not for serving code.

@@ -83,6 +83,19 @@ def library() -> ctypes.CDLL:
         L.fsd_calibrate_workspace_bytes.restype = sz
         L.fsd_calibrate_threshold.argtypes = [vp, i32, i32, f32, vp, vp, vp, sz, vp]
         L.fsd_calibrate_threshold.restype = i32
+        i64 = c.c_int64
+        L.fsd_condition_chain.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]
+        L.fsd_condition_chain.restype = i32
+        L.fsd_condition_tree.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp]
+        L.fsd_condition_tree.restype = i32
+        L.fsd_cache_append.argtypes = [vp, vp, i64, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp]
+        L.fsd_cache_append.restype = i32
+        L.fsd_attend_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.fsd_attend_workspace_bytes.restype = sz
+        L.fsd_attend_chain.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, i32, vp, f32, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.fsd_attend_chain.restype = i32
+        L.fsd_attend_tree.argtypes = [vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, vp, f32, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.fsd_attend_tree.restype = i32
         L.fsd_profile_enable.argtypes = [i32]
         L.fsd_profile_enable.restype = i32
         L.fsd_profile_collect.argtypes = [vp, vp]

@@ -4,10 +4,12 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "fsd_kernels.hip")
+SRC_OPERATORS = os.path.join(HERE, "csrc", "operators.hip")   # the operators around a verify call
 LIB = os.path.join(HERE, "libfsd.so")
 
 FLAGS = [
@@ -28,10 +30,22 @@ LIB_PHASE_TIMING = os.path.join(HERE, "libfsd_phase_timing.so")
 
 def build(verbose: bool = False, phase_timing: bool = False) -> str:
     lib = LIB_PHASE_TIMING if phase_timing else LIB
-    cmd = ["hipcc", *FLAGS, *(["-DFSD_PHASE_TIMING"] if phase_timing else []), "-o", lib, SRC]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    more = ["-DFSD_PHASE_TIMING"] if phase_timing else []
+    with tempfile.TemporaryDirectory() as tmp:
+        jobs, objects = [], []
+        for src in (SRC, SRC_OPERATORS):   # side by side
+            objects.append(os.path.join(tmp, os.path.basename(src) + ".o"))
+            cmd = ["hipcc", *(f for f in FLAGS if f != "-shared"), *more, "-c", "-o", objects[-1], src]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((subprocess.Popen(cmd), cmd))
+        failed = [subprocess.CalledProcessError(p.returncode, cmd) for p, cmd in jobs if p.wait() != 0]
+        if failed:
+            raise failed[0]
+        link = ["hipcc", *FLAGS, "-o", lib, *objects]
+        if verbose:
+            print(" ".join(link), flush=True)
+        subprocess.run(link, check=True)
     return lib
 
 

@@ -1035,6 +1035,7 @@ const char* fsd_status_string(int status) {
         case FSD_ERR_MODE: return "unknown sampling mode";
         case FSD_ERR_LAUNCH: return "kernel launch failed";
         case FSD_ERR_TOO_LARGE: return "sizes need more scratch memory than the static buffer holds (FSD_STATIC_SCRATCH_BYTES)";
+        case FSD_ERR_LAYOUT: return "a stride, an alignment or an overlap that the call does not take";
         default: return "unknown status";
     }
 }

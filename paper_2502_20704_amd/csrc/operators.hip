@@ -1,0 +1,274 @@
+// Host side and C ABI of the operators around a verify call: conditioning of logits (condition.h), the 8-bit paged
+// cache's append (cache_append.h) and the attention that reads it (cache_attend.h).  Kernels for gfx950 (MI355X).
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <limits.h>
+#include <cmath>
+
+#include "fsd.h"
+
+#include "operators_common.h"
+#include "condition.h"
+#include "cache_append.h"
+#include "cache_attend.h"
+
+namespace {
+
+constexpr int kMaxRows = 2048;    // K or N, as in the verify calls
+constexpr int kMaxBatch = 65535;
+
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+inline int launched() { return hipGetLastError() == hipSuccess ? FSD_OK : FSD_ERR_LAUNCH; }
+
+// ------------------------------------------------------------------------------------------ conditioning
+
+constexpr long kConditionWGs = 1024;   // workgroups aimed at: 4 a compute unit
+
+int condition(const void* logits, const int32_t* tokens, const int32_t* parent, int B, int N, int rows, int V, int dtype,
+              const fsd_conditions* conditions, void* out, bool tree, hipStream_t st) {
+    if (!logits || !out || !conditions || (N > 0 && !tokens) || (tree && !parent)) return FSD_ERR_NULL;
+    if (dtype != FSD_F32 && dtype != FSD_BF16) return FSD_ERR_DTYPE;
+    if (B < 1 || B > kMaxBatch || N < (tree ? 1 : 0) || N > kMaxRows || rows < 1 || (rows != N && rows != N + 1) || V < 1 ||
+        V > fsd_max_vocab(dtype) || static_cast<long>(B) * rows >= (1L << 24))
+        return FSD_ERR_SHAPE;
+    const fsd_conditions& c = *conditions;
+    if (c.history_stride < 0 || c.bias_count < 0) return FSD_ERR_SHAPE;
+    if (c.bias_count > 0 && (!c.bias_tokens || !c.bias_values)) return FSD_ERR_NULL;
+    if (c.allowed && c.allowed_contexts != 1 && c.allowed_contexts != N + 1) return FSD_ERR_SHAPE;
+    const size_t es = dtype == FSD_BF16 ? 2 : 4;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) % es != 0) return FSD_ERR_LAYOUT;
+    ConditionParams P;
+    P.logits = static_cast<const char*>(logits);
+    P.out = static_cast<char*>(out);
+    P.tokens = tokens;
+    P.parent = parent;
+    P.c = c;
+    if (c.history_stride == 0) P.c.history = nullptr;
+    P.B = B; P.N = N; P.rows = rows; P.V = V;
+    P.target = rows == N + 1;
+    // A workgroup's slice: the fewer, the fewer times a history is read; but a call of few rows wants workgroups on all compute units.
+    P.slice = 4096;
+    while (P.slice > 1024 && static_cast<long>(B) * rows * ((V + P.slice - 1) / P.slice) < kConditionWGs) P.slice /= 2;
+    P.nslices = (V + P.slice - 1) / P.slice;
+    const long pieces = static_cast<long>(B) * P.nslices;
+    long per = pieces * rows / kConditionWGs;
+    if (per < 1) per = 1;
+    if (per > rows) per = rows;
+    P.ngroups = static_cast<int>((rows + per - 1) / per);
+    P.rows_per_wg = (rows + P.ngroups - 1) / P.ngroups;
+    P.ngroups = (rows + P.rows_per_wg - 1) / P.rows_per_wg;
+    P.nwork = pieces * P.ngroups;
+    const long grid = grid_over_xcds(P.nwork);
+    if (grid > INT_MAX) return FSD_ERR_SHAPE;
+    size_t lds = static_cast<size_t>(P.slice) * 4 * (c.bias_count ? 2 : 1) + P.slice / 8;
+    if (tree) lds += (static_cast<size_t>(P.rows_per_wg) / 32 + 1) * 4 + static_cast<size_t>(N) * 4;
+    const dim3 g(static_cast<unsigned>(grid)), t(kWG);
+    if (dtype == FSD_BF16) {
+        if (tree) hipLaunchKernelGGL((condition_rows<true, true>), g, t, lds, st, P);
+        else hipLaunchKernelGGL((condition_rows<true, false>), g, t, lds, st, P);
+    } else {
+        if (tree) hipLaunchKernelGGL((condition_rows<false, true>), g, t, lds, st, P);
+        else hipLaunchKernelGGL((condition_rows<false, false>), g, t, lds, st, P);
+    }
+    return launched();
+}
+
+// ------------------------------------------------------------------------------------------ the cache
+
+int check_cache(const fsd_cache* c) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->block_table || !c->cache_len) return FSD_ERR_NULL;
+    if (c->layers < 1 || c->num_blocks < 1 || c->kv_heads < 1 || c->kv_heads > 1024 || c->max_blocks < 1 ||
+        c->max_blocks > INT_MAX / kBlock - 1 || (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256))
+        return FSD_ERR_SHAPE;
+    if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || reinterpret_cast<uintptr_t>(c->k_scale) % 4 != 0 ||
+        reinterpret_cast<uintptr_t>(c->v_scale) % 4 != 0)
+        return FSD_ERR_LAYOUT;
+    return FSD_OK;
+}
+// the rotation to hand to a kernel: none where there is no table
+int check_rotation(const fsd_rotation* r, int head_dim, fsd_rotation* out) {
+    *out = fsd_rotation{nullptr, 0, 0, FSD_ROPE_HALVES};
+    if (!r || !r->table) return FSD_OK;
+    if (r->rows < 1 || r->dim < 16 || r->dim % 16 != 0 || r->dim > head_dim) return FSD_ERR_SHAPE;
+    if (r->style != FSD_ROPE_HALVES && r->style != FSD_ROPE_PAIRS) return FSD_ERR_MODE;
+    if (!aligned16(r->table)) return FSD_ERR_LAYOUT;
+    *out = *r;
+    return FSD_OK;
+}
+
+template <int DT, int D>
+void launch_append(hipStream_t st, const AppendParams& P, bool few) {
+    if (few) hipLaunchKernelGGL((append_rows<DT, D, 64>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
+    else hipLaunchKernelGGL((append_rows<DT, D, kWG>), dim3(P.npieces), dim3(kWG), 0, st, P);
+}
+template <int DT>
+void launch_append_d(hipStream_t st, const AppendParams& P, bool few) {
+    if (P.cache.head_dim == 64) launch_append<DT, 64>(st, P, few);
+    else if (P.cache.head_dim == 128) launch_append<DT, 128>(st, P, few);
+    else launch_append<DT, 256>(st, P, few);
+}
+
+// ------------------------------------------------------------------------------------------ attention
+
+// How many of a key head's rows (tokens times query heads of its group) a piece takes, and how its wavefronts share them:
+// up to 64 (32 at head_dim 256) all four take the same rows and every fourth block; beyond that each takes rows of its own.
+struct AttendShape { int rt, tile, target; bool by_keys; };
+AttendShape attend_shape(long rows, int head_dim) {
+    AttendShape s;
+    const int most = head_dim == 256 ? 2 : 4;
+    const long tiles = (rows + 15) / 16;
+    s.by_keys = tiles <= most;
+    if (s.by_keys) {
+        s.rt = static_cast<int>(tiles);
+        s.tile = 16 * s.rt;
+        s.target = 512;
+    } else {
+        s.rt = tiles <= 2 * most ? most / 2 : most;
+        s.tile = 64 * s.rt;
+        s.target = 512;
+    }
+    return s;
+}
+bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
+    return B >= 1 && B <= kMaxBatch && R >= 1 && R <= kMaxRows + 1 && static_cast<long>(B) * R < (1L << 24) && kv_heads >= 1 && heads >= kv_heads &&
+           heads <= 1024 && heads % kv_heads == 0 && heads / kv_heads <= 64 && (head_dim == 64 || head_dim == 128 || head_dim == 256);
+}
+size_t attend_bytes(const AttendShape& s, int head_dim) {
+    return (2 * static_cast<size_t>(s.target) * s.tile * (head_dim + 2) * 4 + 255) / 256 * 256;
+}
+
+template <int D, int RT, bool BYKEYS>
+void launch_attend_k(hipStream_t st, const AttendParams& P, unsigned grid, size_t lds) {
+    hipLaunchKernelGGL((attend_rows<D, RT, BYKEYS>), dim3(grid), dim3(kWG), lds, st, P);
+}
+template <int D>
+void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned grid, size_t lds) {
+    constexpr int kMost = D == 256 ? 2 : 4;
+    if (s.by_keys) {
+        if (s.rt == 1) launch_attend_k<D, 1, true>(st, P, grid, lds);
+        else if (s.rt == 2) launch_attend_k<D, 2, true>(st, P, grid, lds);
+        if constexpr (kMost == 4) {
+            if (s.rt == 3) launch_attend_k<D, 3, true>(st, P, grid, lds);
+            else if (s.rt == 4) launch_attend_k<D, 4, true>(st, P, grid, lds);
+        }
+    } else if (s.rt == kMost) {
+        launch_attend_k<D, kMost, false>(st, P, grid, lds);
+    } else {
+        launch_attend_k<D, kMost / 2, false>(st, P, grid, lds);
+    }
+    const int per_sequence = static_cast<int>((static_cast<long>(P.R) * P.heads + 3) / 4);
+    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * per_sequence), dim3(kWG), 0, st, P, per_sequence);
+}
+
+int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, const int32_t* parent, bool tree, int B, int R,
+           int heads, int dtype, const int32_t* row_count, float scale, const fsd_rotation* rotation, const fsd_cache* cache, int layer,
+           void* out, int32_t* row_status, void* workspace, size_t workspace_bytes, hipStream_t st) {
+    if (!q || !k || !v || !out || (tree && !parent && R > 1)) return FSD_ERR_NULL;
+    AttendParams P;
+    int bad = check_cache(cache);
+    if (bad == FSD_OK) bad = check_rotation(rotation, cache->head_dim, &P.rot);
+    if (bad != FSD_OK) return bad;
+    if (dtype != FSD_BF16 && dtype != FSD_F16) return FSD_ERR_DTYPE;
+    const int H = cache->kv_heads, D = cache->head_dim;
+    if (!attend_sizes(B, R, heads, H, D) || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return FSD_ERR_SHAPE;
+    if (q_stride < static_cast<int64_t>(heads) * D || kv_stride < static_cast<int64_t>(H) * D || q_stride % 8 != 0 || kv_stride % 8 != 0 ||
+        q_stride > (1L << 32) || kv_stride > (1L << 32) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+        return FSD_ERR_LAYOUT;
+    const AttendShape s = attend_shape(static_cast<long>(R) * (heads / H), D);
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < attend_bytes(s, D)) return FSD_ERR_WORKSPACE;
+    P.q = q; P.k = k; P.v = v;
+    P.q_stride = q_stride; P.kv_stride = kv_stride;
+    P.parent = tree && R > 1 ? parent : nullptr;
+    P.row_count = row_count;
+    P.B = B; P.R = R; P.heads = heads; P.G = heads / H;
+    P.dtype = dtype;
+    P.scale = scale * kLog2eF;
+    P.cache = *cache;
+    P.layer = layer;
+    P.out = out;
+    P.status = row_status;
+    P.part = static_cast<float*>(workspace);
+    P.target = s.target;
+    P.least = s.by_keys ? 4 : 1;
+    P.tile = s.tile;
+    const long groups = (static_cast<long>(R) * P.G + s.tile - 1) / s.tile;
+    const long grid = grid_over_xcds(s.target + static_cast<long>(B) * H * groups);
+    if (grid > INT_MAX || static_cast<long>(B) * ((static_cast<long>(R) * heads + 3) / 4) > INT_MAX) return FSD_ERR_SHAPE;
+    const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
+    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(grid), lds);
+    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(grid), lds);
+    else launch_attend<256>(st, P, s, static_cast<unsigned>(grid), lds);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int fsd_condition_chain(const void* logits, const int32_t* cand_tokens, int B, int K, int rows, int V, int dtype,
+                        const fsd_conditions* conditions, void* out, void* hip_stream) {
+    return condition(logits, cand_tokens, nullptr, B, K, rows, V, dtype, conditions, out, false, static_cast<hipStream_t>(hip_stream));
+}
+
+int fsd_condition_tree(const void* logits, const int32_t* node_tokens, const int32_t* parent, int B, int N, int rows, int V, int dtype,
+                       const fsd_conditions* conditions, void* out, void* hip_stream) {
+    return condition(logits, node_tokens, parent, B, N, rows, V, dtype, conditions, out, true, static_cast<hipStream_t>(hip_stream));
+}
+
+int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, int R, int dtype, const int32_t* accept_len,
+                     const int32_t* path_nodes, int max_depth, const fsd_rotation* rotation, const fsd_cache* cache,
+                     int32_t* cache_len_out, int32_t* row_status, void* hip_stream) {
+    if (!k || !v || !accept_len) return FSD_ERR_NULL;
+    AppendParams P;
+    int bad = check_cache(cache);
+    if (bad == FSD_OK) bad = check_rotation(rotation, cache->head_dim, &P.rot);
+    if (bad != FSD_OK) return bad;
+    if (dtype != FSD_F32 && dtype != FSD_BF16 && dtype != FSD_F16) return FSD_ERR_DTYPE;
+    const int H = cache->kv_heads;
+    if (B < 1 || B > kMaxBatch || R < 1 || R > (1 << 20) || (path_nodes && (max_depth < 1 || max_depth > kMaxRows))) return FSD_ERR_SHAPE;
+    if (token_stride < static_cast<int64_t>(H) * cache->head_dim || token_stride % 8 != 0 || token_stride > (1L << 32) || !aligned16(k) ||
+        !aligned16(v) || cache_len_out == cache->cache_len)
+        return FSD_ERR_LAYOUT;
+    P.k = static_cast<const char*>(k);
+    P.v = static_cast<const char*>(v);
+    P.stride = token_stride;
+    P.B = B; P.R = R; P.max_depth = max_depth;
+    P.max_rows = path_nodes && max_depth + 1 < R ? max_depth + 1 : R;
+    P.accept_len = accept_len;
+    P.path = path_nodes;
+    P.cache = *cache;
+    P.len_out = cache_len_out;
+    P.status = row_status;
+    P.slots = (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
+    const long pieces = static_cast<long>(cache->layers) * B * H * P.slots;
+    if (pieces > INT_MAX - 8) return FSD_ERR_SHAPE;
+    P.npieces = static_cast<unsigned>(pieces);
+    const bool few = P.max_rows <= 16;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, few);
+    else if (dtype == FSD_BF16) launch_append_d<FSD_BF16>(st, P, few);
+    else launch_append_d<FSD_F16>(st, P, few);
+    return launched();
+}
+
+size_t fsd_attend_workspace_bytes(int B, int R, int heads, int kv_heads, int head_dim) {
+    if (!attend_sizes(B, R, heads, kv_heads, head_dim)) return 0;
+    return attend_bytes(attend_shape(static_cast<long>(R) * (heads / kv_heads), head_dim), head_dim);
+}
+
+int fsd_attend_chain(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, int B, int R, int heads, int dtype,
+                     const int32_t* row_count, float scale, const fsd_rotation* rotation, const fsd_cache* cache, int layer, void* out,
+                     int32_t* row_status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return attend(q, k, v, q_stride, kv_stride, nullptr, false, B, R, heads, dtype, row_count, scale, rotation, cache, layer, out, row_status,
+                  workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, const int32_t* parent, int B, int R,
+                    int heads, int dtype, const int32_t* row_count, float scale, const fsd_rotation* rotation, const fsd_cache* cache, int layer,
+                    void* out, int32_t* row_status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return attend(q, k, v, q_stride, kv_stride, parent, true, B, R, heads, dtype, row_count, scale, rotation, cache, layer, out, row_status,
+                  workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"

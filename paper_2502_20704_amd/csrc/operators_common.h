@@ -1,0 +1,171 @@
+// Device helpers of the operators around a verify call (condition.h, cache_append.h, cache_attend.h).
+// Part of libfsd (gfx950).
+#ifndef FSD_CSRC_OPERATORS_COMMON_H_
+#define FSD_CSRC_OPERATORS_COMMON_H_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fsd.h"
+
+namespace {
+
+constexpr int kWG = 256;          // threads per workgroup (4 wavefronts of 64)
+constexpr int kBlock = FSD_CACHE_BLOCK;
+constexpr int kXcds = 8;
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+
+// Workgroups are dealt to the 8 XCDs, each with an L2 of its own, in turn.  This gives an XCD a run of consecutive pieces
+// of work instead, so that those that read the same thing (a sequence's history, a head's cache blocks) meet in one L2.
+// -1: nothing left for this workgroup (the grid has 8 * ceil(n / 8) of them).
+__device__ __forceinline__ long spread_over_xcds(long block, long n) {
+    const long per = (n + kXcds - 1) / kXcds, at = block % kXcds * per + block / kXcds;
+    return block / kXcds < per && at < n ? at : -1;
+}
+inline long grid_over_xcds(long n) { return (n + kXcds - 1) / kXcds * kXcds; }
+
+// ---- logits, in 16-byte slots at any address of whole elements
+
+__device__ __forceinline__ uint4 load_any16(const char* p) {
+    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void store_any16(char* p, const uint4& w) {
+    u32x4_any v;
+    v.x = w.x; v.y = w.y; v.z = w.z; v.w = w.w;
+    *reinterpret_cast<u32x4_any*>(p) = v;
+}
+template <bool BF16>
+__device__ __forceinline__ uint4 neg_inf_slot() {
+    const unsigned w = BF16 ? 0xFF80FF80u : 0xFF800000u;
+    return make_uint4(w, w, w, w);
+}
+__device__ __forceinline__ unsigned bf16_bits(float z) {
+    return static_cast<unsigned>(__builtin_bit_cast(unsigned short, static_cast<__bf16>(z)));   // to nearest, ties to even
+}
+template <bool BF16>
+__device__ __forceinline__ void unpack_slot(const uint4& r, float* x) {
+    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        } else {
+            x[i] = __uint_as_float(w[i]);
+        }
+    }
+}
+// the slot with z in the entries of `changed`, -inf in those that `ok` lacks, and the raw bits elsewhere
+template <bool BF16>
+__device__ __forceinline__ uint4 repack_slot(const uint4& raw, const float* z, unsigned changed, unsigned ok) {
+    unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+            unsigned lo = w[i] & 0xFFFFu, hi = w[i] >> 16;
+            if (changed >> (2 * i) & 1u) lo = bf16_bits(z[2 * i]);
+            if (changed >> (2 * i + 1) & 1u) hi = bf16_bits(z[2 * i + 1]);
+            if (!(ok >> (2 * i) & 1u)) lo = 0xFF80u;
+            if (!(ok >> (2 * i + 1) & 1u)) hi = 0xFF80u;
+            w[i] = lo | hi << 16;
+        } else {
+            if (changed >> i & 1u) w[i] = __float_as_uint(z[i]);
+            if (!(ok >> i & 1u)) w[i] = 0xFF800000u;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool BF16>
+__device__ __forceinline__ float load_logit(const char* row, int e) {
+    if constexpr (BF16) return __uint_as_float(static_cast<unsigned>(reinterpret_cast<const unsigned short*>(row)[e]) << 16);
+    else return reinterpret_cast<const float*>(row)[e];
+}
+template <bool BF16>
+__device__ __forceinline__ void store_logit(char* row, int e, float z) {
+    if constexpr (BF16) reinterpret_cast<unsigned short*>(row)[e] = static_cast<unsigned short>(bf16_bits(z));
+    else reinterpret_cast<float*>(row)[e] = z;
+}
+template <bool BF16>
+__device__ __forceinline__ void copy_logit(char* out, const char* in, int e) {
+    if constexpr (BF16) reinterpret_cast<unsigned short*>(out)[e] = reinterpret_cast<const unsigned short*>(in)[e];
+    else reinterpret_cast<unsigned*>(out)[e] = reinterpret_cast<const unsigned*>(in)[e];
+}
+
+// ---- keys, values and queries: 8 elements in a row
+
+template <int DT>
+__device__ __forceinline__ void load8(const void* base, size_t at, float* x) {
+    if constexpr (DT == FSD_F32) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(base) + at);
+        const u32x4 a = p[0], c = p[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __uint_as_float(a[i]);
+            x[4 + i] = __uint_as_float(c[i]);
+        }
+    } else {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(base) + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned w = a[i];                          // (a bit cast of the vector's element itself takes element 0)
+            if constexpr (DT == FSD_BF16) {
+                x[2 * i] = __uint_as_float(w << 16);
+                x[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+            } else {
+                const half2_t h = __builtin_bit_cast(half2_t, w);
+                x[2 * i] = static_cast<float>(h.x);
+                x[2 * i + 1] = static_cast<float>(h.y);
+            }
+        }
+    }
+}
+
+// elements d .. d+7 (d a multiple of 8) of a head at `at`, rotated by the table's row `pos`
+template <int DT>
+__device__ __forceinline__ void load8_turned(const void* base, size_t at, int d, const fsd_rotation& rot, int pos, float* x) {
+    load8<DT>(base, at + d, x);
+    if (rot.table == nullptr || d >= rot.dim) return;
+    const float* t = rot.table + static_cast<size_t>(pos) * rot.dim;
+    const int n = rot.dim / 2;
+    if (rot.style == FSD_ROPE_HALVES) {
+        const bool low = d < n;
+        const int i = low ? d : d - n;                       // of the pair
+        float y[8], c[8], s[8];
+        load8<DT>(base, at + (low ? d + n : d - n), y);
+        load8<FSD_F32>(t, i, c);
+        load8<FSD_F32>(t, n + i, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = low ? x[e] * c[e] - y[e] * s[e] : x[e] * c[e] + y[e] * s[e];
+    } else {
+        const u32x4 c = *reinterpret_cast<const u32x4*>(t + d / 2), s = *reinterpret_cast<const u32x4*>(t + n + d / 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float cc = __uint_as_float(c[e]), ss = __uint_as_float(s[e]), a = x[2 * e], b = x[2 * e + 1];
+            x[2 * e] = a * cc - b * ss;
+            x[2 * e + 1] = b * cc + a * ss;
+        }
+    }
+}
+
+// |x|, or 0 where x is not finite
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = __builtin_fabsf(x);
+    return a < __builtin_inff() ? a : 0.0f;
+}
+__device__ __forceinline__ float wave_max_all(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = __builtin_fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+// 2^e as a number, -126 <= e <= 127
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<unsigned>(e + 127) << 23); }
+
+}  // namespace
+
+#endif  // FSD_CSRC_OPERATORS_COMMON_H_
