@@ -121,20 +121,24 @@ __global__ __launch_bounds__(kWG) void append_rows(AppendParams P) {
         }
         return m;
     };
-    auto load = [&](const char* base, bool turn) {
+    size_t head[kSlots];
+    int dim[kSlots], pos[kSlots];
+    bool there[kSlots];
 #pragma unroll
-        for (int i = 0; i < kSlots; ++i) {
-            const int u = lane + i * LANES, t = u / kPer, d = u % kPer * 8;
+    for (int i = 0; i < kSlots; ++i) {
+        const int u = lane + i * LANES, t = u / kPer;
+        there[i] = t < n;
+        const long i0 = from - len + (there[i] ? t : 0);      // which of the accepted rows (the first one where there is none)
+        const long row = path == nullptr || i0 == 0 ? i0 : path[i0 - 1] + 1;
+        head[i] = (static_cast<size_t>(static_cast<long>(layer) * P.B + b) * P.R + row) * P.stride + static_cast<size_t>(h) * D;
+        dim[i] = u % kPer * 8;
+        pos[i] = static_cast<int>(len + i0);
+    }
+    auto blank = [&]() {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
-            if (t < n) {
-                const long i0 = from - len + t;               // which of the accepted rows
-                const long row = path == nullptr || i0 == 0 ? i0 : path[i0 - 1] + 1;
-                const size_t where = (static_cast<size_t>(static_cast<long>(layer) * P.B + b) * P.R + row) * P.stride + static_cast<size_t>(h) * D;
-                if (turn) load8_turned<DT>(base, where, d, P.rot, static_cast<int>(from + t), x[i]);
-                else load8<DT>(base, where + d, x[i]);
-            }
-        }
+        for (int i = 0; i < kSlots; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = there[i] ? x[i][e] : 0.0f;
     };
     // the scale in force, and what the old codes are multiplied by
     auto scale_of = [&](float* scale, float most, float& ratio) {
@@ -148,7 +152,8 @@ __global__ __launch_bounds__(kWG) void append_rows(AppendParams P) {
         return s;
     };
     // ---- keys
-    load(P.k, true);
+    load_turned<kSlots>(DT, P.k, head, dim, P.rot, pos, x);
+    blank();
     {
         float ratio;
         const float s = scale_of(P.cache.k_scale, largest(), ratio), inv = 1.0f / s;
@@ -167,7 +172,9 @@ __global__ __launch_bounds__(kWG) void append_rows(AppendParams P) {
             }
         }
         // (every lane has read the old scale: the barriers or the shuffles of `largest` of the values stand between)
-        load(P.v, false);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) load8<DT>(P.v, head[i] + dim[i], x[i]);
+        blank();
         const float most = largest();
         if (lane == 0) P.cache.k_scale[at] = s;
         float vratio;

@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <limits.h>
 #include <cmath>
+#include <type_traits>
 
 #include "fsd.h"
 
@@ -111,54 +112,91 @@ void launch_append_d(hipStream_t st, const AppendParams& P, bool few) {
 
 // ------------------------------------------------------------------------------------------ attention
 
-// How many of a key head's rows (tokens times query heads of its group) a piece takes, and how its wavefronts share them:
-// up to 64 (32 at head_dim 256) all four take the same rows and every fourth block; beyond that each takes rows of its own.
-struct AttendShape { int rt, tile, target; bool by_keys; };
-AttendShape attend_shape(long rows, int head_dim) {
+// How many of a key head's rows (tokens times query heads of its group) an item takes, and how its wavefronts share them: up to 48
+// (binary16: 32; 16 at head_dim 256) four wavefronts take the same rows and every fourth block; beyond that each takes rows of its own.
+struct AttendShape { int rt, waves, tile, workers; bool by_keys; };
+AttendShape attend_shape(long rows, int head_dim, int dtype) {
     AttendShape s;
-    const int most = head_dim == 256 ? 2 : 4;
     const long tiles = (rows + 15) / 16;
-    s.by_keys = tiles <= most;
+    s.by_keys = tiles <= (head_dim == 256 ? 1 : dtype == FSD_F16 ? 2 : 3);
     if (s.by_keys) {
         s.rt = static_cast<int>(tiles);
-        s.tile = 16 * s.rt;
-        s.target = 512;
+        s.waves = 4;
+    } else if (head_dim == 256) {
+        s.rt = 1;
+        s.waves = tiles <= 4 ? 4 : 8;
     } else {
-        s.rt = tiles <= 2 * most ? most / 2 : most;
-        s.tile = 64 * s.rt;
-        s.target = 512;
+        s.rt = tiles <= 4 ? 1 : 2;
+        s.waves = tiles <= 8 ? 4 : 8;
     }
+    s.tile = 16 * s.rt * (s.by_keys ? 1 : s.waves);
+    // as many workgroups as the 256 compute units hold at once
+    s.workers = s.by_keys ? (head_dim == 256 ? 256 : 512) : s.waves == 4 ? 512 : 256;
     return s;
 }
 bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
     return B >= 1 && B <= kMaxBatch && R >= 1 && R <= kMaxRows + 1 && static_cast<long>(B) * R < (1L << 24) && kv_heads >= 1 && heads >= kv_heads &&
            heads <= 1024 && heads % kv_heads == 0 && heads / kv_heads <= 64 && (head_dim == 64 || head_dim == 128 || head_dim == 256);
 }
-size_t attend_bytes(const AttendShape& s, int head_dim) {
-    return (2 * static_cast<size_t>(s.target) * s.tile * (head_dim + 2) * 4 + 255) / 256 * 256;
+// Places of the workspace's parts (attend_prepare says what they hold), and its size.
+struct AttendSpace {
+    int row_tiles, tiles;
+    size_t pieces, factor, key_scale, value_scale, broken, sees, q16, k16, v16, part, bytes;
+};
+AttendSpace attend_space(const AttendShape& s, int B, int R, int heads, int H, int D, bool fine) {
+    AttendSpace w;
+    const long rows = static_cast<long>(R) * (heads / H), groups = (rows + s.tile - 1) / s.tile;
+    w.row_tiles = static_cast<int>(groups * s.tile / 16);
+    w.tiles = (R + kBlock - 1) / kBlock;
+    const size_t bh = static_cast<size_t>(B) * H, bht = bh * w.tiles, parts = fine ? 2 : 1;
+    size_t o = 0;
+    auto take = [&o](size_t n) {
+        const size_t at = o;
+        o = (o + n + 255) / 256 * 256;
+        return at;
+    };
+    take((static_cast<size_t>(B) + 2) * 8);                   // the plan
+    w.pieces = take(bh * groups * 8);
+    w.factor = take(bh * w.row_tiles * 64);
+    w.key_scale = take(bht * kBlock * 4);
+    w.value_scale = take(bht * 4);
+    w.broken = take(bht * 8);
+    w.sees = take(static_cast<size_t>(B) * R * w.tiles * 8);
+    w.q16 = take(bh * w.row_tiles * 32 * D * parts);
+    w.k16 = take(bht * kBlock * 2 * D * parts);
+    w.v16 = take(bht * kBlock * 2 * D);
+    w.part = take(2 * static_cast<size_t>(s.workers) * s.tile * (D + 2) * 4);
+    w.bytes = o;
+    return w;
 }
 
-template <int D, int RT, bool BYKEYS>
-void launch_attend_k(hipStream_t st, const AttendParams& P, unsigned grid, size_t lds) {
-    hipLaunchKernelGGL((attend_rows<D, RT, BYKEYS>), dim3(grid), dim3(kWG), lds, st, P);
+template <int D, int RT, int NW, bool BYKEYS>
+void launch_attend_k(hipStream_t st, const AttendParams& P) {
+    const dim3 grid(static_cast<unsigned>(grid_over_xcds(P.workers)));
+    if constexpr (BYKEYS && RT == 3) {
+        hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, false>), grid, dim3(NW * 64), 0, st, P);
+    } else if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, true>), grid, dim3(NW * 64), 0, st, P);
+    else hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, false>), grid, dim3(NW * 64), 0, st, P);
 }
 template <int D>
-void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned grid, size_t lds) {
-    constexpr int kMost = D == 256 ? 2 : 4;
+void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, int joins) {
+    hipLaunchKernelGGL((attend_prepare<D>), dim3(prepare), dim3(kWG), lds, st, P);
     if (s.by_keys) {
-        if (s.rt == 1) launch_attend_k<D, 1, true>(st, P, grid, lds);
-        else if (s.rt == 2) launch_attend_k<D, 2, true>(st, P, grid, lds);
-        if constexpr (kMost == 4) {
-            if (s.rt == 3) launch_attend_k<D, 3, true>(st, P, grid, lds);
-            else if (s.rt == 4) launch_attend_k<D, 4, true>(st, P, grid, lds);
+        if (s.rt == 1) launch_attend_k<D, 1, 4, true>(st, P);
+        if constexpr (D != 256) {
+            if (s.rt == 2) launch_attend_k<D, 2, 4, true>(st, P);
+            else if (s.rt == 3) launch_attend_k<D, 3, 4, true>(st, P);
         }
-    } else if (s.rt == kMost) {
-        launch_attend_k<D, kMost, false>(st, P, grid, lds);
-    } else {
-        launch_attend_k<D, kMost / 2, false>(st, P, grid, lds);
+    } else if (s.rt == 1) {
+        if (s.waves == 4) launch_attend_k<D, 1, 4, false>(st, P);
+        if constexpr (D == 256) {
+            if (s.waves == 8) launch_attend_k<D, 1, 8, false>(st, P);
+        }
+    } else if constexpr (D != 256) {
+        if (s.waves == 4) launch_attend_k<D, 2, 4, false>(st, P);
+        else launch_attend_k<D, 2, 8, false>(st, P);
     }
-    const int per_sequence = static_cast<int>((static_cast<long>(P.R) * P.heads + 3) / 4);
-    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * per_sequence), dim3(kWG), 0, st, P, per_sequence);
+    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * joins), dim3(kWG), 0, st, P, joins);
 }
 
 int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, const int32_t* parent, bool tree, int B, int R,
@@ -175,8 +213,9 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     if (q_stride < static_cast<int64_t>(heads) * D || kv_stride < static_cast<int64_t>(H) * D || q_stride % 8 != 0 || kv_stride % 8 != 0 ||
         q_stride > (1L << 32) || kv_stride > (1L << 32) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return FSD_ERR_LAYOUT;
-    const AttendShape s = attend_shape(static_cast<long>(R) * (heads / H), D);
-    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < attend_bytes(s, D)) return FSD_ERR_WORKSPACE;
+    const AttendShape s = attend_shape(static_cast<long>(R) * (heads / H), D, dtype);
+    const AttendSpace w = attend_space(s, B, R, heads, H, D, dtype == FSD_F16);
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < w.bytes) return FSD_ERR_WORKSPACE;
     P.q = q; P.k = k; P.v = v;
     P.q_stride = q_stride; P.kv_stride = kv_stride;
     P.parent = tree && R > 1 ? parent : nullptr;
@@ -188,17 +227,32 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.layer = layer;
     P.out = out;
     P.status = row_status;
-    P.part = static_cast<float*>(workspace);
-    P.target = s.target;
+    char* base = static_cast<char*>(workspace);
+    P.plan = reinterpret_cast<long*>(base);
+    P.pieces = reinterpret_cast<int2*>(base + w.pieces);
+    P.factor = reinterpret_cast<float*>(base + w.factor);
+    P.key_scale = reinterpret_cast<float*>(base + w.key_scale);
+    P.value_scale = reinterpret_cast<float*>(base + w.value_scale);
+    P.broken = reinterpret_cast<unsigned long long*>(base + w.broken);
+    P.sees = reinterpret_cast<unsigned long long*>(base + w.sees);
+    P.q16 = base + w.q16;
+    P.k16 = base + w.k16;
+    P.v16 = base + w.v16;
+    P.part = reinterpret_cast<float*>(base + w.part);
+    P.workers = s.workers;
     P.least = s.by_keys ? 4 : 1;
     P.tile = s.tile;
-    const long groups = (static_cast<long>(R) * P.G + s.tile - 1) / s.tile;
-    const long grid = grid_over_xcds(s.target + static_cast<long>(B) * H * groups);
-    if (grid > INT_MAX || static_cast<long>(B) * ((static_cast<long>(R) * heads + 3) / 4) > INT_MAX) return FSD_ERR_SHAPE;
+    P.row_tiles = w.row_tiles;
+    P.tiles = w.tiles;
+    // two slots of 8 elements a thread of attend_prepare
+    P.query_groups = static_cast<int>((static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG));
+    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles), joins = (static_cast<long>(R) * heads + 3) / 4;
+    const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
+    if (B * joins > INT_MAX || prepare > INT_MAX || units > INT_MAX) return FSD_ERR_SHAPE;
     const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
-    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(grid), lds);
-    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(grid), lds);
-    else launch_attend<256>(st, P, s, static_cast<unsigned>(grid), lds);
+    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
+    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
+    else launch_attend<256>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
     return launched();
 }
 
@@ -254,7 +308,10 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
 
 size_t fsd_attend_workspace_bytes(int B, int R, int heads, int kv_heads, int head_dim) {
     if (!attend_sizes(B, R, heads, kv_heads, head_dim)) return 0;
-    return attend_bytes(attend_shape(static_cast<long>(R) * (heads / kv_heads), head_dim), head_dim);
+    const long rows = static_cast<long>(R) * (heads / kv_heads);
+    const size_t a = attend_space(attend_shape(rows, head_dim, FSD_BF16), B, R, heads, kv_heads, head_dim, false).bytes;
+    const size_t c = attend_space(attend_shape(rows, head_dim, FSD_F16), B, R, heads, kv_heads, head_dim, true).bytes;
+    return a > c ? a : c;
 }
 
 int fsd_attend_chain(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, int B, int R, int heads, int dtype,

@@ -126,29 +126,73 @@ __device__ __forceinline__ void load8(const void* base, size_t at, float* x) {
     }
 }
 
-// elements d .. d+7 (d a multiple of 8) of a head at `at`, rotated by the table's row `pos`
-template <int DT>
-__device__ __forceinline__ void load8_turned(const void* base, size_t at, int d, const fsd_rotation& rot, int pos, float* x) {
-    load8<DT>(base, at + d, x);
-    if (rot.table == nullptr || d >= rot.dim) return;
-    const float* t = rot.table + static_cast<size_t>(pos) * rot.dim;
+// what lies in 16 bytes (8 elements of 16 bits) as numbers
+__device__ __forceinline__ void unpack8(int dtype, const u32x4& a, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned w = a[i];
+        const half2_t h = __builtin_bit_cast(half2_t, w);
+        x[2 * i] = dtype == FSD_BF16 ? __uint_as_float(w << 16) : static_cast<float>(h.x);
+        x[2 * i + 1] = dtype == FSD_BF16 ? __uint_as_float(w & 0xFFFF0000u) : static_cast<float>(h.y);
+    }
+}
+__device__ __forceinline__ void load8_any(int dtype, const void* base, size_t at, float* x) {
+    if (dtype == FSD_F32) load8<FSD_F32>(base, at, x);
+    else unpack8(dtype, *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(base) + at), x);
+}
+
+// NS slots of 8 elements, d[i] .. d[i]+7 (d a multiple of 8) of the head that begins at element at[i], turned by the table's row
+// pos[i].  All loads of up to ONCE slots are requested before the first is used: one memory latency, not one for each.
+template <int NS, int ONCE = 4>
+__device__ __forceinline__ void load_turned(int dtype, const void* base, const size_t (&at)[NS], const int (&d)[NS], const fsd_rotation& rot,
+                                            const int (&pos)[NS], float (&x)[NS][8]) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) load8_any(dtype, base, at[i] + d[i], x[i]);
+    if (rot.table == nullptr) return;
     const int n = rot.dim / 2;
-    if (rot.style == FSD_ROPE_HALVES) {
-        const bool low = d < n;
-        const int i = low ? d : d - n;                       // of the pair
-        float y[8], c[8], s[8];
-        load8<DT>(base, at + (low ? d + n : d - n), y);
-        load8<FSD_F32>(t, i, c);
-        load8<FSD_F32>(t, n + i, s);
+    constexpr int kOnce = NS < ONCE ? NS : ONCE;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = low ? x[e] * c[e] - y[e] * s[e] : x[e] * c[e] + y[e] * s[e];
-    } else {
-        const u32x4 c = *reinterpret_cast<const u32x4*>(t + d / 2), s = *reinterpret_cast<const u32x4*>(t + n + d / 2);
+    for (int i0 = 0; i0 < NS; i0 += kOnce) {
+        if (rot.style == FSD_ROPE_HALVES) {
+            float y[kOnce][8], c[kOnce][8], s[kOnce][8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float cc = __uint_as_float(c[e]), ss = __uint_as_float(s[e]), a = x[2 * e], b = x[2 * e + 1];
-            x[2 * e] = a * cc - b * ss;
-            x[2 * e + 1] = b * cc + a * ss;
+            for (int e = 0; e < kOnce; ++e) {
+                const int i = i0 + e, low = d[i] < n, in = d[i] < rot.dim;
+                load8_any(dtype, base, at[i] + (low ? d[i] + n : in ? d[i] - n : d[i]), y[e]);
+                const float* t = rot.table + static_cast<size_t>(pos[i]) * rot.dim + (low ? d[i] : in ? d[i] - n : 0);
+                load8<FSD_F32>(t, 0, c[e]);
+                load8<FSD_F32>(t, n, s[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < kOnce; ++e) {
+                const int i = i0 + e;
+                const bool low = d[i] < n, in = d[i] < rot.dim;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float a = x[i][k] * c[e][k], b = y[e][k] * s[e][k];
+                    x[i][k] = in ? (low ? a - b : a + b) : x[i][k];
+                }
+            }
+        } else {
+            u32x4 c[kOnce], s[kOnce];
+#pragma unroll
+            for (int e = 0; e < kOnce; ++e) {
+                const int i = i0 + e;
+                const float* t = rot.table + static_cast<size_t>(pos[i]) * rot.dim + (d[i] < rot.dim ? d[i] / 2 : 0);
+                c[e] = *reinterpret_cast<const u32x4*>(t);
+                s[e] = *reinterpret_cast<const u32x4*>(t + n);
+            }
+#pragma unroll
+            for (int e = 0; e < kOnce; ++e) {
+                const int i = i0 + e;
+                const bool in = d[i] < rot.dim;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float cc = __uint_as_float(c[e][k]), ss = __uint_as_float(s[e][k]), a = x[i][2 * k], b = x[i][2 * k + 1];
+                    x[i][2 * k] = in ? a * cc - b * ss : a;
+                    x[i][2 * k + 1] = in ? b * cc + a * ss : b;
+                }
+            }
         }
     }
 }
