@@ -72,7 +72,10 @@ struct AttendParams {
 
 // The work is a line of units.  An item is one (sequence, key head, run of `tile` rows); its units are the blocks of the sequence's
 // cache, then its tiles of 64 rows; kStart more stand for what an item costs at its beginning, whoever begins it.
-constexpr int kStart = 2;
+#ifndef KST
+#define KST 6
+#endif
+constexpr int kStart = KST;
 struct Share { int rows, blocks, tiles, groups; };
 __device__ __forceinline__ Share share_of(const AttendParams& P, int b) {
     Share s;
@@ -167,19 +170,30 @@ __device__ __forceinline__ int not_kept(int x) {
     return x;
 }
 
+// The value is in its register from here on: the compiler waits for what it has requested here, and not in a loop behind, where it
+// would wait for the fetches as well.
+template <typename T>
+__device__ __forceinline__ void settle(T& x) {
+    asm volatile("" : "+v"(x));
+}
+
 // ---- blocks come to LDS without passing through registers: a lane's 16 bytes of a fragment land at 16 * lane of its 1 KB, and
 // the same lane (or the same lane of another wavefront) reads them back, so that nothing is exchanged between lanes
 
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) void global_void;
 
-__device__ __forceinline__ void fetch_1k(const char* from, unsigned char* to) {   // from: this lane's 16 bytes; to: the same for all lanes
-    __builtin_amdgcn_global_load_lds((global_void*)(from), (lds_void*)(to), 16, 0, 0);
-}
 __device__ __forceinline__ unsigned lds_address(const unsigned char* p) {
     return static_cast<unsigned>(reinterpret_cast<uintptr_t>((const lds_void*)(p)));
 }
-// four fragments 1 KB apart.  (In assembly because the compiler would wait for every fetch in flight before it reads LDS.)
+// from: this lane's 16 bytes; to: the same for all lanes.  (In assembly, as the reads below, because the compiler would have every access of
+// LDS wait for every fetch in flight.  What it counts itself is less than what there is: its own waits are long enough.)
+__device__ __forceinline__ void fetch_1k(const char* from, const unsigned char* to) {
+    asm volatile("s_mov_b32 m0, %1\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, off"
+                 :: "v"(from), "s"(__builtin_amdgcn_readfirstlane(static_cast<int>(lds_address(to)))) : "memory", "m0");
+}
+// four fragments 1 KB apart
 __device__ __forceinline__ void read_4k(unsigned at, u32x4 (&w)[4]) {
     asm volatile("ds_read_b128 %0, %4\n\t"
                  "ds_read_b128 %1, %4 offset:1024\n\t"
@@ -193,6 +207,20 @@ __device__ __forceinline__ void read_2k(unsigned at, u32x4 (&w)[2]) {
                  "ds_read_b128 %1, %2 offset:1024\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : "=&v"(w[0]), "=&v"(w[1]) : "v"(at) : "memory");
+}
+__device__ __forceinline__ void read_1k(unsigned at, u32x4& w) {
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(at) : "memory");
+}
+template <int N, int M>
+__device__ __forceinline__ void read_some(unsigned at, u32x4 (&w)[M]) {
+    static_assert((N == 1 || N == 2 || N == 4) && N <= M, "fragments");
+    if constexpr (N == 1) read_1k(at, w[0]);
+    else if constexpr (N == 2) read_2k(at, reinterpret_cast<u32x4(&)[2]>(w));
+    else read_4k(at, reinterpret_cast<u32x4(&)[4]>(w));
+}
+// A barrier that leaves fetches under way: what the wavefronts exchange goes through LDS by ordinary stores.
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 // waits until at most N of this wavefront's fetches are under way
 template <int N>
@@ -401,58 +429,88 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     }
 }
 
-// LDS of a workgroup: blocks in flight, or the join of the wavefronts' results
-template <int D, int RT, int NW, bool BYKEYS, bool FINE>
+// An item, or the part of one that a worker has
+struct Item {
+    int b, h, group, len, nrho;    // nrho: (row, head) pairs of the sequence
+    int first, last;               // cached blocks
+    int tile0, tile1;              // tiles of the rows themselves
+    bool whole;
+    size_t slot;                   // for the result where it is not whole
+};
+// A worker's way along the line.  (All of it is the same for every thread of the workgroup.)
+struct Line {
+    long per, worker, begin, finish, x, before;
+    int b;
+    __device__ __forceinline__ explicit Line(const AttendParams& P) {
+        worker = spread_over_xcds(blockIdx.x, P.workers);
+        per = P.plan[0];
+        const long total = P.plan[1 + P.B];
+        begin = x = worker < 0 ? total : per * worker;
+        finish = begin + per < total ? begin + per : total;
+        b = 0;                                                // the sequence in which the units begin
+        for (int n = P.B; n > 1;) {                           // (of those that begin at the same unit the last one has units)
+            const int half = n / 2;
+            if (P.plan[1 + b + half] <= begin) b += half;
+            n -= half;
+        }
+        before = P.plan[1 + b];                               // units before sequence b
+    }
+    __device__ __forceinline__ bool more() const { return x < finish; }
+    __device__ __forceinline__ Item next(const AttendParams& P) {
+        while (x >= P.plan[2 + b]) before = P.plan[1 + ++b];
+        const Share share = share_of(P, b);
+        const int units = units_of(share), item = static_cast<int>(static_cast<unsigned>(x - before) / static_cast<unsigned>(units));
+        const long item0 = before + static_cast<long>(item) * units;
+        const int u0 = static_cast<int>(x - item0), u1 = static_cast<int>(finish - item0 < units ? finish - item0 : units);
+        const int end = max(0, u1 - kStart);
+        Item it;
+        it.b = b;
+        it.group = item % share.groups;
+        it.h = item / share.groups;
+        it.len = max(0, min(P.cache.cache_len[b], P.cache.max_blocks * kBlock));
+        it.nrho = share.rows * P.G;
+        it.first = max(0, u0 - kStart);
+        it.last = min(share.blocks, end);
+        const int row1 = min(share.rows - 1, (it.group * P.tile + P.tile - 1) / P.G);   // last row of the item
+        it.tile0 = max(0, it.first - share.blocks);
+        it.tile1 = min(row1 / kBlock + 1, end - share.blocks);
+        it.whole = u0 == 0 && u1 == units;
+        // slot 0: of the item in which this worker's units begin; slot 1: of one that begins behind that and goes on with the next worker
+        it.slot = 2 * static_cast<size_t>(worker) + (item0 > begin ? 1 : 0);
+        if (u0 == 0 && threadIdx.x == 0) {                    // for the join: the item's first slot and its workers
+            const long w1 = (item0 + units - 1) / per;
+            P.pieces[(static_cast<size_t>(b) * P.cache.kv_heads + it.h) * (P.row_tiles * 16 / P.tile) + it.group] =
+                make_int2(static_cast<int>(it.slot), static_cast<int>(w1 - worker) + 1);
+        }
+        x = item0 + u1;
+        return it;
+    }
+};
+
+template <int D>
 struct AttendShapeOf {
     static constexpr int kI = D / 64;                         // 64-dimension steps of a head
     static constexpr int kT = D / 16;                         // tiles of 16 dimensions; also the fragments of a block's keys, and of its values
     static constexpr int kStage = 2 * kT * 1024;              // a block; also a tile's keys, and its values, in binary16
-    static constexpr int kStages = BYKEYS ? 1 : 4;
-    static constexpr int kFlight = kStages * kStage * (BYKEYS ? NW : 1);
-    static constexpr int kJoin = BYKEYS ? 2 * RT * kT * 64 * 16 : 0;   // two wavefronts' sums
-    static constexpr int kBytes = kJoin > kFlight ? kJoin : kFlight;
 };
 
-// BYKEYS: the wavefronts take the same rows (16 RT) and each every NW-th block; otherwise each its own 16 RT rows and all blocks.
+// Many rows: each of NW wavefronts takes 16 RT rows of its own and goes over all blocks, which they fetch together.
 // FINE: see attend_prepare.
-template <int D, int RT, int NW, bool BYKEYS, bool FINE>
+template <int D, int RT, int NW, bool FINE>
 __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
-    using Shape = AttendShapeOf<D, RT, NW, BYKEYS, FINE>;
+    using Shape = AttendShapeOf<D>;
     constexpr int kI = Shape::kI, kT = Shape::kT;
-    __shared__ __align__(16) unsigned char lds[Shape::kBytes];
-    __shared__ float stat[2][NW][16 * RT];                    // maximum and sum of every wavefront's columns
+    __shared__ __align__(16) unsigned char lds[4 * Shape::kStage];   // blocks in flight
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int G = P.G, H = P.cache.kv_heads, R = P.R;
-    const long worker = spread_over_xcds(blockIdx.x, P.workers), per = P.plan[0], total = P.plan[1 + P.B];
-    const long begin = per * worker, finish = begin + per < total ? begin + per : total;
-    if (worker < 0 || begin >= finish) return;
-    int b = 0;                                                // the sequence in which the units begin
-    for (int n = P.B; n > 1;) {                               // (of those that begin at the same unit the last one has units)
-        const int half = n / 2;
-        if (P.plan[1 + b + half] <= begin) b += half;
-        n -= half;
-    }
-    long before = P.plan[1 + b];                              // units before sequence b
-
-    for (long x = begin; x < finish;) {
+    Line line(P);
+    while (line.more()) {
         // (what follows from a thread's number is worked out anew for every item: kept in registers from one to the next, as the
         // compiler would, it leaves the loop over blocks too few of them)
         const int tid = not_kept(thread), lane = tid & 63, col = lane & 15, g = lane >> 4;
-        // ---- which item, and which of its units
-        while (x >= P.plan[2 + b]) before = P.plan[1 + ++b];
-        const Share share = share_of(P, b);
-        const int units = units_of(share), item = static_cast<int>(static_cast<unsigned>(x - before) / static_cast<unsigned>(units));
-        const int group = item % share.groups, h = item / share.groups;
-        const long item0 = before + static_cast<long>(item) * units;
-        const int u0 = static_cast<int>(x - item0), u1 = static_cast<int>(finish - item0 < units ? finish - item0 : units);
-        const int first = max(0, u0 - kStart), end = max(0, u1 - kStart);    // cached blocks, then tiles
-        x = item0 + u1;
-
-        const int len = max(0, min(P.cache.cache_len[b], P.cache.max_blocks * kBlock));
-        const int rho0 = group * P.tile + (BYKEYS ? 0 : wave * 16 * RT);      // first (row, head) pair of this wavefront
-        const int nrho = share.rows * G;
-        const int row1 = min(share.rows - 1, (group * P.tile + P.tile - 1) / G);   // last row of the item
-        const int last = min(share.blocks, end), tile0 = max(0, first - share.blocks), tile1 = min(row1 / kBlock + 1, end - share.blocks);
+        const Item it = line.next(P);
+        const int b = it.b, h = it.h, group = it.group, first = it.first, last = it.last, tile0 = it.tile0, tile1 = it.tile1, len = it.len, nrho = it.nrho;
+        const int rho0 = group * P.tile + wave * 16 * RT;   // first (row, head) pair of this wavefront
         const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
         const size_t bh = static_cast<size_t>(b) * H + h;
 
@@ -485,6 +543,15 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                     if constexpr (FINE) q2[rt][i] = zero;
                 }
             }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            settle(factor[rt]);
+#pragma unroll
+            for (int i = 0; i < 2 * kI; ++i) {
+                settle(q[rt][i]);
+                if constexpr (FINE) settle(q2[rt][i]);
+            }
+        }
         float4_t o[RT][kT];
         float m[RT], l[RT];                                   // maximum of s + log2(value scale); sum (of all lanes of the column)
 #pragma unroll
@@ -500,14 +567,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         // Weights of 64 tokens from their products.  With `part` only those of kept(rt) count (a bit for each of the 16 tokens of this
         // lane's group), and those of spoilt(rt) are NaN.  Their sum is a product with ones: two instructions of the matrix unit for
         // 16 additions, and it sums what the second product will use.
-        auto weigh = [&](float4_t (&s)[RT][4], float ks, float vs, bool part, auto kept, auto spoilt, half8_t (&p)[RT][2]) {
-            const float lift = __builtin_amdgcn_logf(vs), inv_vs = 1.0f / vs;
+        auto weigh = [&](float4_t (&s)[RT][4], float ks, float vs, auto part, auto kept, auto spoilt, half8_t (&p)[RT][2]) {
+            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs);   // (exact for powers of two)
             float high[RT], f[RT];
             bool over = false;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 f[rt] = factor[rt] * ks;
-                if (part) {
+                if constexpr (part) {
                     const unsigned keep = kept(rt);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) s[rt][j / 4][j % 4] = keep >> j & 1u ? s[rt][j / 4][j % 4] : -3.0e38f;
@@ -539,7 +606,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         w[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][j / 4][j % 4 + e], f[rt], from));
-                        if (part) w[e] = keep >> (j + e) & 1u ? (spoil >> (j + e) & 1u ? __builtin_nanf("") : w[e]) : 0.0f;
+                        if constexpr (part) w[e] = keep >> (j + e) & 1u ? (spoil >> (j + e) & 1u ? __builtin_nanf("") : w[e]) : 0.0f;
                     }
                     const half2_t two = __builtin_convertvector(w, half2_t);
                     p[rt][j / 8][j % 8] = two.x;
@@ -552,6 +619,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             }
         };
         auto nothing = [](int) { return 0u; };
+        const std::integral_constant<bool, true> in_part;
+        const std::integral_constant<bool, false> in_full;
 
         // ---- cached blocks
         {
@@ -559,7 +628,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
             const char* kbase = static_cast<const char*>(P.cache.k_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + ((col >> 2) * 16 + (col & 3)) * D + g * 16;
             const char* vbase = static_cast<const char*>(P.cache.v_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + (g * D + col) * 16;
-            unsigned char* flight = lds + (BYKEYS ? wave * Shape::kStages * Shape::kStage : 0);
+            unsigned char* flight = lds;
             // fragment f of the keys is tile f / kI, 64-dimension step f % kI; of the values tile f
             auto fetch_key = [&](size_t id, int f, unsigned char* to) { fetch_1k(kbase + id * per_block + (f / kI) * 4 * D + (f % kI) * 64, to + f * 1024); };
             auto fetch_value = [&](size_t id, int f, unsigned char* to) { fetch_1k(vbase + id * per_block + f * 256, to + (kT + f) * 1024); };
@@ -586,12 +655,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             };
             // mine: how many of the 16 tokens of this lane's group there are.  What lies behind the last one may be anything: a weight of 0
             // would not make a NaN harmless
-            auto sums = [&](unsigned at, const half8_t (&p)[RT][2], bool part, int mine) {
+            auto sums = [&](unsigned at, const half8_t (&p)[RT][2], auto part, int mine) {
 #pragma unroll
                 for (int t0 = 0; t0 < kT; t0 += 4) {
                     u32x4 w[4];
                     read_4k(at + (kT + t0) * 1024, w);
-                    if (part) {
+                    if constexpr (part) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int bytes = max(0, min(4, mine - 4 * i));
@@ -611,16 +680,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                     }
                 }
             };
-            constexpr int kStep = BYKEYS ? NW : 1;
             // 64 blocks at a time: a lane looks up one block's number and scales
-            for (int j0 = first; j0 < last; j0 += 64 * kStep) {
-                const int mine0 = j0 + (BYKEYS ? wave : 0);
-                const int n = min(64, (last - mine0 + kStep - 1) / kStep);   // blocks of this wavefront
+            for (int j0 = first; j0 < last; j0 += 64) {
+                const int n = min(64, last - j0);
                 int my_id = 0;
                 float my_ks = 1.0f, my_vs = 1.0f;
                 bool good = false;
                 if (lane < n) {
-                    my_id = table[mine0 + lane * kStep];
+                    my_id = table[j0 + lane];
                     good = my_id >= 0 && my_id < P.cache.num_blocks;
                     if (!good) my_id = 0;                      // in bounds, and none of its tokens counts
                     const size_t at = (layer0 + my_id) * H + h;
@@ -631,74 +698,52 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 auto id_of = [&](int i) { return static_cast<size_t>(__builtin_amdgcn_readlane(my_id, i)); };
                 auto float_of = [](float y, int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), i)); };
                 // tokens of the i-th block that count
-                auto left_of = [&](int i) { return fine >> i & 1ull ? len - (mine0 + i * kStep) * kBlock : 0; };
+                auto left_of = [&](int i) { return fine >> i & 1ull ? len - (j0 + i) * kBlock : 0; };
+                // blocks all of whose tokens count come first and have a loop of their own: only a sequence's last block has others
+                // (a number out of range apart).  (With selections between the two the compiler makes a hundred instructions more a block.)
+                const int full = n > 0 && fine == ~0ull >> (64 - n) ? n - (left_of(n - 1) < kBlock ? 1 : 0) : 0;
+                settle(my_id);
+                settle(my_ks);
+                settle(my_vs);
                 wait_fetches<0>();                            // (nothing of the loads above is counted below)
-                if constexpr (BYKEYS) {
-                    if (n > 0) {
-                        const size_t id = id_of(0);
+                // four stages: while block i is worked on, the three behind it are under way; a wavefront fetches every NW-th fragment
+                constexpr int kMine = 2 * kT / NW;
+                static_assert(2 * kT % NW == 0, "every wavefront fetches as many fragments");
+                auto fetch_block = [&](int i) {
+                    const size_t id = id_of(min(i, n - 1));
+                    unsigned char* to = flight + i % 4 * Shape::kStage;
 #pragma unroll
-                        for (int f = 0; f < kT; ++f) fetch_key(id, f, flight);
-#pragma unroll
-                        for (int f = 0; f < kT; ++f) fetch_value(id, f, flight);
+                    for (int e = 0; e < kMine; ++e) {
+                        const int f = wave + e * NW;
+                        if (f < kT) fetch_key(id, f, to);
+                        else fetch_value(id, f - kT, to);
                     }
-                    const unsigned at = lds_address(flight) + lane * 16;
-                    for (int i = 0; i < n; ++i) {
-                        const size_t next = id_of(min(i + 1, n - 1));   // (behind the last one it comes again, unused)
+                };
+                __syncthreads();                          // (the stages are free)
+                fetch_block(0);
+                fetch_block(1);
+                fetch_block(2);
+                auto step = [&](int i, auto part) {
+                    wait_fetches<2 * kMine>();
+                    __builtin_amdgcn_s_barrier();         // block i is there, and everyone is done with block i - 1
+                    fetch_block(i + 3);
+                    if (rho0 < nrho) {
+                        const unsigned at = lds_address(flight + i % 4 * Shape::kStage) + lane * 16;
                         float4_t s[RT][4];
                         half8_t p[RT][2];
-                        wait_fetches<kT>();
                         products(at, s);
-#pragma unroll
-                        for (int f = 0; f < kT; ++f) fetch_key(next, f, flight);
-                        const int left = left_of(i);
-                        const bool part = left < kBlock;
-                        const int mine = max(0, min(16, left - 16 * g));
+                        const int mine = max(0, min(16, left_of(i) - 16 * g));
                         weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return (1u << mine) - 1u; }, nothing, p);
-                        wait_fetches<kT>();
                         sums(at, p, part, mine);
-#pragma unroll
-                        for (int f = 0; f < kT; ++f) fetch_value(next, f, flight);
                     }
-                    wait_fetches<0>();
-                } else {
-                    // three stages: while block i is worked on, the two behind it are under way; a wavefront fetches every NW-th fragment
-                    constexpr int kMine = 2 * kT / NW;
-                    static_assert(2 * kT % NW == 0, "every wavefront fetches as many fragments");
-                    auto fetch_block = [&](int i) {
-                        const size_t id = id_of(min(i, n - 1));
-                        unsigned char* to = flight + i % 3 * Shape::kStage;
-#pragma unroll
-                        for (int e = 0; e < kMine; ++e) {
-                            const int f = wave + e * NW;
-                            if (f < kT) fetch_key(id, f, to);
-                            else fetch_value(id, f - kT, to);
-                        }
-                    };
-                    __syncthreads();                          // (the stages are free)
-                    fetch_block(0);
-                    fetch_block(1);
-                    for (int i = 0; i < n; ++i) {
-                        wait_fetches<kMine>();
-                        __builtin_amdgcn_s_barrier();         // block i is there, and everyone is done with block i - 1
-                        fetch_block(i + 2);
-                        if (rho0 < nrho) {
-                            const unsigned at = lds_address(flight + i % 3 * Shape::kStage) + lane * 16;
-                            float4_t s[RT][4];
-                            half8_t p[RT][2];
-                            products(at, s);
-                            const int left = left_of(i);
-                            const bool part = left < kBlock;
-                            const int mine = max(0, min(16, left - 16 * g));
-                            weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return (1u << mine) - 1u; }, nothing, p);
-                            sums(at, p, part, mine);
-                        }
-                    }
-                    wait_fetches<0>();
-                }
+                };
+                int i = 0;
+                for (; i < full; ++i) step(i, in_full);
+                for (; i < n; ++i) step(i, in_part);
+                wait_fetches<0>();
             }
         }
         // ---- the tail: the rows themselves, in binary16
-        __syncthreads();
         {
             // weights and sums of tile `tile`, whose keys lie at `keys` and whose values come when values() is called
             auto one_tile = [&](int tile, auto keys, auto values) {
@@ -723,7 +768,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 }
                 const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g)) & 0xFFFFu;
                 half8_t p[RT][2];
-                weigh(s, 1.0f, P.value_scale[bht], true, [&](int rt) { return see[rt]; }, [&](int) { return spoilt; }, p);
+                weigh(s, 1.0f, P.value_scale[bht], in_part, [&](int rt) { return see[rt]; }, [&](int) { return spoilt; }, p);
                 values(p);
             };
             auto products16 = [&](unsigned at, auto second, float4_t (&s)[RT][4]) {   // second: the keys' second parts, or the first ones again
@@ -765,33 +810,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             const size_t size = static_cast<size_t>(P.B) * H * P.tiles * Shape::kStage;
             const char* k16 = P.k16 + bh * P.tiles * Shape::kStage + lane * 16;
             const char* v16 = P.v16 + bh * P.tiles * Shape::kStage + lane * 16;
-            if constexpr (BYKEYS) {
-                unsigned char* flight = lds + wave * Shape::kStage;
-                const unsigned at = lds_address(flight) + lane * 16;
-                auto fetch = [&](const char* from) {
-#pragma unroll
-                    for (int f = 0; f < 2 * kT; ++f) fetch_1k(from + f * 1024, flight + f * 1024);
-                };
-                for (int tile = tile0; tile < tile1; ++tile) {
-                    if (tile % NW != wave) continue;
-                    fetch(k16 + static_cast<size_t>(tile) * Shape::kStage);
-                    one_tile(tile, [&](float4_t (&s)[RT][4]) {
-                        wait_fetches<0>();
-                        products16(at, first_parts, s);
-                        if constexpr (FINE) {
-                            fetch(k16 + size + static_cast<size_t>(tile) * Shape::kStage);
-                            wait_fetches<0>();
-                            products16(at, second_parts, s);
-                        }
-                        fetch(v16 + static_cast<size_t>(tile) * Shape::kStage);
-                    }, [&](const half8_t (&p)[RT][2]) {
-                        wait_fetches<0>();
-                        sums16(at, p);
-                    });
-                }
-                __syncthreads();
-            } else if (tile0 < tile1) {
+            if (tile0 < tile1) {
                 // stages: keys, values (and the keys' second parts); without the latter the next tile is under way in the other two
+                __syncthreads();                              // (the blocks' stages are free)
                 constexpr int kMine = 2 * kT / NW;
                 auto fetch = [&](const char* from, int stage) {
 #pragma unroll
@@ -823,78 +844,343 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             }
         }
 
-        // ---- with BYKEYS the wavefronts' results are put together
-        if constexpr (BYKEYS) {
-            if (g == 0) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    stat[0][wave][rt * 16 + col] = m[rt];
-                    stat[1][wave][rt * 16 + col] = l[rt];
-                }
-            }
-            __syncthreads();
+        if (it.whole) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                float top = -__builtin_inff();
-                for (int w = 0; w < NW; ++w) top = __builtin_fmaxf(top, stat[0][w][rt * 16 + col]);
-                const float from = top == -__builtin_inff() ? 0.0f : top;
-                float sum = 0.0f;
-                for (int w = 0; w < NW; ++w) sum += stat[1][w][rt * 16 + col] * __builtin_amdgcn_exp2f(stat[0][w][rt * 16 + col] - from);
-                const float by = __builtin_amdgcn_exp2f(m[rt] - from);
-                m[rt] = top;
-                l[rt] = sum;
+                const int rho = rho0 + rt * 16 + col;
+                if (rho >= nrho) continue;
+                const int r = rho / G, head = h * G + (rho - r * G);
+                const float inv = 1.0f / l[rt];
+                const size_t at = ((static_cast<size_t>(b) * R + r) * P.heads + head) * D;
 #pragma unroll
-                for (int t = 0; t < kT; ++t) o[rt][t] *= by;
+                for (int t = 0; t < kT; ++t) store4(P.dtype, P.out, at + t * 16 + g * 4, o[rt][t] * inv);
             }
-            float4_t* box = reinterpret_cast<float4_t*>(lds);
-            static_assert(!BYKEYS || NW == 4, "the steps of the join");
+        } else {
+            float* part = P.part + it.slot * P.tile * (D + 2);
 #pragma unroll
-            for (int step = 2; step >= 1; --step) {           // wavefronts 2, 3 to 0, 1, then 1 to 0
-                if (wave >= step && wave < 2 * step) {
+            for (int rt = 0; rt < RT; ++rt) {
+                const int rho = rho0 + rt * 16 + col, at = wave * 16 * RT + rt * 16 + col;
+                if (rho >= nrho) continue;
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int t = 0; t < kT; ++t) box[((wave - step) * RT * kT + rt * kT + t) * 64 + lane] = o[rt][t];
+                for (int t = 0; t < kT; ++t) *reinterpret_cast<float4_t*>(part + static_cast<size_t>(at) * D + t * 16 + g * 4) = o[rt][t];
+                if (g == 0) {
+                    part[static_cast<size_t>(P.tile) * D + 2 * at] = m[rt];
+                    part[static_cast<size_t>(P.tile) * D + 2 * at + 1] = l[rt];
                 }
-                __syncthreads();
-                if (wave < step) {
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int t = 0; t < kT; ++t) o[rt][t] += box[(wave * RT * kT + rt * kT + t) * 64 + lane];
-                }
-                __syncthreads();
             }
         }
-        if (u0 == 0 && tid == 0) {                            // for the join: the item's first slot and its workers
-            const long w1 = (item0 + units - 1) / per;
-            P.pieces[bh * (P.row_tiles * 16 / P.tile) + group] = make_int2(static_cast<int>(2 * worker + (item0 > begin ? 1 : 0)), static_cast<int>(w1 - worker) + 1);
+    }
+}
+
+// Few rows (up to 16 RT = 64): four wavefronts share every block without doing anything twice.  Wavefront w takes the products of
+// token tile w with all rows, and the sums of a quarter of the dimensions: it fetches and widens a quarter of the keys and a quarter of the
+// values, its own, and only the weights go round, through LDS, with one barrier a block (two buffers: who is a block ahead writes
+// the other one).  A wavefront that sees a maximum run away says so beside its weights; then all of them agree on a new one and form the weights again.
+// O' is complete in every dimension, so nothing is joined between wavefronts but the sums of weights.
+template <int D, int RT, bool FINE>
+__global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
+    using Shape = AttendShapeOf<D>;
+    constexpr int kI = Shape::kI, kT = Shape::kT, kV = kT / 4;          // kV: tiles of 16 dimensions of a wavefront
+    constexpr int kPart = (kI + kV) * 1024;                             // a block's keys and values of a wavefront
+    constexpr int kStages = D == 256 ? 2 : RT == 4 ? 3 : 4;             // (two workgroups a compute unit)
+    __shared__ __align__(16) unsigned char lds[4 * kStages * kPart];    // a wavefront's blocks in flight lie side by side
+    __shared__ __align__(16) unsigned char weights[2][RT * 2 * 1024];   // of a block, as the second product takes them
+    __shared__ __align__(16) int over[2][4];
+    __shared__ float highs[4][16 * RT];
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int H = P.cache.kv_heads, R = P.R, G = P.G;
+    int turn = 0;                                                       // which of the two buffers is next
+    Line line(P);
+    while (line.more()) {
+        const int tid = not_kept(thread), lane = tid & 63, col = lane & 15, g = lane >> 4;
+        const Item it = line.next(P);
+        const int b = it.b, h = it.h, len = it.len, first = it.first, last = it.last, rho0 = it.group * P.tile;
+        const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
+        const size_t bh = static_cast<size_t>(b) * H + h;
+
+        half8_t q[RT][2 * kI], q2[FINE ? RT : 1][2 * kI];
+        float factor[RT];                                               // of the products of a row: its power of two back, scale, log2(e)
+        int row_of[RT];                                                 // the row, -1 behind the last
+        const size_t parts = static_cast<size_t>(P.B) * H * P.row_tiles * 2 * kI * 1024;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int rho = rho0 + rt * 16 + col;
+            row_of[rt] = rho < it.nrho ? rho / G : -1;
+            factor[rt] = P.factor[bh * P.row_tiles * 16 + rho];
+            const char* from = P.q16 + ((bh * P.row_tiles + rho0 / 16 + rt) * 2 * kI) * 1024 + lane * 16;
+#pragma unroll
+            for (int i = 0; i < 2 * kI; ++i) {
+                q[rt][i] = *reinterpret_cast<const half8_t*>(from + i * 1024);
+                if constexpr (FINE) q2[rt][i] = *reinterpret_cast<const half8_t*>(from + parts + i * 1024);
+            }
         }
-        if (!BYKEYS || wave == 0) {
-            if (u0 == 0 && u1 == units) {
+        // (columns behind the last row hold anything; they are never stored, and must not hold up the others)
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const int rho = rho0 + rt * 16 + col;
-                    if (rho >= nrho) continue;
-                    const int r = rho / G, head = h * G + (rho - r * G);
-                    const float inv = 1.0f / l[rt];
-                    const size_t at = ((static_cast<size_t>(b) * R + r) * P.heads + head) * D;
+        for (int rt = 0; rt < RT; ++rt)
+            if (row_of[rt] < 0) {
+                const half8_t zero = {};
+                factor[rt] = 0.0f;
 #pragma unroll
-                    for (int t = 0; t < kT; ++t) store4(P.dtype, P.out, at + t * 16 + g * 4, o[rt][t] * inv);
+                for (int i = 0; i < 2 * kI; ++i) {
+                    q[rt][i] = zero;
+                    if constexpr (FINE) q2[rt][i] = zero;
                 }
-            } else {
-                // slot 0: of the item in which this worker's units begin; slot 1: of one that begins behind that and goes on with the next worker
-                float* part = P.part + (2 * static_cast<size_t>(worker) + (item0 > begin ? 1 : 0)) * P.tile * (D + 2);
+            }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            settle(factor[rt]);
+#pragma unroll
+            for (int i = 0; i < 2 * kI; ++i) {
+                settle(q[rt][i]);
+                if constexpr (FINE) settle(q2[rt][i]);
+            }
+        }
+        float4_t o[RT][kV];
+        float m[RT], l[RT];                                             // maximum of s + log2(value scale); sum of this lane's tokens' weights
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            m[rt] = -__builtin_inff();
+            l[rt] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < kV; ++t) o[rt][t] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        // From this wavefront's products to everyone's weights p.  With `part` only the tokens of kept(rt) count (a bit for each of this
+        // lane's four), and the weights of spoilt are NaN.
+        auto weigh = [&](float4_t (&s)[RT], float ks, float vs, auto part, auto kept, unsigned spoilt, half8_t (&p)[RT][2]) {
+            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs);   // (exact for powers of two)
+            float high[RT], f[RT];
+            bool run = false;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                f[rt] = factor[rt] * ks;
+                if constexpr (part) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[rt][i] = kept(rt) >> i & 1u ? s[rt][i] : -3.0e38f;
+                }
+                high[rt] = fmaf(__builtin_fmaxf(__builtin_fmaxf(s[rt][0], s[rt][1]), __builtin_fmaxf(s[rt][2], s[rt][3])), f[rt], lift);
+                run |= high[rt] > m[rt] + kLazy;
+            }
+            float sum[RT];
+            unsigned char* box = weights[turn] + (wave >> 1) * 1024 + lane * 16 + (wave & 1) * 8;
+            auto form = [&]() {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    const int rho = rho0 + rt * 16 + col, at = (BYKEYS ? 0 : wave * 16 * RT) + rt * 16 + col;
-                    if (rho >= nrho) continue;
+                    const float from = lift - (m[rt] == -__builtin_inff() ? 0.0f : m[rt]);
+                    float w[4];
 #pragma unroll
-                    for (int t = 0; t < kT; ++t) *reinterpret_cast<float4_t*>(part + static_cast<size_t>(at) * D + t * 16 + g * 4) = o[rt][t];
-                    if (g == 0) {
-                        part[static_cast<size_t>(P.tile) * D + 2 * at] = m[rt];
-                        part[static_cast<size_t>(P.tile) * D + 2 * at + 1] = l[rt];
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from));
+                        if constexpr (part) w[i] = kept(rt) >> i & 1u ? (spoilt >> i & 1u ? __builtin_nanf("") : w[i]) : 0.0f;
                     }
+                    sum[rt] = (w[0] + w[1]) + (w[2] + w[3]);
+                    const float2_t lo = {w[0], w[1]}, hi = {w[2], w[3]};
+                    uint2 y;
+                    y.x = __builtin_bit_cast(unsigned, __builtin_convertvector(lo, half2_t));
+                    y.y = __builtin_bit_cast(unsigned, __builtin_convertvector(hi, half2_t));
+                    *reinterpret_cast<uint2*>(box + rt * 2048) = y;
+                }
+            };
+            form();
+            const bool mine = __any(run);
+            if (lane == 0) over[turn][wave] = mine ? 1 : 0;
+            meet();
+            if ((over[turn][0] | over[turn][1] | over[turn][2] | over[turn][3]) != 0) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float top = column_max(high[rt]);
+                    if (g == 0) highs[wave][rt * 16 + col] = top;
+                }
+                meet();
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    float to = m[rt];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) to = __builtin_fmaxf(to, highs[w][rt * 16 + col]);
+                    const float by = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - to);
+                    m[rt] = to;
+                    l[rt] *= by;
+#pragma unroll
+                    for (int t = 0; t < kV; ++t) o[rt][t] *= by;
+                }
+                form();
+                meet();
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                l[rt] = fmaf(sum[rt], inv_vs, l[rt]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) p[rt][k] = *reinterpret_cast<const half8_t*>(weights[turn] + (rt * 2 + k) * 1024 + lane * 16);
+            }
+            turn ^= 1;
+        };
+        const std::integral_constant<bool, true> in_part;
+        const std::integral_constant<bool, false> in_full;
+        unsigned char* flight = lds + wave * kStages * kPart;
+
+        // ---- cached blocks
+        {
+            const size_t per_block = static_cast<size_t>(H) * kBlock * D;
+            const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
+            const char* kbase = static_cast<const char*>(P.cache.k_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + ((col >> 2) * 16 + (col & 3) + 4 * wave) * D + g * 16;
+            const char* vbase = static_cast<const char*>(P.cache.v_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + (g * D + wave * kV * 16 + col) * 16;
+            // 64 blocks at a time: a lane looks up one block's number and scales
+            for (int j0 = first; j0 < last; j0 += 64) {
+                const int n = min(64, last - j0);
+                int my_id = 0;
+                float my_ks = 1.0f, my_vs = 1.0f;
+                bool good = false;
+                if (lane < n) {
+                    my_id = table[j0 + lane];
+                    good = my_id >= 0 && my_id < P.cache.num_blocks;
+                    if (!good) my_id = 0;                               // in bounds, and none of its tokens counts
+                    const size_t at = (layer0 + my_id) * H + h;
+                    my_ks = P.cache.k_scale[at];
+                    my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+                }
+                const unsigned long long fine = __ballot(good);
+                auto float_of = [](float y, int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), i)); };
+                // tokens of the i-th block that count
+                auto left_of = [&](int i) { return fine >> i & 1ull ? len - (j0 + i) * kBlock : 0; };
+                // blocks all of whose tokens count come first and have a loop of their own: only a sequence's last block has others
+                // (a number out of range apart)
+                const int full = fine == ~0ull >> (64 - n) ? n - (left_of(n - 1) < kBlock ? 1 : 0) : 0;
+                auto fetch = [&](int i) {                               // (behind the last one it comes again, unused: the count of fetches stays)
+                    const size_t id = static_cast<size_t>(__builtin_amdgcn_readlane(my_id, min(i, n - 1)));
+                    unsigned char* to = flight + i % kStages * kPart;
+#pragma unroll
+                    for (int f = 0; f < kI; ++f) fetch_1k(kbase + id * per_block + f * 64, to + f * 1024);
+#pragma unroll
+                    for (int f = 0; f < kV; ++f) fetch_1k(vbase + id * per_block + f * 256, to + (kI + f) * 1024);
+                };
+                settle(my_id);
+                settle(my_ks);
+                settle(my_vs);
+                wait_fetches<0>();                                      // (nothing of the loads above is counted below)
+#pragma unroll
+                for (int i = 0; i < kStages; ++i) fetch(i);
+                auto step = [&](int i, auto part) {
+                    const unsigned at = lds_address(flight + i % kStages * kPart) + lane * 16;
+                    float4_t s[RT];
+                    half8_t p[RT][2];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) s[rt] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                    wait_fetches<(kStages - 1) * (kI + kV) + kV>();
+                    u32x4 w[kI > kV ? kI : kV];
+                    read_some<kI>(at, w);
+#pragma unroll
+                    for (int f = 0; f < kI; ++f) {
+                        const half8_t a = widened(w[f].x, w[f].y), c = widened(w[f].z, w[f].w);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            s[rt] = product<FINE>(a, q[rt][2 * f], q2[FINE ? rt : 0][2 * f], s[rt]);
+                            s[rt] = product<FINE>(c, q[rt][2 * f + 1], q2[FINE ? rt : 0][2 * f + 1], s[rt]);
+                        }
+                    }
+                    const int mine = max(0, min(16, left_of(i) - 16 * g));          // of the 16 tokens of this lane's group
+                    const unsigned keep = ((1u << mine) - 1u) >> (4 * wave) & 15u;
+                    weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return keep; }, 0u, p);
+                    wait_fetches<(kStages - 1) * (kI + kV)>();
+                    read_some<kV>(at + kI * 1024, w);
+#pragma unroll
+                    for (int t = 0; t < kV; ++t) {
+                        // what lies behind the last token may be anything: a weight of 0 would not make a NaN harmless
+                        if constexpr (part) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int bytes = max(0, min(4, mine - 4 * k));
+                                w[t][k] = bytes == 4 ? w[t][k] : w[t][k] & ((1u << (8 * bytes)) - 1u);
+                            }
+                        }
+                        const half8_t a = widened(w[t].x, w[t].y), c = widened(w[t].z, w[t].w);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, p[rt][0], o[rt][t], 0, 0, 0);
+                            o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, p[rt][1], o[rt][t], 0, 0, 0);
+                        }
+                    }
+                    fetch(i + kStages);
+                };
+                int i = 0;
+                for (; i < full; ++i) step(i, in_full);
+                for (; i < n; ++i) step(i, in_part);
+                wait_fetches<0>();
+            }
+        }
+
+        // ---- the tail: the rows themselves, in binary16 (straight from memory: there is one tile, seldom two)
+        for (int tile = it.tile0; tile < it.tile1; ++tile) {
+            const size_t bht = bh * P.tiles + tile, size = static_cast<size_t>(P.B) * H * P.tiles * Shape::kStage;
+            const int t0 = tile * kBlock;
+            const char* keys = P.k16 + bht * Shape::kStage + wave * 2 * kI * 1024 + lane * 16;
+            const char* values = P.v16 + bht * Shape::kStage + wave * kV * 2048 + lane * 16;
+            half8_t a[2 * kI], a2[FINE ? 2 * kI : 1], v[2 * kV];
+#pragma unroll
+            for (int k = 0; k < 2 * kI; ++k) {
+                a[k] = *reinterpret_cast<const half8_t*>(keys + k * 1024);
+                if constexpr (FINE) a2[k] = *reinterpret_cast<const half8_t*>(keys + size + k * 1024);
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * kV; ++k) v[k] = *reinterpret_cast<const half8_t*>(values + k * 1024);
+            const float4_t ks = *reinterpret_cast<const float4_t*>(P.key_scale + bht * kBlock + g * 16 + 4 * wave);
+            const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g + 4 * wave)) & 15u;
+            const float vs = P.value_scale[bht];
+            float4_t s[RT];
+            half8_t p[RT][2];
+            unsigned see[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                s[rt] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < 2 * kI; ++k) {
+                    s[rt] = product<FINE>(a[k], q[rt][k], q2[FINE ? rt : 0][k], s[rt]);
+                    if constexpr (FINE) s[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a2[k], q[rt][k], s[rt], 0, 0, 0);
+                }
+                s[rt] *= ks;
+                const int r = row_of[rt], r0 = t0 + 16 * g + 4 * wave;            // this lane's tokens: rows r0 .. r0 + 3
+                if (r < t0) see[rt] = 0u;
+                else if (P.parent) see[rt] = static_cast<unsigned>(P.sees[(static_cast<size_t>(b) * R + r) * P.tiles + tile] >> (16 * g + 4 * wave)) & 15u;
+                else see[rt] = (1u << max(0, min(4, r - r0 + 1))) - 1u;
+            }
+            weigh(s, 1.0f, vs, in_part, [&](int rt) { return see[rt]; }, spoilt, p);
+#pragma unroll
+            for (int t = 0; t < 2 * kV; ++t)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[rt][t / 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[t], p[rt][t & 1], o[rt][t / 2], 0, 0, 0);
+        }
+
+        // ---- sums of all wavefronts' weights
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const float sum = column_sum(l[rt]);
+            if (g == 0) highs[wave][rt * 16 + col] = sum;
+        }
+        meet();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) l[rt] = (highs[0][rt * 16 + col] + highs[1][rt * 16 + col]) + (highs[2][rt * 16 + col] + highs[3][rt * 16 + col]);
+        meet();
+        if (it.whole) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int rho = rho0 + rt * 16 + col;
+                if (rho >= it.nrho) continue;
+                const int r = rho / G, head = h * G + (rho - r * G);
+                const float inv = 1.0f / l[rt];
+                const size_t at = ((static_cast<size_t>(b) * R + r) * P.heads + head) * D + wave * kV * 16 + g * 4;
+#pragma unroll
+                for (int t = 0; t < kV; ++t) store4(P.dtype, P.out, at + t * 16, o[rt][t] * inv);
+            }
+        } else {
+            float* part = P.part + it.slot * P.tile * (D + 2);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int at = rt * 16 + col;
+                if (rho0 + at >= it.nrho) continue;
+#pragma unroll
+                for (int t = 0; t < kV; ++t) *reinterpret_cast<float4_t*>(part + static_cast<size_t>(at) * D + wave * kV * 16 + t * 16 + g * 4) = o[rt][t];
+                if (g == 0 && wave == 0) {
+                    part[static_cast<size_t>(P.tile) * D + 2 * at] = m[rt];
+                    part[static_cast<size_t>(P.tile) * D + 2 * at + 1] = l[rt];
                 }
             }
         }

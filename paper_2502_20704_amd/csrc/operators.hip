@@ -112,26 +112,26 @@ void launch_append_d(hipStream_t st, const AppendParams& P, bool few) {
 
 // ------------------------------------------------------------------------------------------ attention
 
-// How many of a key head's rows (tokens times query heads of its group) an item takes, and how its wavefronts share them: up to 48
-// (binary16: 32; 16 at head_dim 256) four wavefronts take the same rows and every fourth block; beyond that each takes rows of its own.
-struct AttendShape { int rt, waves, tile, workers; bool by_keys; };
+// How many of a key head's rows (tokens times query heads of its group) an item takes: up to 64 attend_few (binary16 48, as its second parts take registers;
+// at head_dim 256 32 and 16), beyond that attend_rows with 128 or 256 rows, each wavefront some of them.
+struct AttendShape { int rt, waves, tile, workers; bool few; };
 AttendShape attend_shape(long rows, int head_dim, int dtype) {
     AttendShape s;
     const long tiles = (rows + 15) / 16;
-    s.by_keys = tiles <= (head_dim == 256 ? 1 : dtype == FSD_F16 ? 2 : 3);
-    if (s.by_keys) {
+    s.few = tiles <= (head_dim == 256 ? 2 : 4) - (dtype == FSD_F16 ? 1 : 0);
+    if (s.few) {
         s.rt = static_cast<int>(tiles);
         s.waves = 4;
     } else if (head_dim == 256) {
         s.rt = 1;
         s.waves = tiles <= 4 ? 4 : 8;
     } else {
-        s.rt = tiles <= 4 ? 1 : 2;
+        s.rt = 2;
         s.waves = tiles <= 8 ? 4 : 8;
     }
-    s.tile = 16 * s.rt * (s.by_keys ? 1 : s.waves);
+    s.tile = 16 * s.rt * (s.few ? 1 : s.waves);
     // as many workgroups as the 256 compute units hold at once
-    s.workers = s.by_keys ? (head_dim == 256 ? 256 : 512) : s.waves == 4 ? 512 : 256;
+    s.workers = s.few || s.waves == 4 ? (s.few || head_dim != 256 ? 512 : 256) : 256;
     return s;
 }
 bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
@@ -170,31 +170,37 @@ AttendSpace attend_space(const AttendShape& s, int B, int R, int heads, int H, i
     return w;
 }
 
-template <int D, int RT, int NW, bool BYKEYS>
-void launch_attend_k(hipStream_t st, const AttendParams& P) {
+template <int D, int RT>
+void launch_attend_few(hipStream_t st, const AttendParams& P) {
     const dim3 grid(static_cast<unsigned>(grid_over_xcds(P.workers)));
-    if constexpr (BYKEYS && RT == 3) {
-        hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, false>), grid, dim3(NW * 64), 0, st, P);
-    } else if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, true>), grid, dim3(NW * 64), 0, st, P);
-    else hipLaunchKernelGGL((attend_rows<D, RT, NW, BYKEYS, false>), grid, dim3(NW * 64), 0, st, P);
+    if constexpr (RT < (D == 256 ? 2 : 4)) {
+        if (P.dtype == FSD_F16) {
+            hipLaunchKernelGGL((attend_few<D, RT, true>), grid, dim3(kWG), 0, st, P);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((attend_few<D, RT, false>), grid, dim3(kWG), 0, st, P);
+}
+template <int D, int RT, int NW>
+void launch_attend_rows(hipStream_t st, const AttendParams& P) {
+    const dim3 grid(static_cast<unsigned>(grid_over_xcds(P.workers)));
+    if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_rows<D, RT, NW, true>), grid, dim3(NW * 64), 0, st, P);
+    else hipLaunchKernelGGL((attend_rows<D, RT, NW, false>), grid, dim3(NW * 64), 0, st, P);
 }
 template <int D>
 void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, int joins) {
     hipLaunchKernelGGL((attend_prepare<D>), dim3(prepare), dim3(kWG), lds, st, P);
-    if (s.by_keys) {
-        if (s.rt == 1) launch_attend_k<D, 1, 4, true>(st, P);
-        if constexpr (D != 256) {
-            if (s.rt == 2) launch_attend_k<D, 2, 4, true>(st, P);
-            else if (s.rt == 3) launch_attend_k<D, 3, 4, true>(st, P);
-        }
+    constexpr int kRows = D == 256 ? 1 : 2;
+    if (!s.few) {
+        if (s.waves == 4) launch_attend_rows<D, kRows, 4>(st, P);
+        else launch_attend_rows<D, kRows, 8>(st, P);
     } else if (s.rt == 1) {
-        if (s.waves == 4) launch_attend_k<D, 1, 4, false>(st, P);
-        if constexpr (D == 256) {
-            if (s.waves == 8) launch_attend_k<D, 1, 8, false>(st, P);
-        }
+        launch_attend_few<D, 1>(st, P);
+    } else if (s.rt == 2) {
+        launch_attend_few<D, 2>(st, P);
     } else if constexpr (D != 256) {
-        if (s.waves == 4) launch_attend_k<D, 2, 4, false>(st, P);
-        else launch_attend_k<D, 2, 8, false>(st, P);
+        if (s.rt == 3) launch_attend_few<D, 3>(st, P);
+        else launch_attend_few<D, 4>(st, P);
     }
     hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * joins), dim3(kWG), 0, st, P, joins);
 }
@@ -240,7 +246,7 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.v16 = base + w.v16;
     P.part = reinterpret_cast<float*>(base + w.part);
     P.workers = s.workers;
-    P.least = s.by_keys ? 4 : 1;
+    P.least = 1;
     P.tile = s.tile;
     P.row_tiles = w.row_tiles;
     P.tiles = w.tiles;
