@@ -164,6 +164,7 @@ __device__ __forceinline__ int to_half_range(float most) {
 }
 
 constexpr int kMaxNodes = 2048;
+constexpr int kWalk = 64;           // depths up to this are found by walking
 
 __device__ __forceinline__ int not_kept(int x) {
     asm volatile("" : "+v"(x));
@@ -247,13 +248,13 @@ __device__ __forceinline__ void two_parts(const float (&y)[8], float by, half8_t
 }
 
 // Queries and the rows' keys and values in the layout of the products; the plan; the sequences' reports.  Workgroup 0 deals the work out; of the others
-// each belongs to one sequence and takes some of its query rows, or one tile of 64 rows of a key head.
+// each belongs to one sequence and takes one tile of 64 rows of a key head, or some query rows.  What it costs is latencies: everything a thread reads
+// is requested at once, and nothing changes places between threads.
 // FINE (binary16 inputs): a turned query or key is held in two parts of 11 bits, as one rounding of them would cost more than that of the result:
 // 0.00047 of the result's norm in place of 0.00025 at 131072 tokens.
 template <int D>
 __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     constexpr int kI = D / 64, kPer = D / 8, kThreads = kWG;
-    __shared__ __align__(16) _Float16 turned[kBlock * D];     // values: [16-dimension tile][2][lane][8]
     __shared__ float most_of[kWG / 64];
     __shared__ unsigned long long broken;
     extern __shared__ short tree[];                           // trees: [R] parent's row, [R] depth, [R] ancestors found so far
@@ -262,8 +263,9 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         deal(P);
         return;
     }
-    const int H = P.cache.kv_heads, R = P.R, G = P.G;
-    const int per_sequence = P.query_groups + H * P.tiles, b = static_cast<int>((blockIdx.x - 1) / per_sequence), part = static_cast<int>((blockIdx.x - 1) % per_sequence);
+    const int H = P.cache.kv_heads, R = P.R, G = P.G, all_tiles = P.B * H * P.tiles, at_block = static_cast<int>(blockIdx.x) - 1;
+    const bool is_tile = at_block < all_tiles;                // (tiles first: they take longest)
+    const int b = is_tile ? at_block / (H * P.tiles) : (at_block - all_tiles) / P.query_groups;
     const Share share = share_of(P, b);
     const int len = max(0, min(P.cache.cache_len[b], P.cache.max_blocks * kBlock));
     short* up = tree;
@@ -271,10 +273,9 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     short* stands = tree + 2 * R;
     bool bad_tree = false;
     if (P.parent) {
-        // depths by doubling: after step i a row knows its 2^i-th ancestor and how far that is
         const int32_t* parent = P.parent + static_cast<size_t>(b) * (R - 1);
         for (int r = tid; r < R; r += kThreads) {
-            int p = -1;                                   // row 0 has none
+            int p = -1;                                       // row 0 has none
             if (r > 0) {
                 p = parent[r - 1];
                 const bool bad = p < -1 || p >= r - 1;
@@ -282,37 +283,52 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
                 p = bad ? 0 : p + 1;
             }
             up[r] = static_cast<short>(p);
-            stands[r] = static_cast<short>(p);
-            depth[r] = r > 0 ? 1 : 0;
         }
         bad_tree = __syncthreads_or(bad_tree);
-        for (;;) {
-            constexpr int kEach = (kMaxNodes + kThreads) / kThreads;
-            short jump[kEach], more[kEach];
-            bool moved = false;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int r = tid + i * kThreads, p = r < R ? stands[r] : -1;
-                jump[i] = p > 0 ? stands[p] : static_cast<short>(-1);
-                more[i] = p > 0 ? depth[p] : static_cast<short>(0);
-                moved |= p > 0;
-            }
-            if (!__syncthreads_or(moved)) break;
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int r = tid + i * kThreads;
-                if (r >= R) continue;
-                depth[r] = static_cast<short>(depth[r] + more[i]);
-                stands[r] = jump[i];
+        // depths: by walking up, which is short in most trees
+        bool far = false;
+        for (int r = tid; r < R; r += kThreads) {
+            int n = 0;
+            for (int at = r; at > 0 && n <= kWalk; at = up[at]) ++n;
+            far |= n > kWalk;
+            depth[r] = static_cast<short>(n);
+        }
+        if (__syncthreads_or(far)) {
+            // in deep ones by doubling: after step i a row knows its 2^i-th ancestor and how far that is
+            for (int r = tid; r < R; r += kThreads) {
+                stands[r] = up[r];
+                depth[r] = r > 0 ? 1 : 0;
             }
             __syncthreads();
+            for (;;) {
+                constexpr int kEach = (kMaxNodes + kThreads) / kThreads;
+                short jump[kEach], more[kEach];
+                bool moved = false;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int r = tid + i * kThreads, p = r < R ? stands[r] : -1;
+                    jump[i] = p > 0 ? stands[p] : static_cast<short>(-1);
+                    more[i] = p > 0 ? depth[p] : static_cast<short>(0);
+                    moved |= p > 0;
+                }
+                if (!__syncthreads_or(moved)) break;
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int r = tid + i * kThreads;
+                    if (r >= R) continue;
+                    depth[r] = static_cast<short>(depth[r] + more[i]);
+                    stands[r] = jump[i];
+                }
+                __syncthreads();
+            }
         }
     }
     auto position = [&](int r) { return len + (P.parent ? depth[r] : r); };
     auto table_row = [&](int pos) { return P.rot.table ? min(pos, P.rot.rows - 1) : 0; };
     const bool fine = P.dtype == FSD_F16;
 
-    if (part < P.query_groups) {
+    if (!is_tile) {
+        const int part = (at_block - all_tiles) % P.query_groups;
         if (part == 0 && P.status) {                          // the sequence's report
             const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
             bool bad = P.cache.cache_len[b] < 0 || P.cache.cache_len[b] > P.cache.max_blocks * kBlock ||
@@ -323,23 +339,35 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             bad = __syncthreads_or(bad);
             if (tid == 0) P.status[b] = (bad ? FSD_ROW_BAD_CACHE : 0) | (bad_tree ? FSD_ROW_BAD_PARENT : 0);
         }
-        // a thread takes 8 dimensions of a row, D / 8 neighbours the whole of it
+        // a thread takes 8 dimensions of kSlots rows, D / 8 neighbours the whole of a row
+        constexpr int kSlots = 2;
         const size_t parts = static_cast<size_t>(P.B) * H * P.row_tiles * 2 * kI * 1024;
-        const int n = share.rows * P.heads;
-        for (int u = part * kThreads + tid; u / kPer < n; u += P.query_groups * kThreads) {
-            const int r = u / kPer / P.heads, head = u / kPer % P.heads, dim = u % kPer * 8, h = head / G, rho = r * G + head % G;
-            const size_t at[1] = {(static_cast<size_t>(b) * R + r) * P.q_stride + static_cast<size_t>(head) * D};
-            const int dims[1] = {dim}, pos[1] = {table_row(position(r))};
-            float y[1][8];
-            load_turned<1>(P.dtype, P.q, at, dims, P.rot, pos, y);
+        const int n = share.rows * P.heads, row0 = part * (kSlots * kThreads / kPer) + tid / kPer, dim = tid % kPer * 8;
+        if (row0 >= n) return;
+        size_t at[kSlots];
+        int dims[kSlots], pos[kSlots], row[kSlots];
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            row[i] = row0 + i * (kThreads / kPer);
+            const int there = min(row[i], n - 1), r = there / P.heads;
+            at[i] = (static_cast<size_t>(b) * R + r) * P.q_stride + static_cast<size_t>(there - r * P.heads) * D;
+            dims[i] = dim;
+            pos[i] = table_row(position(r));
+        }
+        float y[kSlots][8];
+        load_turned<kSlots>(P.dtype, P.q, at, dims, P.rot, pos, y);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
             float most = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[0][e]));
+            for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[i][e]));
 #pragma unroll
             for (int o = kPer / 2; o > 0; o >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, o, 64));
+            if (row[i] >= n) continue;
             const float by = pow2(max(to_half_range(most), -126));
             half8_t a, c;
-            two_parts(y[0], P.scale < 0.0f ? -by : by, a, c);  // (a negative scale goes in here: a larger product is always a larger score)
+            two_parts(y[i], P.scale < 0.0f ? -by : by, a, c);  // (a negative scale goes in here: a larger product is always a larger score)
+            const int r = row[i] / P.heads, head = row[i] - r * P.heads, h = head / G, rho = r * G + head - h * G;
             const size_t bh = static_cast<size_t>(b) * H + h, fragment = (bh * P.row_tiles + rho / 16) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1);
             char* to = P.q16 + fragment * 1024 + ((dim / 16 & 3) * 16 + (rho & 15)) * 16;
             *reinterpret_cast<half8_t*>(to) = a;
@@ -348,17 +376,26 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         }
         return;
     }
-    const int tile = (part - P.query_groups) % P.tiles, h = (part - P.query_groups) / P.tiles, t0 = tile * kBlock, n = min(kBlock, share.rows - t0);
+    const int tile = at_block % P.tiles, h = at_block / P.tiles % H, t0 = tile * kBlock, n = min(kBlock, share.rows - t0);
     if (n <= 0) return;
     const size_t bht = (static_cast<size_t>(b) * H + h) * P.tiles + tile, size = static_cast<size_t>(P.B) * H * P.tiles * 8 * kI * 1024;
     const size_t base = (static_cast<size_t>(b) * R + t0) * P.kv_stride + static_cast<size_t>(h) * D;
-    constexpr int kUnits = kBlock * kPer / kThreads;
-    u32x4 raw[kUnits];                                        // values as they are
+    // values: a thread takes 8 tokens of one dimension, which lie in one of the product's fragments
+    constexpr int kUnits = kBlock * D / 8 / kThreads;
+    unsigned raw[kUnits][4];
+    const unsigned short* values = static_cast<const unsigned short*>(P.v) + base;
+    auto token_of = [&](int i) { return (lane >> 4) * 16 + ((tid + i * kThreads) >> 6 & 1) * 8; };   // the first of unit i
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-        const int u = tid + i * kThreads, t = u / kPer;
-        raw[i] = u32x4{0, 0, 0, 0};
-        if (t < n) raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(P.v) + base + t * P.kv_stride + u % kPer * 8);
+        const int d = (tid + i * kThreads) / 128 * 16 + (lane & 15), t = token_of(i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[i][e] = 0;
+        if (t >= n) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const unsigned w = values[min(t + e, n - 1) * P.kv_stride + d];   // (behind the last row it comes again, and is blanked)
+            raw[i][e / 2] |= (t + e < n ? w : 0u) << (16 * (e & 1));
+        }
     }
     // keys: every token scaled by a power of two of its own.  (What lies behind the last row is not written: no weight comes of it.)
     for (int u = tid; u / kPer < n; u += kThreads) {
@@ -381,12 +418,12 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         if (fine) *reinterpret_cast<half8_t*>(to + size) = c;
         if (dim == 0) P.key_scale[bht * kBlock + t] = 1.0f / by;
     }
-    // values: all scaled by one power of two; one that is not finite is noted, as no weight of 0 makes it harmless
+    // all values are scaled by one power of two; one that is not finite is noted, as no weight of 0 makes it harmless
     float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         float y[8];
-        unpack8(P.dtype, raw[i], y);
+        unpack8(P.dtype, u32x4{raw[i][0], raw[i][1], raw[i][2], raw[i][3]}, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[e]));
     }
@@ -398,22 +435,20 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     const float by = pow2(max(to_half_range(most), -126));
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-        const int u = tid + i * kThreads, t = u / kPer, dim = u % kPer * 8;
         float y[8];
-        unpack8(P.dtype, raw[i], y);
-        bool good = true;
+        unpack8(P.dtype, u32x4{raw[i][0], raw[i][1], raw[i][2], raw[i][3]}, y);
+        half8_t a;
+        unsigned long long bad = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool finite = __builtin_fabsf(y[e]) < __builtin_inff();
-            good &= finite;
-            const int d = dim + e;                            // tile d / 16, half t / 8 % 2, lane (t / 16) * 16 + d % 16, place t % 8
-            turned[((d / 16 * 2 + (t >> 3 & 1)) * 64 + (t >> 4) * 16 + d % 16) * 8 + (t & 7)] = static_cast<_Float16>(finite ? y[e] * by : 0.0f);
+            if (!finite) bad |= 1ull << (token_of(i) + e);
+            a[e] = static_cast<_Float16>(finite ? y[e] * by : 0.0f);
         }
-        if (!good) atomicOr(&broken, 1ull << t);
+        if (bad != 0) atomicOr(&broken, bad);
+        *reinterpret_cast<half8_t*>(P.v16 + bht * (8 * kI * 1024) + static_cast<size_t>(tid + i * kThreads) * 16) = a;
     }
     __syncthreads();
-    char* to = P.v16 + bht * (8 * kI * 1024);
-    for (int i = tid; i < kBlock * D / 8; i += kThreads) *reinterpret_cast<half8_t*>(to + i * 16) = *reinterpret_cast<const half8_t*>(turned + i * 8);
     if (tid == 0) {
         P.value_scale[bht] = 1.0f / by;
         P.broken[bht] = broken;
@@ -1187,45 +1222,51 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
     }
 }
 
-// Joins the items that several workers share: a wavefront a (row, head), the pieces in their order.
+// Joins the items that several workers share.  D / 4 lanes hold a row's dimensions, four each; such groups of lanes take a row each, or (by_pieces)
+// those of a workgroup share the pieces of one row, where the call has few rows and their pieces may be many.  8 pieces are requested at once.
 template <int D>
-__global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_sequence) {
-    constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes;      // lanes with 4 dimensions each; pieces a wavefront takes at once
-    const int b = blockIdx.x / per_sequence, lane = threadIdx.x & 63, d = lane % kLanes * 4, which = lane / kLanes;
+__global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_sequence, int by_pieces) {
+    constexpr int kLanes = D / 4, kGroups = kWG / kLanes;
+    __shared__ float stats[kGroups][2];
+    __shared__ __align__(16) float4_t sums[kGroups][kLanes];
+    const int b = blockIdx.x / per_sequence, at_row = static_cast<int>(blockIdx.x % per_sequence);
+    const int d = static_cast<int>(threadIdx.x) % kLanes * 4, which = static_cast<int>(threadIdx.x) / kLanes;
     const int nrho = (P.row_count ? max(0, min(P.row_count[b], P.R)) : P.R) * P.G, H = P.cache.kv_heads;
-    const int i = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x % per_sequence) * (kWG / 64) + static_cast<int>(threadIdx.x >> 6));
-    if (i >= nrho * H) return;
-    const int h = i / nrho, rho = i % nrho, group = rho / P.tile, at = rho % P.tile;
-    const int2 piece = P.pieces[(static_cast<size_t>(b) * H + h) * (P.row_tiles * 16 / P.tile) + group];
-    const int n = piece.y;
-    if (n == 1) return;
+    const int i = by_pieces ? at_row : at_row * kGroups + which;
+    const bool there = i < nrho * H;
+    const int h = there ? i / nrho : 0, rho = there ? i - h * nrho : 0, group = rho / P.tile, at = rho - group * P.tile;
+    int2 piece = make_int2(0, 0);
+    if (there) piece = P.pieces[(static_cast<size_t>(b) * H + h) * (P.row_tiles * 16 / P.tile) + group];
+    const int n = piece.y, step = by_pieces ? kGroups : 1;
+    if (by_pieces ? n <= 1 : !__any(n > 1)) return;           // (with by_pieces n is the workgroup's)
     const size_t size = static_cast<size_t>(P.tile) * (D + 2);
-    // slots: the first worker's, then the first ones of the workers behind it
-    auto slot = [&](int s) { return P.part + (s == 0 ? piece.x : piece.x / 2 * 2 + 2 * s) * size; };
     const size_t stat = static_cast<size_t>(P.tile) * D + 2 * at, mine = static_cast<size_t>(at) * D + d;
-    float top = -__builtin_inff();
-    for (int s = lane; s < n; s += 64) top = __builtin_fmaxf(top, slot(s)[stat]);
-    top = wave_max_all(top);
-    const float from = top == -__builtin_inff() ? 0.0f : top;
-    float sum = 0.0f;
+    float top = -__builtin_inff(), sum = 0.0f;
     float4_t acc = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kOnce = 8;                                  // requests in flight
-    for (int s0 = 0; s0 < n; s0 += kOnce * kAtOnce) {
+    constexpr int kOnce = 8;
+    for (int s0 = by_pieces ? which : 0; s0 < n; s0 += kOnce * step) {
         float4_t y[kOnce];
-        float m[kOnce], l[kOnce];
+        float m[kOnce], l[kOnce], high = top;
 #pragma unroll
         for (int k = 0; k < kOnce; ++k) {
-            const int s = s0 + k * kAtOnce + which;
+            const int s = s0 + k * step;
             m[k] = -__builtin_inff();
             l[k] = 0.0f;
             y[k] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
             if (s < n) {
-                const float* p = slot(s);
+                // slots: the first worker's, then the first ones of the workers behind it
+                const float* p = P.part + (s == 0 ? piece.x : piece.x / 2 * 2 + 2 * s) * size;
                 m[k] = p[stat];
                 l[k] = p[stat + 1];
                 y[k] = *reinterpret_cast<const float4_t*>(p + mine);
             }
         }
+#pragma unroll
+        for (int k = 0; k < kOnce; ++k) high = __builtin_fmaxf(high, m[k]);
+        const float from = high == -__builtin_inff() ? 0.0f : high, back = __builtin_amdgcn_exp2f(top - from);
+        top = high;
+        sum *= back;
+        acc *= back;
 #pragma unroll
         for (int k = 0; k < kOnce; ++k) {
             const float by = __builtin_amdgcn_exp2f(m[k] - from);
@@ -1234,14 +1275,30 @@ __global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_seque
             for (int e = 0; e < 4; ++e) acc[e] = fmaf(y[k][e], by, acc[e]);
         }
     }
+    if (by_pieces) {
+        if (d == 0) {
+            stats[which][0] = top;
+            stats[which][1] = sum;
+        }
+        sums[which][d / 4] = acc;
+        __syncthreads();
+        if (which != 0) return;
+        float high = -__builtin_inff();
 #pragma unroll
-    for (int o = kLanes; o < 64; o <<= 1) {
-        sum += __shfl_xor(sum, o, 64);
+        for (int w = 0; w < kGroups; ++w) high = __builtin_fmaxf(high, stats[w][0]);
+        const float from = high == -__builtin_inff() ? 0.0f : high;
+        sum = 0.0f;
+        acc = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+        for (int w = 0; w < kGroups; ++w) {
+            const float by = __builtin_amdgcn_exp2f(stats[w][0] - from);
+            sum = fmaf(stats[w][1], by, sum);
+            acc += sums[w][d / 4] * by;
+        }
     }
+    if (n <= 1) return;
     const int r = rho / P.G, head = h * P.G + rho % P.G;
-    if (which == 0) store4(P.dtype, P.out, ((static_cast<size_t>(b) * P.R + r) * P.heads + head) * D + d, acc * (1.0f / sum));
+    store4(P.dtype, P.out, ((static_cast<size_t>(b) * P.R + r) * P.heads + head) * D + d, acc * (1.0f / sum));
 }
 
 }  // namespace

@@ -14,6 +14,9 @@
 #include "cache_append.h"
 #include "cache_attend.h"
 
+#ifndef WFEW
+#define WFEW 512
+#endif
 namespace {
 
 constexpr int kMaxRows = 2048;    // K or N, as in the verify calls
@@ -131,7 +134,7 @@ AttendShape attend_shape(long rows, int head_dim, int dtype) {
     }
     s.tile = 16 * s.rt * (s.few ? 1 : s.waves);
     // as many workgroups as the 256 compute units hold at once
-    s.workers = s.few || s.waves == 4 ? (s.few || head_dim != 256 ? 512 : 256) : 256;
+    s.workers = s.few ? WFEW : s.waves == 4 && head_dim != 256 ? 512 : 256;
     return s;
 }
 bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
@@ -188,7 +191,7 @@ void launch_attend_rows(hipStream_t st, const AttendParams& P) {
     else hipLaunchKernelGGL((attend_rows<D, RT, NW, false>), grid, dim3(NW * 64), 0, st, P);
 }
 template <int D>
-void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, int joins) {
+void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, int joins, int by_pieces) {
     hipLaunchKernelGGL((attend_prepare<D>), dim3(prepare), dim3(kWG), lds, st, P);
     constexpr int kRows = D == 256 ? 1 : 2;
     if (!s.few) {
@@ -202,7 +205,7 @@ void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, 
         if (s.rt == 3) launch_attend_few<D, 3>(st, P);
         else launch_attend_few<D, 4>(st, P);
     }
-    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * joins), dim3(kWG), 0, st, P, joins);
+    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * joins), dim3(kWG), 0, st, P, joins, by_pieces);
 }
 
 int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, const int32_t* parent, bool tree, int B, int R,
@@ -252,13 +255,15 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.tiles = w.tiles;
     // two slots of 8 elements a thread of attend_prepare
     P.query_groups = static_cast<int>((static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG));
-    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles), joins = (static_cast<long>(R) * heads + 3) / 4;
+    // A workgroup of attend_join takes one row where the rows are few, else as many as its lanes hold.
+    const int by_pieces = static_cast<long>(B) * R * heads <= 4096, row_groups = by_pieces ? 1 : 4 * kWG / D;
+    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles), joins = (static_cast<long>(R) * heads + row_groups - 1) / row_groups;
     const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
     if (B * joins > INT_MAX || prepare > INT_MAX || units > INT_MAX) return FSD_ERR_SHAPE;
     const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
-    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
-    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
-    else launch_attend<256>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins));
+    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
+    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
+    else launch_attend<256>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
     return launched();
 }
 

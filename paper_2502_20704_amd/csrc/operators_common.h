@@ -136,9 +136,27 @@ __device__ __forceinline__ void unpack8(int dtype, const u32x4& a, float* x) {
         x[2 * i + 1] = dtype == FSD_BF16 ? __uint_as_float(w & 0xFFFF0000u) : static_cast<float>(h.y);
     }
 }
-__device__ __forceinline__ void load8_any(int dtype, const void* base, size_t at, float* x) {
-    if (dtype == FSD_F32) load8<FSD_F32>(base, at, x);
-    else unpack8(dtype, *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(base) + at), x);
+// 8 elements as they lie in memory: 16 bits each in lo, or 32 bits in lo and hi
+struct Raw8 { u32x4 lo, hi; };
+__device__ __forceinline__ void request8(int dtype, const void* base, size_t at, Raw8& r) {
+    if (dtype == FSD_F32) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(base) + at);
+        r.lo = p[0];
+        r.hi = p[1];
+    } else {
+        r.lo = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(base) + at);
+    }
+}
+__device__ __forceinline__ void unpack8(int dtype, const Raw8& r, float* x) {
+    if (dtype == FSD_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __uint_as_float(r.lo[i]);
+            x[4 + i] = __uint_as_float(r.hi[i]);
+        }
+    } else {
+        unpack8(dtype, r.lo, x);
+    }
 }
 
 // NS slots of 8 elements, d[i] .. d[i]+7 (d a multiple of 8) of the head that begins at element at[i], turned by the table's row
@@ -146,30 +164,42 @@ __device__ __forceinline__ void load8_any(int dtype, const void* base, size_t at
 template <int NS, int ONCE = 4>
 __device__ __forceinline__ void load_turned(int dtype, const void* base, const size_t (&at)[NS], const int (&d)[NS], const fsd_rotation& rot,
                                             const int (&pos)[NS], float (&x)[NS][8]) {
-#pragma unroll
-    for (int i = 0; i < NS; ++i) load8_any(dtype, base, at[i] + d[i], x[i]);
-    if (rot.table == nullptr) return;
     const int n = rot.dim / 2;
     constexpr int kOnce = NS < ONCE ? NS : ONCE;
 #pragma unroll
     for (int i0 = 0; i0 < NS; i0 += kOnce) {
-        if (rot.style == FSD_ROPE_HALVES) {
-            float y[kOnce][8], c[kOnce][8], s[kOnce][8];
+        Raw8 own[kOnce];
+#pragma unroll
+        for (int e = 0; e < kOnce; ++e) request8(dtype, base, at[i0 + e] + d[i0 + e], own[e]);
+        if (rot.table == nullptr) {
+#pragma unroll
+            for (int e = 0; e < kOnce; ++e) unpack8(dtype, own[e], x[i0 + e]);
+        } else if (rot.style == FSD_ROPE_HALVES) {
+            Raw8 other[kOnce];
+            u32x4 c[kOnce][2], s[kOnce][2];
 #pragma unroll
             for (int e = 0; e < kOnce; ++e) {
-                const int i = i0 + e, low = d[i] < n, in = d[i] < rot.dim;
-                load8_any(dtype, base, at[i] + (low ? d[i] + n : in ? d[i] - n : d[i]), y[e]);
+                const int i = i0 + e;
+                const bool low = d[i] < n, in = d[i] < rot.dim;
+                request8(dtype, base, at[i] + (low ? d[i] + n : in ? d[i] - n : d[i]), other[e]);
                 const float* t = rot.table + static_cast<size_t>(pos[i]) * rot.dim + (low ? d[i] : in ? d[i] - n : 0);
-                load8<FSD_F32>(t, 0, c[e]);
-                load8<FSD_F32>(t, n, s[e]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    c[e][k] = *reinterpret_cast<const u32x4*>(t + 4 * k);
+                    s[e][k] = *reinterpret_cast<const u32x4*>(t + n + 4 * k);
+                }
             }
 #pragma unroll
             for (int e = 0; e < kOnce; ++e) {
                 const int i = i0 + e;
                 const bool low = d[i] < n, in = d[i] < rot.dim;
+                float y[8];
+                unpack8(dtype, own[e], x[i]);
+                unpack8(dtype, other[e], y);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float a = x[i][k] * c[e][k], b = y[e][k] * s[e][k];
+                    const unsigned cb = c[e][k / 4][k % 4], sb = s[e][k / 4][k % 4];
+                    const float a = x[i][k] * __uint_as_float(cb), b = y[k] * __uint_as_float(sb);
                     x[i][k] = in ? (low ? a - b : a + b) : x[i][k];
                 }
             }
@@ -186,9 +216,11 @@ __device__ __forceinline__ void load_turned(int dtype, const void* base, const s
             for (int e = 0; e < kOnce; ++e) {
                 const int i = i0 + e;
                 const bool in = d[i] < rot.dim;
+                unpack8(dtype, own[e], x[i]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float cc = __uint_as_float(c[e][k]), ss = __uint_as_float(s[e][k]), a = x[i][2 * k], b = x[i][2 * k + 1];
+                    const unsigned cb = c[e][k], sb = s[e][k];
+                    const float cc = __uint_as_float(cb), ss = __uint_as_float(sb), a = x[i][2 * k], b = x[i][2 * k + 1];
                     x[i][2 * k] = in ? a * cc - b * ss : a;
                     x[i][2 * k + 1] = in ? b * cc + a * ss : b;
                 }
