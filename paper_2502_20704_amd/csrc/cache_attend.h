@@ -164,7 +164,7 @@ __device__ __forceinline__ int to_half_range(float most) {
 }
 
 constexpr int kMaxNodes = 2048;
-constexpr int kWalk = 64;           // depths up to this are found by walking
+constexpr int kWalk = 256;          // nodes of trees whose depths are found by walking
 
 __device__ __forceinline__ int not_kept(int x) {
     asm volatile("" : "+v"(x));
@@ -272,6 +272,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     short* depth = tree + R;
     short* stands = tree + 2 * R;
     bool bad_tree = false;
+    const bool deep = P.parent && R - 1 > kWalk;              // paths may be too long to walk up for every row
     if (P.parent) {
         const int32_t* parent = P.parent + static_cast<size_t>(b) * (R - 1);
         for (int r = tid; r < R; r += kThreads) {
@@ -284,46 +285,44 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             }
             up[r] = static_cast<short>(p);
         }
-        bad_tree = __syncthreads_or(bad_tree);
-        // depths: by walking up, which is short in most trees
-        bool far = false;
+        __syncthreads();
+    }
+    if (deep) {
+        // in deep ones by doubling: after step i a row knows its 2^i-th ancestor and how far that is
         for (int r = tid; r < R; r += kThreads) {
-            int n = 0;
-            for (int at = r; at > 0 && n <= kWalk; at = up[at]) ++n;
-            far |= n > kWalk;
-            depth[r] = static_cast<short>(n);
+            stands[r] = up[r];
+            depth[r] = r > 0 ? 1 : 0;
         }
-        if (__syncthreads_or(far)) {
-            // in deep ones by doubling: after step i a row knows its 2^i-th ancestor and how far that is
-            for (int r = tid; r < R; r += kThreads) {
-                stands[r] = up[r];
-                depth[r] = r > 0 ? 1 : 0;
+        __syncthreads();
+        for (;;) {
+            constexpr int kEach = (kMaxNodes + kThreads) / kThreads;
+            short jump[kEach], more[kEach];
+            bool moved = false;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = tid + i * kThreads, p = r < R ? stands[r] : -1;
+                jump[i] = p > 0 ? stands[p] : static_cast<short>(-1);
+                more[i] = p > 0 ? depth[p] : static_cast<short>(0);
+                moved |= p > 0;
+            }
+            if (!__syncthreads_or(moved)) break;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = tid + i * kThreads;
+                if (r >= R) continue;
+                depth[r] = static_cast<short>(depth[r] + more[i]);
+                stands[r] = jump[i];
             }
             __syncthreads();
-            for (;;) {
-                constexpr int kEach = (kMaxNodes + kThreads) / kThreads;
-                short jump[kEach], more[kEach];
-                bool moved = false;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int r = tid + i * kThreads, p = r < R ? stands[r] : -1;
-                    jump[i] = p > 0 ? stands[p] : static_cast<short>(-1);
-                    more[i] = p > 0 ? depth[p] : static_cast<short>(0);
-                    moved |= p > 0;
-                }
-                if (!__syncthreads_or(moved)) break;
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int r = tid + i * kThreads;
-                    if (r >= R) continue;
-                    depth[r] = static_cast<short>(depth[r] + more[i]);
-                    stands[r] = jump[i];
-                }
-                __syncthreads();
-            }
         }
     }
-    auto position = [&](int r) { return len + (P.parent ? depth[r] : r); };
+    auto position = [&](int r) {
+        if (!P.parent) return len + r;
+        if (deep) return len + depth[r];
+        int n = len;
+        for (int at = r; at > 0; at = up[at]) ++n;
+        return n;
+    };
     auto table_row = [&](int pos) { return P.rot.table ? min(pos, P.rot.rows - 1) : 0; };
     const bool fine = P.dtype == FSD_F16;
 
@@ -337,6 +336,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             if (P.rot.table)
                 for (int r = tid; r < share.rows; r += kThreads) bad |= position(r) >= P.rot.rows;
             bad = __syncthreads_or(bad);
+            bad_tree = __syncthreads_or(bad_tree);
             if (tid == 0) P.status[b] = (bad ? FSD_ROW_BAD_CACHE : 0) | (bad_tree ? FSD_ROW_BAD_PARENT : 0);
         }
         // a thread takes 8 dimensions of kSlots rows, D / 8 neighbours the whole of a row

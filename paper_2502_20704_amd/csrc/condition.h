@@ -16,7 +16,9 @@
 
 namespace {
 
-constexpr unsigned kInPrompt = 1u << 31;   // of a table word; the rest counts generated occurrences
+constexpr unsigned kInPrompt = 1u << 31;   // of a token's word; the low bits count its generated occurrences
+constexpr unsigned kElsewhere = 1u << 30;  // the token has a bias: the low bits say where its word and its bias stand
+constexpr int kConditionSlots = 4;         // 16-byte slots of a row that a thread takes, at most
 
 struct ConditionParams {
     const char* logits;
@@ -27,12 +29,13 @@ struct ConditionParams {
     int B, N, rows, V;
     int target;               // rows are contexts 0 .. N (target rows); 0: row r is the context of node r's parent
     int slice, nslices, rows_per_wg, ngroups;
+    int side;                 // biased tokens a slice can have
     long nwork;
 };
 
-// logit after penalties and bias
-__device__ __forceinline__ float conditioned(float z, unsigned word, float r, float f, float p, bool biased, float bias) {
-    if (word != 0) z = z > 0.0f ? __fdiv_rn(z, r) : z * r;
+// logit after penalties and bias; inv is 1 / r (a product costs one rounding of 2^-24 more than the quotient, and 20 instructions less)
+__device__ __forceinline__ float conditioned(float z, unsigned word, float r, float inv, float f, float p, bool biased, float bias) {
+    if (word != 0) z *= z > 0.0f ? inv : r;
     const unsigned count = word & ~kInPrompt;
     if (count != 0) {
         z = z - f * static_cast<float>(count);
@@ -41,8 +44,10 @@ __device__ __forceinline__ float conditioned(float z, unsigned word, float r, fl
     return biased ? z + bias : z;
 }
 
-template <bool BF16, bool TREE>
-__global__ __launch_bounds__(kWG) void condition_rows(ConditionParams P) {
+// Wavefronts a SIMD: bfloat16 has LDS for 4 workgroups a compute unit; binary32 tables are half as large, and 6 of them take 48 sequences of
+// 17 rows of 128259 entries 203 us where 5 take 242 (1536 workgroups: one round in place of 1.2).
+template <bool BF16, bool TREE, bool STREAM>
+__global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionParams P) {
     constexpr int VE = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
     extern __shared__ unsigned lds[];
     const long work = spread_over_xcds(blockIdx.x, P.nwork);
@@ -52,14 +57,15 @@ __global__ __launch_bounds__(kWG) void condition_rows(ConditionParams P) {
     const int v0 = si * P.slice, n = min(P.slice, P.V - v0);
     const int r0 = group * P.rows_per_wg, r1 = min(P.rows, r0 + P.rows_per_wg);
     const int tid = threadIdx.x, nb = P.c.bias_count;
-    unsigned* table = lds;                                   // [slice]
-    unsigned* touched = table + P.slice;                     // [slice / 32] the table or the biases say something
-    unsigned* which = touched + P.slice / 32;                // [slice] with biases: 1 + index of the last of this token
-    unsigned* wayed = which + (nb ? P.slice : 0);            // trees: [rows_per_wg / 32 + 1] the row's way has a token here
+    unsigned* table = lds;                                   // [slice] a word for every token
+    unsigned* touched = table + P.slice;                     // [slice / 32] its word or its bias says something
+    unsigned* side = touched + P.slice / 32;                 // [side][2] of biased tokens: word, 1 + index of the last bias
+    unsigned* taken = side + 2 * P.side;                     // how many of them there are
+    unsigned* wayed = taken + 1;                             // trees: [rows_per_wg / 32 + 1] the row's way has a token here
     short* up = reinterpret_cast<short*>(wayed + (TREE ? P.rows_per_wg / 32 + 1 : 0));   // trees: [N] parent
     short* here = up + (TREE ? P.N : 0);                     // trees: [N] token - v0, or -1
 
-    for (int i = tid; i < P.slice + P.slice / 32 + (nb ? P.slice : 0) + (TREE ? P.rows_per_wg / 32 + 1 : 0); i += kWG) lds[i] = 0;
+    for (int i = tid; i < P.slice + P.slice / 32 + 2 * P.side + 1 + (TREE ? P.rows_per_wg / 32 + 1 : 0); i += kWG) lds[i] = 0;
     const int32_t* tokens = P.tokens + static_cast<size_t>(b) * P.N;
     if constexpr (TREE) {
         const int32_t* parent = P.parent + static_cast<size_t>(b) * P.N;
@@ -71,39 +77,60 @@ __global__ __launch_bounds__(kWG) void condition_rows(ConditionParams P) {
         }
     }
     __syncthreads();
+    auto touch = [&](unsigned at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
+    auto place = [&](int t, unsigned& at) {                  // whether a token is of this slice, and where
+        at = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
+        return at < static_cast<unsigned>(n);
+    };
+    if (nb > 0) {
+        // biased tokens move out of the table: one of those that name a token finds it a place, then the last one is noted there
+        const int32_t* list = P.c.bias_tokens + static_cast<size_t>(b) * nb;
+        unsigned at;
+        for (int i = tid; i < nb; i += kWG)
+            if (place(list[i], at) && atomicCAS(&table[at], 0u, kElsewhere) == 0u) {
+                atomicOr(&table[at], atomicAdd(taken, 1u));
+                touch(at);
+            }
+        __syncthreads();
+        for (int i = tid; i < nb; i += kWG)
+            if (place(list[i], at)) atomicMax(&side[2 * (table[at] & ~kElsewhere) + 1], static_cast<unsigned>(i) + 1u);
+    }
+    auto word_of = [&](unsigned at) -> unsigned* {
+        const unsigned w = nb > 0 ? table[at] : 0u;
+        return (w & kElsewhere) != 0 ? &side[2 * (w & ~kElsewhere)] : &table[at];
+    };
     auto say = [&](unsigned at, unsigned add) {
-        atomicAdd(&table[at], add);
-        atomicOr(&touched[at >> 5], 1u << (at & 31));
+        atomicAdd(word_of(at), add);
+        touch(at);
     };
     if (P.c.history) {
         const int32_t* h = P.c.history + static_cast<size_t>(b) * P.c.history_stride;
         int len = P.c.history_len ? P.c.history_len[b] : P.c.history_stride;
         len = max(0, min(len, P.c.history_stride));
-        int prompt = P.c.prompt_len ? P.c.prompt_len[b] : 0;
+        const int prompt = P.c.prompt_len ? P.c.prompt_len[b] : 0;
         auto one = [&](int i, int t) {
-            const unsigned at = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
-            if (at < static_cast<unsigned>(n)) {
-                if (i < prompt) {
-                    atomicOr(&table[at], kInPrompt);
-                    atomicOr(&touched[at >> 5], 1u << (at & 31));
-                } else {
-                    say(at, 1u);
-                }
+            unsigned at;
+            if (!place(t, at)) return;
+            if (i < prompt) {
+                atomicOr(word_of(at), kInPrompt);
+                touch(at);
+            } else {
+                say(at, 1u);
             }
         };
-        int i = tid;
-        for (; i + 3 * kWG < len; i += 4 * kWG) {            // four requests in flight
-            const int t0 = h[i], t1 = h[i + kWG], t2 = h[i + 2 * kWG], t3 = h[i + 3 * kWG];
-            one(i, t0); one(i + kWG, t1); one(i + 2 * kWG, t2); one(i + 3 * kWG, t3);
+        // (four requests of 16 bytes a thread in flight: the histories of a sequence's slices come from one L2, what counts is latency)
+        constexpr int kOnce = 4 * kWG, kAhead = 4;
+        auto four = [&](int e, const uint4& x) { one(e, x.x); one(e + 1, x.y); one(e + 2, x.z); one(e + 3, x.w); };
+        int i = 0;
+        for (; i + kAhead * kOnce <= len; i += kAhead * kOnce) {
+            uint4 x[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) x[k] = load_any16(reinterpret_cast<const char*>(h + i + k * kOnce + 4 * tid));
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) four(i + k * kOnce + 4 * tid, x[k]);
         }
-        for (; i < len; i += kWG) one(i, h[i]);
-    }
-    for (int i = tid; i < nb; i += kWG) {
-        const unsigned at = static_cast<unsigned>(P.c.bias_tokens[static_cast<size_t>(b) * nb + i]) - static_cast<unsigned>(v0);
-        if (at < static_cast<unsigned>(n)) {
-            atomicMax(&which[at], static_cast<unsigned>(i) + 1u);
-            atomicOr(&touched[at >> 5], 1u << (at & 31));
-        }
+        for (; i + kOnce <= len; i += kOnce) four(i + 4 * tid, load_any16(reinterpret_cast<const char*>(h + i + 4 * tid)));
+        for (i += tid; i < len; i += kWG) one(i, h[i]);
     }
     if constexpr (TREE) {
         for (int r = r0 + tid; r < r1; r += kWG) {
@@ -113,17 +140,17 @@ __global__ __launch_bounds__(kWG) void condition_rows(ConditionParams P) {
         }
     } else {
         for (int j = tid; j < min(r0, P.N); j += kWG) {      // the candidates on the way to the first row
-            const unsigned at = static_cast<unsigned>(tokens[j]) - static_cast<unsigned>(v0);
-            if (at < static_cast<unsigned>(n)) say(at, 1u);
+            unsigned at;
+            if (place(tokens[j], at)) say(at, 1u);
         }
     }
     __syncthreads();
-    const float rep = P.c.repetition ? P.c.repetition[b] : 1.0f;
+    const float rep = P.c.repetition ? P.c.repetition[b] : 1.0f, inv_rep = 1.0f / rep;
     const float freq = P.c.frequency ? P.c.frequency[b] : 0.0f, pres = P.c.presence ? P.c.presence[b] : 0.0f;
     const float* bias = P.c.bias_values + static_cast<size_t>(b) * nb;
     const int words = (P.V + 31) / 32;
 
-    // a node's token is taken into the table, or out of it (the bit stays: a zero word says nothing)
+    // the tokens on the way to a row are taken into the table, or out of it (the bit stays: a zero word says nothing)
     auto along = [&](int r, unsigned add) {
         if (tid == 0) {
             for (int j = P.target ? r - 1 : up[r]; j >= 0; j = up[j])
@@ -131,69 +158,117 @@ __global__ __launch_bounds__(kWG) void condition_rows(ConditionParams P) {
         }
     };
     auto adjusted = [&](float z, int at) {
-        const unsigned w = nb ? which[at] : 0u;
-        return conditioned(z, table[at], rep, freq, pres, w != 0, w != 0 ? bias[w - 1] : 0.0f);
+        unsigned w = table[at], last = 0;
+        if ((w & kElsewhere) != 0) {
+            const unsigned* s = &side[2 * (w & ~kElsewhere)];
+            w = s[0];
+            last = s[1];
+        }
+        return conditioned(z, w, rep, inv_rep, freq, pres, last != 0, last != 0 ? bias[last - 1] : 0.0f);
     };
+    auto meet = []() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };   // (of LDS: what is requested stays so)
+    // A thread's slots of a row are requested while it works on the row before, their masks one row earlier still: a slot
+    // without an allowed entry is not read.
+    constexpr unsigned kAll = (1u << VE) - 1u;
+    auto row_at = [&](int r) { return ((static_cast<size_t>(b) * P.rows + r) * P.V + v0) * ES; };
+    auto masks = [&](int r, unsigned (&ok)[kConditionSlots]) {
+        if (P.c.allowed && r < r1) {
+            const int context = P.c.allowed_contexts == 1 ? 0 : TREE && !P.target ? up[r] + 1 : r;
+            const uint32_t* mask = P.c.allowed + (static_cast<size_t>(b) * P.c.allowed_contexts + context) * words + v0 / 32;
+#pragma unroll
+            for (int k = 0; k < kConditionSlots; ++k) {
+                const int at = (tid + k * kWG) * VE;
+                ok[k] = at < n ? mask[at >> 5] : 0u;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kConditionSlots; ++k) ok[k] = ~0u;
+        }
+    };
+    auto mask_of = [&](unsigned word, int k) { return word >> ((tid + k * kWG) * VE & 31) & kAll; };
+    auto request = [&](int r, const unsigned (&ok)[kConditionSlots], uint4 (&w)[kConditionSlots]) {
+        if (r >= r1) return;
+        const char* in = P.logits + row_at(r);
+#pragma unroll
+        for (int k = 0; k < kConditionSlots; ++k) {
+            const int at = (tid + k * kWG) * VE;
+            if (at + VE <= n && mask_of(ok[k], k) != 0) w[k] = load_any16<STREAM>(in + static_cast<size_t>(at) * ES);
+        }
+    };
+    unsigned ok[kConditionSlots], ok1[kConditionSlots], ok2[kConditionSlots];
+    uint4 now[kConditionSlots], next[kConditionSlots];
+    masks(r0, ok);
+    masks(r0 + 1, ok1);
+    request(r0, ok, now);
     for (int r = r0; r < r1; ++r) {
+        request(r + 1, ok1, next);
+        masks(r + 2, ok2);
         bool mine = false;
         if constexpr (TREE) {
             mine = (wayed[(r - r0) >> 5] >> ((r - r0) & 31)) & 1u;
             if (mine) {
-                __syncthreads();
+                meet();
                 along(r, 1u);
-                __syncthreads();
+                meet();
             }
         } else if (r > r0) {                                  // (uniform: every thread reads the same token)
-            const unsigned at = static_cast<unsigned>(tokens[r - 1]) - static_cast<unsigned>(v0);
-            if (at < static_cast<unsigned>(n)) {
-                __syncthreads();
+            unsigned at;
+            if (place(tokens[r - 1], at)) {
+                meet();
                 if (tid == 0) say(at, 1u);
-                __syncthreads();
+                meet();
             }
         }
-        const int context = TREE && !P.target ? up[r] + 1 : r;
-        const size_t row = (static_cast<size_t>(b) * P.rows + r) * P.V + v0;
-        const char* in = P.logits + row * ES;
-        char* out = P.out + row * ES;
-        const uint32_t* mask = nullptr;
-        if (P.c.allowed)
-            mask = P.c.allowed + (static_cast<size_t>(b) * P.c.allowed_contexts + (P.c.allowed_contexts > 1 ? context : 0)) * words + v0 / 32;
-        constexpr unsigned kAll = (1u << VE) - 1u;
-        for (int at = tid * VE; at < n; at += kWG * VE) {
-            unsigned ok = mask ? (mask[at >> 5] >> (at & 31)) & kAll : kAll;
+        const char* in = P.logits + row_at(r);
+        char* out = P.out + row_at(r);
+#pragma unroll
+        for (int k = 0; k < kConditionSlots; ++k) {
+            const int at = (tid + k * kWG) * VE;
+            if (at >= n) continue;
+            const unsigned let = mask_of(ok[k], k);
             if (at + VE <= n) {
                 uint4 w = neg_inf_slot<BF16>();
-                if (ok != 0) {                                // (a slot without an allowed entry is not read)
-                    w = load_any16(in + static_cast<size_t>(at) * ES);
-                    unsigned t = (touched[at >> 5] >> (at & 31)) & ok;
-                    if ((t | (ok ^ kAll)) != 0) {
-                        float z[VE];
-                        unpack_slot<BF16>(w, z);
-                        const uint4 raw = w;
-#pragma unroll
-                        for (int e = 0; e < VE; ++e)
-                            if (t >> e & 1u) z[e] = adjusted(z[e], at + e);
-                        w = repack_slot<BF16>(raw, z, t, ok);
+                if (let != 0) {
+                    // one touched entry of every lane's slot at a time: there are few, and each costs a wavefront the same
+                    unsigned a = now[k].x, c = now[k].y, d = now[k].z, f = now[k].w;
+                    for (unsigned t = (touched[at >> 5] >> (at & 31)) & let; t != 0; t &= t - 1) {
+                        const int e = __builtin_ctz(t), i = BF16 ? e >> 1 : e, up_by = BF16 ? 16 * (e & 1) : 0;
+                        const unsigned of = (BF16 ? 0xFFFFu : ~0u) << up_by, old = i < 2 ? (i == 0 ? a : c) : (i == 2 ? d : f);
+                        const float z = adjusted(__uint_as_float(BF16 ? (old >> up_by) << 16 : old), at + e);
+                        const unsigned put = (old & ~of) | (BF16 ? bf16_bits(z) << up_by : __float_as_uint(z));
+                        a = i == 0 ? put : a;
+                        c = i == 1 ? put : c;
+                        d = i == 2 ? put : d;
+                        f = i == 3 ? put : f;
                     }
+                    w = make_uint4(a, c, d, f);
+                    if (let != kAll) w = masked_slot<BF16>(w, let);
                 }
-                store_any16(out + static_cast<size_t>(at) * ES, w);
+                store_any16<STREAM>(out + static_cast<size_t>(at) * ES, w);
             } else {
                 for (int e = 0; at + e < n; ++e) {            // the end of a ragged row
                     float z = load_logit<BF16>(in, at + e);
-                    if ((touched[at >> 5] >> ((at + e) & 31)) & 1u) {
+                    if (!(let >> e & 1u)) {
+                        store_logit<BF16>(out, at + e, -__builtin_inff());
+                    } else if ((touched[at >> 5] >> ((at + e) & 31)) & 1u) {
                         z = adjusted(z, at + e);
-                        if (ok >> e & 1u) store_logit<BF16>(out, at + e, z);
-                    } else if (ok >> e & 1u) {
+                        store_logit<BF16>(out, at + e, z);
+                    } else {
                         copy_logit<BF16>(out, in, at + e);
                     }
-                    if (!(ok >> e & 1u)) store_logit<BF16>(out, at + e, -__builtin_inff());
                 }
             }
         }
+#pragma unroll
+        for (int k = 0; k < kConditionSlots; ++k) {
+            now[k] = next[k];
+            ok[k] = ok1[k];
+            ok1[k] = ok2[k];
+        }
         if (TREE && mine) {
-            __syncthreads();
+            meet();
             along(r, 0xFFFFFFFFu);                            // (adds -1)
-            __syncthreads();
+            meet();
         }
     }
 }

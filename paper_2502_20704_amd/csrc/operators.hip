@@ -14,9 +14,6 @@
 #include "cache_append.h"
 #include "cache_attend.h"
 
-#ifndef WFEW
-#define WFEW 512
-#endif
 namespace {
 
 constexpr int kMaxRows = 2048;    // K or N, as in the verify calls
@@ -27,7 +24,19 @@ inline int launched() { return hipGetLastError() == hipSuccess ? FSD_OK : FSD_ER
 
 // ------------------------------------------------------------------------------------------ conditioning
 
-constexpr long kConditionWGs = 1024;   // workgroups aimed at: 4 a compute unit
+constexpr long kConditionWGs = 1024;   // workgroups aimed at: 4 a compute unit, which is what their LDS allows at once
+
+template <bool BF16>
+void launch_condition(hipStream_t st, unsigned grid, size_t lds, bool tree, bool stream, const ConditionParams& P) {
+    const dim3 g(grid), t(kWG);
+    if (tree) {
+        if (stream) hipLaunchKernelGGL((condition_rows<BF16, true, true>), g, t, lds, st, P);
+        else hipLaunchKernelGGL((condition_rows<BF16, true, false>), g, t, lds, st, P);
+    } else {
+        if (stream) hipLaunchKernelGGL((condition_rows<BF16, false, true>), g, t, lds, st, P);
+        else hipLaunchKernelGGL((condition_rows<BF16, false, false>), g, t, lds, st, P);
+    }
+}
 
 int condition(const void* logits, const int32_t* tokens, const int32_t* parent, int B, int N, int rows, int V, int dtype,
               const fsd_conditions* conditions, void* out, bool tree, hipStream_t st) {
@@ -37,7 +46,7 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
         V > fsd_max_vocab(dtype) || static_cast<long>(B) * rows >= (1L << 24))
         return FSD_ERR_SHAPE;
     const fsd_conditions& c = *conditions;
-    if (c.history_stride < 0 || c.bias_count < 0) return FSD_ERR_SHAPE;
+    if (c.history_stride < 0 || c.history_stride > (1 << 29) || c.bias_count < 0) return FSD_ERR_SHAPE;
     if (c.bias_count > 0 && (!c.bias_tokens || !c.bias_values)) return FSD_ERR_NULL;
     if (c.allowed && c.allowed_contexts != 1 && c.allowed_contexts != N + 1) return FSD_ERR_SHAPE;
     const size_t es = dtype == FSD_BF16 ? 2 : 4;
@@ -52,8 +61,11 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     P.B = B; P.N = N; P.rows = rows; P.V = V;
     P.target = rows == N + 1;
     // A workgroup's slice: the fewer, the fewer times a history is read; but a call of few rows wants workgroups on all compute units.
-    P.slice = 4096;
+    P.slice = kConditionSlots * kWG * (dtype == FSD_BF16 ? 8 : 4);
     while (P.slice > 1024 && static_cast<long>(B) * rows * ((V + P.slice - 1) / P.slice) < kConditionWGs) P.slice /= 2;
+    // (many biases: their places and the table share 64 KB with the tree)
+    auto lds_of = [&](int slice) { return static_cast<size_t>(slice) * 4 + slice / 8 + static_cast<size_t>(c.bias_count < slice ? c.bias_count : slice) * 8 + 4; };
+    while (P.slice > 1024 && lds_of(P.slice) > (52u << 10)) P.slice /= 2;
     P.nslices = (V + P.slice - 1) / P.slice;
     const long pieces = static_cast<long>(B) * P.nslices;
     long per = pieces * rows / kConditionWGs;
@@ -65,16 +77,15 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     P.nwork = pieces * P.ngroups;
     const long grid = grid_over_xcds(P.nwork);
     if (grid > INT_MAX) return FSD_ERR_SHAPE;
-    size_t lds = static_cast<size_t>(P.slice) * 4 * (c.bias_count ? 2 : 1) + P.slice / 8;
+    P.side = c.bias_count < P.slice ? c.bias_count : P.slice;
+    size_t lds = lds_of(P.slice);
     if (tree) lds += (static_cast<size_t>(P.rows_per_wg) / 32 + 1) * 4 + static_cast<size_t>(N) * 4;
-    const dim3 g(static_cast<unsigned>(grid)), t(kWG);
-    if (dtype == FSD_BF16) {
-        if (tree) hipLaunchKernelGGL((condition_rows<true, true>), g, t, lds, st, P);
-        else hipLaunchKernelGGL((condition_rows<true, false>), g, t, lds, st, P);
-    } else {
-        if (tree) hipLaunchKernelGGL((condition_rows<false, true>), g, t, lds, st, P);
-        else hipLaunchKernelGGL((condition_rows<false, false>), g, t, lds, st, P);
-    }
+    // Past the caches where the logits are more than these hold and lines are written whole: 64 sequences of 9 rows of 128256 bfloat16
+    // entries 77 -> 73 us; but 48 of 17 rows of 128259 binary32 entries 203 -> 207, and a small call's reader finds its rows in the caches.
+    const size_t bytes = static_cast<size_t>(B) * rows * V * es;
+    const bool stream = bytes >= (64u << 20) && V * es % 16 == 0 && aligned16(logits) && aligned16(out);
+    if (dtype == FSD_BF16) launch_condition<true>(st, static_cast<unsigned>(grid), lds, tree, stream, P);
+    else launch_condition<false>(st, static_cast<unsigned>(grid), lds, tree, stream, P);
     return launched();
 }
 
@@ -102,15 +113,16 @@ int check_rotation(const fsd_rotation* r, int head_dim, fsd_rotation* out) {
 }
 
 template <int DT, int D>
-void launch_append(hipStream_t st, const AppendParams& P, bool few) {
-    if (few) hipLaunchKernelGGL((append_rows<DT, D, 64>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
-    else hipLaunchKernelGGL((append_rows<DT, D, kWG>), dim3(P.npieces), dim3(kWG), 0, st, P);
+void launch_append(hipStream_t st, const AppendParams& P, int tokens) {
+    if (tokens <= 8) hipLaunchKernelGGL((append_few<DT, D, 8>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
+    else if (tokens <= 16) hipLaunchKernelGGL((append_few<DT, D, 16>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
+    else hipLaunchKernelGGL((append_many<DT, D>), dim3(P.npieces), dim3(kWG), 0, st, P);
 }
 template <int DT>
-void launch_append_d(hipStream_t st, const AppendParams& P, bool few) {
-    if (P.cache.head_dim == 64) launch_append<DT, 64>(st, P, few);
-    else if (P.cache.head_dim == 128) launch_append<DT, 128>(st, P, few);
-    else launch_append<DT, 256>(st, P, few);
+void launch_append_d(hipStream_t st, const AppendParams& P, int tokens) {
+    if (P.cache.head_dim == 64) launch_append<DT, 64>(st, P, tokens);
+    else if (P.cache.head_dim == 128) launch_append<DT, 128>(st, P, tokens);
+    else launch_append<DT, 256>(st, P, tokens);
 }
 
 // ------------------------------------------------------------------------------------------ attention
@@ -134,7 +146,7 @@ AttendShape attend_shape(long rows, int head_dim, int dtype) {
     }
     s.tile = 16 * s.rt * (s.few ? 1 : s.waves);
     // as many workgroups as the 256 compute units hold at once
-    s.workers = s.few ? WFEW : s.waves == 4 && head_dim != 256 ? 512 : 256;
+    s.workers = s.few ? 512 : s.waves == 4 && head_dim != 256 ? 512 : 256;
     return s;
 }
 bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
@@ -305,15 +317,15 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
     P.cache = *cache;
     P.len_out = cache_len_out;
     P.status = row_status;
-    P.slots = (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
+    // up to 16 rows: a wavefront a head, whichever blocks they touch; else a workgroup for each block
+    P.slots = P.max_rows <= 16 ? 1 : (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
     const long pieces = static_cast<long>(cache->layers) * B * H * P.slots;
     if (pieces > INT_MAX - 8) return FSD_ERR_SHAPE;
     P.npieces = static_cast<unsigned>(pieces);
-    const bool few = P.max_rows <= 16;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, few);
-    else if (dtype == FSD_BF16) launch_append_d<FSD_BF16>(st, P, few);
-    else launch_append_d<FSD_F16>(st, P, few);
+    if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, P.max_rows);
+    else if (dtype == FSD_BF16) launch_append_d<FSD_BF16>(st, P, P.max_rows);
+    else launch_append_d<FSD_F16>(st, P, P.max_rows);
     return launched();
 }
 

@@ -31,14 +31,21 @@ inline long grid_over_xcds(long n) { return (n + kXcds - 1) / kXcds * kXcds; }
 
 // ---- logits, in 16-byte slots at any address of whole elements
 
+// (STREAM: past the caches, for what is not read again soon)
+template <bool STREAM = false>
 __device__ __forceinline__ uint4 load_any16(const char* p) {
-    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
+    const u32x4_any* at = reinterpret_cast<const u32x4_any*>(p);
+    u32x4_any v;
+    if constexpr (STREAM) v = __builtin_nontemporal_load(at);
+    else v = *at;
     return make_uint4(v.x, v.y, v.z, v.w);
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store_any16(char* p, const uint4& w) {
     u32x4_any v;
     v.x = w.x; v.y = w.y; v.z = w.z; v.w = w.w;
-    *reinterpret_cast<u32x4_any*>(p) = v;
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(p));
+    else *reinterpret_cast<u32x4_any*>(p) = v;
 }
 template <bool BF16>
 __device__ __forceinline__ uint4 neg_inf_slot() {
@@ -48,36 +55,15 @@ __device__ __forceinline__ uint4 neg_inf_slot() {
 __device__ __forceinline__ unsigned bf16_bits(float z) {
     return static_cast<unsigned>(__builtin_bit_cast(unsigned short, static_cast<__bf16>(z)));   // to nearest, ties to even
 }
+// the slot with -inf in the entries that `ok` lacks
 template <bool BF16>
-__device__ __forceinline__ void unpack_slot(const uint4& r, float* x) {
-    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+__device__ __forceinline__ uint4 masked_slot(const uint4& r, unsigned ok) {
+    unsigned w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        } else {
-            x[i] = __uint_as_float(w[i]);
-        }
-    }
-}
-// the slot with z in the entries of `changed`, -inf in those that `ok` lacks, and the raw bits elsewhere
-template <bool BF16>
-__device__ __forceinline__ uint4 repack_slot(const uint4& raw, const float* z, unsigned changed, unsigned ok) {
-    unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) {
-            unsigned lo = w[i] & 0xFFFFu, hi = w[i] >> 16;
-            if (changed >> (2 * i) & 1u) lo = bf16_bits(z[2 * i]);
-            if (changed >> (2 * i + 1) & 1u) hi = bf16_bits(z[2 * i + 1]);
-            if (!(ok >> (2 * i) & 1u)) lo = 0xFF80u;
-            if (!(ok >> (2 * i + 1) & 1u)) hi = 0xFF80u;
-            w[i] = lo | hi << 16;
-        } else {
-            if (changed >> i & 1u) w[i] = __float_as_uint(z[i]);
-            if (!(ok >> i & 1u)) w[i] = 0xFF800000u;
-        }
+        auto all = [&](int bit) { return static_cast<unsigned>(static_cast<int>(ok << (31 - bit)) >> 31); };   // the bit, 32 times
+        const unsigned keep = BF16 ? (all(2 * i) & 0xFFFFu) | (all(2 * i + 1) & 0xFFFF0000u) : all(i);
+        w[i] = (w[i] & keep) | ((BF16 ? 0xFF80FF80u : 0xFF800000u) & ~keep);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
