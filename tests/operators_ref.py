@@ -123,8 +123,8 @@ def block_values(v_codes):
     return np.swapaxes(v, -1, -2).reshape(*v.shape[:-3], BLOCK, v.shape[-2])
 
 
-def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halves, dtype):
-    """(out [B,R,heads,D], bound) in 64 bits.  cache: dict of numpy arrays as fsd.Cache names them.
+def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halves, dtype, left_out=()):
+    """(out [B,R,heads,D], bound) in 64 bits; left_out: (sequence, block of it) pairs none of whose tokens counts.  cache: dict of numpy arrays as fsd.Cache names them.
 
     The bound: a product's error is scale * sum |q||k| times (one rounding of q to 11 bits, for the rows' keys one of k as well,
     4 more of 2^-24 each for the rotation of either, D sums of 2^-24), delta for the row's largest.  Weights then lie within
@@ -146,7 +146,11 @@ def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halve
         qa, ka = np.abs(q[b, :count]), np.abs(k[b, :count])
         if turns is not None:                                    # |a cos - b sin| is at most |a| + |b|
             qa, ka = qa + np.abs(qr), ka + np.abs(kr)
-        blocks = table[b, :(n + BLOCK - 1) // BLOCK]
+        blocks = table[b, :(n + BLOCK - 1) // BLOCK].copy()
+        held = np.ones(n, dtype=bool)
+        for bb, j in left_out:
+            if bb == b:
+                blocks[j], held[64 * j:64 * j + 64] = 0, False
         sees = np.zeros((count, count), dtype=bool)
         for r, w in enumerate(ways):
             sees[r, w] = True
@@ -156,7 +160,7 @@ def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halve
             kk = np.concatenate([ck.reshape(-1, D)[:n], kr[:, h]])
             vv = np.concatenate([cv.reshape(-1, D)[:n], v[b, :count, h]])
             kabs = np.concatenate([np.abs(ck.reshape(-1, D)[:n]) * 1.0, ka[:, h] * 2.0])
-            seen = np.concatenate([np.ones((count, n), dtype=bool), sees], 1)
+            seen = np.concatenate([np.broadcast_to(held, (count, n)), sees], 1)
             for i in range(h * G, h * G + G):
                 with np.errstate(invalid="ignore", over="ignore"):
                     s = qr[:, i] @ np.nan_to_num(kk, nan=0.0, posinf=0.0, neginf=0.0).T * scale

@@ -340,3 +340,515 @@ def test_append(counts, lens, R, H, D, dtype, L, tree, turn, halves, big):
     rest = [i for i in range(P) if i not in touched]
     for name, a in (("k_codes", new_k), ("v_codes", new_v), ("k_scale", ks), ("v_scale", vs)):
         assert np.array_equal(a[:, rest], c[name][:, rest]), name
+
+
+# ------------------------------------------------------------------------------------------ attention: edges
+
+
+def _case(rng, lens, R, heads, H, D, dt, *, L=1, top=0x70, extra=0, scale_exponents=None):
+    B = len(lens)
+    table, P = _tables(rng, B, max(1, (max(lens) + 63) // 64) + extra)
+    c = _random_cache(rng, L, P, H, D, table, lens, top=top)
+    if scale_exponents is not None:
+        for n in ("k_scale", "v_scale"):
+            c[n] = np.exp2(rng.integers(*scale_exponents, c[n].shape)).astype(np.float32)
+    mixed = torch.from_numpy(rng.standard_normal((B, R, heads + 2 * H, D)) * 0.7).to(dt).cuda()
+    return table, c, mixed[:, :, :heads], mixed[:, :, heads:heads + H], mixed[:, :, heads + H:]
+
+
+def _within(got, want, bound, what=""):
+    d = np.abs(_host(got) - want)
+    assert (d <= bound).all(), f"{what}: {(d / np.maximum(bound, 1e-30)).max():.2f} bounds"
+
+
+SHAPES = [
+    # lens, R, heads, kv_heads, D, dtype, tree: rows of an item and types that the list above lacks
+    ([700, 3], 5, 7, 1, 128, "f16", False),             # 35 rows, binary16
+    ([200], 3, 48, 2, 64, "bf16", False),               # 72 rows at head_dim 64
+    ([150, 64], 2, 64, 2, 64, "f16", False),            # 64 rows, binary16
+    ([150, 64], 2, 64, 2, 64, "bf16", False),
+    ([100, 31], 1, 64, 1, 128, "bf16", False),          # 64 query heads on one key head
+    ([90], 6, 4, 4, 256, "f16", True),
+    ([90, 700], 24, 4, 4, 256, "f16", True),
+    ([500], 25, 1, 1, 256, "bf16", True),
+    ([128, 129, 127], 1, 16, 16, 128, "bf16", False),
+    ([1] * 300, 2, 2, 1, 64, "bf16", False),            # more sequences than a workgroup has threads
+    (list(range(0, 1400, 2)), 1, 4, 2, 64, "f16", False),
+]
+
+
+@pytest.mark.parametrize("lens,R,heads,H,D,dtype,tree", SHAPES)
+def test_attend_shapes(lens, R, heads, H, D, dtype, tree):
+    rng = np.random.default_rng(len(lens) * 100 + R + D)
+    B, dt = len(lens), DT[dtype]
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, dt)
+    parent = _rand_parents(rng, B, R - 1) if tree else None
+    turns = _turns(max(lens) + R, D)
+    cache = _to_cache(c, table, lens)
+    if tree:
+        got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, rotation=_rotation(turns, True))
+    else:
+        got = fsd.fsd_attend_chain(q, k, v, cache, rotation=_rotation(turns, True))
+    torch.cuda.synchronize()
+    assert (got["row_status"].cpu().numpy() == 0).all()
+    want, bound = ref.attend(_host(q), _host(k), _host(v), parent, np.full(B, R), c, 0, lens, table, D ** -0.5, turns, True, dt)
+    _within(got["out"], want, bound)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attend_scales(scale, dtype):
+    """Any finite scale: none at all (every token counts the same), a negative one, one that leaves a row a single token; and value
+    scales of blocks that lie 2^24 apart."""
+    rng = np.random.default_rng(3)
+    lens = [300, 70]
+    table, c, q, k, v = _case(rng, lens, 4, 6, 2, 128, DT[dtype], scale_exponents=(-16, 8))
+    c["k_scale"][:] = 2.0 ** -8
+    got = fsd.fsd_attend_chain(q, k, v, _to_cache(c, table, lens), scale=scale)["out"]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(2, 4), c, 0, lens, table, scale, None, True, DT[dtype])
+    # the weights of a block count relative to the largest contribution, not to the largest weight: an output of small values
+    # beside a block of large ones is off by 2^-24 of the latter's (the bound's term in max |v|)
+    _within(got, want, bound)
+
+
+def test_attend_large_magnitudes():
+    """Queries, keys and values far outside binary16's range, and rows of zeros."""
+    rng = np.random.default_rng(4)
+    lens = [130]
+    table, c, q, k, v = _case(rng, lens, 5, 4, 2, 64, torch.bfloat16)
+    q, k, v = q * 2.0 ** 60, k.clone() * 2.0 ** -70, v.clone() * 2.0 ** 90
+    q[0, 1] = 0
+    k[0, 2], v[0, 3] = 0, 0
+    c["k_scale"][:] = 2.0 ** -70
+    c["v_scale"][:] = 2.0 ** 80
+    got = fsd.fsd_attend_chain(q.contiguous(), k.contiguous(), v.contiguous(), _to_cache(c, table, lens), scale=16.0)["out"]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(1, 5), c, 0, lens, table, 16.0, None, True, torch.bfloat16)
+    _within(got, want, bound)
+
+
+def test_attend_what_is_not_seen_does_not_matter():
+    """NaN and infinities in keys and values of rows that a row does not see leave its result bit for bit; rows that see them are NaN."""
+    rng = np.random.default_rng(6)
+    lens, R = [100], 6
+    table, c, q, k, v = _case(rng, lens, R, 4, 2, 128, torch.bfloat16)
+    parent = torch.tensor([[-1, 0, -1, 2, 3]], dtype=torch.int32, device="cuda")        # rows 1-2 and 3-4-5
+    cache = _to_cache(c, table, lens)
+    q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    clean = fsd.fsd_attend_tree(q, k, v, parent, cache)["out"].clone()
+    chain = fsd.fsd_attend_chain(q, k, v, cache)["out"].clone()
+    for t, x in ((k, float("nan")), (v, float("nan")), (v, float("inf")), (v, -float("inf"))):
+        bad = t.clone()
+        bad[0, 3, 1, 7] = x
+        kk, vv = (bad, v) if t is k else (k, bad)
+        got = fsd.fsd_attend_tree(q, kk, vv, parent, cache)["out"]
+        assert torch.equal(got[0, :3], clean[0, :3]) and torch.equal(got[0, 3:, :2], clean[0, 3:, :2])
+        assert torch.isnan(got[0, 3:, 2:]).all()
+        got = fsd.fsd_attend_chain(q, kk, vv, cache)["out"]
+        assert torch.equal(got[0, :3], chain[0, :3]) and torch.isnan(got[0, 3:, 2:]).all()
+
+
+@pytest.mark.parametrize("G", [1, 8])
+def test_attend_out_of_range(G):
+    """What the device finds out of range is reported and taken as the header says; the other sequences are not concerned."""
+    rng = np.random.default_rng(7)
+    lens = [200, 130, 64, 10, 70, 300]
+    B, R, H, D, dt = len(lens), 9, 2, 64, torch.bfloat16
+    table, c, q, k, v = _case(rng, lens, R, H * G, H, D, dt)
+    per, P = table.shape[1], c["k_scale"].shape[1]
+    parent = _rand_parents(rng, B, R - 1)
+    turns = _turns(206, D)                                     # sequence 5's rows lie behind its end, and the last ones of sequence 0 may
+    broken, said = table.copy(), np.array(lens, dtype=np.int32)
+    broken[1, 1], broken[1, 2] = P, -5
+    said[2], said[3] = per * 64 + 7, -4
+    counts = np.array([R, R, R, R, R + 3, -2], dtype=np.int32)
+    parent[0, 4] = 4
+    cache = fsd.Cache(*(torch.from_numpy(c[n]).cuda() for n in ("k_codes", "v_codes", "k_scale", "v_scale")), torch.from_numpy(broken).cuda(),
+                      torch.from_numpy(said).cuda())
+    out = dict(out=torch.full((B, R, H * G, D), 7.0, dtype=dt, device="cuda"), row_status=torch.full((B,), -1, dtype=torch.int32, device="cuda"))
+    # (what sequence 2 is taken to hold reaches to the end of its table: no NaN codes there)
+    for n in ("k_codes", "v_codes"):
+        codes = getattr(cache, n)
+        codes[(codes & 0x7F) == 0x7F] = 0x30
+        c[n] = codes.cpu().numpy()
+    fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, rotation=_rotation(turns, True), row_count=torch.from_numpy(counts).cuda(), out=out)
+    torch.cuda.synchronize()
+    depth = max(len(ref.way(parent[0], j)) for j in range(R - 1))
+    first = fsd.ROW_BAD_PARENT | (fsd.ROW_BAD_CACHE if 200 + depth >= 206 else 0)
+    assert out["row_status"].tolist() == [first, 32, 32, 32, 32, 32]
+    now = [200, 130, per * 64, 0, 70, 300]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), parent, np.array([R, R, R, R, R, 0]), c, 0, now, broken, D ** -0.5, turns, True, dt,
+                             left_out=((1, 1), (1, 2)))
+    got = _host(out["out"])
+    assert (np.abs(got - want)[:5] <= bound[:5]).all() and (got[5] == 7.0).all()
+
+
+@pytest.mark.parametrize("R", [300, 900])
+def test_attend_deep_tree_is_a_chain(R):
+    """A tree that is a chain gives the chain's result bit for bit (paths too long to be walked; tiles that a walk passes through)."""
+    rng = np.random.default_rng(8)
+    lens = [70, 0]
+    table, c, q, k, v = _case(rng, lens, R, 2, 1, 64, torch.bfloat16)
+    cache, turns = _to_cache(c, table, lens), _turns(70 + R, 64)
+    parent = torch.arange(-1, R - 2, dtype=torch.int32, device="cuda").expand(2, R - 1).contiguous()
+    a = fsd.fsd_attend_tree(q, k, v, parent, cache, rotation=_rotation(turns, True))
+    b = fsd.fsd_attend_chain(q, k, v, cache, rotation=_rotation(turns, True))
+    assert torch.equal(a["out"], b["out"]) and (a["row_status"] == 0).all()
+    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(2, R), c, 0, lens, table, 0.125, turns, True, torch.bfloat16)
+    _within(b["out"], want, bound)
+
+
+def test_attend_far_blocks_and_layers():
+    """Blocks and layers whose bytes lie beyond what 32 bits count."""
+    rng = np.random.default_rng(10)
+    L, P, H, D, lens = 2, 40000, 8, 128, [200]                 # 2.6 GB a layer and array
+    need = 2 * L * P * H * 64 * D + (2 << 30)
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip("not enough device memory")
+    kc, vc = (torch.empty((L, P, H, *s), dtype=torch.uint8, device="cuda") for s in ((64, D), (4, D, 16)))
+    ks, vs = (torch.full((L, P, H), 2.0 ** -6, device="cuda") for _ in range(2))
+    table = np.array([[P - 1, 3, P - 7, 39000]], dtype=np.int32)
+    small = _random_cache(rng, 1, 4, H, D, np.arange(4, dtype=np.int32)[None], lens, top=0x70)
+    at = torch.from_numpy(table[0]).long().cuda()
+    kc[1, at], vc[1, at] = torch.from_numpy(small["k_codes"][0]).cuda(), torch.from_numpy(small["v_codes"][0]).cuda()
+    mixed = torch.from_numpy(rng.standard_normal((1, 3, 3 * H, D))).to(torch.bfloat16).cuda()
+    q, k, v = mixed[:, :, :H], mixed[:, :, H:2 * H], mixed[:, :, 2 * H:]
+    cache = fsd.Cache(kc, vc, ks, vs, torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    got = fsd.fsd_attend_chain(q, k, v, cache, layer=1)["out"]
+    small["k_scale"][:], small["v_scale"][:] = 2.0 ** -6, 2.0 ** -6
+    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(1, 3), small, 0, lens, np.arange(4, dtype=np.int32)[None], D ** -0.5, None,
+                             True, torch.bfloat16)
+    _within(got, want, bound)
+    # and what is appended goes there
+    new = torch.stack([mixed[:, :, H:2 * H], mixed[:, :, H:2 * H] * 2])
+    fsd.fsd_cache_append(new, new, cache, torch.tensor([2], dtype=torch.int32, device="cuda"))
+    for layer, factor in ((0, 1.0), (1, 2.0)):
+        x = _host(mixed[0, :, H:2 * H]) * factor
+        for h in range(H):
+            s = max(ref.block_scale(x[:, h]), 2.0 ** -6)
+            codes = kc[layer, 39000, h, 8:11].cpu().numpy()
+            assert np.array_equal(ref.code_values(codes) * s, ref.nearest_code_value(x[:, h] / s) * s)
+            assert vs[layer, 39000, h] == s
+
+
+# ------------------------------------------------------------------------------------------ appending: edges
+
+
+def test_append_refuses_a_sequence_whole():
+    """What the device finds out of range: that sequence is reported and left alone, whatever layer, head and block; the others are appended."""
+    rng = np.random.default_rng(11)
+    L, B, R, H, D = 2, 9, 20, 3, 64
+    table, P = _tables(rng, B, 3)
+    lens = [100, 60, 60, 180, 60, -1, 60, 60, 5]
+    accept = [3, 20, -2, 12, 3, 2, 3, 3, 1]
+    path = np.tile(np.arange(8, dtype=np.int32), (B, 1))
+    path[4, 2], path[6, 0] = R - 1, -1
+    path = np.concatenate([path, np.full((B, 12), -1, dtype=np.int32)], 1)
+    accept[1], accept[3] = 21, 8
+    lens[3] = 184                                              # 184 + 9 > 192
+    broken = table.copy()
+    broken[7, 1] = P                                           # the second of the blocks it would write
+    lens[7] = 62
+    for few in (False, True):
+        depth = 15 if few else 20
+        c = _random_cache(rng, L, P, H, D, table, [max(0, n) for n in lens])
+        cache = _to_cache(c, broken, lens)
+        k = torch.from_numpy(rng.standard_normal((L, B, R, H, D)).astype(np.float32)).cuda()
+        got = fsd.fsd_cache_append(k, k, cache, torch.tensor(accept, dtype=torch.int32, device="cuda"),
+                                   path_nodes=torch.from_numpy(np.ascontiguousarray(path[:, :depth])).cuda(), rotation=_rotation(_turns(110, 64), False))
+        torch.cuda.synchronize()
+        bad = [0, 32, 32, 32, 32, 32, 32, 32, 0]
+        assert got["row_status"].tolist() == bad
+        assert got["cache_len"].tolist() == [n if s else n + m + 1 for n, m, s in zip(lens, accept, bad)]
+        written = {int(table[0, 1]), int(table[8, 0])}
+        for n in ("k_codes", "v_codes", "k_scale", "v_scale"):
+            now, rest = getattr(cache, n).cpu().numpy(), [i for i in range(P) if i not in written]
+            assert np.array_equal(now[:, rest], c[n][:, rest]), n
+            if n.endswith("codes"):
+                assert all((now[:, i] != c[n][:, i]).any() for i in written)
+
+
+@pytest.mark.parametrize("count", [3, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_append_values_that_are_not_finite(count, dtype):
+    """They are held as NaN and leave the scale to the others; rows of zeros get the smallest scale."""
+    x = torch.zeros((1, 2, count, 2, 64), device="cuda")
+    x[0, 0, :, 0] = torch.linspace(-3, 3, 64, device="cuda")
+    x[0, 0, 1, 0, 5], x[0, 0, 2, 0, 6], x[0, 0, 0, 0, 7] = float("nan"), float("inf"), -float("inf")
+    x[0, 1, 0, 1, 3] = float("inf")
+    x = x.to(DT[dtype])
+    cache = fsd.Cache.empty(1, 2, 2, 64, torch.tensor([[1], [0]], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"))
+    got = fsd.fsd_cache_append(x, x, cache, torch.full((2,), count - 1, dtype=torch.int32, device="cuda"))
+    assert (got["row_status"] == 0).all()
+    host = _host(x)
+    for b, block in ((0, 1), (1, 0)):
+        for h in range(2):
+            s = ref.block_scale(host[0, b, :, h])
+            assert cache.k_scale[0, block, h] == s and cache.v_scale[0, block, h] == s
+            want = ref.nearest_code_value(host[0, b, :, h] / s)
+            assert np.array_equal(ref.block_keys(cache.k_codes[0, block, h].cpu().numpy())[:count], want, equal_nan=True)
+            assert np.array_equal(ref.block_values(cache.v_codes[0, block, h].cpu().numpy())[:count], want, equal_nan=True)
+    assert cache.k_scale[0, 1, 1] == 2.0 ** -100
+
+
+def test_append_every_code_is_rounded_again():
+    """Old codes of every value and every distance between two scales: rounding again, small codes, none left at last."""
+    for up in range(0, 24):
+        codes = np.arange(256, dtype=np.uint8).reshape(1, 1, 1, 4, 64).repeat(16, axis=3)            # 64 tokens, 4 patterns
+        kc = torch.from_numpy(np.ascontiguousarray(codes.reshape(1, 1, 1, 64, 64))).cuda()
+        vc = torch.from_numpy(np.ascontiguousarray(codes.reshape(1, 1, 1, 4, 16, 64).swapaxes(-1, -2))).cuda()
+        scale = torch.full((1, 1, 1), 2.0 ** -20, device="cuda")
+        cache = fsd.Cache(kc.clone(), vc.clone(), scale.clone(), scale.clone(), torch.zeros((1, 1), dtype=torch.int32, device="cuda"),
+                          torch.full((1,), 63, dtype=torch.int32, device="cuda"))
+        x = torch.full((1, 1, 1, 64), 448.0 * 2.0 ** (up - 20), device="cuda")
+        fsd.fsd_cache_append(x, x, cache, torch.zeros(1, dtype=torch.int32, device="cuda"))
+        old = ref.code_values(codes.reshape(64, 64))[:63]
+        want = ref.nearest_code_value(old * 2.0 ** -up)
+        assert cache.k_scale.item() == 2.0 ** (up - 20)
+        assert np.array_equal(ref.block_keys(cache.k_codes[0, 0, 0].cpu().numpy())[:63], want, equal_nan=True)
+        assert np.array_equal(ref.block_values(cache.v_codes[0, 0, 0].cpu().numpy())[:63], want, equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------------ conditioning: large calls
+
+
+def _plain32(z, tokens, c, contexts):
+    """fsd_condition_chain in elementary operations, 32 bits"""
+    B, rows, V = z.shape
+    held = torch.arange(c["history"].shape[1], device="cuda") < c["history_len"][:, None]
+    said = held & (torch.arange(c["history"].shape[1], device="cuda") >= c["prompt_len"][:, None])
+    seen = torch.zeros((B, V), device="cuda").scatter_add_(1, c["history"].long(), held.float())[:, None].repeat(1, rows, 1)
+    count = torch.zeros((B, V), device="cuda").scatter_add_(1, c["history"].long(), said.float())[:, None].repeat(1, rows, 1)
+    for r in range(1, rows):
+        for t in (seen, count):
+            t[:, r:].scatter_add_(2, tokens[:, r - 1:r, None].long().expand(B, rows - r, 1).contiguous(), torch.ones((B, rows - r, 1), device="cuda"))
+    y = z.float()
+    r_ = c["repetition"][:, None, None]
+    y = torch.where(seen > 0, torch.where(y > 0, y / r_, y * r_), y)
+    y = y - c["frequency"][:, None, None] * count - c["presence"][:, None, None] * (count > 0)
+    bias = torch.zeros((B, V), device="cuda")
+    for i in range(c["bias_tokens"].shape[1]):                 # one after the other: of equal ids the last counts
+        bias.scatter_(1, c["bias_tokens"][:, i:i + 1].long(), c["bias_values"][:, i:i + 1])
+    y = y + bias[:, None]
+    if c.get("allowed") is not None:
+        bits = (c["allowed"][..., None] >> torch.arange(32, dtype=torch.int32, device="cuda")) & 1
+        y = y.masked_fill(bits.flatten(2)[:, :, :V] == 0, -float("inf"))
+    return y
+
+
+@pytest.mark.parametrize("B,K,V,dtype,history,biases", [(20, 8, 256000, "bf16", 5000, 40), (8, 16, 131076, "f32", 40001, 300), (3, 4, 100003, "bf16", 70000, 20000),
+                                                        (64, 0, 32000, "bf16", 100, 3)])
+def test_condition_large(B, K, V, dtype, history, biases):
+    """Calls that go past the caches, long histories, more biases than a slice has entries."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    ids = lambda *n: (torch.rand(n, generator=g, device="cuda").square_() * V).int()  # noqa: E731
+    z = (torch.randn((B, K + 1, V), generator=g, device="cuda") * 3).to(DT[dtype])
+    tokens = ids(B, K)
+    c = dict(history=ids(B, history), history_len=torch.randint(0, history + 1, (B,), generator=g, device="cuda").int(),
+             prompt_len=torch.randint(0, history + 1, (B,), generator=g, device="cuda").int(), repetition=torch.rand(B, generator=g, device="cuda") + 0.5,
+             presence=torch.rand(B, generator=g, device="cuda"), frequency=torch.rand(B, generator=g, device="cuda") * 0.1,
+             bias_tokens=ids(B, biases), bias_values=torch.randn((B, biases), generator=g, device="cuda"),
+             allowed=torch.randint(-2 ** 31, 2 ** 31 - 1, (B, K + 1, (V + 31) // 32), generator=g, device="cuda").int())
+    got = fsd.fsd_condition_chain(z, tokens if K else None, fsd.Conditions(**c))["out"]
+    want = _plain32(z, tokens, c, K + 1)
+    assert torch.equal(torch.isneginf(got.float()), torch.isneginf(want))
+    fine = torch.isfinite(want)
+    # both sides: 5 operations of 2^-24 of magnitudes up to |z| * 2 + count + 10; counts reach 2^12 here at the squares' small end
+    size = z.float().abs()[fine] * 2 + 10 + want.abs()[fine]
+    off = (got.float() - want).abs()[fine]
+    assert (off <= ref.HALF_STEP[DT[dtype]] * want.abs()[fine] + 10 * 2.0 ** -24 * size).all()
+
+
+# ------------------------------------------------------------------------------------------ together
+
+
+def _step_state(seed, B=3, N=11, H=2, G=4, D=64, V=1000, lens=(70, 5, 130)):
+    rng = np.random.default_rng(seed)
+    table, P = _tables(rng, B, 5)
+    c = _random_cache(rng, 2, P, H, D, table, lens, top=0x70)
+    s = dict(B=B, N=N, H=H, G=G, D=D, V=V)
+    s["x"] = torch.from_numpy(rng.standard_normal((2, B, N + 1, (G + 2) * H, D)) * 0.7).to(torch.bfloat16).cuda()
+    s["head"] = torch.from_numpy(rng.standard_normal((G * H * D, V)) * 0.2).to(torch.bfloat16).cuda()
+    s["draft"] = torch.from_numpy(rng.standard_normal((B, N, V)) * 2).to(torch.bfloat16).cuda()
+    s["tokens"] = torch.from_numpy(rng.integers(0, V, (B, N)).astype(np.int32)).cuda()
+    s["parent"] = torch.from_numpy(_rand_parents(rng, B, N)).cuda()
+    s["cond"] = _conditions(rng, B, V, N + 1, history=30, biases=5, few=100)
+    s["c"], s["table"], s["lens"] = c, table, list(lens)
+    s["cache"] = _to_cache(c, table, lens)
+    s["turns"] = _turns(400, D)
+    return s
+
+
+def _step(s, conditions, rotation):
+    """one step of a serving loop: both layers' attention, the product with the head, conditioning of both models' rows, the verify
+    call, and the accepted rows into the cache"""
+    H, G, B, N = s["H"], s["G"], s["B"], s["N"]
+    outs = []
+    for layer in range(2):
+        x = s["x"][layer]
+        outs.append(fsd.fsd_attend_tree(x[:, :, :G * H], x[:, :, G * H:G * H + H], x[:, :, G * H + H:], s["parent"], s["cache"], layer=layer, rotation=rotation)["out"])
+    logits = (outs[0] + outs[1]).reshape(B, N + 1, -1) @ s["head"]
+    target = fsd.fsd_condition_tree(logits, s["tokens"], s["parent"], conditions)["out"]
+    draft = fsd.fsd_condition_tree(s["draft"], s["tokens"], s["parent"], conditions)["out"]
+    v = fsd.fsd_verify_tree(target, draft, s["tokens"], s["parent"], 6, 0.5, mode=fsd.GREEDY)
+    k, val = s["x"][:, :, :, G * H:G * H + H], s["x"][:, :, :, G * H + H:]
+    a = fsd.fsd_cache_append(k, val, s["cache"], v["path_len"], path_nodes=v["path_nodes"], rotation=rotation)
+    return outs, logits, target, draft, v, a
+
+
+def test_a_serving_step():
+    """The operators as they are used, each against the plain implementation on what the one before gave."""
+    s = _step_state(21)
+    conditions, rotation = _dev(s["cond"]), _rotation(s["turns"], True)
+    outs, logits, target, draft, v, a = _step(s, conditions, rotation)
+    torch.cuda.synchronize()
+    H, G = s["H"], s["G"]
+    parent = s["parent"].cpu().numpy()
+    for layer in range(2):
+        x = _host(s["x"][layer])
+        want, bound = ref.attend(x[:, :, :G * H], x[:, :, G * H:G * H + H], x[:, :, G * H + H:], parent, np.full(3, s["N"] + 1), s["c"], layer, s["lens"],
+                                 s["table"], s["D"] ** -0.5, s["turns"], True, torch.bfloat16)
+        _within(outs[layer], want, bound)
+    tokens = s["tokens"].cpu().numpy()
+    for got, z, is_target in ((target, logits, True), (draft, s["draft"], False)):
+        want, err = ref.condition(_host(z), tokens, parent, is_target, s["cond"])
+        _close(got, want, err, torch.bfloat16)
+    assert (v["row_status"] == 0).all()
+    assert a["cache_len"].tolist() == [n + m + 1 for n, m in zip(s["lens"], v["path_len"].tolist())]
+    # the next step reads what was appended: the row appended last is where the table says, in the scale of its block
+    s["cache"].cache_len.copy_(a["cache_len"])
+    for b, n in enumerate(a["cache_len"].tolist()):
+        block, place, m = s["table"][b, (n - 1) // 64], (n - 1) % 64, v["path_len"][b].item()
+        row = v["path_nodes"][b, m - 1].item() + 1 if m else 0
+        for layer in range(2):
+            x = _host(s["x"][layer, b, row, G * H:G * H + H])
+            key = ref.turned(x, s["turns"], np.full(H, n - 1), True)
+            val = _host(s["x"][layer, b, row, G * H + H:])
+            ks, vs = s["cache"].k_scale[layer, block].cpu().numpy()[:, None], s["cache"].v_scale[layer, block].cpu().numpy()[:, None]
+            got_k = ref.code_values(s["cache"].k_codes[layer, block, :, place].cpu().numpy()) * ks
+            got_v = ref.code_values(s["cache"].v_codes[layer, block, :, place // 16, :, place % 16].cpu().numpy()) * vs
+            assert (np.abs(got_k - key) <= np.maximum(2.0 ** -4 * np.abs(key), 2.0 ** -10 * ks) * (1 + 2.0 ** -20) + 4 * 2.0 ** -24 * 4).all()
+            assert np.array_equal(got_v, ref.nearest_code_value(val / vs) * vs)
+
+
+def test_steps_replay_from_a_graph():
+    """Captured and replayed several times, with other work and synchronizations between: each replay gives the eager result, also where
+    two graphs share the workspace memory that torch hands them in turn."""
+    s = _step_state(22)
+    conditions, rotation = _dev(s["cond"]), _rotation(s["turns"], True)
+    saved = {n: getattr(s["cache"], n).clone() for n in ("k_codes", "v_codes", "k_scale", "v_scale")}
+
+    def reset():
+        for n, t in saved.items():
+            getattr(s["cache"], n).copy_(t)
+
+    eager = [t.clone() for t in _flat(_step(s, conditions, rotation))]
+    eager_cache = {n: getattr(s["cache"], n).clone() for n in saved}
+    pool, graphs = None, []
+    for _ in range(2):
+        reset()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, pool=pool):
+            out = _step(s, conditions, rotation)
+        pool = g.pool()
+        graphs.append((g, _flat(out)))
+    for i in range(6):
+        g, out = graphs[i % 2]
+        reset()
+        junk = torch.randn(1 << 20, device="cuda").mul_(2).sum()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.isfinite(junk)
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b), i
+        for n, t in eager_cache.items():
+            assert torch.equal(getattr(s["cache"], n), t), (i, n)
+
+
+def _flat(out):
+    outs, logits, target, draft, v, a = out
+    return [*outs, logits, target, draft, v["path_len"], v["path_nodes"], v["out_tokens"], v["row_status"], a["cache_len"], a["row_status"]]
+
+
+def test_attend_workspace_holds_anything_and_results_repeat():
+    """A workspace full of NaN patterns, one that a call of other sizes has left, and two calls at once on two streams."""
+    rng = np.random.default_rng(30)
+    big = _case(rng, [3000, 100, 64], 9, 8, 2, 128, torch.bfloat16)
+    small = _case(rng, [200, 10], 3, 4, 2, 64, torch.float16)
+    sizes = [(3, 9, 8, 2, 128), (2, 3, 4, 2, 64)]
+    caches = [_to_cache(c, table, lens) for (table, c, *_), lens in ((big, [3000, 100, 64]), (small, [200, 10]))]
+    first = [fsd.fsd_attend_chain(*x[2:], cache)["out"].clone() for x, cache in zip((big, small), caches)]
+    ws = torch.full((max(fsd.fsd_attend_workspace_bytes(*n) for n in sizes) + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    for i in (0, 1, 0, 1, 1, 0):
+        x = (big, small)[i]
+        assert torch.equal(fsd.fsd_attend_chain(*x[2:], caches[i], workspace=ws)["out"], first[i])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, x in enumerate((big, small)):
+            got[i].append(fsd.fsd_attend_chain(*x[2:], caches[i], stream=streams[i])["out"])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(t, first[i]) for t in got[i])
+
+
+def test_calls_on_another_stream():
+    """`stream`: what the binding allocates stays allocated until that stream has used it."""
+    rng = np.random.default_rng(31)
+    side = torch.cuda.Stream()
+    z = torch.randn(8, 5, 32000, device="cuda")
+    tokens = torch.randint(0, 32000, (8, 4), dtype=torch.int32, device="cuda")
+    c = fsd.Conditions(frequency=torch.full((8,), 0.5, device="cuda"))
+    want = fsd.fsd_condition_chain(z, tokens, c)["out"].clone()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = fsd.fsd_condition_chain(z, tokens, c, stream=side)["out"]
+        torch.empty_like(z).fill_(float("nan"))
+        side.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_binding_refusals_on_the_gpu():
+    i32 = dict(dtype=torch.int32, device="cuda")
+    z, tokens = torch.zeros(2, 4, 100, device="cuda"), torch.zeros((2, 3), **i32)
+    with pytest.raises(ValueError):
+        fsd.fsd_condition_chain(z, tokens[:, :1].contiguous(), fsd.Conditions())                 # rows and candidates do not go together
+    with pytest.raises(ValueError):
+        fsd.fsd_condition_chain(z, tokens, fsd.Conditions(repetition=torch.ones(3, device="cuda")))
+    with pytest.raises(ValueError):
+        fsd.fsd_condition_chain(z, tokens, fsd.Conditions(allowed=torch.zeros((2, 1, 3), **i32)))
+    with pytest.raises(ValueError):
+        fsd.fsd_condition_chain(z, tokens, fsd.Conditions(allowed=torch.zeros((2, 3, 4), **i32)))
+    with pytest.raises(TypeError):
+        fsd.fsd_condition_chain(z.half(), tokens, fsd.Conditions())
+    with pytest.raises(ValueError):
+        fsd.fsd_condition_chain(z.transpose(0, 1), tokens, fsd.Conditions())
+    with pytest.raises(ValueError):
+        fsd.Conditions(bias_tokens=torch.zeros((2, 3), **i32))
+    with pytest.raises(ValueError):
+        fsd.Conditions(history=torch.zeros((2, 3), **i32), history_len=torch.zeros(3, **i32))
+    cache = fsd.Cache.empty(1, 4, 2, 64, torch.zeros((2, 2), **i32), torch.zeros(2, **i32))
+    q, k = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(TypeError):
+        fsd.fsd_attend_chain(q.float(), k.float(), k.float(), cache)
+    with pytest.raises(TypeError):
+        fsd.fsd_attend_chain(q, k.half(), k, cache)
+    with pytest.raises(ValueError):
+        fsd.fsd_attend_chain(q[:1], k[:1], k[:1], cache)
+    with pytest.raises(ValueError):
+        fsd.fsd_attend_chain(q, k[:, :, :1], k, cache)
+    with pytest.raises(ValueError):
+        fsd.fsd_attend_tree(q, k, k, torch.zeros((2, 3), **i32), cache)
+    with pytest.raises(fsd.FsdError):
+        fsd.fsd_attend_chain(q, k, k, cache, layer=1)
+    with pytest.raises(fsd.FsdError):
+        fsd.fsd_attend_chain(q, k, k, cache, workspace=torch.empty(512, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(fsd.FsdError):
+        fsd.fsd_attend_chain(q[:, :, :3].contiguous(), k, k, cache)                               # 3 heads on 2 key heads
+    with pytest.raises(fsd.FsdError):
+        fsd.fsd_cache_append(k, k, cache, torch.zeros(2, **i32), out=dict(cache_len=cache.cache_len))
+    with pytest.raises(ValueError):
+        fsd.fsd_cache_append(k, k, cache, torch.zeros(3, **i32))
+    with pytest.raises(ValueError):
+        fsd.Cache(cache.k_codes, cache.k_codes, cache.k_scale, cache.v_scale, cache.block_table, cache.cache_len)
