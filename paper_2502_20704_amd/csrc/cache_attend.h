@@ -16,8 +16,10 @@
 // 64 i + 16 g .. + 15 of queries and keys alike.
 //
 // A block's value scale enters the weights' exponent: p = exp2(s + log2(vs) - m), with m the running maximum of s + log2(vs), and
-// sum += p / vs.  So p is at most 2^8 whatever the scales are (binary16 holds it), codes enter the product exactly,
-// and O' / sum is the result.  m follows the maximum only where that is more than 2^8 above it: a rescaling of O' is rare.
+// sum += p / vs.  So p is at most 2^15 whatever the scales are (binary16 holds it), codes enter the product exactly,
+// and O' / sum is the result.  m is kept 7 below the maximum, so that weights lose less at binary16's small end (2^-25 absolutely, beside 2^7), and
+// follows only where the maximum is more than 15 above it: a rescaling of O' is rare.  A block whose value scale is far below one before
+// it (values that are all zero have the smallest scale there is) may add nothing to O' and yet much to the sum: there the sum takes exp2(s - m) itself.
 //
 // Three kernels: attend_prepare turns queries and the rows' keys, brings them and the rows' values into binary16's range by powers of two and lays them
 // out in the workspace as the matrix instruction takes them, so that no piece of the work does this again; it deals out the work, which takes the
@@ -32,7 +34,10 @@ namespace {
 
 typedef float float2_t __attribute__((ext_vector_type(2)));
 
-constexpr float kLazy = 8.0f;      // how far (in powers of two) weights may pass 1 before they are scaled down again
+constexpr float kRoom = 7.0f;      // powers of two that a weight formed anew is above 1
+constexpr float kLazy = 15.0f;     // how far (likewise) weights may pass 1 before they are scaled down again
+constexpr float kUnit = 10.0f;     // sums are in units of 2^10: value scales from 2^-100 on leave room for 2^22 tokens, those up to 2^119 do not vanish
+constexpr float kPerUnit = 0x1p-10f;
 constexpr float kLog2eF = 1.44269504088896340736f;
 
 struct AttendParams {
@@ -72,10 +77,8 @@ struct AttendParams {
 
 // The work is a line of units.  An item is one (sequence, key head, run of `tile` rows); its units are the blocks of the sequence's
 // cache, then its tiles of 64 rows; kStart more stand for what an item costs at its beginning, whoever begins it.
-#ifndef KST
-#define KST 6
-#endif
-constexpr int kStart = KST;
+// (64 sequences of 300 to 2048 tokens, 8 key heads: 211 us with 3, 205 with 6, 201 with 10; 25-row trees: best with 3 to 6.)
+constexpr int kStart = 6;
 struct Share { int rows, blocks, tiles, groups; };
 __device__ __forceinline__ Share share_of(const AttendParams& P, int b) {
     Share s;
@@ -157,11 +160,19 @@ __device__ __forceinline__ float column_sum(float v) {
     v += __shfl_xor(v, 16, 64);
     return v + __shfl_xor(v, 32, 64);
 }
-// the power of two that brings `most` into [2^13, 2^14) (1 where there is nothing to bring there), as an exponent
-__device__ __forceinline__ int to_half_range(float most) {
-    const int e = static_cast<int>(__float_as_uint(most) >> 23) - 127;
-    return most > 0.0f ? min(13 - e, 126) : 0;
+// What is relative to 2^from becomes relative to 2^to by this factor's square: a sum of weights may be as large as the step is far (scales of values lie up to
+// 2^219 apart), and outlives it only in two halves.
+__device__ __forceinline__ float back_from(float from, float to) {
+    return to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(0.5f * (from - to));
 }
+// the power of two that brings `most` into [2^at, 2 * 2^at) (1 where there is nothing to bring there), as an exponent
+__device__ __forceinline__ int to_half_range(float most, int at, int limit) {
+    const int e = static_cast<int>(__float_as_uint(most) >> 23) - 127;
+    return most > 0.0f ? min(at - e, limit) : 0;
+}
+// queries and keys: as large as products allow; values: as large as the cache's codes, so that their scales are alike
+__device__ __forceinline__ float key_range(float most) { return pow2(to_half_range(most, 13, 126)); }
+__device__ __forceinline__ float value_range(float most) { return pow2(to_half_range(most, 8, 100)); }
 
 constexpr int kMaxNodes = 2048;
 constexpr int kWalk = 256;          // nodes of trees whose depths are found by walking
@@ -364,7 +375,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
 #pragma unroll
             for (int o = kPer / 2; o > 0; o >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, o, 64));
             if (row[i] >= n) continue;
-            const float by = pow2(max(to_half_range(most), -126));
+            const float by = key_range(most);
             half8_t a, c;
             two_parts(y[i], P.scale < 0.0f ? -by : by, a, c);  // (a negative scale goes in here: a larger product is always a larger score)
             const int r = row[i] / P.heads, head = row[i] - r * P.heads, h = head / G, rho = r * G + head - h * G;
@@ -409,7 +420,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[0][e]));
 #pragma unroll
         for (int o = kPer / 2; o > 0; o >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, o, 64));
-        const float by = pow2(max(to_half_range(most), -126));
+        const float by = key_range(most);
         half8_t a, c;
         two_parts(y[0], by, a, c);
         const int fragment = (t >> 2 & 3) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1), place = (dim / 16 & 3) * 16 + (t >> 4) * 4 + (t & 3);
@@ -432,7 +443,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     if (tid == 0) broken = 0;
     __syncthreads();
     most = __builtin_fmaxf(__builtin_fmaxf(most_of[0], most_of[1]), __builtin_fmaxf(most_of[2], most_of[3]));
-    const float by = pow2(max(to_half_range(most), -126));
+    const float by = value_range(most);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         float y[8];
@@ -588,7 +599,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             }
         }
         float4_t o[RT][kT];
-        float m[RT], l[RT];                                   // maximum of s + log2(value scale); sum (of all lanes of the column)
+        float most_vs = 0.0f;                                 // largest value scale so far
+        float m[RT], l[RT];                                   // maximum of s + log2(value scale), less kRoom; sum (of all lanes of the column)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -__builtin_inff();
@@ -603,7 +615,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         // lane's group), and those of spoilt(rt) are NaN.  Their sum is a product with ones: two instructions of the matrix unit for
         // 16 additions, and it sums what the second product will use.
         auto weigh = [&](float4_t (&s)[RT][4], float ks, float vs, auto part, auto kept, auto spoilt, half8_t (&p)[RT][2]) {
-            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs);   // (exact for powers of two)
+            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs) * kPerUnit;   // (exact for powers of two)
+            // 2^6 below: a weight of 2^-25 that binary16 loses is 2^-26 of the largest
+            const bool low = vs < most_vs * 0x1p-6f;
+            most_vs = __builtin_fmaxf(most_vs, vs);
             float high[RT], f[RT];
             bool over = false;
 #pragma unroll
@@ -623,12 +638,23 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
             if (__any(over)) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    const float to = __builtin_fmaxf(m[rt], column_max(high[rt]));
-                    const float by = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - to);
+                    const float to = __builtin_fmaxf(m[rt], column_max(high[rt]) - kRoom);
+                    const float root = back_from(m[rt], to), by = root * root;
                     m[rt] = to;
-                    l[rt] *= by;
+                    l[rt] = l[rt] * root * root;
 #pragma unroll
                     for (int t = 0; t < kT; ++t) o[rt][t] *= by;
+                }
+            }
+            if (low) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float from = -kUnit - (m[rt] == -__builtin_inff() ? 0.0f : m[rt]);
+                    const unsigned keep = part ? kept(rt) : 0xFFFFu;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum += keep >> j & 1u ? __builtin_amdgcn_exp2f(fmaf(s[rt][j / 4][j % 4], f[rt], from)) : 0.0f;
+                    l[rt] += column_sum(sum);
                 }
             }
 #pragma unroll
@@ -650,7 +676,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 float4_t z = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
                 z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[rt][0], z, 0, 0, 0);
                 z = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[rt][1], z, 0, 0, 0);
-                l[rt] = fmaf(z[0], inv_vs, l[rt]);
+                l[rt] = fmaf(z[0], low ? 0.0f : inv_vs, l[rt]);
             }
         };
         auto nothing = [](int) { return 0u; };
@@ -885,7 +911,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 const int rho = rho0 + rt * 16 + col;
                 if (rho >= nrho) continue;
                 const int r = rho / G, head = h * G + (rho - r * G);
-                const float inv = 1.0f / l[rt];
+                const float inv = kPerUnit / l[rt];
                 const size_t at = ((static_cast<size_t>(b) * R + r) * P.heads + head) * D;
 #pragma unroll
                 for (int t = 0; t < kT; ++t) store4(P.dtype, P.out, at + t * 16 + g * 4, o[rt][t] * inv);
@@ -971,7 +997,8 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
             }
         }
         float4_t o[RT][kV];
-        float m[RT], l[RT];                                             // maximum of s + log2(value scale); sum of this lane's tokens' weights
+        float most_vs = 0.0f;                                           // largest value scale so far
+        float m[RT], l[RT];                                             // maximum of s + log2(value scale), less kRoom; sum of this lane's tokens' weights
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -__builtin_inff();
@@ -983,7 +1010,9 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
         // From this wavefront's products to everyone's weights p.  With `part` only the tokens of kept(rt) count (a bit for each of this
         // lane's four), and the weights of spoilt are NaN.
         auto weigh = [&](float4_t (&s)[RT], float ks, float vs, auto part, auto kept, unsigned spoilt, half8_t (&p)[RT][2]) {
-            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs);   // (exact for powers of two)
+            const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs) * kPerUnit;   // (exact for powers of two)
+            const bool low = vs < most_vs * 0x1p-60f;                   // weights may vanish in binary32
+            most_vs = __builtin_fmaxf(most_vs, vs);
             float high[RT], f[RT];
             bool run = false;
 #pragma unroll
@@ -1008,7 +1037,12 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                         w[i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from));
                         if constexpr (part) w[i] = kept(rt) >> i & 1u ? (spoilt >> i & 1u ? __builtin_nanf("") : w[i]) : 0.0f;
                     }
-                    sum[rt] = (w[0] + w[1]) + (w[2] + w[3]);
+                    sum[rt] = ((w[0] + w[1]) + (w[2] + w[3])) * inv_vs;
+                    if (low) {
+                        sum[rt] = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[rt] += !part || (kept(rt) >> i & 1u) ? __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from - lift - kUnit)) : 0.0f;
+                    }
                     const float2_t lo = {w[0], w[1]}, hi = {w[2], w[3]};
                     uint2 y;
                     y.x = __builtin_bit_cast(unsigned, __builtin_convertvector(lo, half2_t));
@@ -1031,10 +1065,10 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                 for (int rt = 0; rt < RT; ++rt) {
                     float to = m[rt];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) to = __builtin_fmaxf(to, highs[w][rt * 16 + col]);
-                    const float by = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - to);
+                    for (int w = 0; w < 4; ++w) to = __builtin_fmaxf(to, highs[w][rt * 16 + col] - kRoom);
+                    const float root = back_from(m[rt], to), by = root * root;
                     m[rt] = to;
-                    l[rt] *= by;
+                    l[rt] = l[rt] * root * root;
 #pragma unroll
                     for (int t = 0; t < kV; ++t) o[rt][t] *= by;
                 }
@@ -1043,7 +1077,7 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
             }
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                l[rt] = fmaf(sum[rt], inv_vs, l[rt]);
+                l[rt] += sum[rt];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) p[rt][k] = *reinterpret_cast<const half8_t*>(weights[turn] + (rt * 2 + k) * 1024 + lane * 16);
             }
@@ -1200,7 +1234,7 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                 const int rho = rho0 + rt * 16 + col;
                 if (rho >= it.nrho) continue;
                 const int r = rho / G, head = h * G + (rho - r * G);
-                const float inv = 1.0f / l[rt];
+                const float inv = kPerUnit / l[rt];
                 const size_t at = ((static_cast<size_t>(b) * R + r) * P.heads + head) * D + wave * kV * 16 + g * 4;
 #pragma unroll
                 for (int t = 0; t < kV; ++t) store4(P.dtype, P.out, at + t * 16, o[rt][t] * inv);
@@ -1263,14 +1297,14 @@ __global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_seque
         }
 #pragma unroll
         for (int k = 0; k < kOnce; ++k) high = __builtin_fmaxf(high, m[k]);
-        const float from = high == -__builtin_inff() ? 0.0f : high, back = __builtin_amdgcn_exp2f(top - from);
+        const float back = back_from(top, high);
         top = high;
-        sum *= back;
-        acc *= back;
+        sum = sum * back * back;
+        acc *= back * back;
 #pragma unroll
         for (int k = 0; k < kOnce; ++k) {
-            const float by = __builtin_amdgcn_exp2f(m[k] - from);
-            sum = fmaf(l[k], by, sum);
+            const float root = back_from(m[k], high), by = root * root;
+            sum = fmaf(l[k] * root, root, sum);
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] = fmaf(y[k][e], by, acc[e]);
         }
@@ -1286,19 +1320,18 @@ __global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_seque
         float high = -__builtin_inff();
 #pragma unroll
         for (int w = 0; w < kGroups; ++w) high = __builtin_fmaxf(high, stats[w][0]);
-        const float from = high == -__builtin_inff() ? 0.0f : high;
         sum = 0.0f;
         acc = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < kGroups; ++w) {
-            const float by = __builtin_amdgcn_exp2f(stats[w][0] - from);
-            sum = fmaf(stats[w][1], by, sum);
-            acc += sums[w][d / 4] * by;
+            const float root = back_from(stats[w][0], high);
+            sum = fmaf(stats[w][1] * root, root, sum);
+            acc += sums[w][d / 4] * (root * root);
         }
     }
     if (n <= 1) return;
     const int r = rho / P.G, head = h * P.G + rho % P.G;
-    store4(P.dtype, P.out, ((static_cast<size_t>(b) * P.R + r) * P.heads + head) * D + d, acc * (1.0f / sum));
+    store4(P.dtype, P.out, ((static_cast<size_t>(b) * P.R + r) * P.heads + head) * D + d, acc * (kPerUnit / sum));
 }
 
 }  // namespace

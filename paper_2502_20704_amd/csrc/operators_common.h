@@ -85,38 +85,11 @@ __device__ __forceinline__ void copy_logit(char* out, const char* in, int e) {
 
 // ---- keys, values and queries: 8 elements in a row
 
-template <int DT>
-__device__ __forceinline__ void load8(const void* base, size_t at, float* x) {
-    if constexpr (DT == FSD_F32) {
-        const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(base) + at);
-        const u32x4 a = p[0], c = p[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = __uint_as_float(a[i]);
-            x[4 + i] = __uint_as_float(c[i]);
-        }
-    } else {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const unsigned short*>(base) + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned w = a[i];                          // (a bit cast of the vector's element itself takes element 0)
-            if constexpr (DT == FSD_BF16) {
-                x[2 * i] = __uint_as_float(w << 16);
-                x[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
-            } else {
-                const half2_t h = __builtin_bit_cast(half2_t, w);
-                x[2 * i] = static_cast<float>(h.x);
-                x[2 * i + 1] = static_cast<float>(h.y);
-            }
-        }
-    }
-}
-
 // what lies in 16 bytes (8 elements of 16 bits) as numbers
 __device__ __forceinline__ void unpack8(int dtype, const u32x4& a, float* x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const unsigned w = a[i];
+        const unsigned w = a[i];                              // (a bit cast of the vector's element itself takes element 0)
         const half2_t h = __builtin_bit_cast(half2_t, w);
         x[2 * i] = dtype == FSD_BF16 ? __uint_as_float(w << 16) : static_cast<float>(h.x);
         x[2 * i + 1] = dtype == FSD_BF16 ? __uint_as_float(w & 0xFFFF0000u) : static_cast<float>(h.y);

@@ -123,14 +123,18 @@ def block_values(v_codes):
     return np.swapaxes(v, -1, -2).reshape(*v.shape[:-3], BLOCK, v.shape[-2])
 
 
-def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halves, dtype, left_out=()):
+def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halves, dtype, left_out=(), by_contribution=False):
     """(out [B,R,heads,D], bound) in 64 bits; left_out: (sequence, block of it) pairs none of whose tokens counts.  cache: dict of numpy arrays as fsd.Cache names them.
 
     The bound: a product's error is scale * sum |q||k| times (one rounding of q to 11 bits, for the rows' keys one of k as well,
     4 more of 2^-24 each for the rotation of either, D sums of 2^-24), delta for the row's largest.  Weights then lie within
     exp(+-delta), so their shares within exp(+-2 delta); their rounding to 11 bits and the exponential's and sums' own errors (under 2^-14
     together) come on top, all relative to sum w |v|; a weight under 2^-24 of the row's largest is lost to binary16 (2^-24 of max |v|
-    each).  Last the rounding to the result's type."""
+    each).  Last the rounding to the result's type.
+
+    by_contribution: where value scales lie far apart, max |v| says little.  A token's weight times its block's value scale is what binary16
+    holds, 2^7 or more for the largest of them: what is lost is at most 2^-32 of the largest such product, times codes of up to 512, a
+    token.  The sum of weights loses at most 2^-26 a token: 2^-25 beside 2^7 where its scale is up to 2^6 below another's, nothing else."""
     B, R, heads, D = q.shape
     H = k.shape[2]
     G = heads // H
@@ -160,6 +164,8 @@ def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halve
             kk = np.concatenate([ck.reshape(-1, D)[:n], kr[:, h]])
             vv = np.concatenate([cv.reshape(-1, D)[:n], v[b, :count, h]])
             kabs = np.concatenate([np.abs(ck.reshape(-1, D)[:n]) * 1.0, ka[:, h] * 2.0])
+            own = [np.abs(v[b, t // BLOCK * BLOCK:min(count, t // BLOCK * BLOCK + BLOCK), h]).max() / 256 for t in range(count)]
+            vscale = np.concatenate([np.repeat(cache["v_scale"][layer, blocks, h].astype(np.float64), BLOCK)[:n], own])
             seen = np.concatenate([np.broadcast_to(held, (count, n)), sees], 1)
             for i in range(h * G, h * G + G):
                 with np.errstate(invalid="ignore", over="ignore"):
@@ -176,5 +182,8 @@ def attend(q, k, v, parent, rows, cache, layer, lens, table, scale, turns, halve
                     size = w[r, at] @ np.abs(vv[at])
                     out[b, r, i] = o
                     vmax = np.abs(vv[at]).max()
-                    bound[b, r, i] = (np.expm1(2 * delta[r]) + 2.0 ** -11 + 2.0 ** -14) * size + 2.0 ** -24 * vmax * min(at.sum(), 64) + HALF_STEP[dtype] * np.abs(o)
+                    lost = 2.0 ** -24 * vmax * min(at.sum(), 64)
+                    if by_contribution:
+                        lost = 2.0 ** -32 * 512 * (w[r, at] * vscale[at]).max() * at.sum() + 2.0 ** -26 * at.sum() * size
+                    bound[b, r, i] = (np.expm1(2 * delta[r]) + 2.0 ** -11 + 2.0 ** -14) * size + lost + HALF_STEP[dtype] * np.abs(o)
     return out, bound

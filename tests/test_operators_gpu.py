@@ -357,7 +357,7 @@ def _case(rng, lens, R, heads, H, D, dt, *, L=1, top=0x70, extra=0, scale_expone
 
 
 def _within(got, want, bound, what=""):
-    d = np.abs(_host(got) - want)
+    d = np.abs((got if isinstance(got, np.ndarray) else _host(got)) - want)
     assert (d <= bound).all(), f"{what}: {(d / np.maximum(bound, 1e-30)).max():.2f} bounds"
 
 
@@ -409,6 +409,29 @@ def test_attend_scales(scale, dtype):
     # the weights of a block count relative to the largest contribution, not to the largest weight: an output of small values
     # beside a block of large ones is off by 2^-24 of the latter's (the bound's term in max |v|)
     _within(got, want, bound)
+
+
+@pytest.mark.parametrize("R,heads,H,D,dtype", [(4, 6, 2, 128, "bf16"), (20, 12, 2, 64, "bf16"), (20, 12, 2, 128, "f16"), (9, 2, 1, 256, "bf16"), (40, 2, 1, 256, "f16")])
+@pytest.mark.parametrize("order", [1, -1])
+def test_attend_value_scales_far_apart(R, heads, H, D, dtype, order):
+    """Blocks of values that are all zero (their scale is the smallest there is), and scales from 2^-90 to 2^40: small values add nothing to the
+    products, but their weights count in the sum like all others."""
+    rng = np.random.default_rng(R + D)
+    lens = [320, 127, 64]
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, DT[dtype])
+    for b, exponents in enumerate(([-100, 0, -90, 40, -7][::order], [-100, 3][::order], [-100])):
+        for j, e in enumerate(exponents):
+            c["v_scale"][0, table[b, j]] = 2.0 ** e
+            if e == -100:
+                c["v_codes"][0, table[b, j]] = 0x80 * rng.integers(0, 2, c["v_codes"].shape[2:])
+    c["k_scale"][:] = 2.0 ** -8
+    got = fsd.fsd_attend_chain(q, k, v, _to_cache(c, table, lens))["out"]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(3, R), c, 0, lens, table, D ** -0.5, None, True, DT[dtype], by_contribution=True)
+    # (binary16's largest number is 65504, and 65520 and more round to infinity: a result of 2^40 is one)
+    most = 65520.0 if dtype == "f16" else np.inf
+    beyond, inside = np.abs(want) - bound >= most, np.abs(want) + bound < most
+    assert np.array_equal(_host(got)[beyond], np.sign(want[beyond]) * np.inf)
+    _within(np.where(inside, _host(got), 0.0), np.where(inside, want, 0.0), bound)
 
 
 def test_attend_large_magnitudes():
