@@ -5,9 +5,12 @@
 //   old codes: round(code s_old / s);  new codes: round(x / s), e4m3, ties to even
 //
 // A block of a head is one piece of work: nothing is shared between two of them, so they need not agree on anything.  Its new keys
-// are in registers when their largest magnitude is known, and are then written as codes; so are its new values, which are requested
-// together with the keys.  What bounds both kernels is how much is requested at once.
-//   append_few   a step's accepted rows (at most 16): a wavefront a head, which takes the blocks they touch (one, seldom two) in turn
+// are in registers when their largest magnitude is known, and are then written as codes; so are its new values.
+// Measured: the accepted rows of 64 trees, 8 key heads of 128, 32 layers: 44 us for 93 MB that cross the memory's pins (the codes of a dimension's 16
+// tokens lie together, so values are read and written 2 KB at a time; without that, 50 MB), in pieces of 128 bytes to 2 KB all over 1.6 GB: neither more
+// wavefronts a compute unit (6 in place of 4: 49 us) nor a sequence's heads in one XCD (47) change that.  20000 prompt tokens: 55 us for 151 MB.
+//   append_few   a step's accepted rows (at most 16): a wavefront for a head's keys and one for its values, which take the blocks they touch (one, seldom
+//                two) in turn
 //   append_many  a prompt's: a workgroup a block and head
 #ifndef FSD_CSRC_CACHE_APPEND_H_
 #define FSD_CSRC_CACHE_APPEND_H_
@@ -113,108 +116,200 @@ __device__ __forceinline__ float largest_of(const float (&x)[NS][8]) {
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], float by) {
     return make_uint2(codes4(x[0] * by, x[1] * by, x[2] * by, x[3] * by), codes4(x[4] * by, x[5] * by, x[6] * by, x[7] * by));
 }
-// the keys of a block's first `fill` tokens, rounded to a larger scale
-template <int D>
-__device__ __forceinline__ void rescale_keys(unsigned char* kc, int fill, float ratio, int lane, int lanes) {
-    uint2* w = reinterpret_cast<uint2*>(kc);
-#pragma unroll 1                                              // (rare: not worth the registers)
-    for (int i = lane; i < fill * (D / 8); i += lanes) {
-        const uint2 old = w[i];
-        w[i] = make_uint2(rescaled4(old.x, ratio), rescaled4(old.y, ratio));
+// `slots` times 16 old codes, rounded to a larger scale.  (Few calls have such blocks, but one that has waits for them: four slots at once.)
+__device__ __forceinline__ void rescale(unsigned char* codes, int slots, float ratio, int lane, int lanes) {
+    constexpr int kOnce = 4;
+    u32x4* w = reinterpret_cast<u32x4*>(codes);
+#pragma unroll 1
+    for (int i = lane; i < slots; i += kOnce * lanes) {
+        u32x4 z[kOnce];
+#pragma unroll
+        for (int e = 0; e < kOnce; ++e) z[e] = w[min(i + e * lanes, slots - 1)];
+#pragma unroll
+        for (int e = 0; e < kOnce; ++e) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[e][k] = rescaled4(z[e][k], ratio);
+            if (i + e * lanes < slots) w[i + e * lanes] = z[e];
+        }
     }
 }
 
-template <int DT, int D, int TOKENS>
+constexpr int kFew = 16;         // rows of append_few: they touch two blocks, and two runs of 16 tokens of a block, at most
+
+// The rows of a step that append_few takes, looked up once by a wavefront: lane i holds the i-th row's place in k and v, lanes 0 and 1 the blocks.
+struct Few {
+    long len, count;
+    int row, block;
+    bool bad;                    // for everyone
+    __device__ __forceinline__ Few(const AppendParams& P, int b, int lane) {
+        len = P.cache.cache_len[b];
+        count = static_cast<long>(P.accept_len[b]) + 1;
+        row = lane;
+        if (P.path != nullptr && lane > 0 && lane <= min(P.max_depth, kFew)) row = P.path[static_cast<size_t>(b) * P.max_depth + lane - 1] + 1;
+        bad = count < 0 || count > P.max_rows || len < 0 || len + count > static_cast<long>(P.cache.max_blocks) * kBlock ||
+              (count > 0 && P.rot.table != nullptr && len + count > P.rot.rows);
+        block = 0;
+        if (bad || count == 0) return;
+        bool found = false;
+        if (lane < 2 && len / kBlock + lane <= (len + count - 1) / kBlock) {
+            block = P.cache.block_table[static_cast<size_t>(b) * P.cache.max_blocks + len / kBlock + lane];
+            found = block < 0 || block >= P.cache.num_blocks;
+        }
+        if (lane > 0 && lane < count) found |= row < 1 || row >= P.R;
+        row = max(0, min(P.R - 1, row));                      // (requested before it has been looked at)
+        bad = __any(found);
+    }
+};
+
+// Keys: D / 8 lanes a token, 8 dimensions each; a token's codes are a run of D bytes.  SLOTS: such steps over the wavefront's lanes, which hold
+// 512 / D tokens each.
+template <int DT, int D, int SLOTS>
+__device__ __forceinline__ void append_keys(const AppendParams& P, size_t at, int fill, int n, size_t rows, int h, int row, int i0, int pos0, int lane) {
+    constexpr int kPer = D / 8, kAtOnce = 64 / kPer;
+    unsigned char* kc = static_cast<unsigned char*>(P.cache.k_codes) + at * (kBlock * D);
+    const float old = P.cache.k_scale[at];
+    float x[SLOTS][8];
+    const int dim[1] = {lane % kPer * 8};
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
+        if (i > 0 && i * kAtOnce >= n) continue;
+        const int t = i * kAtOnce + lane / kPer, there = min(t, n - 1);   // (the last one again: it does not change the largest)
+        const size_t head[1] = {(rows + __shfl(row, i0 + there, 64)) * P.stride + static_cast<size_t>(h) * D};
+        const int pos[1] = {pos0 + there};
+        load_turned<1>(DT, P.k, head, dim, P.rot, pos, reinterpret_cast<float(&)[1][8]>(x[i]));
+    }
+    float ratio;
+    const float s = scale_in_force(largest_of<SLOTS>(x), fill, old, ratio), inv = 1.0f / s;
+    if (ratio != 1.0f) rescale(kc, fill * (D / 16), ratio, lane, 64);
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        const int t = i * kAtOnce + lane / kPer;
+        if (t < n) *reinterpret_cast<uint2*>(kc + (fill + t) * D + dim[0]) = codes8(x[i], inv);
+    }
+    if (lane == 0) P.cache.k_scale[at] = s;
+}
+
+// Values: D / 64 dimensions a lane, all tokens of which it has: a dimension's codes of 16 tokens are 16 bytes, so whole ones are read, changed and written.
+// (With a lane a token's 8 dimensions, as for keys, and stores of single bytes that step took 54 us.)  N: tokens, at most.
+template <int DT, int D, int N>
+__device__ __forceinline__ void append_values(const AppendParams& P, size_t at, int fill, int n, size_t rows, int h, int row, int i0, int lane) {
+    constexpr int kE = D / 64, kBytes = kE * (DT == FSD_F32 ? 4 : 2);
+    unsigned char* vc = static_cast<unsigned char*>(P.cache.v_codes) + at * (kBlock * D);
+    const float old_s = P.cache.v_scale[at];
+    struct alignas(kBytes) Raw { unsigned char of[kBytes]; };
+    Raw raw[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        raw[t] = Raw{};
+        if (t >= n) continue;
+        const size_t r = rows + __builtin_amdgcn_readlane(row, i0 + t);
+        raw[t] = *reinterpret_cast<const Raw*>(P.v + (r * P.stride + static_cast<size_t>(h) * D + lane * kE) * (DT == FSD_F32 ? 4 : 2));
+    }
+    const int run = fill / 16, f = fill % 16;                 // the first of the two runs of 16 tokens, and the first new place in it
+    const bool two = f + n > 16;
+    u32x4* to = reinterpret_cast<u32x4*>(vc) + run * D + lane * kE;
+    u32x4 old[2][kE];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        old[0][e] = to[e];
+        old[1][e] = u32x4{0u, 0u, 0u, 0u};
+        if (two) old[1][e] = to[D + e];
+    }
+    float y[N][kE], m = 0.0f;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            if constexpr (DT == FSD_F32) y[t][e] = __builtin_bit_cast(float, *reinterpret_cast<const unsigned*>(raw[t].of + 4 * e));
+            else if constexpr (DT == FSD_BF16) y[t][e] = __uint_as_float(static_cast<unsigned>(*reinterpret_cast<const unsigned short*>(raw[t].of + 2 * e)) << 16);
+            else y[t][e] = static_cast<float>(*reinterpret_cast<const _Float16*>(raw[t].of + 2 * e));
+            m = __builtin_fmaxf(m, __builtin_fabsf(y[t][e]));  // (a NaN is passed over)
+        }
+    if (__any(m == __builtin_inff())) {                       // only finite ones count
+        m = 0.0f;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int e = 0; e < kE; ++e) m = __builtin_fmaxf(m, finite_abs(y[t][e]));
+    }
+    float ratio;
+    const float s = scale_in_force(wave_max_all(m), fill, old_s, ratio), inv = 1.0f / s;
+    if (ratio != 1.0f) {                                      // (rare)
+        rescale(vc, run * D, ratio, lane, 64);
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int held = max(0, min(4, f - 4 * k));    // of this word's tokens
+                const unsigned keep = held == 4 ? ~0u : (1u << (8 * held)) - 1u, now = old[0][e][k];
+                old[0][e][k] = (rescaled4(now, ratio) & keep) | (now & ~keep);
+            }
+    }
+    // The new codes of a dimension move to their place in the runs by bytes, then by words; `places`: which bytes of these words are new
+    const unsigned places = ((1u << n) - 1u) << (f & 3);
+    auto put = [&](auto word) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            unsigned before = 0u;
+#pragma unroll
+            for (int j = 0; j <= N / 4; ++j) {
+                unsigned c = 0u;
+                if (j < N / 4) c = codes4(y[4 * (j % (N / 4))][e] * inv, y[4 * (j % (N / 4)) + 1][e] * inv, y[4 * (j % (N / 4)) + 2][e] * inv, y[4 * (j % (N / 4)) + 3][e] * inv);
+                const unsigned w = static_cast<unsigned>((static_cast<unsigned long long>(c) << 32 | before) >> (32 - 8 * (f & 3)));
+                const unsigned bits = places >> (4 * j) & 15u, is_new = (bits * 0x00204081u & 0x01010101u) * 0xFFu;
+                constexpr int at0 = decltype(word)::value;
+                const int k = at0 + j;
+                old[k / 4][e][k % 4] = (w & is_new) | (old[k / 4][e][k % 4] & ~is_new);
+                before = c;
+            }
+        }
+    };
+    switch (f / 4) {
+        case 0: put(std::integral_constant<int, 0>()); break;
+        case 1: put(std::integral_constant<int, 1>()); break;
+        case 2: put(std::integral_constant<int, 2>()); break;
+        default: put(std::integral_constant<int, 3>()); break;
+    }
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+        to[e] = old[0][e];
+        if (two) to[D + e] = old[1][e];
+    }
+    if (lane == 0) P.cache.v_scale[at] = s;
+}
+
+// Grid: two wavefronts for each key head, sequences, layers.
+template <int DT, int D>
 __global__ __launch_bounds__(kWG) void append_few(AppendParams P) {
-    constexpr int kPer = D / 8, kSlots = TOKENS * kPer / 64;  // slots of 8 elements: of a token, of a lane
     const int lane = threadIdx.x % 64, H = P.cache.kv_heads;
-    const unsigned piece = blockIdx.x * (kWG / 64) + threadIdx.x / 64;
-    if (piece >= P.npieces) return;
-    const int h = static_cast<int>(piece % H), b = static_cast<int>(piece / H % P.B), layer = static_cast<int>(piece / H / P.B);
-    const Appended a(P, b);
-    const bool bad = a.bad || (a.count > 0 && __any(a.look(P, lane, 64)));
-    if (h == 0 && layer == 0 && lane == 0) report(P, b, a, bad);
-    if (bad || a.count <= 0) return;
+    const int at_wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (kWG / 64) + threadIdx.x / 64), h = at_wave / 2;
+    if (h >= H) return;
+    const bool values = at_wave & 1;
+    const int b = static_cast<int>(blockIdx.y), layer = static_cast<int>(blockIdx.z);
+    const Few a(P, b, lane);
+    if (h == 0 && layer == 0 && lane == 0 && !values) {
+        if (P.len_out) P.len_out[b] = static_cast<int32_t>(a.bad ? a.len : a.len + a.count);
+        if (P.status) P.status[b] = a.bad ? FSD_ROW_BAD_CACHE : 0;
+    }
+    if (a.bad || a.count <= 0) return;
     const size_t rows = (static_cast<size_t>(layer) * P.B + b) * P.R;
-    for (long from = a.len; from < a.len + a.count;) {
-        const long block = from / kBlock, to = (block + 1) * kBlock < a.len + a.count ? (block + 1) * kBlock : a.len + a.count;
-        const int fill = static_cast<int>(from - block * kBlock);   // tokens of the sequence that the block holds already
-        const int n = static_cast<int>(to - from);
-        const size_t at = (static_cast<size_t>(layer) * P.cache.num_blocks + a.table[block]) * H + h;   // block and head
-        unsigned char* kc = static_cast<unsigned char*>(P.cache.k_codes) + at * (kBlock * D);
-        unsigned char* vc = static_cast<unsigned char*>(P.cache.v_codes) + at * (kBlock * D);
-        const float old_k = P.cache.k_scale[at], old_v = P.cache.v_scale[at];
-        size_t head[kSlots];
-        int dim[kSlots], pos[kSlots], token[kSlots];
-        Raw8 raw[kSlots];
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i) {
-            const int u = lane + i * 64, t = u / kPer;
-            token[i] = t < n ? t : -1;
-            const long i0 = from - a.len + (t < n ? t : 0);   // (the first one where there is none)
-            head[i] = (rows + a.row(i0)) * P.stride + static_cast<size_t>(h) * D;
-            dim[i] = u % kPer * 8;
-            pos[i] = static_cast<int>(a.len + i0);
-        }
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i)
-            if (i * 64 / kPer < n) request8(DT, P.v, head[i] + dim[i], raw[i]);
-        float x[kSlots][8];
-        if (kSlots > 1 && n * kPer <= 64) {                   // one slot a lane holds them all
-            const size_t one_head[1] = {head[0]};
-            const int one_dim[1] = {dim[0]}, one_pos[1] = {pos[0]};
-            float y[1][8];
-            load_turned<1>(DT, P.k, one_head, one_dim, P.rot, one_pos, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[0][e] = y[0][e];
+    int done = 0;
+    for (int which = 0; done < a.count; ++which) {            // the blocks: one, seldom two
+        const int fill = which == 0 ? static_cast<int>(a.len % kBlock) : 0;   // tokens of the sequence that the block holds already
+        const int n = min(static_cast<int>(a.count) - done, kBlock - fill);
+        const size_t at = (static_cast<size_t>(layer) * P.cache.num_blocks + __builtin_amdgcn_readlane(a.block, which)) * H + h;   // block and head
+        const int pos0 = static_cast<int>(a.len) + done;
+        // (few tokens: most of the instructions are left out)
+        if (values) {
+            if (n <= 4) append_values<DT, D, 4>(P, at, fill, n, rows, h, a.row, done, lane);
+            else append_values<DT, D, kFew>(P, at, fill, n, rows, h, a.row, done, lane);
         } else {
-            load_turned<kSlots, 1>(DT, P.k, head, dim, P.rot, pos, x);
+            if (n <= 512 / D) append_keys<DT, D, 1>(P, at, fill, n, rows, h, a.row, done, pos0, lane);
+            else append_keys<DT, D, kFew * D / 512>(P, at, fill, n, rows, h, a.row, done, pos0, lane);
         }
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = token[i] >= 0 ? x[i][e] : 0.0f;
-        float ratio;
-        const float ks = scale_in_force(largest_of<kSlots>(x), fill, old_k, ratio), kinv = 1.0f / ks;
-        if (ratio != 1.0f) rescale_keys<D>(kc, fill, ratio, lane, 64);
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i)
-            if (token[i] >= 0) *reinterpret_cast<uint2*>(kc + (fill + token[i]) * D + dim[i]) = codes8(x[i], kinv);
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i) {
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = 0.0f;
-            if (token[i] >= 0) unpack8(DT, raw[i], y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = y[e];
-        }
-        const float vs = scale_in_force(largest_of<kSlots>(x), fill, old_v, ratio), vinv = 1.0f / vs;
-        if (ratio != 1.0f) {
-            const int words = (fill + 3) / 4;                 // of a row of d: 4 a group
-#pragma unroll 1
-            for (int i = lane; i < words * D; i += 64) {
-                const int q = i / D, d = i % D;
-                unsigned* w = reinterpret_cast<unsigned*>(vc + (q / 4 * D + d) * 16) + q % 4;
-                const unsigned old = *w, keep = q * 4 + 4 <= fill ? 0u : ~0u << (8 * (fill - q * 4));
-                *w = (rescaled4(old, ratio) & ~keep) | (old & keep);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");   // before the new bytes of the same words
-        }
-#pragma unroll
-        for (int i = 0; i < kSlots; ++i)
-            if (token[i] >= 0) {
-                const int place = fill + token[i];
-                unsigned char* p = vc + (place / 16 * D + dim[i]) * 16 + place % 16;
-                const uint2 w = codes8(x[i], vinv);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e * 16] = static_cast<unsigned char>((e < 4 ? w.x : w.y) >> (e % 4 * 8));
-            }
-        if (lane == 0) {
-            P.cache.k_scale[at] = ks;
-            P.cache.v_scale[at] = vs;
-        }
-        from = to;
+        done += n;
     }
 }
 
@@ -302,7 +397,7 @@ __global__ __launch_bounds__(kWG) void append_many(AppendParams P) {
     float kratio, vratio;
     const float ks = scale_in_force(most(0), fill, old_k, kratio), kinv = 1.0f / ks;
     const float vs = scale_in_force(most(1), fill, old_v, vratio), vinv = 1.0f / vs;
-    if (kratio != 1.0f) rescale_keys<D>(kc, fill, kratio, tid, kWG);
+    if (kratio != 1.0f) rescale(kc, fill * (D / 16), kratio, tid, kWG);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
         const int t = (tid + i * kWG) / kPer;

@@ -114,8 +114,7 @@ int check_rotation(const fsd_rotation* r, int head_dim, fsd_rotation* out) {
 
 template <int DT, int D>
 void launch_append(hipStream_t st, const AppendParams& P, int tokens) {
-    if (tokens <= 8) hipLaunchKernelGGL((append_few<DT, D, 8>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
-    else if (tokens <= 16) hipLaunchKernelGGL((append_few<DT, D, 16>), dim3((P.npieces + 3) / 4), dim3(kWG), 0, st, P);
+    if (tokens <= kFew) hipLaunchKernelGGL((append_few<DT, D>), dim3((P.cache.kv_heads + 1) / 2, P.B, P.cache.layers), dim3(kWG), 0, st, P);
     else hipLaunchKernelGGL((append_many<DT, D>), dim3(P.npieces), dim3(kWG), 0, st, P);
 }
 template <int DT>
@@ -317,10 +316,10 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
     P.cache = *cache;
     P.len_out = cache_len_out;
     P.status = row_status;
-    // up to 16 rows: a wavefront a head, whichever blocks they touch; else a workgroup for each block
-    P.slots = P.max_rows <= 16 ? 1 : (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
+    // few rows: two wavefronts a head, whichever blocks they touch; else a workgroup for each block
+    P.slots = P.max_rows <= kFew ? 1 : (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
     const long pieces = static_cast<long>(cache->layers) * B * H * P.slots;
-    if (pieces > INT_MAX - 8) return FSD_ERR_SHAPE;
+    if (pieces > INT_MAX - 8 || cache->layers > 65535) return FSD_ERR_SHAPE;
     P.npieces = static_cast<unsigned>(pieces);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, P.max_rows);
