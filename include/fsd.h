@@ -322,8 +322,8 @@ int fsd_calibrate_threshold(const float* divergences, int B, int K, float target
  *   z2 = z1 - frequency * count(v) - (count(v) > 0 ? presence : 0)
  *   z3 = z2 + bias(v);  -inf where the mask does not allow v
  *
- * in binary32 in this order, rounded once to the logits' type; an entry that
- * none of this touches keeps its bits.  A masked entry is -inf whatever it held
+ * in binary32 in this order (z / r as z * (1 / r), which costs one rounding of 2^-24 more), rounded
+ * once to the logits' type; an entry that none of this touches keeps its bits.  A masked entry is -inf whatever it held
  * (NaN as well); a mask that allows nothing leaves a row of -inf, which a verify
  * call reports (FSD_ROW_NONFINITE).
  *
@@ -333,7 +333,7 @@ typedef struct {
     const int32_t* history;      /* [B, history_stride] token ids, in order; ids outside [0, V) are passed over */
     const int32_t* history_len;  /* [B] how many count (taken as within [0, history_stride]); NULL: all */
     const int32_t* prompt_len;   /* [B] how many of them are the prompt; NULL: none */
-    int history_stride;
+    int history_stride;          /* 0 .. 2^29 */
     int bias_count;
     const int32_t* bias_tokens;  /* [B, bias_count]; ids outside [0, V) are passed over; of equal ids the last counts */
     const float* bias_values;    /* [B, bias_count] */
@@ -349,7 +349,8 @@ typedef struct {
  *                             rows.  Row i stands behind candidates 0 .. i-1 (both kinds).
  *   cand_tokens [B, K]        candidate token ids (0 <= K <= 2048; may be NULL when K is 0: a
  *                             step without candidates); ids outside [0, V) are passed over
- *   out         [B, rows, V]  out; may be logits itself (in place), else must not overlap it
+ *   out         [B, rows, V]  out; may be logits itself (in place), else must not overlap it; both on addresses of whole elements
+ *                             (FSD_F32 or FSD_BF16), B * rows < 2^24
  * A mask per context has K+1 of them, also for draft rows: context i stands behind candidates 0 .. i-1.
  */
 int fsd_condition_chain(const void* logits, const int32_t* cand_tokens, int B, int K, int rows, int V, int dtype,
@@ -430,7 +431,8 @@ typedef struct {
  * set, if accept_len is outside [-1, R) (or over max_depth), a path node outside [0, R-1), cache_len or the new length
  * outside [0, 64 * max_blocks], a block to be written outside [0, num_blocks) or a position outside the rotation's table.
  * Two sequences that append to one block in one call race on it.
- * R <= 2^20, B <= 65535, layers * B * kv_heads * blocks a sequence < 2^31.
+ * R <= 2^20, B <= 65535.  Calls of up to 16 rows a sequence (R, or max_depth + 1): layers <= 65535; of more: layers * B *
+ * kv_heads * (blocks that R rows can touch) < 2^24.
  */
 int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, int R, int dtype,
                      const int32_t* accept_len, const int32_t* path_nodes, int max_depth,
@@ -448,7 +450,8 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
  *   k, v     [B, R, kv_heads, head_dim]   same type
  *   q_stride, kv_stride                   elements from one token to the next (multiples of 8;
  *                                         sequences are R tokens apart); q, k, v are 16-byte aligned
- *   row_count [B]  optional: rows of the sequence (taken as within [0, R]); what lies behind them is neither read nor written
+ *   row_count [B]  optional: rows of the sequence (taken as within [0, R]); what lies behind them (their nodes' parents as well)
+ *                  is neither read nor written
  *   scale          of the products before the softmax (any finite number)
  *   rotation       of q and k, at position cache_len + (number of rows before it that the row sees); NULL: none
  *   layer          which of the cache's layers
@@ -459,9 +462,11 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
  *   workspace      fsd_attend_workspace_bytes(...) bytes, 256-byte aligned
  *
  * Products of 16-bit operands are summed in binary32; the rotated queries and keys and the softmax's weights
- * enter them with the 11 significant bits of binary16 (scaled so that they stay in its range), the codes exactly; statistics are
- * binary32, the result is rounded once.  A NaN among the keys, values or codes a row sees makes its outputs NaN.
- * 1 <= R <= 2049, 1 <= heads / kv_heads <= 64, heads <= 1024, B <= 65535, B * R < 2^24.
+ * enter them with the 11 significant bits of binary16 (scaled so that they stay in its range; FSD_F16's queries and keys, which may use
+ * all 11, in two parts), the codes exactly; statistics are binary32, the result is rounded once.  Magnitudes of values up to
+ * 2^120 and value scales from 2^-100 to 2^111 are in range.  A NaN among the keys or codes a row sees makes its outputs NaN, and so does
+ * a value among the rows that is not finite (all head_dim outputs of the heads that read it); what a row does not see never matters.
+ * 1 <= R <= 2049, 1 <= heads / kv_heads <= 64, heads <= 1024, B <= 65535, B * R < 2^24, B * R * heads * head_dim < 2^33.
  */
 size_t fsd_attend_workspace_bytes(int B, int R, int heads, int kv_heads, int head_dim);
 int fsd_attend_chain(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, int B, int R,

@@ -259,7 +259,7 @@ __device__ __forceinline__ void two_parts(const float (&y)[8], float by, half8_t
 }
 
 // Queries and the rows' keys and values in the layout of the products; the plan; the sequences' reports.  Workgroup 0 deals the work out; of the others
-// each belongs to one sequence and takes one tile of 64 rows of a key head, or some query rows.  What it costs is latencies: everything a thread reads
+// each belongs to one sequence and takes some query rows, or keys or values of one tile of 64 rows of a key head.  What it costs is latencies: everything a thread reads
 // is requested at once, and nothing changes places between threads.
 // FINE (binary16 inputs): a turned query or key is held in two parts of 11 bits, as one rounding of them would cost more than that of the result:
 // 0.00047 of the result's norm in place of 0.00025 at 131072 tokens.
@@ -274,9 +274,9 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         deal(P);
         return;
     }
-    const int H = P.cache.kv_heads, R = P.R, G = P.G, all_tiles = P.B * H * P.tiles, at_block = static_cast<int>(blockIdx.x) - 1;
+    const int H = P.cache.kv_heads, R = P.R, G = P.G, all_tiles = P.B * H * P.tiles * (kI + 1), at_block = static_cast<int>(blockIdx.x) - 1;
     const bool is_tile = at_block < all_tiles;                // (tiles first: they take longest)
-    const int b = is_tile ? at_block / (H * P.tiles) : (at_block - all_tiles) / P.query_groups;
+    const int b = is_tile ? at_block / (H * P.tiles * (kI + 1)) : (at_block - all_tiles) / P.query_groups;
     const Share share = share_of(P, b);
     const int len = max(0, min(P.cache.cache_len[b], P.cache.max_blocks * kBlock));
     short* up = tree;
@@ -287,8 +287,8 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     if (P.parent) {
         const int32_t* parent = P.parent + static_cast<size_t>(b) * (R - 1);
         for (int r = tid; r < R; r += kThreads) {
-            int p = -1;                                       // row 0 has none
-            if (r > 0) {
+            int p = -1;                                       // row 0 has none, and those behind the sequence's last row are not looked at
+            if (r > 0 && r < share.rows) {
                 p = parent[r - 1];
                 const bool bad = p < -1 || p >= r - 1;
                 bad_tree |= bad;
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         // in deep ones by doubling: after step i a row knows its 2^i-th ancestor and how far that is
         for (int r = tid; r < R; r += kThreads) {
             stands[r] = up[r];
-            depth[r] = r > 0 ? 1 : 0;
+            depth[r] = up[r] >= 0 ? 1 : 0;
         }
         __syncthreads();
         for (;;) {
@@ -336,6 +336,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     };
     auto table_row = [&](int pos) { return P.rot.table ? min(pos, P.rot.rows - 1) : 0; };
     const bool fine = P.dtype == FSD_F16;
+    constexpr int kSlots = 2;                                 // rows of which a thread takes 8 dimensions, D / 8 neighbours the whole of a row
 
     if (!is_tile) {
         const int part = (at_block - all_tiles) % P.query_groups;
@@ -350,8 +351,6 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             bad_tree = __syncthreads_or(bad_tree);
             if (tid == 0) P.status[b] = (bad ? FSD_ROW_BAD_CACHE : 0) | (bad_tree ? FSD_ROW_BAD_PARENT : 0);
         }
-        // a thread takes 8 dimensions of kSlots rows, D / 8 neighbours the whole of a row
-        constexpr int kSlots = 2;
         const size_t parts = static_cast<size_t>(P.B) * H * P.row_tiles * 2 * kI * 1024;
         const int n = share.rows * P.heads, row0 = part * (kSlots * kThreads / kPer) + tid / kPer, dim = tid % kPer * 8;
         if (row0 >= n) return;
@@ -387,10 +386,46 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         }
         return;
     }
-    const int tile = at_block % P.tiles, h = at_block / P.tiles % H, t0 = tile * kBlock, n = min(kBlock, share.rows - t0);
-    if (n <= 0) return;
+    // kI workgroups a tile and head for the keys, one for the values
+    const int kind = at_block % (kI + 1), tile = at_block / (kI + 1) % P.tiles, h = at_block / (kI + 1) / P.tiles % H, t0 = tile * kBlock, n = min(kBlock, share.rows - t0);
     const size_t bht = (static_cast<size_t>(b) * H + h) * P.tiles + tile, size = static_cast<size_t>(P.B) * H * P.tiles * 8 * kI * 1024;
     const size_t base = (static_cast<size_t>(b) * R + t0) * P.kv_stride + static_cast<size_t>(h) * D;
+    if (kind < kI) {
+        // keys: every token scaled by a power of two of its own.  (What lies behind the last row is not written: no weight comes of it.)
+        const int first = kind * (kBlock / kI) + tid / kPer, dim = tid % kPer * 8;
+        if (first >= n) return;
+        size_t at[kSlots];
+        int dims[kSlots], pos[kSlots];
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            const int t = min(first + i * (kThreads / kPer), n - 1);
+            at[i] = base + t * P.kv_stride;
+            dims[i] = dim;
+            pos[i] = table_row(position(t0 + t));
+        }
+        float y[kSlots][8];
+        load_turned<kSlots>(P.dtype, P.k, at, dims, P.rot, pos, y);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) {
+            const int t = first + i * (kThreads / kPer);
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[i][e]));
+#pragma unroll
+            for (int o = kPer / 2; o > 0; o >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, o, 64));
+            if (t >= n) continue;
+            const float by = key_range(most);
+            half8_t a, c;
+            two_parts(y[i], by, a, c);
+            const int fragment = (t >> 2 & 3) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1), place = (dim / 16 & 3) * 16 + (t >> 4) * 4 + (t & 3);
+            char* to = P.k16 + bht * (8 * kI * 1024) + fragment * 1024 + place * 16;
+            *reinterpret_cast<half8_t*>(to) = a;
+            if (fine) *reinterpret_cast<half8_t*>(to + size) = c;
+            if (dim == 0) P.key_scale[bht * kBlock + t] = 1.0f / by;
+        }
+        return;
+    }
+    if (n <= 0) return;
     // values: a thread takes 8 tokens of one dimension, which lie in one of the product's fragments
     constexpr int kUnits = kBlock * D / 8 / kThreads;
     unsigned raw[kUnits][4];
@@ -407,27 +442,6 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             const unsigned w = values[min(t + e, n - 1) * P.kv_stride + d];   // (behind the last row it comes again, and is blanked)
             raw[i][e / 2] |= (t + e < n ? w : 0u) << (16 * (e & 1));
         }
-    }
-    // keys: every token scaled by a power of two of its own.  (What lies behind the last row is not written: no weight comes of it.)
-    for (int u = tid; u / kPer < n; u += kThreads) {
-        const int t = u / kPer, dim = u % kPer * 8;
-        const size_t at[1] = {base + t * P.kv_stride};
-        const int dims[1] = {dim}, pos[1] = {table_row(position(t0 + t))};
-        float y[1][8];
-        load_turned<1>(P.dtype, P.k, at, dims, P.rot, pos, y);
-        float most = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[0][e]));
-#pragma unroll
-        for (int o = kPer / 2; o > 0; o >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, o, 64));
-        const float by = key_range(most);
-        half8_t a, c;
-        two_parts(y[0], by, a, c);
-        const int fragment = (t >> 2 & 3) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1), place = (dim / 16 & 3) * 16 + (t >> 4) * 4 + (t & 3);
-        char* to = P.k16 + bht * (8 * kI * 1024) + fragment * 1024 + place * 16;
-        *reinterpret_cast<half8_t*>(to) = a;
-        if (fine) *reinterpret_cast<half8_t*>(to + size) = c;
-        if (dim == 0) P.key_scale[bht * kBlock + t] = 1.0f / by;
     }
     // all values are scaled by one power of two; one that is not finite is noted, as no weight of 0 makes it harmless
     float most = 0.0f;

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kMaxRows = 2048;    // K or N, as in the verify calls
 constexpr int kMaxBatch = 65535;
+constexpr long kMaxGroups = (1L << 32) / kWG - 1;   // workgroups of a launch: less than 2^32 threads
 
 inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 inline int launched() { return hipGetLastError() == hipSuccess ? FSD_OK : FSD_ERR_LAUNCH; }
@@ -76,7 +77,7 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     P.ngroups = (rows + P.rows_per_wg - 1) / P.rows_per_wg;
     P.nwork = pieces * P.ngroups;
     const long grid = grid_over_xcds(P.nwork);
-    if (grid > INT_MAX) return FSD_ERR_SHAPE;
+    if (grid > kMaxGroups) return FSD_ERR_SHAPE;
     P.side = c.bias_count < P.slice ? c.bias_count : P.slice;
     size_t lds = lds_of(P.slice);
     if (tree) lds += (static_cast<size_t>(P.rows_per_wg) / 32 + 1) * 4 + static_cast<size_t>(N) * 4;
@@ -229,7 +230,7 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     if (bad != FSD_OK) return bad;
     if (dtype != FSD_BF16 && dtype != FSD_F16) return FSD_ERR_DTYPE;
     const int H = cache->kv_heads, D = cache->head_dim;
-    if (!attend_sizes(B, R, heads, H, D) || layer < 0 || layer >= cache->layers || !std::isfinite(scale)) return FSD_ERR_SHAPE;
+    if (!attend_sizes(B, R, heads, H, D) || layer < 0 || layer >= cache->layers || !std::isfinite(scale * kLog2eF)) return FSD_ERR_SHAPE;
     if (q_stride < static_cast<int64_t>(heads) * D || kv_stride < static_cast<int64_t>(H) * D || q_stride % 8 != 0 || kv_stride % 8 != 0 ||
         q_stride > (1L << 32) || kv_stride > (1L << 32) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return FSD_ERR_LAYOUT;
@@ -268,9 +269,9 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.query_groups = static_cast<int>((static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG));
     // A workgroup of attend_join takes one row where the rows are few, else as many as its lanes hold.
     const int by_pieces = static_cast<long>(B) * R * heads <= 4096, row_groups = by_pieces ? 1 : 4 * kWG / D;
-    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles), joins = (static_cast<long>(R) * heads + row_groups - 1) / row_groups;
+    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles * (D / 64 + 1)), joins = (static_cast<long>(R) * heads + row_groups - 1) / row_groups;
     const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
-    if (B * joins > INT_MAX || prepare > INT_MAX || units > INT_MAX) return FSD_ERR_SHAPE;
+    if (B * joins > kMaxGroups || prepare > kMaxGroups || units > INT_MAX) return FSD_ERR_SHAPE;
     const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
     if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
     else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
@@ -319,8 +320,8 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
     // few rows: two wavefronts a head, whichever blocks they touch; else a workgroup for each block
     P.slots = P.max_rows <= kFew ? 1 : (P.max_rows - 1 + kBlock - 1) / kBlock + 1;
     const long pieces = static_cast<long>(cache->layers) * B * H * P.slots;
-    if (pieces > INT_MAX - 8 || cache->layers > 65535) return FSD_ERR_SHAPE;
-    P.npieces = static_cast<unsigned>(pieces);
+    if (P.max_rows <= kFew ? cache->layers > 65535 : pieces > kMaxGroups) return FSD_ERR_SHAPE;
+    P.npieces = static_cast<unsigned>(pieces);                // (append_many's grid)
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, P.max_rows);
     else if (dtype == FSD_BF16) launch_append_d<FSD_BF16>(st, P, P.max_rows);

@@ -505,6 +505,32 @@ def test_attend_out_of_range(G):
     assert (np.abs(got - want)[:5] <= bound[:5]).all() and (got[5] == 7.0).all()
 
 
+@pytest.mark.parametrize("R", [12, 400])
+def test_attend_parents_behind_the_last_row(R):
+    """A padded batch: the nodes behind a sequence's rows may have any parents; its result is that of the rows alone."""
+    rng = np.random.default_rng(R)
+    lens, rows = [90, 30], [R - 3, R // 2]
+    table, c, q, k, v = _case(rng, lens, R, 4, 2, 64, torch.bfloat16)
+    cache, turns = _to_cache(c, table, lens), _turns(100 + R, 64)
+    parent = _rand_parents(rng, 2, R - 1)
+    for b in range(2):
+        parent[b, rows[b] - 1:] = rng.integers(-2 ** 31, 2 ** 31 - 1, R - rows[b])
+    out = dict(out=torch.full((2, R, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda"), row_status=torch.full((2,), -1, dtype=torch.int32, device="cuda"))
+    fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, rotation=_rotation(turns, True),
+                        row_count=torch.tensor(rows, dtype=torch.int32, device="cuda"), out=out)
+    assert out["row_status"].tolist() == [0, 0]
+    for b in range(2):
+        n = rows[b]
+        one = fsd.Cache(cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, cache.block_table[b:b + 1], cache.cache_len[b:b + 1])
+        alone = fsd.fsd_attend_tree(q[b:b + 1, :n], k[b:b + 1, :n], v[b:b + 1, :n], torch.from_numpy(parent[b:b + 1, :n - 1].copy()).cuda(), one,
+                                    rotation=_rotation(turns, True))["out"]
+        want, bound = ref.attend(_host(q[b:b + 1, :n]), _host(k[b:b + 1, :n]), _host(v[b:b + 1, :n]), parent[b:b + 1, :n - 1], np.array([n]), c, 0,
+                                 lens[b:b + 1], table[b:b + 1], 0.125, turns, True, torch.bfloat16)
+        _within(alone, want, bound)
+        _within(out["out"][b:b + 1, :n], want, bound)
+        assert (out["out"][b, n:] == 7.0).all()
+
+
 @pytest.mark.parametrize("R", [300, 900])
 def test_attend_deep_tree_is_a_chain(R):
     """A tree that is a chain gives the chain's result bit for bit (paths too long to be walked; tiles that a walk passes through)."""
