@@ -202,24 +202,29 @@ def fsd_condition_tree(logits, node_tokens, parent, conditions, *, out=None, str
     return _condition("fsd_condition_tree", logits, node_tokens, parent, conditions, out, stream)
 
 
-def _dtype_code(t, names, codes):
-    torch = _torch()
-    for name, code in zip(names, codes):
-        if t.dtype == getattr(torch, name):
-            return code
-    raise TypeError(f"{' or '.join(names)} wanted, got {t.dtype}")
+_codes = {}
+
+
+def _dtype_code(t, floats):
+    if not _codes:
+        torch = _torch()
+        _codes.update({torch.float32: binding.F32, torch.bfloat16: binding.BF16, torch.float16: F16})
+    code = _codes.get(t.dtype)
+    if code is None or (code == binding.F32 and not floats):
+        raise TypeError(f"{'float32, ' if floats else ''}bfloat16 or float16 wanted, got {t.dtype}")
+    return code
 
 
 def _token_stride(t, name, shape, dtype, device):
     """Elements between tokens of [..., B, R, heads, head_dim]: heads lie side by side, and the tokens at one distance."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    if t.device != device:
+    if t.device != device:                   # (the others': a GPU)
         raise ValueError(f"{name} lives on {t.device}, the others on {device}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.is_contiguous():
+        return shape[-1] * shape[-2]
     size, stride = t.shape, t.stride()
     if size[-1] > 1 and stride[-1] != 1 or size[-2] > 1 and stride[-2] != size[-1]:
         raise ValueError(f"{name}: the heads of a token must be contiguous")
@@ -241,15 +246,15 @@ def fsd_cache_append(k, v, cache, accept_len, *, path_nodes=None, rotation=None,
     path_nodes int32 [B,max_depth] as a verify call gives them -> dict with cache_len (the new lengths, to be
     copied into the cache's own once no call reads those) and row_status."""
     torch = _torch()
-    dt = _dtype_code(k, ("float32", "bfloat16", "float16"), (binding.F32, binding.BF16, F16))
+    dt = _dtype_code(k, True)
     dev = cache.device
     _on_current(dev)
-    if k.dim() == 4:
-        k, v = k.unsqueeze(0), v.unsqueeze(0)
-    if k.dim() != 5:
+    if k.dim() not in (4, 5):
         raise ValueError("k has 4 or 5 dimensions")
-    B, R = k.shape[1:3]
-    shape = (cache.layers, cache.batch, R, cache.kv_heads, cache.head_dim)
+    B, R = k.shape[-4:-2]
+    shape = (cache.batch, R, cache.kv_heads, cache.head_dim)
+    if k.dim() == 5 or cache.layers != 1:
+        shape = (cache.layers, *shape)
     step = _token_stride(k, "k", shape, k.dtype, dev)
     if _token_stride(v, "v", shape, k.dtype, dev) != step:
         raise ValueError("k and v differ in the distance between tokens")
@@ -287,7 +292,7 @@ def fsd_attend_workspace_bytes(B: int, R: int, heads: int, kv_heads: int, head_d
 
 def _attend(call, q, k, v, parent, cache, layer, row_count, rotation, scale, out, workspace, stream):
     torch = _torch()
-    dt = _dtype_code(q, ("bfloat16", "float16"), (binding.BF16, F16))
+    dt = _dtype_code(q, False)
     dev = cache.device
     _on_current(dev)
     if q.dim() != 4:
