@@ -60,7 +60,7 @@ struct AttendParams {
     int tile;                      // rows of an item
     int row_tiles;                 // of 16 rows, of a (sequence, key head): whole items
     int tiles;                     // of 64 tokens of the R rows
-    int query_groups;              // workgroups of attend_prepare that a sequence's queries take
+    unsigned by_heads, by_G, by_tile;   // for dividing by heads, G and tile
     // workspace
     long* plan;                    // [0] units of a workgroup, [1 + b] units of the sequences before b
     int2* pieces;                  // [B, kv_heads, groups] of an item: its first slot, and how many workers share it
@@ -122,6 +122,10 @@ __device__ __forceinline__ void deal(const AttendParams& P) {
         P.plan[1 + P.B] = base;
     }
 }
+
+// n / d for n d < 2^32, with by = ceil(2^32 / d).  (The division that the compiler writes out is 30 instructions, and the kernels around the products
+// are bound by theirs.)
+__device__ __forceinline__ int divided(int n, int d, unsigned by) { return d == 1 ? n : static_cast<int>(__umulhi(static_cast<unsigned>(n), by)); }
 
 __device__ __forceinline__ half8_t widened(unsigned lo, unsigned hi) {
     half8_t r;
@@ -248,35 +252,36 @@ __device__ __forceinline__ float4_t product(const half8_t& a, const half8_t& b, 
     if constexpr (FINE) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b2, c, 0, 0, 0);
     return c;
 }
-// y times a power of two in binary16: the first part, and what is left in a second
+// y times a power of two in binary16: the first part, and with FINE what is left in a second
+template <bool FINE>
 __device__ __forceinline__ void two_parts(const float (&y)[8], float by, half8_t& a, half8_t& c) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float z = y[e] * by;
         a[e] = static_cast<_Float16>(z);
-        c[e] = static_cast<_Float16>(z - static_cast<float>(a[e]));
+        if constexpr (FINE) c[e] = static_cast<_Float16>(z - static_cast<float>(a[e]));
     }
 }
 
-// Queries and the rows' keys and values in the layout of the products; the plan; the sequences' reports.  Workgroup 0 deals the work out; of the others
-// each belongs to one sequence and takes some query rows, or keys or values of one tile of 64 rows of a key head.  What it costs is latencies: everything a thread reads
+// Queries and the rows' keys and values in the layout of the products; the plan; the sequences' reports.  Grid: pieces of work, sequences.  The first workgroup
+// deals the work out; of the others each belongs to one sequence and takes some query rows, or keys or values of one tile of 64 rows of a key head.  What it costs is latencies: everything a thread reads
 // is requested at once, and nothing changes places between threads.
 // FINE (binary16 inputs): a turned query or key is held in two parts of 11 bits, as one rounding of them would cost more than that of the result:
 // 0.00047 of the result's norm in place of 0.00025 at 131072 tokens.
-template <int D>
+template <int D, bool FINE>
 __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
-    constexpr int kI = D / 64, kPer = D / 8, kThreads = kWG;
+    constexpr int kType = FINE ? FSD_F16 : FSD_BF16, kI = D / 64, kPer = D / 8, kThreads = kWG;
     __shared__ float most_of[kWG / 64];
     __shared__ unsigned long long broken;
     extern __shared__ short tree[];                           // trees: [R] parent's row, [R] depth, [R] ancestors found so far
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (blockIdx.x == 0) {
-        deal(P);
+        if (blockIdx.y == 0) deal(P);
         return;
     }
-    const int H = P.cache.kv_heads, R = P.R, G = P.G, all_tiles = P.B * H * P.tiles * (kI + 1), at_block = static_cast<int>(blockIdx.x) - 1;
+    const int H = P.cache.kv_heads, R = P.R, G = P.G, all_tiles = H * P.tiles * (kI + 1), at_block = static_cast<int>(blockIdx.x) - 1;
     const bool is_tile = at_block < all_tiles;                // (tiles first: they take longest)
-    const int b = is_tile ? at_block / (H * P.tiles * (kI + 1)) : (at_block - all_tiles) / P.query_groups;
+    const int b = static_cast<int>(blockIdx.y);
     const Share share = share_of(P, b);
     const int len = max(0, min(P.cache.cache_len[b], P.cache.max_blocks * kBlock));
     short* up = tree;
@@ -335,11 +340,10 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         return n;
     };
     auto table_row = [&](int pos) { return P.rot.table ? min(pos, P.rot.rows - 1) : 0; };
-    const bool fine = P.dtype == FSD_F16;
     constexpr int kSlots = 2;                                 // rows of which a thread takes 8 dimensions, D / 8 neighbours the whole of a row
 
     if (!is_tile) {
-        const int part = (at_block - all_tiles) % P.query_groups;
+        const int part = at_block - all_tiles;
         if (part == 0 && P.status) {                          // the sequence's report
             const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
             bool bad = P.cache.cache_len[b] < 0 || P.cache.cache_len[b] > P.cache.max_blocks * kBlock ||
@@ -359,13 +363,13 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             row[i] = row0 + i * (kThreads / kPer);
-            const int there = min(row[i], n - 1), r = there / P.heads;
+            const int there = min(row[i], n - 1), r = divided(there, P.heads, P.by_heads);
             at[i] = (static_cast<size_t>(b) * R + r) * P.q_stride + static_cast<size_t>(there - r * P.heads) * D;
             dims[i] = dim;
             pos[i] = table_row(position(r));
         }
         float y[kSlots][8];
-        load_turned<kSlots>(P.dtype, P.q, at, dims, P.rot, pos, y);
+        load_turned<kSlots>(kType, P.q, at, dims, P.rot, pos, y);
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             float most = 0.0f;
@@ -376,12 +380,12 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             if (row[i] >= n) continue;
             const float by = key_range(most);
             half8_t a, c;
-            two_parts(y[i], P.scale < 0.0f ? -by : by, a, c);  // (a negative scale goes in here: a larger product is always a larger score)
-            const int r = row[i] / P.heads, head = row[i] - r * P.heads, h = head / G, rho = r * G + head - h * G;
+            two_parts<FINE>(y[i], P.scale < 0.0f ? -by : by, a, c);  // (a negative scale goes in here: a larger product is always a larger score)
+            const int r = divided(row[i], P.heads, P.by_heads), head = row[i] - r * P.heads, h = divided(head, G, P.by_G), rho = r * G + head - h * G;
             const size_t bh = static_cast<size_t>(b) * H + h, fragment = (bh * P.row_tiles + rho / 16) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1);
             char* to = P.q16 + fragment * 1024 + ((dim / 16 & 3) * 16 + (rho & 15)) * 16;
             *reinterpret_cast<half8_t*>(to) = a;
-            if (fine) *reinterpret_cast<half8_t*>(to + parts) = c;
+            if constexpr (FINE) *reinterpret_cast<half8_t*>(to + parts) = c;
             if (dim == 0) P.factor[bh * P.row_tiles * 16 + rho] = __builtin_fabsf(P.scale) / by;
         }
         return;
@@ -404,7 +408,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             pos[i] = table_row(position(t0 + t));
         }
         float y[kSlots][8];
-        load_turned<kSlots>(P.dtype, P.k, at, dims, P.rot, pos, y);
+        load_turned<kSlots>(kType, P.k, at, dims, P.rot, pos, y);
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) {
             const int t = first + i * (kThreads / kPer);
@@ -416,11 +420,11 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             if (t >= n) continue;
             const float by = key_range(most);
             half8_t a, c;
-            two_parts(y[i], by, a, c);
+            two_parts<FINE>(y[i], by, a, c);
             const int fragment = (t >> 2 & 3) * 2 * kI + dim / 64 * 2 + (dim / 8 & 1), place = (dim / 16 & 3) * 16 + (t >> 4) * 4 + (t & 3);
             char* to = P.k16 + bht * (8 * kI * 1024) + fragment * 1024 + place * 16;
             *reinterpret_cast<half8_t*>(to) = a;
-            if (fine) *reinterpret_cast<half8_t*>(to + size) = c;
+            if constexpr (FINE) *reinterpret_cast<half8_t*>(to + size) = c;
             if (dim == 0) P.key_scale[bht * kBlock + t] = 1.0f / by;
         }
         return;
@@ -1272,27 +1276,27 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
 
 // Joins the items that several workers share.  D / 4 lanes hold a row's dimensions, four each; such groups of lanes take a row each, or (by_pieces)
 // those of a workgroup share the pieces of one row, where the call has few rows and their pieces may be many.  8 pieces are requested at once.
+// Grid: runs of a key head's rows, key heads, sequences.
 template <int D>
-__global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_sequence, int by_pieces) {
+__global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int by_pieces) {
     constexpr int kLanes = D / 4, kGroups = kWG / kLanes;
     __shared__ float stats[kGroups][2];
     __shared__ __align__(16) float4_t sums[kGroups][kLanes];
-    const int b = blockIdx.x / per_sequence, at_row = static_cast<int>(blockIdx.x % per_sequence);
+    const int b = static_cast<int>(blockIdx.z), h = static_cast<int>(blockIdx.y), at_row = static_cast<int>(blockIdx.x);
     const int d = static_cast<int>(threadIdx.x) % kLanes * 4, which = static_cast<int>(threadIdx.x) / kLanes;
     const int nrho = (P.row_count ? max(0, min(P.row_count[b], P.R)) : P.R) * P.G, H = P.cache.kv_heads;
-    const int i = by_pieces ? at_row : at_row * kGroups + which;
-    const bool there = i < nrho * H;
-    const int h = there ? i / nrho : 0, rho = there ? i - h * nrho : 0, group = rho / P.tile, at = rho - group * P.tile;
+    const int rho = by_pieces ? at_row : at_row * kGroups + which, group = divided(rho, P.tile, P.by_tile), at = rho - group * P.tile;
     int2 piece = make_int2(0, 0);
-    if (there) piece = P.pieces[(static_cast<size_t>(b) * H + h) * (P.row_tiles * 16 / P.tile) + group];
+    if (rho < nrho) piece = P.pieces[(static_cast<size_t>(b) * H + h) * (P.row_tiles * 16 / P.tile) + group];
     const int n = piece.y, step = by_pieces ? kGroups : 1;
     if (by_pieces ? n <= 1 : !__any(n > 1)) return;           // (with by_pieces n is the workgroup's)
     const size_t size = static_cast<size_t>(P.tile) * (D + 2);
     const size_t stat = static_cast<size_t>(P.tile) * D + 2 * at, mine = static_cast<size_t>(at) * D + d;
     float top = -__builtin_inff(), sum = 0.0f;
     float4_t acc = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kOnce = 8;
-    for (int s0 = by_pieces ? which : 0; s0 < n; s0 += kOnce * step) {
+    // as many pieces at once as there are, up to 8
+    auto some = [&](int s0, auto once) {
+        constexpr int kOnce = decltype(once)::value;
         float4_t y[kOnce];
         float m[kOnce], l[kOnce], high = top;
 #pragma unroll
@@ -1322,7 +1326,10 @@ __global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_seque
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] = fmaf(y[k][e], by, acc[e]);
         }
-    }
+    };
+    int s0 = by_pieces ? which : 0;
+    if (!__any(s0 + 2 * step < n)) some(s0, std::integral_constant<int, 2>());
+    else for (; s0 < n; s0 += 8 * step) some(s0, std::integral_constant<int, 8>());
     if (by_pieces) {
         if (d == 0) {
             stats[which][0] = top;
@@ -1344,7 +1351,7 @@ __global__ __launch_bounds__(kWG) void attend_join(AttendParams P, int per_seque
         }
     }
     if (n <= 1) return;
-    const int r = rho / P.G, head = h * P.G + rho % P.G;
+    const int r = divided(rho, P.G, P.by_G), head = h * P.G + rho - r * P.G;
     store4(P.dtype, P.out, ((static_cast<size_t>(b) * P.R + r) * P.heads + head) * D + d, acc * (kPerUnit / sum));
 }
 

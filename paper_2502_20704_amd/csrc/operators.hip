@@ -203,8 +203,10 @@ void launch_attend_rows(hipStream_t st, const AttendParams& P) {
     else hipLaunchKernelGGL((attend_rows<D, RT, NW, false>), grid, dim3(NW * 64), 0, st, P);
 }
 template <int D>
-void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, int joins, int by_pieces) {
-    hipLaunchKernelGGL((attend_prepare<D>), dim3(prepare), dim3(kWG), lds, st, P);
+void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, unsigned prepare, size_t lds, unsigned joins, int by_pieces) {
+    const dim3 g(prepare, static_cast<unsigned>(P.B));
+    if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_prepare<D, true>), g, dim3(kWG), lds, st, P);
+    else hipLaunchKernelGGL((attend_prepare<D, false>), g, dim3(kWG), lds, st, P);
     constexpr int kRows = D == 256 ? 1 : 2;
     if (!s.few) {
         if (s.waves == 4) launch_attend_rows<D, kRows, 4>(st, P);
@@ -217,7 +219,7 @@ void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, 
         if (s.rt == 3) launch_attend_few<D, 3>(st, P);
         else launch_attend_few<D, 4>(st, P);
     }
-    hipLaunchKernelGGL((attend_join<D>), dim3(static_cast<unsigned>(P.B) * joins), dim3(kWG), 0, st, P, joins, by_pieces);
+    hipLaunchKernelGGL((attend_join<D>), dim3(joins, static_cast<unsigned>(P.cache.kv_heads), static_cast<unsigned>(P.B)), dim3(kWG), 0, st, P, by_pieces);
 }
 
 int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride, const int32_t* parent, bool tree, int B, int R,
@@ -265,17 +267,21 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.tile = s.tile;
     P.row_tiles = w.row_tiles;
     P.tiles = w.tiles;
-    // two slots of 8 elements a thread of attend_prepare
-    P.query_groups = static_cast<int>((static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG));
+    auto for_dividing = [](int d) { return d == 1 ? 0u : static_cast<unsigned>(((1ul << 32) + d - 1) / d); };
+    P.by_heads = for_dividing(heads);
+    P.by_G = for_dividing(P.G);
+    P.by_tile = for_dividing(s.tile);
+    // Of attend_prepare a sequence's queries take 8 elements in each of two slots of a thread, a key head's tile D / 64 workgroups and one.
+    const long prepare = 1 + (static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG) + static_cast<long>(H) * P.tiles * (D / 64 + 1);
     // A workgroup of attend_join takes one row where the rows are few, else as many as its lanes hold.
     const int by_pieces = static_cast<long>(B) * R * heads <= 4096, row_groups = by_pieces ? 1 : 4 * kWG / D;
-    const long prepare = 1 + static_cast<long>(B) * (P.query_groups + static_cast<long>(H) * P.tiles * (D / 64 + 1)), joins = (static_cast<long>(R) * heads + row_groups - 1) / row_groups;
+    const unsigned joins = static_cast<unsigned>((static_cast<long>(R) * P.G + row_groups - 1) / row_groups);
     const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
-    if (B * joins > kMaxGroups || prepare > kMaxGroups || units > INT_MAX) return FSD_ERR_SHAPE;
+    if (prepare > kMaxGroups || units > INT_MAX) return FSD_ERR_SHAPE;
     const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
-    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
-    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
-    else launch_attend<256>(st, P, s, static_cast<unsigned>(prepare), lds, static_cast<int>(joins), by_pieces);
+    if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, joins, by_pieces);
+    else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, joins, by_pieces);
+    else launch_attend<256>(st, P, s, static_cast<unsigned>(prepare), lds, joins, by_pieces);
     return launched();
 }
 
