@@ -56,7 +56,6 @@ struct AttendParams {
     void* out;
     int32_t* status;
     int workers;                   // workgroups of attend_rows
-    int least;                     // units of a workgroup, at least
     int tile;                      // rows of an item
     int row_tiles;                 // of 16 rows, of a (sequence, key head): whole items
     int tiles;                     // of 64 tokens of the R rows
@@ -118,7 +117,7 @@ __device__ __forceinline__ void deal(const AttendParams& P) {
     }
     if (tid == 0) {
         const long per = (base + P.workers - 1) / P.workers;
-        P.plan[0] = per < P.least ? P.least : per;
+        P.plan[0] = per < 1 ? 1 : per;
         P.plan[1 + P.B] = base;
     }
 }
@@ -506,9 +505,9 @@ struct Line {
     long per, worker, begin, finish, x, before;
     int b;
     __device__ __forceinline__ explicit Line(const AttendParams& P) {
-        worker = spread_over_xcds(blockIdx.x, P.workers);
         per = P.plan[0];
         const long total = P.plan[1 + P.B];
+        worker = spread_over_xcds(blockIdx.x, (total + per - 1) / per);   // (of those that have units, however few)
         begin = x = worker < 0 ? total : per * worker;
         finish = begin + per < total ? begin + per : total;
         b = 0;                                                // the sequence in which the units begin

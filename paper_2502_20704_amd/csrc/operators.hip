@@ -128,25 +128,19 @@ void launch_append_d(hipStream_t st, const AppendParams& P, int tokens) {
 // ------------------------------------------------------------------------------------------ attention
 
 // How many of a key head's rows (tokens times query heads of its group) an item takes: up to 64 attend_few (binary16 48, as its second parts take registers;
-// at head_dim 256 32 and 16), beyond that attend_rows with 128 or 256 rows, each wavefront some of them.
-struct AttendShape { int rt, waves, tile, workers; bool few; };
+// at head_dim 256 32 and 16), beyond that attend_rows with 128.  64 sequences of up to 8192 tokens, 36 rows a key head: 171 us with attend_few, 200 with
+// attend_rows.  Twice the rows an item (8 wavefronts, 256 workgroups): 162 us as well for trees of 244 rows, 115 in place of 110 for a prompt's 1000.
+struct AttendShape { int rt, tile, workers; bool few; };
+constexpr int rows_waves(int head_dim) { return head_dim == 256 ? 8 : 4; }   // of attend_rows: 16 sequences of 256 rows at head_dim 256 62 us with 8, 68 with 4
+constexpr int rows_tiles(int head_dim) { return head_dim == 256 ? 1 : 2; }   // of 16 rows, of each of them
 AttendShape attend_shape(long rows, int head_dim, int dtype) {
     AttendShape s;
     const long tiles = (rows + 15) / 16;
     s.few = tiles <= (head_dim == 256 ? 2 : 4) - (dtype == FSD_F16 ? 1 : 0);
-    if (s.few) {
-        s.rt = static_cast<int>(tiles);
-        s.waves = 4;
-    } else if (head_dim == 256) {
-        s.rt = 1;
-        s.waves = tiles <= 4 ? 4 : 8;
-    } else {
-        s.rt = 2;
-        s.waves = tiles <= 8 ? 4 : 8;
-    }
-    s.tile = 16 * s.rt * (s.few ? 1 : s.waves);
+    s.rt = s.few ? static_cast<int>(tiles) : rows_tiles(head_dim);
+    s.tile = 16 * s.rt * (s.few ? 1 : rows_waves(head_dim));
     // as many workgroups as the 256 compute units hold at once
-    s.workers = s.few ? 512 : s.waves == 4 && head_dim != 256 ? 512 : 256;
+    s.workers = s.few || head_dim != 256 ? 512 : 256;
     return s;
 }
 bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
@@ -196,8 +190,9 @@ void launch_attend_few(hipStream_t st, const AttendParams& P) {
     }
     hipLaunchKernelGGL((attend_few<D, RT, false>), grid, dim3(kWG), 0, st, P);
 }
-template <int D, int RT, int NW>
+template <int D>
 void launch_attend_rows(hipStream_t st, const AttendParams& P) {
+    constexpr int RT = rows_tiles(D), NW = rows_waves(D);
     const dim3 grid(static_cast<unsigned>(grid_over_xcds(P.workers)));
     if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_rows<D, RT, NW, true>), grid, dim3(NW * 64), 0, st, P);
     else hipLaunchKernelGGL((attend_rows<D, RT, NW, false>), grid, dim3(NW * 64), 0, st, P);
@@ -207,10 +202,8 @@ void launch_attend(hipStream_t st, const AttendParams& P, const AttendShape& s, 
     const dim3 g(prepare, static_cast<unsigned>(P.B));
     if (P.dtype == FSD_F16) hipLaunchKernelGGL((attend_prepare<D, true>), g, dim3(kWG), lds, st, P);
     else hipLaunchKernelGGL((attend_prepare<D, false>), g, dim3(kWG), lds, st, P);
-    constexpr int kRows = D == 256 ? 1 : 2;
     if (!s.few) {
-        if (s.waves == 4) launch_attend_rows<D, kRows, 4>(st, P);
-        else launch_attend_rows<D, kRows, 8>(st, P);
+        launch_attend_rows<D>(st, P);
     } else if (s.rt == 1) {
         launch_attend_few<D, 1>(st, P);
     } else if (s.rt == 2) {
@@ -263,7 +256,6 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.v16 = base + w.v16;
     P.part = reinterpret_cast<float*>(base + w.part);
     P.workers = s.workers;
-    P.least = 1;
     P.tile = s.tile;
     P.row_tiles = w.row_tiles;
     P.tiles = w.tiles;
