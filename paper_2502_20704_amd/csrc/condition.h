@@ -9,6 +9,10 @@
 // slot is copied (or masked) as it is.  What a row's own way adds is put into the table when the row needs it: along a chain
 // the contexts contain one another and each row adds one candidate; in a tree the few rows whose way has a token in
 // the slice add it and take it away again.  No row keeps another one waiting otherwise: there is no barrier between them.
+//
+// What bounds it is memory: 64 x 9 rows of 128256 bfloat16 entries 70 us (4.2 TB/s read and written; a copy of that size 58), 32 trees of 60 rows under
+// a mask each 185 (5.4 TB/s if all were read; slots without an allowed entry are not), 48 x 17 rows of 128259 binary32 entries with histories of 32768
+// 200 (4.2 TB/s).  One row of 32000: 4.5 us, a kernel's start and its two round trips, history and row.
 #ifndef FSD_CSRC_CONDITION_H_
 #define FSD_CSRC_CONDITION_H_
 

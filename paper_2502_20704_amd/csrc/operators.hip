@@ -265,7 +265,7 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.by_tile = for_dividing(s.tile);
     // Of attend_prepare a sequence's queries take 8 elements in each of two slots of a thread, a key head's tile D / 64 workgroups and one.
     const long prepare = 1 + (static_cast<long>(R) * heads * (D / 8) + 2 * kWG - 1) / (2 * kWG) + static_cast<long>(H) * P.tiles * (D / 64 + 1);
-    // A workgroup of attend_join takes one row where the rows are few, else as many as its lanes hold.
+    // A workgroup of attend_join takes one row where the rows are few, else as many as its lanes hold (measured there).
     const int by_pieces = static_cast<long>(B) * R * heads <= 4096, row_groups = by_pieces ? 1 : 4 * kWG / D;
     const unsigned joins = static_cast<unsigned>((static_cast<long>(R) * P.G + row_groups - 1) / row_groups);
     const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
