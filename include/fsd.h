@@ -430,7 +430,7 @@ typedef struct {
  * Nothing of a sequence is appended, its cache_len_out is its cache_len and FSD_ROW_BAD_CACHE is
  * set, if accept_len is outside [-1, R) (or over max_depth), a path node outside [0, R-1), cache_len or the new length
  * outside [0, 64 * max_blocks], a block to be written outside [0, num_blocks) or a position outside the rotation's table.
- * Two sequences that append to one block in one call race on it.
+ * Two sequences that append to one block in one call race on it, and so do two places of one sequence's table that name one.
  * R <= 2^20, B <= 65535.  Calls of up to 16 rows a sequence (R, or max_depth + 1): layers <= 65535; of more: layers * B *
  * kv_heads * (blocks that R rows can touch) < 2^24.
  */

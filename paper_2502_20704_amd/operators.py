@@ -223,8 +223,6 @@ def _token_stride(t, name, shape, dtype, device):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.is_contiguous():
-        return shape[-1] * shape[-2]
     size, stride = t.shape, t.stride()
     if size[-1] > 1 and stride[-1] != 1 or size[-2] > 1 and stride[-2] != size[-1]:
         raise ValueError(f"{name}: the heads of a token must be contiguous")

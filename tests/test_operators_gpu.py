@@ -819,6 +819,73 @@ def _flat(out):
     return [*outs, logits, target, draft, v["path_len"], v["path_nodes"], v["out_tokens"], v["row_status"], a["cache_len"], a["row_status"]]
 
 
+def test_replays_follow_what_the_tensors_hold():
+    """Lengths, tables, row counts, histories and masks are read at every replay, up to what the shapes allow and down to nothing."""
+    rng = np.random.default_rng(40)
+    lens, B, R = [500, 100, 0, 321], 4, 9
+    table, c, q, k, v = _case(rng, lens, R, 8, 2, 64, torch.bfloat16, extra=1)
+    c["k_codes"][(c["k_codes"] & 0x7F) == 0x7F] = 0x21
+    c["v_codes"][(c["v_codes"] & 0x7F) == 0x7F] = 0x21
+    cache = _to_cache(c, table, lens)
+    count = torch.full((B,), R, dtype=torch.int32, device="cuda")
+    z = torch.randn(B, R, 3001, device="cuda")
+    tokens = torch.randint(0, 3001, (B, R - 1), dtype=torch.int32, device="cuda")
+    cond = fsd.Conditions(history=torch.randint(0, 3001, (B, 700), dtype=torch.int32, device="cuda"),
+                          history_len=torch.full((B,), 300, dtype=torch.int32, device="cuda"), frequency=torch.full((B,), 0.3, device="cuda"),
+                          allowed=torch.full((B, 1, 94), -1, dtype=torch.int32, device="cuda"))
+    out = dict(out=torch.zeros((B, R, 8, 64), dtype=torch.bfloat16, device="cuda"), row_status=torch.zeros(B, dtype=torch.int32, device="cuda"))
+    ws = torch.empty(fsd.fsd_attend_workspace_bytes(B, R, 8, 2, 64) + 256, dtype=torch.uint8, device="cuda")
+    logits = dict(out=torch.empty_like(z))
+
+    def run(out, logits, ws):
+        fsd.fsd_attend_chain(q, k, v, cache, row_count=count, out=out, workspace=ws)
+        fsd.fsd_condition_chain(z, tokens, cond, out=logits)
+
+    run(out, logits, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run(out, logits, ws)
+    whole = table.shape[1] * 64
+    for step in range(6):
+        now = [[500, 100, 0, 321], [1, 0, 64, 65], [whole, whole, whole, whole], [0, 0, 0, 0], [128, 127, 63, 500], [3, 500, 500, 3]][step]
+        rows = [[R] * 4, [1, R, 0, 2], [R, 0, R, 1], [0, 0, 0, 0], [2, 2, 2, 2], [R, 1, 0, R]][step]
+        cache.cache_len.copy_(torch.tensor(now, dtype=torch.int32))
+        count.copy_(torch.tensor(rows, dtype=torch.int32))
+        cache.block_table.copy_(cache.block_table.flip(1))
+        cond._held[0].copy_(torch.randint(0, 3001, (B, 700), dtype=torch.int32, device="cuda"))
+        cond._held[1].copy_(torch.tensor([0, 700, 1, 350 + step], dtype=torch.int32))
+        cond._held[-1].copy_(torch.randint(-2 ** 31, 2 ** 31 - 1, (B, 1, 94), device="cuda").int())
+        out["out"].fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        other = dict(out=torch.full_like(out["out"], 7.0), row_status=torch.zeros_like(out["row_status"]))
+        fresh = dict(out=torch.empty_like(z))
+        run(other, fresh, torch.empty_like(ws))
+        assert torch.equal(out["out"], other["out"]) and torch.equal(logits["out"], fresh["out"]), step
+        assert (out["row_status"] == 0).all()
+        want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.array(rows), c, 0, now, cache.block_table.cpu().numpy(), 0.125, None, True, torch.bfloat16)
+        for b in range(B):
+            _within(out["out"][b, :rows[b]], want[b, :rows[b]], bound[b, :rows[b]], f"{step} {b}")
+            assert (out["out"][b, rows[b]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_attend_most_rows(tree):
+    rng = np.random.default_rng(41)
+    lens, R = [77], 2049
+    table, c, q, k, v = _case(rng, lens, R, 1, 1, 64, torch.float16)
+    parent = _rand_parents(rng, 1, R - 1) if tree else None
+    cache, turns = _to_cache(c, table, lens), _turns(77 + R, 64)
+    if tree:
+        got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, rotation=_rotation(turns, False))
+    else:
+        got = fsd.fsd_attend_chain(q, k, v, cache, rotation=_rotation(turns, False))
+    assert got["row_status"].tolist() == [0]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), parent, np.full(1, R), c, 0, lens, table, 0.125, turns, False, torch.float16)
+    _within(got["out"], want, bound)
+
+
 def test_attend_workspace_holds_anything_and_results_repeat():
     """A workspace full of NaN patterns, one that a call of other sizes has left, and two calls at once on two streams."""
     rng = np.random.default_rng(30)
