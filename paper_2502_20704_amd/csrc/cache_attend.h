@@ -518,11 +518,13 @@ struct Line {
         worker = spread_over_xcds(blockIdx.x, (total + per - 1) / per);   // (of those that have units, however few)
         begin = x = worker < 0 ? total : per * worker;
         finish = begin + per < total ? begin + per : total;
-        b = 0;                                                // the sequence in which the units begin
+        b = 0;                                                // the sequence in which the units begin: 64 of them looked at at once
         for (int n = P.B; n > 1;) {                           // (of those that begin at the same unit the last one has units)
-            const int half = n / 2;
-            if (P.plan[1 + b + half] <= begin) b += half;
-            n -= half;
+            const int lane = static_cast<int>(threadIdx.x) & 63, step = (n + 63) / 64;
+            const unsigned long long up_to = __ballot(lane * step < n && P.plan[1 + b + min(lane * step, n - 1)] <= begin);
+            const int past = (__popcll(up_to) - 1) * step;
+            b += past;
+            n = min(step, n - past);
         }
         before = P.plan[1 + b];                               // units before sequence b
     }
@@ -586,6 +588,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
         const size_t bh = static_cast<size_t>(b) * H + h;
 
+        // 64 cached blocks at a time: a lane looks up one block's number and scales.  (The first of them together with the queries, so that an item
+        // begins with two round trips and not with four.)
+        const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
+        int my_id = 0;
+        auto look = [&](int j0) { my_id = table[min(j0 + lane, last - 1)]; };
+        if (first < last) look(first);
         // ---- queries
         half8_t q[RT][2 * kI], q2[FINE ? RT : 1][2 * kI];
         float factor[RT];                                     // of the products of a row: its power of two back, scale, log2(e)
@@ -603,6 +611,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 if constexpr (FINE) q2[rt][i] = *reinterpret_cast<const half8_t*>(from + parts + i * 1024);
             }
         }
+        bool good = false;
+        float my_ks = 1.0f, my_vs = 1.0f;
+        auto look_further = [&](int j0) {
+            good = j0 + lane < last && my_id >= 0 && my_id < P.cache.num_blocks;
+            if (!good) my_id = 0;                             // in bounds, and none of its tokens counts
+            const size_t at = (layer0 + my_id) * H + h;
+            my_ks = P.cache.k_scale[at];
+            my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+        };
+        if (first < last) look_further(first);
         // (columns behind the last row hold anything; they are never stored, and must not hold up the others)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -712,7 +730,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         // ---- cached blocks
         {
             const size_t per_block = static_cast<size_t>(H) * kBlock * D;
-            const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
             const char* kbase = static_cast<const char*>(P.cache.k_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + ((col >> 2) * 16 + (col & 3)) * D + g * 16;
             const char* vbase = static_cast<const char*>(P.cache.v_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + (g * D + col) * 16;
             unsigned char* flight = lds;
@@ -767,19 +784,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                     }
                 }
             };
-            // 64 blocks at a time: a lane looks up one block's number and scales
             for (int j0 = first; j0 < last; j0 += 64) {
                 const int n = min(64, last - j0);
-                int my_id = 0;
-                float my_ks = 1.0f, my_vs = 1.0f;
-                bool good = false;
-                if (lane < n) {
-                    my_id = table[j0 + lane];
-                    good = my_id >= 0 && my_id < P.cache.num_blocks;
-                    if (!good) my_id = 0;                      // in bounds, and none of its tokens counts
-                    const size_t at = (layer0 + my_id) * H + h;
-                    my_ks = P.cache.k_scale[at];
-                    my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+                if (j0 > first) {
+                    look(j0);
+                    look_further(j0);
                 }
                 const unsigned long long fine = __ballot(good);
                 auto id_of = [&](int i) { return static_cast<size_t>(__builtin_amdgcn_readlane(my_id, i)); };
@@ -986,6 +995,12 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
         const int32_t* table = P.cache.block_table + static_cast<size_t>(b) * P.cache.max_blocks;
         const size_t bh = static_cast<size_t>(b) * H + h;
 
+        // 64 cached blocks at a time: a lane looks up one block's number and scales.  (The first of them together with the queries, so that an item
+        // begins with two round trips and not with four.)
+        const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
+        int my_id = 0;
+        auto look = [&](int j0) { my_id = table[min(j0 + lane, last - 1)]; };
+        if (first < last) look(first);
         half8_t q[RT][2 * kI], q2[FINE ? RT : 1][2 * kI];
         float factor[RT];                                               // of the products of a row: its power of two back, scale, log2(e)
         int row_of[RT];                                                 // the row, -1 behind the last
@@ -1002,6 +1017,16 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                 if constexpr (FINE) q2[rt][i] = *reinterpret_cast<const half8_t*>(from + parts + i * 1024);
             }
         }
+        bool good = false;
+        float my_ks = 1.0f, my_vs = 1.0f;
+        auto look_further = [&](int j0) {
+            good = j0 + lane < last && my_id >= 0 && my_id < P.cache.num_blocks;
+            if (!good) my_id = 0;                             // in bounds, and none of its tokens counts
+            const size_t at = (layer0 + my_id) * H + h;
+            my_ks = P.cache.k_scale[at];
+            my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+        };
+        if (first < last) look_further(first);
         // (columns behind the last row hold anything; they are never stored, and must not hold up the others)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -1117,22 +1142,13 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
         // ---- cached blocks
         {
             const size_t per_block = static_cast<size_t>(H) * kBlock * D;
-            const size_t layer0 = static_cast<size_t>(P.layer) * P.cache.num_blocks;
             const char* kbase = static_cast<const char*>(P.cache.k_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + ((col >> 2) * 16 + (col & 3) + 4 * wave) * D + g * 16;
             const char* vbase = static_cast<const char*>(P.cache.v_codes) + (layer0 * H + h) * (static_cast<size_t>(kBlock) * D) + (g * D + wave * kV * 16 + col) * 16;
-            // 64 blocks at a time: a lane looks up one block's number and scales
             for (int j0 = first; j0 < last; j0 += 64) {
                 const int n = min(64, last - j0);
-                int my_id = 0;
-                float my_ks = 1.0f, my_vs = 1.0f;
-                bool good = false;
-                if (lane < n) {
-                    my_id = table[j0 + lane];
-                    good = my_id >= 0 && my_id < P.cache.num_blocks;
-                    if (!good) my_id = 0;                               // in bounds, and none of its tokens counts
-                    const size_t at = (layer0 + my_id) * H + h;
-                    my_ks = P.cache.k_scale[at];
-                    my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+                if (j0 > first) {
+                    look(j0);
+                    look_further(j0);
                 }
                 const unsigned long long fine = __ballot(good);
                 auto float_of = [](float y, int i) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), i)); };
