@@ -378,7 +378,7 @@ int fsd_condition_tree(const void* logits, const int32_t* node_tokens, const int
  * (Values lie by groups of 16 tokens because the attention's matrix instruction takes them with
  * the token index running fastest: 16 bytes of one head dimension are then one load, and a token that is
  * appended still touches 2 KB at head_dim 128, not the whole block.)
- * head_dim is 64, 128 or 256.  What lies behind a sequence's last token in its last block is never
+ * head_dim is 64, 128 or 256, kv_heads at most 1024.  What lies behind a sequence's last token in its last block is never
  * used: it may hold anything.  Blocks may be shared by sequences as long as nothing is appended to
  * them.  Code and scale arrays start on 16-byte boundaries.
  */
