@@ -107,6 +107,14 @@ def test_rotation_refusals(rotation, status):
     assert _attend(rotation=rotation) == status
 
 
+def test_limits_of_a_launch():
+    """Calls whose grids or counts would not fit: refused before anything is launched."""
+    assert _append(cache=_cache(layers=65536)) == -2
+    assert _append(cache=_cache(layers=1 << 22), R=17) == -2
+    assert _attend(scale=3.0e38) == -2
+    assert _attend(cache=_cache(kv_heads=128, max_blocks=1 << 24), heads=128, q_stride=128 * 128, kv_stride=128 * 128) == -2
+
+
 def test_workspace_planning():
     f = fsd.fsd_attend_workspace_bytes
     assert f(1, 1, 1, 1, 64) > 0 and f(64, 9, 32, 8, 128) % 256 == 0
