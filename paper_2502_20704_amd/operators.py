@@ -223,20 +223,23 @@ def _token_stride(t, name, shape, dtype, device):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    size, stride = t.shape, t.stride()
-    if size[-1] > 1 and stride[-1] != 1 or size[-2] > 1 and stride[-2] != size[-1]:
+    stride = t.stride()
+    if shape[-1] > 1 and stride[-1] != 1 or shape[-2] > 1 and stride[-2] != shape[-1]:
         raise ValueError(f"{name}: the heads of a token must be contiguous")
     step, run = None, 1                      # run: tokens that the dimensions behind the current one hold
-    for n, s in zip(reversed(size[:-2]), reversed(stride[:-2])):
+    for i in range(len(shape) - 3, -1, -1):
+        n = shape[i]
         if n > 1:
             if step is None:
-                if s % run:
-                    raise ValueError(f"{name}: tokens must lie at one distance from one another")
-                step = s // run
-            if s != step * run:
+                step = stride[i] // run
+            if stride[i] != step * run:
                 raise ValueError(f"{name}: tokens must lie at one distance from one another")
-        run *= n
-    return step if step is not None else size[-1] * size[-2]
+            run *= n
+    return step if step is not None else shape[-1] * shape[-2]
+
+
+def _laid_out_alike(a, b):
+    return a.stride() == b.stride() and a.shape == b.shape and a.dtype == b.dtype and a.device == b.device
 
 
 def fsd_cache_append(k, v, cache, accept_len, *, path_nodes=None, rotation=None, out=None, stream=None):
@@ -254,7 +257,7 @@ def fsd_cache_append(k, v, cache, accept_len, *, path_nodes=None, rotation=None,
     if k.dim() == 5 or cache.layers != 1:
         shape = (cache.layers, *shape)
     step = _token_stride(k, "k", shape, k.dtype, dev)
-    if _token_stride(v, "v", shape, k.dtype, dev) != step:
+    if not _laid_out_alike(v, k) and _token_stride(v, "v", shape, k.dtype, dev) != step:
         raise ValueError("k and v differ in the distance between tokens")
     _check(accept_len, "accept_len", (B,), torch.int32, dev)
     depth = 0
@@ -299,7 +302,7 @@ def _attend(call, q, k, v, parent, cache, layer, row_count, rotation, scale, out
     q_step = _token_stride(q, "q", (cache.batch, R, heads, cache.head_dim), q.dtype, dev)
     shape = (B, R, cache.kv_heads, D)
     kv_step = _token_stride(k, "k", shape, q.dtype, dev)
-    if _token_stride(v, "v", shape, q.dtype, dev) != kv_step:
+    if not _laid_out_alike(v, k) and _token_stride(v, "v", shape, q.dtype, dev) != kv_step:
         raise ValueError("k and v differ in the distance between tokens")
     if parent is not None:
         _check(parent, "parent", (B, R - 1), torch.int32, dev)
