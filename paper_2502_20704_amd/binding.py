@@ -162,11 +162,13 @@ def _ptr(t):
 
 
 def _workspace(workspace, need, device):
+    """the tensor, its first address that the library takes, and the bytes from there (none, where a view ends before it:
+    less than none would reach the library as a size of about 2^64)"""
     if workspace is None:
         workspace = torch.empty(need + 256, dtype=torch.uint8, device=device)
     base = workspace.data_ptr()
     pad = (-base) % 256
-    return workspace, base + pad, workspace.numel() - pad
+    return workspace, base + pad, max(0, workspace.numel() - pad)
 
 
 def _stream(stream):

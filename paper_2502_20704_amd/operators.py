@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding
-from .binding import FsdError, _ptr, _stream, library
+from .binding import FsdError, _ptr, _stream, _workspace, library
 
 F16 = 2
 CACHE_BLOCK = 64
@@ -322,18 +322,17 @@ def _attend(call, q, k, v, parent, cache, layer, row_count, rotation, scale, out
         _used_on(stream, workspace)
     elif not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
         raise ValueError(f"workspace: contiguous uint8 on {dev} wanted")
-    base = workspace.data_ptr()
-    pad = (-base) % 256
+    workspace, base, size = _workspace(workspace, 0, dev)
     scale = D ** -0.5 if scale is None else float(scale)
     rot = rotation._ref if rotation is not None else None
     L = library()
     if call == "fsd_attend_tree":
         st = L.fsd_attend_tree(_ptr(q), _ptr(k), _ptr(v), q_step, kv_step, _ptr(parent), B, R, heads, dt, _ptr(row_count), scale, rot,
-                               cache._ref, layer, _ptr(out["out"]), _ptr(out.get("row_status")), base + pad, workspace.numel() - pad,
+                               cache._ref, layer, _ptr(out["out"]), _ptr(out.get("row_status")), base, size,
                                _stream(stream))
     else:
         st = L.fsd_attend_chain(_ptr(q), _ptr(k), _ptr(v), q_step, kv_step, B, R, heads, dt, _ptr(row_count), scale, rot, cache._ref,
-                                layer, _ptr(out["out"]), _ptr(out.get("row_status")), base + pad, workspace.numel() - pad, _stream(stream))
+                                layer, _ptr(out["out"]), _ptr(out.get("row_status")), base, size, _stream(stream))
     if st != 0:
         raise FsdError(st, call)
     out["_workspace"] = workspace

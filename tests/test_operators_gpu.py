@@ -968,3 +968,20 @@ def test_binding_refusals_on_the_gpu():
         fsd.fsd_cache_append(k, k, cache, torch.zeros(3, **i32))
     with pytest.raises(ValueError):
         fsd.Cache(cache.k_codes, cache.k_codes, cache.k_scale, cache.v_scale, cache.block_table, cache.cache_len)
+
+
+def test_workspace_view_without_an_aligned_address():
+    """Refused for its size, by the verify calls as well, and nothing behind it is written."""
+    arena = torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda")
+    view = arena[16:116]
+    cache = fsd.Cache.empty(1, 4, 2, 64, torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"))
+    q, k = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(fsd.FsdError) as e:
+        fsd.fsd_attend_chain(q, k, k, cache, workspace=view)
+    assert e.value.status == -5
+    z, cand = torch.zeros(2, 3, 100, device="cuda"), torch.zeros((2, 2), dtype=torch.int32, device="cuda")
+    with pytest.raises(fsd.FsdError) as e:
+        fsd.fsd_verify_chain(z, z[:, :2].contiguous(), cand, 0.1, workspace=view)
+    assert e.value.status == -5
+    torch.cuda.synchronize()
+    assert (arena == 7).all()

@@ -167,3 +167,16 @@ def test_distance_between_tokens():
         step(whole.transpose(0, 1), (2, 3, 5, 6, 64))
     with pytest.raises(ValueError):
         step(whole, (3, 2, 5, 6, 128))
+
+
+@pytest.mark.parametrize("at,size", [(1, 1), (16, 100), (1, 254)])
+def test_workspace_that_ends_before_the_first_aligned_address(at, size):
+    """A view that holds no aligned address has room for nothing, not for 2^64 bytes."""
+    import torch
+
+    from paper_2502_20704_amd import binding
+
+    arena = torch.zeros(1024, dtype=torch.uint8)
+    at += (-arena.data_ptr()) % 256
+    assert binding._workspace(arena[at:at + size], 0, arena.device)[2] == 0
+    assert ops._workspace is binding._workspace
