@@ -339,14 +339,16 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             __syncthreads();
         }
     }
-    auto position = [&](int r) {
-        if (!P.parent) return len + r;
-        if (deep) return len + depth[r];
-        int n = len;
-        for (int at = r; at > 0; at = up[at]) ++n;
-        return n;
+    // (a cache of nearly 2^31 tokens and the rows behind it: more than an int holds)
+    auto position = [&](int r) -> unsigned {
+        const unsigned n = static_cast<unsigned>(len);
+        if (!P.parent) return n + static_cast<unsigned>(r);
+        if (deep) return n + static_cast<unsigned>(depth[r]);
+        unsigned way = 0;
+        for (int at = r; at > 0; at = up[at]) ++way;
+        return n + way;
     };
-    auto table_row = [&](int pos) { return P.rot.table ? min(pos, P.rot.rows - 1) : 0; };
+    auto table_row = [&](unsigned pos) { return P.rot.table ? static_cast<int>(min(pos, static_cast<unsigned>(P.rot.rows) - 1u)) : 0; };
     constexpr int kSlots = 2;                                 // rows of which a thread takes 8 dimensions, D / 8 neighbours the whole of a row
 
     if (!is_tile) {
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
                        (P.row_count && (P.row_count[b] < 0 || P.row_count[b] > R));
             for (int i = tid; i < share.blocks; i += kThreads) bad |= table[i] < 0 || table[i] >= P.cache.num_blocks;
             if (P.rot.table)
-                for (int r = tid; r < share.rows; r += kThreads) bad |= position(r) >= P.rot.rows;
+                for (int r = tid; r < share.rows; r += kThreads) bad |= position(r) >= static_cast<unsigned>(P.rot.rows);
             bad = __syncthreads_or(bad);
             bad_tree = __syncthreads_or(bad_tree);
             if (tid == 0) P.status[b] = (bad ? FSD_ROW_BAD_CACHE : 0) | (bad_tree ? FSD_ROW_BAD_PARENT : 0);

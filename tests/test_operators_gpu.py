@@ -985,3 +985,29 @@ def test_workspace_view_without_an_aligned_address():
     assert e.value.status == -5
     torch.cuda.synchronize()
     assert (arena == 7).all()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("R", [3, 300])
+def test_attend_positions_beyond_31_bits(R, tree):
+    """A table as long as a call takes: the rows' positions pass 2^31.  All of its blocks are out of range, so that what counts is the rows, turned by the
+    last position of the rotation's table."""
+    rng = np.random.default_rng(50 + R)
+    H, D, blocks = 1, 64, 2 ** 25 - 2
+    if torch.cuda.mem_get_info()[0] < 8 * blocks:
+        pytest.skip("not enough device memory")
+    table, c, q, k, v = _case(rng, [64], R, 2, H, D, torch.bfloat16)
+    turns = _turns(50, D)
+    parent = np.arange(-1, R - 2, dtype=np.int32)[None]
+    parent[0, R // 2:] = -1
+    cache = _to_cache(c, table, [64])
+    far = fsd.Cache(cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, torch.full((1, blocks), -1, dtype=torch.int32, device="cuda"),
+                    torch.full((1,), blocks * 64, dtype=torch.int32, device="cuda"))
+    if tree:
+        got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), far, rotation=_rotation(turns, True))
+    else:
+        got = fsd.fsd_attend_chain(q, k, v, far, rotation=_rotation(turns, True))
+    assert got["row_status"].tolist() == [fsd.ROW_BAD_CACHE]
+    want, bound = ref.attend(_host(q), _host(k), _host(v), parent if tree else None, np.array([R]), c, 0, [64], table, 0.125, turns, True, torch.bfloat16,
+                             left_out=((0, 0),))
+    _within(got["out"], want, bound)
