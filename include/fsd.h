@@ -421,6 +421,7 @@ typedef struct {
  *   cache_len_out [B]          out  optional: cache_len + accept_len + 1.  Not cache_len itself (other
  *                              workgroups of the call still read that): copy it over afterwards.
  *   row_status [B]             out  optional
+ * cache_len_out and row_status share no byte with cache_len, block_table, accept_len, path_nodes or one another (FSD_ERR_LAYOUT).
  *
  * A block's scale is the smallest power of two s with |x| <= 448 s for every (finite) x appended to it, but
  * at least 2^-100 and at least the scale the block has if it holds tokens of the sequence already: those are rounded again
@@ -458,7 +459,8 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
  *   out      [B, R, heads, head_dim] dense, out, 16-byte aligned
  *   row_status [B] out optional: FSD_ROW_BAD_CACHE where cache_len is outside [0, 64 * max_blocks], a
  *                  block outside [0, num_blocks), row_count outside [0, R] or a position outside the rotation's table (the call then
- *                  takes the nearest length and position, and leaves such blocks out)
+ *                  takes the nearest length and position, and leaves such blocks out).  It shares no byte with cache_len, block_table,
+ *                  row_count or parent (FSD_ERR_LAYOUT)
  *   workspace      fsd_attend_workspace_bytes(...) bytes, 256-byte aligned
  *
  * Products of 16-bit operands are summed in binary32; the rotated queries and keys and the softmax's weights

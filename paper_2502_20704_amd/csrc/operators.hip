@@ -21,6 +21,11 @@ constexpr int kMaxBatch = 65535;
 constexpr long kMaxGroups = (1L << 32) / kWG - 1;   // workgroups of a launch: less than 2^32 threads
 
 inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+// whether two runs of bytes share one (an absent one shares none)
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && (x < y ? y - x < na : x - y < nb);
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? FSD_OK : FSD_ERR_LAUNCH; }
 
 // ------------------------------------------------------------------------------------------ conditioning
@@ -101,6 +106,16 @@ int check_cache(const fsd_cache* c) {
         reinterpret_cast<uintptr_t>(c->v_scale) % 4 != 0)
         return FSD_ERR_LAYOUT;
     return FSD_OK;
+}
+// A sequence's new length and report are written by one workgroup, which no other waits for: they must not lie in what all of them read, nor in one another.
+bool report_overlaps(const int32_t* length, const int32_t* status, int B, const fsd_cache& c, const int32_t* first, size_t n_first, const int32_t* second,
+                     size_t n_second) {
+    const size_t own = static_cast<size_t>(B) * 4, table = own * static_cast<size_t>(c.max_blocks);
+    auto meets = [&](const int32_t* out) {
+        return overlap(out, own, c.cache_len, own) || overlap(out, own, c.block_table, table) || overlap(out, own, first, n_first * 4) ||
+               overlap(out, own, second, n_second * 4);
+    };
+    return meets(length) || meets(status) || overlap(length, own, status, own);
 }
 // the rotation to hand to a kernel: none where there is no table
 int check_rotation(const fsd_rotation* r, int head_dim, fsd_rotation* out) {
@@ -270,6 +285,7 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     const unsigned joins = static_cast<unsigned>((static_cast<long>(R) * P.G + row_groups - 1) / row_groups);
     const long units = (kStart + static_cast<long>(cache->max_blocks) + P.tiles) * H * (P.row_tiles * 16 / s.tile);   // of a sequence, at most
     if (prepare > kMaxGroups || units > INT_MAX) return FSD_ERR_SHAPE;
+    if (report_overlaps(nullptr, row_status, B, *cache, row_count, static_cast<size_t>(B), P.parent, static_cast<size_t>(B) * (R - 1))) return FSD_ERR_LAYOUT;
     const size_t lds = P.parent ? static_cast<size_t>(R) * 6 : 0;
     if (D == 64) launch_attend<64>(st, P, s, static_cast<unsigned>(prepare), lds, joins, by_pieces);
     else if (D == 128) launch_attend<128>(st, P, s, static_cast<unsigned>(prepare), lds, joins, by_pieces);
@@ -303,7 +319,7 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
     const int H = cache->kv_heads;
     if (B < 1 || B > kMaxBatch || R < 1 || R > (1 << 20) || (path_nodes && (max_depth < 1 || max_depth > kMaxRows))) return FSD_ERR_SHAPE;
     if (token_stride < static_cast<int64_t>(H) * cache->head_dim || token_stride % 8 != 0 || token_stride > (1L << 32) || !aligned16(k) ||
-        !aligned16(v) || cache_len_out == cache->cache_len)
+        !aligned16(v))
         return FSD_ERR_LAYOUT;
     P.k = static_cast<const char*>(k);
     P.v = static_cast<const char*>(v);
@@ -320,6 +336,8 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
     const long pieces = static_cast<long>(cache->layers) * B * H * P.slots;
     if (P.max_rows <= kFew ? cache->layers > 65535 : pieces > kMaxGroups) return FSD_ERR_SHAPE;
     P.npieces = static_cast<unsigned>(pieces);                // (append_many's grid)
+    if (report_overlaps(cache_len_out, row_status, B, *cache, accept_len, static_cast<size_t>(B), path_nodes, static_cast<size_t>(B) * max_depth))
+        return FSD_ERR_LAYOUT;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (dtype == FSD_F32) launch_append_d<FSD_F32>(st, P, P.max_rows);
     else if (dtype == FSD_BF16) launch_append_d<FSD_BF16>(st, P, P.max_rows);

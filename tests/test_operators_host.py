@@ -180,3 +180,27 @@ def test_workspace_that_ends_before_the_first_aligned_address(at, size):
     at += (-arena.data_ptr()) % 256
     assert binding._workspace(arena[at:at + size], 0, arena.device)[2] == 0
     assert ops._workspace is binding._workspace
+
+
+def test_reports_that_lie_in_what_a_call_reads():
+    """cache_len_out and row_status, byte by byte beside and inside every array that other workgroups read, and one another."""
+    B, blocks, depth = 2, 4, 3
+    at = dict(cache_len=0x10000, block_table=0x20000, accept_len=0x30000, path_nodes=0x40000, parent=0x50000, row_count=0x60000)
+    size = dict(cache_len=4 * B, block_table=4 * B * blocks, accept_len=4 * B, path_nodes=4 * B * depth, parent=4 * B * 8, row_count=4 * B)
+    cache = _cache(cache_len=at["cache_len"], block_table=at["block_table"])
+    L = fsd.library()
+
+    def append(length, status):
+        return L.fsd_cache_append(A, A, 256, B, 9, fsd.BF16, at["accept_len"], at["path_nodes"], depth, None, cache, length, status, None)
+
+    def attend(status):
+        return L.fsd_attend_tree(A, A, A, 8 * 128, 256, at["parent"], B, 9, 8, fsd.BF16, at["row_count"], 0.1, None, cache, 0, A, status, A, 1 << 40, None)
+
+    for name in ("cache_len", "block_table", "accept_len", "path_nodes"):
+        for where in (at[name], at[name] - 4, at[name] + size[name] - 4):
+            assert append(where, None) == -9 and append(None, where) == -9, (name, where)
+    for where in (0x70000, 0x70004, 0x6fffc):
+        assert append(0x70000, where) == -9
+    for name in ("cache_len", "block_table", "parent", "row_count"):
+        for where in (at[name], at[name] - 4, at[name] + size[name] - 4):
+            assert attend(where) == -9, (name, where)
