@@ -349,7 +349,7 @@ typedef struct {
  *                             rows.  Row i stands behind candidates 0 .. i-1 (both kinds).
  *   cand_tokens [B, K]        candidate token ids (0 <= K <= 2048; may be NULL when K is 0: a
  *                             step without candidates); ids outside [0, V) are passed over
- *   out         [B, rows, V]  out; may be logits itself (in place), else must not overlap it; both on addresses of whole elements
+ *   out         [B, rows, V]  out; may be logits itself (in place), else no overlap with it (FSD_ERR_LAYOUT); both on addresses of whole elements
  *                             (FSD_F32 or FSD_BF16), B * rows < 2^24
  * A mask per context has K+1 of them, also for draft rows: context i stands behind candidates 0 .. i-1.
  */

@@ -57,6 +57,8 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     if (c.allowed && c.allowed_contexts != 1 && c.allowed_contexts != N + 1) return FSD_ERR_SHAPE;
     const size_t es = dtype == FSD_BF16 ? 2 : 4;
     if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) % es != 0) return FSD_ERR_LAYOUT;
+    const size_t bytes = static_cast<size_t>(B) * rows * V * es;
+    if (out != logits && overlap(logits, bytes, out, bytes)) return FSD_ERR_LAYOUT;
     ConditionParams P;
     P.logits = static_cast<const char*>(logits);
     P.out = static_cast<char*>(out);
@@ -88,7 +90,6 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     if (tree) lds += (static_cast<size_t>(P.rows_per_wg) / 32 + 1) * 4 + static_cast<size_t>(N) * 4;
     // Past the caches where the logits are more than these hold and lines are written whole: 64 sequences of 9 rows of 128256 bfloat16
     // entries 77 -> 73 us; but 48 of 17 rows of 128259 binary32 entries 203 -> 207, and a small call's reader finds its rows in the caches.
-    const size_t bytes = static_cast<size_t>(B) * rows * V * es;
     const bool stream = bytes >= (64u << 20) && V * es % 16 == 0 && aligned16(logits) && aligned16(out);
     if (dtype == FSD_BF16) launch_condition<true>(st, static_cast<unsigned>(grid), lds, tree, stream, P);
     else launch_condition<false>(st, static_cast<unsigned>(grid), lds, tree, stream, P);

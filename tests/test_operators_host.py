@@ -204,3 +204,12 @@ def test_reports_that_lie_in_what_a_call_reads():
     for name in ("cache_len", "block_table", "parent", "row_count"):
         for where in (at[name], at[name] - 4, at[name] + size[name] - 4):
             assert attend(where) == -9, (name, where)
+
+
+@pytest.mark.parametrize("dtype,step", [(fsd.F32, 4), (fsd.BF16, 2)])
+def test_conditioned_logits_that_overlap_the_logits_by_a_part(dtype, step):
+    """In place is one address for both; rows that another workgroup writes before this one reads them are not."""
+    size, at = 2 * 5 * 1000 * step, 1 << 20
+    for tree in (False, True):
+        for out in (at + step, at - step, at + size - step, at - size + step):
+            assert _chain(logits=at, out=out, dtype=dtype, tree=tree, parent=A) == -9
