@@ -52,11 +52,17 @@ def _on_current(device):
         raise ValueError(f"the tensors live on {device}, which is not the current device")
 
 
-def _used_on(stream, *tensors):
-    """memory that this module allocated is not given out again before `stream` has used it"""
-    if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+def _new(stream, device, **tensors):
+    """Tensors (shape, dtype) that a call of `stream` writes, out of that stream's memory: what the current stream has given back may be in use there
+    still.  Nor are they given out again before the current stream, whose program has them, is done with them."""
+    torch = _torch()
+    if stream is None:
+        return {n: torch.empty(shape, dtype=dtype, device=device) for n, (shape, dtype) in tensors.items()}
+    with torch.cuda.stream(stream):
+        out = {n: torch.empty(shape, dtype=dtype, device=device) for n, (shape, dtype) in tensors.items()}
+    for t in out.values():
+        t.record_stream(torch.cuda.current_stream())
+    return out
 
 
 class Conditions:
@@ -176,8 +182,7 @@ def _condition(call, logits, tokens, parent, conditions, out, stream):
         _check(parent, "parent", (B, n), torch.int32, dev)
     conditions._fits(B, V, dev, n + 1)
     if out is None:
-        out = dict(out=torch.empty_like(logits))
-        _used_on(stream, out["out"])
+        out = _new(stream, dev, out=(logits.shape, logits.dtype))
     else:
         _check(out["out"], "out", logits.shape, logits.dtype, dev)
     L = library()
@@ -267,8 +272,7 @@ def fsd_cache_append(k, v, cache, accept_len, *, path_nodes=None, rotation=None,
     if rotation is not None and rotation.device != dev:
         raise ValueError(f"the rotation lives on {rotation.device}, the cache on {dev}")
     if out is None:
-        out = dict(cache_len=torch.empty(B, dtype=torch.int32, device=dev), row_status=torch.empty(B, dtype=torch.int32, device=dev))
-        _used_on(stream, *out.values())
+        out = _new(stream, dev, cache_len=((B,), torch.int32), row_status=((B,), torch.int32))
     for name in ("cache_len", "row_status"):
         if out.get(name) is not None:
             _check(out[name], name, (B,), torch.int32, dev)
@@ -311,15 +315,14 @@ def _attend(call, q, k, v, parent, cache, layer, row_count, rotation, scale, out
     if rotation is not None and rotation.device != dev:
         raise ValueError(f"the rotation lives on {rotation.device}, the cache on {dev}")
     if out is None:
-        out = dict(out=torch.empty((B, R, heads, D), dtype=q.dtype, device=dev), row_status=torch.empty(B, dtype=torch.int32, device=dev))
-        _used_on(stream, *out.values())
+        out = _new(stream, dev, out=((B, R, heads, D), q.dtype), row_status=((B,), torch.int32))
     else:
         _check(out["out"], "out", q.shape, q.dtype, dev)
         if out.get("row_status") is not None:
             _check(out["row_status"], "row_status", (B,), torch.int32, dev)
     if workspace is None:
-        workspace = torch.empty(fsd_attend_workspace_bytes(B, R, heads, cache.kv_heads, D) + 256, dtype=torch.uint8, device=dev)
-        _used_on(stream, workspace)
+        need = fsd_attend_workspace_bytes(B, R, heads, cache.kv_heads, D) + 256
+        workspace = _new(stream, dev, workspace=((need,), torch.uint8))["workspace"]
     elif not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous() or workspace.dtype != torch.uint8:
         raise ValueError(f"workspace: contiguous uint8 on {dev} wanted")
     workspace, base, size = _workspace(workspace, 0, dev)

@@ -1011,3 +1011,38 @@ def test_attend_positions_beyond_31_bits(R, tree):
     want, bound = ref.attend(_host(q), _host(k), _host(v), parent if tree else None, np.array([R]), c, 0, [64], table, 0.125, turns, True, torch.bfloat16,
                              left_out=((0, 0),))
     _within(got["out"], want, bound)
+
+
+@pytest.mark.parametrize("call", ["condition", "append", "attend", "workspace"])
+def test_outputs_on_another_stream_leave_the_current_streams_memory(call):
+    """What the binding allocates for a call of `stream` is not memory that the current stream has given back and still has work on."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    z = torch.randn(4, 5, 100000, device="cuda")
+    B, R, H, D = 2, 130, 8, 128
+    cache = fsd.Cache.empty(1, 8, H, D, torch.arange(8, **i32).view(2, 4), torch.zeros(B, **i32))
+    q = torch.randn(B, R, 4 * H, D, device="cuda").to(torch.bfloat16)
+    k = torch.randn(B, R, H, D, device="cuda").to(torch.bfloat16)
+    tokens, accepted, conditions = torch.zeros((4, 4), **i32), torch.full((B,), 3, **i32), fsd.Conditions()
+    if call == "condition":
+        size, run = z.numel() * 4, lambda: fsd.fsd_condition_chain(z, tokens, conditions, stream=side)
+    elif call == "append":
+        size, run = B * 4, lambda: fsd.fsd_cache_append(k, k, cache, accepted, stream=side)
+    elif call == "attend":
+        size, run = q.numel() * 2, lambda: fsd.fsd_attend_chain(q, k, k, cache, stream=side)
+    else:
+        out = dict(out=torch.empty_like(q))
+        size, run = fsd.fsd_attend_workspace_bytes(B, R, 4 * H, H, D) + 256, lambda: fsd.fsd_attend_chain(q, k, k, cache, out=out, stream=side)
+    run()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    kept = [torch.zeros_like(t) for t in held]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    for a, b in zip(held, kept):
+        b.copy_(a)
+    del held, a                                                # given back while the copies are under way
+    got = run()
+    torch.cuda.synchronize()
+    assert got is not None and all((t == 7).all() for t in kept)
