@@ -47,9 +47,11 @@ def _check(t, name, shape=None, dtype=None, device=None):
         raise ValueError(f"{name} lives on {t.device}, the others on {device}")
 
 
-def _on_current(device):
+def _on_current(device, stream):
     if device.index != _torch().cuda.current_device():
         raise ValueError(f"the tensors live on {device}, which is not the current device")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is one of {stream.device}, the tensors live on {device}")
 
 
 def _new(stream, device, **tensors):
@@ -171,7 +173,7 @@ def _condition(call, logits, tokens, parent, conditions, out, stream):
     dt = binding._dtype_code(logits)
     dev = logits.device
     _check(logits, "logits")
-    _on_current(dev)
+    _on_current(dev, stream)
     n = 0
     if tokens is not None:
         n = tokens.shape[-1]
@@ -254,7 +256,7 @@ def fsd_cache_append(k, v, cache, accept_len, *, path_nodes=None, rotation=None,
     torch = _torch()
     dt = _dtype_code(k, True)
     dev = cache.device
-    _on_current(dev)
+    _on_current(dev, stream)
     if k.dim() not in (4, 5):
         raise ValueError("k has 4 or 5 dimensions")
     B, R = k.shape[-4:-2]
@@ -299,7 +301,7 @@ def _attend(call, q, k, v, parent, cache, layer, row_count, rotation, scale, out
     torch = _torch()
     dt = _dtype_code(q, False)
     dev = cache.device
-    _on_current(dev)
+    _on_current(dev, stream)
     if q.dim() != 4:
         raise ValueError("q has 4 dimensions")
     B, R, heads, D = q.shape

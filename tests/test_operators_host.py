@@ -213,3 +213,17 @@ def test_conditioned_logits_that_overlap_the_logits_by_a_part(dtype, step):
     for tree in (False, True):
         for out in (at + step, at - step, at + size - step, at - size + step):
             assert _chain(logits=at, out=out, dtype=dtype, tree=tree, parent=A) == -9
+
+
+def test_streams_of_another_device(monkeypatch):
+    import types
+
+    import torch
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    here, there = torch.device("cuda", 0), torch.device("cuda", 1)
+    ops._on_current(here, None)
+    ops._on_current(here, types.SimpleNamespace(device=here))
+    for device, stream in ((there, None), (here, types.SimpleNamespace(device=there))):
+        with pytest.raises(ValueError):
+            ops._on_current(device, stream)
