@@ -617,10 +617,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         float my_ks = 1.0f, my_vs = 1.0f;
         auto look_further = [&](int j0) {
             good = j0 + lane < last && my_id >= 0 && my_id < P.cache.num_blocks;
-            if (!good) my_id = 0;                             // in bounds, and none of its tokens counts
+            if (!good) my_id = 0;                             // in bounds, and neither its tokens nor its scales count
             const size_t at = (layer0 + my_id) * H + h;
-            my_ks = P.cache.k_scale[at];
-            my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+            const float ks = P.cache.k_scale[at], vs = P.cache.v_scale[at];
+            my_ks = good ? ks : 1.0f;
+            my_vs = good ? __builtin_fmaxf(vs, 0x1p-100f) : 0x1p-100f;
         };
         if (first < last) look_further(first);
         // (columns behind the last row hold anything; they are never stored, and must not hold up the others)
@@ -679,6 +680,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
 #pragma unroll
                 for (int j = 1; j < 16; ++j) top = __builtin_fmaxf(top, s[rt][j / 4][j % 4]);
                 high[rt] = fmaf(top, f[rt], lift);
+                if constexpr (part) high[rt] = kept(rt) != 0u ? high[rt] : -__builtin_inff();   // (a factor near 0 takes a masked product to a score near 0)
                 over |= high[rt] > m[rt] + kLazy;
             }
             if (__any(over)) {
@@ -1023,10 +1025,11 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
         float my_ks = 1.0f, my_vs = 1.0f;
         auto look_further = [&](int j0) {
             good = j0 + lane < last && my_id >= 0 && my_id < P.cache.num_blocks;
-            if (!good) my_id = 0;                             // in bounds, and none of its tokens counts
+            if (!good) my_id = 0;                             // in bounds, and neither its tokens nor its scales count
             const size_t at = (layer0 + my_id) * H + h;
-            my_ks = P.cache.k_scale[at];
-            my_vs = __builtin_fmaxf(P.cache.v_scale[at], 0x1p-100f);
+            const float ks = P.cache.k_scale[at], vs = P.cache.v_scale[at];
+            my_ks = good ? ks : 1.0f;
+            my_vs = good ? __builtin_fmaxf(vs, 0x1p-100f) : 0x1p-100f;
         };
         if (first < last) look_further(first);
         // (columns behind the last row hold anything; they are never stored, and must not hold up the others)
@@ -1077,6 +1080,7 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                     for (int i = 0; i < 4; ++i) s[rt][i] = kept(rt) >> i & 1u ? s[rt][i] : -3.0e38f;
                 }
                 high[rt] = fmaf(__builtin_fmaxf(__builtin_fmaxf(s[rt][0], s[rt][1]), __builtin_fmaxf(s[rt][2], s[rt][3])), f[rt], lift);
+                if constexpr (part) high[rt] = kept(rt) != 0u ? high[rt] : -__builtin_inff();   // (a factor near 0 takes a masked product to a score near 0)
                 run |= high[rt] > m[rt] + kLazy;
             }
             float sum[RT];
