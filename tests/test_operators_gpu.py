@@ -1052,46 +1052,54 @@ def test_outputs_on_another_stream_leave_the_current_streams_memory(call):
 @pytest.mark.parametrize("scale", [0.0, 2.0 ** -133, 0.1])
 def test_attend_unseen_tile_of_large_values(D, H, G, dtype, scale):
     """A tree of three tiles of rows: those of the third see the first, not the second, whose values are 2^23 (binary16) or 2^40 times as large.  Scores
-    near 0 (a scale of 0, or a tiny one) are no reason to let what is masked into the running maximum."""
+    near 0 (a scale of 0, or a tiny one) are no reason to let what is masked into the running maximum.  (So many sequences that one worker goes over
+    all tiles of an item.)"""
     rng = np.random.default_rng(D + H)
-    R, lens = 192, [0, 70]
+    R, B = 192, 120
+    lens = [0] * B
+    lens[1::40] = [70] * 3
     table, c, q, k, v = _case(rng, lens, R, H * G, H, D, DT[dtype])
     q, k, v = q.contiguous(), k.contiguous(), v.clone()
     if dtype == "f16":
         v *= 2.0 ** -10
     v[:, 64:128] *= 2.0 ** (23 if dtype == "f16" else 40)
-    parent = np.empty((2, R - 1), dtype=np.int32)
+    parent = np.empty((B, R - 1), dtype=np.int32)
     for j in range(R - 1):
         row = j + 1                                            # rows 64 .. 127 and those behind them: trees that meet in the first tile only
         parent[:, j] = -1 if row < 3 else rng.integers(0, row if row < 64 else 64) - 1 if row < 66 or 128 <= row < 130 else rng.integers(row // 64 * 64, row) - 1
     got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), _to_cache(c, table, lens), scale=scale)
-    assert got["row_status"].tolist() == [0, 0]
-    want, bound = ref.attend(_host(q), _host(k), _host(v), parent, np.full(2, R), c, 0, lens, table, scale, None, True, DT[dtype])
+    assert (got["row_status"] == 0).all()
+    some = [0, 1, 41, 60, 81, B - 1]
+    want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), parent[some], np.full(6, R), c, 0, [lens[b] for b in some], table[some], scale, None,
+                             True, DT[dtype])
     if dtype == "f16":
         # The result's rounding: the bound counts half a step relative to the value, which binary16 keeps down to 2^-14 only.  Below that its numbers lie
         # 2^-24 apart, so that the nearest one may be 2^-25 away (-292.5 units of 2^-24 come out as -292), and results of these values are that small.
         bound = bound + 2.0 ** -25
     for rows in (slice(0, 64), slice(64, 128), slice(128, 192)):
-        _within(got["out"][:, rows], want[:, rows], bound[:, rows], str(rows))
+        _within(got["out"][some][:, rows], want[:, rows], bound[:, rows], str(rows))
 
 
 @pytest.mark.parametrize("R,heads,H,D,dtype", [(3, 4, 2, 128, "bf16"), (40, 4, 1, 64, "bf16"), (30, 4, 1, 256, "f16"), (2, 4, 4, 64, "f16")])
-@pytest.mark.parametrize("theirs", [2.0 ** 60, float("inf"), float("nan")])
+@pytest.mark.parametrize("theirs,keys", [(2.0 ** 60, 2.0 ** -8), (float("inf"), 2.0 ** -8), (float("inf"), float("inf")), (float("nan"), float("nan"))])
 @pytest.mark.parametrize("scale", [0.0, 0.1])
-def test_attend_left_out_blocks_lend_no_scale(R, heads, H, D, dtype, theirs, scale):
-    """A block number out of range is left out, whatever the scales of the cache's block 0 are, which nobody asked for."""
+@pytest.mark.parametrize("B", [2, 120])
+def test_attend_left_out_blocks_lend_no_scale(R, heads, H, D, dtype, theirs, keys, scale, B):
+    """A block number out of range is left out, whatever the scales of the cache's block 0 are, which nobody asked for.  (2 sequences: every unit of work
+    stands alone; 120: a worker has whole items.)"""
     rng = np.random.default_rng(R + D)
-    lens = [320, 100]
-    _, c, q, k, v = _case(rng, [320, 320], R, heads, H, D, DT[dtype])
-    table = np.arange(1, 11, dtype=np.int32).reshape(2, 5)
+    lens = [320, 100] * (B // 2)
+    _, c, q, k, v = _case(rng, [320] * B, R, heads, H, D, DT[dtype])
+    table = np.arange(1, 5 * B + 1, dtype=np.int32).reshape(B, 5)
     for n in ("k_codes", "v_codes"):                           # (the list of lengths above was for other blocks)
         c[n][(c[n] & 0x7F) == 0x7F] = 0x21
-    c["k_scale"][:, 0], c["v_scale"][:, 0] = theirs, theirs
+    c["k_scale"][:, 0], c["v_scale"][:, 0] = keys, theirs
     broken = table.copy()
-    broken[0, 0], broken[0, 2], broken[1, 1] = -1, 1 << 20, 11 + 3
+    broken[::2, 0], broken[::2, 2], broken[1::2, 1] = -1, 1 << 20, 5 * B + 4
     got = fsd.fsd_attend_chain(q, k, v, _to_cache(c, broken, lens), scale=scale)
-    assert got["row_status"].tolist() == [32, 32]
+    assert (got["row_status"] == 32).all()
     c["k_scale"][:, 0], c["v_scale"][:, 0] = 1.0, 1.0
-    want, bound = ref.attend(_host(q), _host(k), _host(v), None, np.full(2, R), c, 0, lens, broken, scale, None, True, DT[dtype],
-                             left_out=((0, 0), (0, 2), (1, 1)))
-    _within(got["out"], want, bound)
+    some = [0, 1] if B == 2 else [0, 1, 58, 59, 118, 119]
+    want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), None, np.full(len(some), R), c, 0, [lens[b] for b in some], broken[some], scale, None,
+                             True, DT[dtype], left_out=[(i, j) for i, b in enumerate(some) for j in ((0, 2) if b % 2 == 0 else (1,))])
+    _within(got["out"][some], want, bound)
