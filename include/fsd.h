@@ -467,7 +467,8 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
  * enter them with the 11 significant bits of binary16 (scaled so that they stay in its range; FSD_F16's queries and keys, which may use
  * all 11, in two parts), the codes exactly; statistics are binary32, the result is rounded once.  Magnitudes of values up to
  * 2^120 and value scales from 2^-100 to 2^111 are in range.  A NaN among the keys or codes a row sees makes its outputs NaN, and so does
- * a value among the rows that is not finite (all head_dim outputs of the heads that read it); what a row does not see never matters.
+ * a value among the rows that is not finite (all head_dim outputs of the heads that read it); what a row does not see
+ * changes its result by a rounding at most, whatever it holds.
  * 1 <= R <= 2049, 1 <= heads / kv_heads <= 64, heads <= 1024, B <= 65535, B * R < 2^24.
  */
 size_t fsd_attend_workspace_bytes(int B, int R, int heads, int kv_heads, int head_dim);

@@ -46,6 +46,8 @@ constexpr float kRoom = 7.0f;      // powers of two that a weight formed anew is
 constexpr float kLazy = 15.0f;     // how far (likewise) weights may pass 1 before they are scaled down again
 constexpr float kUnit = 10.0f;     // sums are in units of 2^10: value scales from 2^-100 on leave room for 2^22 tokens, those up to 2^119 do not vanish
 constexpr float kPerUnit = 0x1p-10f;
+constexpr int kLeast = 100;        // units of the rows' values are 2^-100 to 2^119
+constexpr float kNarrow = 0x1p-6f; // a tile's values have one unit where the smallest row (its largest magnitude) is no further below the largest
 constexpr float kLog2eF = 1.44269504088896340736f;
 
 struct AttendParams {
@@ -73,7 +75,8 @@ struct AttendParams {
     int2* pieces;                  // [B, kv_heads, groups] of an item: its first slot, and how many workers share it
     float* factor;                 // [B, kv_heads, row_tiles * 16] of the products of a row: its power of two back, scale, log2(e)
     float* key_scale;              // [B, kv_heads, tiles, 64]
-    float* value_scale;            // [B, kv_heads, tiles]
+    int* value_lift;               // [B, kv_heads, tiles] log2 of what a tile's values are in units of, plus kLeast; -1: each row's are in units of their own
+    unsigned char* row_lift;       // [B, kv_heads, tiles, 64] these, where they are
     unsigned long long* broken;    // [B, kv_heads, tiles] tokens of a tile with a value that is not finite
     unsigned long long* sees;      // [B, R, tiles] trees: tokens of a tile that a row sees
     char* q16;                     // [B, kv_heads, row_tiles, 2 * (D / 64)] fragments of 1 KB; binary16 inputs: second parts behind them
@@ -162,6 +165,7 @@ __device__ __forceinline__ void store4(int dtype, void* base, size_t at, const f
     }
     *reinterpret_cast<uint2*>(static_cast<unsigned short*>(base) + at) = w;
 }
+__device__ __forceinline__ float byte_of(unsigned w, int i) { return static_cast<float>(w >> (8 * i) & 0xFFu); }   // (one instruction)
 // maximum over the four lanes that hold one column
 __device__ __forceinline__ float column_max(float v) {
     v = __builtin_fmaxf(v, __shfl_xor(v, 16, 64));
@@ -176,14 +180,22 @@ __device__ __forceinline__ float column_sum(float v) {
 __device__ __forceinline__ float back_from(float from, float to) {
     return to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(0.5f * (from - to));
 }
-// the power of two that brings `most` into [2^at, 2 * 2^at) (1 where there is nothing to bring there), as an exponent
-__device__ __forceinline__ int to_half_range(float most, int at, int limit) {
-    const int e = static_cast<int>(__float_as_uint(most) >> 23) - 127;
-    return most > 0.0f ? min(at - e, limit) : 0;
+// the power of two that brings `most` into [2^at, 2 * 2^at), as an exponent
+__device__ __forceinline__ int to_half_range(float most, int at, int limit) { return min(at + 127 - static_cast<int>(__float_as_uint(most) >> 23), limit); }
+// queries and keys: as large as products allow; values (as an exponent): as large as the cache's codes, so that their scales are alike (nothing but zeros
+// gets the smallest unit there is, as in the cache)
+__device__ __forceinline__ float key_range(float most) { return most > 0.0f ? pow2(to_half_range(most, 13, 126)) : 1.0f; }
+__device__ __forceinline__ int value_range(float most) { return to_half_range(most, 8, kLeast); }
+// maximum over the 16 lanes of a row, in all of them: lanes 1 and 2 apart, then mirrored in halves and as a whole
+__device__ __forceinline__ float row_max(float v) {
+    auto other = [&](auto ctrl) {
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    v = __builtin_fmaxf(v, other(std::integral_constant<int, 0xB1>()));
+    v = __builtin_fmaxf(v, other(std::integral_constant<int, 0x4E>()));
+    v = __builtin_fmaxf(v, other(std::integral_constant<int, 0x141>()));
+    return __builtin_fmaxf(v, other(std::integral_constant<int, 0x140>()));
 }
-// queries and keys: as large as products allow; values: as large as the cache's codes, so that their scales are alike
-__device__ __forceinline__ float key_range(float most) { return pow2(to_half_range(most, 13, 126)); }
-__device__ __forceinline__ float value_range(float most) { return pow2(to_half_range(most, 8, 100)); }
 
 constexpr int kMaxNodes = 2048;
 constexpr int kWalk = 256;          // nodes of trees whose depths are found by walking
@@ -278,7 +290,7 @@ __device__ __forceinline__ void two_parts(const float (&y)[8], float by, half8_t
 template <int D, bool FINE>
 __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
     constexpr int kType = FINE ? FSD_F16 : FSD_BF16, kI = D / 64, kPer = D / 8, kThreads = kWG;
-    __shared__ float most_of[kWG / 64];
+    __shared__ __align__(16) float most_of[2][kBlock];
     __shared__ unsigned long long broken;
     extern __shared__ short tree[];                           // trees: [R] parent's row, [R] depth, [R] ancestors found so far
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -439,14 +451,14 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
         return;
     }
     if (n <= 0) return;
-    // values: a thread takes 8 tokens of one dimension, which lie in one of the product's fragments
+    // values: a thread takes 8 tokens of one dimension, which lie in one of the product's fragments; its tokens are the same in all units
     constexpr int kUnits = kBlock * D / 8 / kThreads;
     unsigned raw[kUnits][4];
     const unsigned short* values = static_cast<const unsigned short*>(P.v) + base;
-    auto token_of = [&](int i) { return (lane >> 4) * 16 + ((tid + i * kThreads) >> 6 & 1) * 8; };   // the first of unit i
+    const int t = (lane >> 4) * 16 + (wave & 1) * 8;          // the first of them
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-        const int d = (tid + i * kThreads) / 128 * 16 + (lane & 15), t = token_of(i);
+        const int d = (tid + i * kThreads) / 128 * 16 + (lane & 15);
 #pragma unroll
         for (int e = 0; e < 4; ++e) raw[i][e] = 0;
         if (t >= n) continue;
@@ -456,21 +468,39 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
             raw[i][e / 2] |= (t + e < n ? w : 0u) << (16 * (e & 1));
         }
     }
-    // all values are scaled by one power of two; one that is not finite is noted, as no weight of 0 makes it harmless
-    float most = 0.0f;
+    // Values are scaled by a power of two, for all rows of the tile where they are of one size, else for each its own: what a row sees must not be lost
+    // beside what it does not see.  One that is not finite is noted, as no weight of 0 makes it harmless.  (A row's dimensions lie in 16 lanes of this
+    // wavefront and of the one two further.)
+    float most[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most[e] = 0.0f;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         float y[8];
         unpack8(P.dtype, u32x4{raw[i][0], raw[i][1], raw[i][2], raw[i][3]}, y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, finite_abs(y[e]));
+        for (int e = 0; e < 8; ++e) most[e] = __builtin_fmaxf(most[e], finite_abs(y[e]));
     }
-    most = wave_max_all(most);
-    if (lane == 0) most_of[wave] = most;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most[e] = row_max(most[e]);
+    if ((lane & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4_t*>(&most_of[wave >> 1][t + e]) = float4_t{most[e], most[e + 1], most[e + 2], most[e + 3]};
+    }
     if (tid == 0) broken = 0;
     __syncthreads();
-    most = __builtin_fmaxf(__builtin_fmaxf(most_of[0], most_of[1]), __builtin_fmaxf(most_of[2], most_of[3]));
-    const float by = value_range(most);
+    const float of_row = __builtin_fmaxf(most_of[0][lane], most_of[1][lane]);
+    const float high = column_max(row_max(of_row)), least = -column_max(row_max(of_row > 0.0f ? -of_row : -__builtin_inff()));
+    const bool narrow = least >= high * kNarrow;
+    float by[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) by[e] = pow2(value_range(high));
+    if (!narrow) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) by[e] = pow2(value_range(__builtin_fmaxf(most_of[0][t + e], most_of[1][t + e])));
+        if (wave == 0) P.row_lift[bht * kBlock + lane] = static_cast<unsigned char>(kLeast - value_range(of_row));
+    }
+    if (tid == 0) P.value_lift[bht] = narrow ? kLeast - value_range(high) : -1;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
         float y[8];
@@ -480,17 +510,14 @@ __global__ __launch_bounds__(kWG) void attend_prepare(AttendParams P) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool finite = __builtin_fabsf(y[e]) < __builtin_inff();
-            if (!finite) bad |= 1ull << (token_of(i) + e);
-            a[e] = static_cast<_Float16>(finite ? y[e] * by : 0.0f);
+            if (!finite) bad |= 1ull << (t + e);
+            a[e] = static_cast<_Float16>(finite ? y[e] * by[e] : 0.0f);
         }
         if (bad != 0) atomicOr(&broken, bad);
         *reinterpret_cast<half8_t*>(P.v16 + bht * (8 * kI * 1024) + static_cast<size_t>(tid + i * kThreads) * 16) = a;
     }
     __syncthreads();
-    if (tid == 0) {
-        P.value_scale[bht] = 1.0f / by;
-        P.broken[bht] = broken;
-    }
+    if (tid == 0) P.broken[bht] = broken;
     if (P.parent && h == 0) {                                 // who of this tile lies on the way to a row
         for (int r = t0 + tid; r < share.rows; r += kThreads) {
             unsigned long long bits = 0;
@@ -658,10 +685,21 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         const _Float16 one = static_cast<_Float16>(1.0f);
         const half8_t ones = {one, one, one, one, one, one, one, one};
 
+        auto raise = [&](const float (&high)[RT]) {           // to maxima that have run away
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float to = __builtin_fmaxf(m[rt], column_max(high[rt]) - kRoom);
+                const float root = back_from(m[rt], to), by = root * root;
+                m[rt] = to;
+                l[rt] = l[rt] * root * root;
+#pragma unroll
+                for (int t = 0; t < kT; ++t) o[rt][t] *= by;
+            }
+        };
         // Weights of 64 tokens from their products.  With `part` only those of kept(rt) count (a bit for each of the 16 tokens of this
-        // lane's group), and those of spoilt(rt) are NaN.  Their sum is a product with ones: two instructions of the matrix unit for
-        // 16 additions, and it sums what the second product will use.
-        auto weigh = [&](float4_t (&s)[RT][4], float ks, float vs, auto part, auto kept, auto spoilt, half8_t (&p)[RT][2]) {
+        // lane's group).  Their sum is a product with ones: two instructions of the matrix unit for 16 additions, and it sums what the second product
+        // will use.
+        auto weigh = [&](float4_t (&s)[RT][4], float ks, float vs, auto part, auto kept, half8_t (&p)[RT][2]) {
             const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs) * kPerUnit;   // (exact for powers of two)
             // 2^6 below: a weight of 2^-25 that binary16 loses is 2^-26 of the largest
             const bool low = vs < most_vs * 0x1p-6f;
@@ -683,17 +721,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 if constexpr (part) high[rt] = kept(rt) != 0u ? high[rt] : -__builtin_inff();   // (a factor near 0 takes a masked product to a score near 0)
                 over |= high[rt] > m[rt] + kLazy;
             }
-            if (__any(over)) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float to = __builtin_fmaxf(m[rt], column_max(high[rt]) - kRoom);
-                    const float root = back_from(m[rt], to), by = root * root;
-                    m[rt] = to;
-                    l[rt] = l[rt] * root * root;
-#pragma unroll
-                    for (int t = 0; t < kT; ++t) o[rt][t] *= by;
-                }
-            }
+            if (__any(over)) raise(high);
             if (low) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
@@ -708,14 +736,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const float from = lift - (m[rt] == -__builtin_inff() ? 0.0f : m[rt]);
-                const unsigned keep = part ? kept(rt) : 0xFFFFu, spoil = part ? spoilt(rt) : 0u;
+                const unsigned keep = part ? kept(rt) : 0xFFFFu;
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) {
                     float2_t w;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         w[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][j / 4][j % 4 + e], f[rt], from));
-                        if constexpr (part) w[e] = keep >> (j + e) & 1u ? (spoil >> (j + e) & 1u ? __builtin_nanf("") : w[e]) : 0.0f;
+                        if constexpr (part) w[e] = keep >> (j + e) & 1u ? w[e] : 0.0f;
                     }
                     const half2_t two = __builtin_convertvector(w, half2_t);
                     p[rt][j / 8][j % 8] = two.x;
@@ -727,7 +755,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 l[rt] = fmaf(z[0], low ? 0.0f : inv_vs, l[rt]);
             }
         };
-        auto nothing = [](int) { return 0u; };
         const std::integral_constant<bool, true> in_part;
         const std::integral_constant<bool, false> in_full;
 
@@ -833,7 +860,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                         half8_t p[RT][2];
                         products(at, s);
                         const int mine = max(0, min(16, left_of(i) - 16 * g));
-                        weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return (1u << mine) - 1u; }, nothing, p);
+                        weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return (1u << mine) - 1u; }, p);
                         sums(at, p, part, mine);
                     }
                 };
@@ -845,6 +872,42 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
         }
         // ---- the tail: the rows themselves, in binary16
         {
+            // Weights where the rows of a tile have units of their own: each token's is in its weight's exponent (`lift`).  They lie far apart, so the sum
+            // takes every weight without its own.  (Seldom: two exponentials a weight are well enough.)
+            auto weigh_rows = [&](float4_t (&s)[RT][4], u32x4 lift, const unsigned (&see)[RT], half8_t (&p)[RT][2]) {
+                float high[RT];
+                bool over = false;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    high[rt] = -__builtin_inff();
+                    settle(lift);                             // (its bytes are taken out anew each time: as numbers they would fill 16 registers)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float x = see[rt] >> j & 1u ? fmaf(s[rt][j / 4][j % 4], factor[rt], byte_of(lift[j / 4], j % 4)) : -__builtin_inff();
+                        s[rt][j / 4][j % 4] = x;
+                        high[rt] = __builtin_fmaxf(high[rt], x);
+                    }
+                    high[rt] -= kLeast;
+                    over |= high[rt] > m[rt] + kLazy;
+                }
+                if (__any(over)) raise(high);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float from = (m[rt] == -__builtin_inff() ? 0.0f : m[rt]) + kLeast;
+                    settle(lift);
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum += __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4] - from - byte_of(lift[j / 4], j % 4) + (kLeast - kUnit));
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        const float2_t w = {__builtin_amdgcn_exp2f(s[rt][j / 4][j % 4] - from), __builtin_amdgcn_exp2f(s[rt][j / 4][j % 4 + 1] - from)};
+                        const half2_t two = __builtin_convertvector(w, half2_t);
+                        p[rt][j / 8][j % 8] = two.x;
+                        p[rt][j / 8][j % 8 + 1] = two.y;
+                    }
+                    l[rt] += column_sum(sum);
+                }
+            };
             // weights and sums of tile `tile`, whose keys lie at `keys` and whose values come when values() is called
             auto one_tile = [&](int tile, auto keys, auto values) {
                 const size_t bht = bh * P.tiles + tile;
@@ -852,9 +915,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                 float4_t s[RT][4];
                 keys(s);
                 const float* scales = P.key_scale + bht * kBlock + g * 16;
+                const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g)) & 0xFFFFu;
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    const float4_t ks = *reinterpret_cast<const float4_t*>(scales + 4 * t);   // of rows 4 g .. of token tile t
+                    float4_t ks = *reinterpret_cast<const float4_t*>(scales + 4 * t);   // of rows 4 g .. of token tile t
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ks[i] = spoilt >> (4 * t + i) & 1u ? __builtin_nanf("") : ks[i];
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) s[rt][t] *= ks;
                 }
@@ -866,9 +932,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                     else if (P.parent) see[rt] = static_cast<unsigned>(P.sees[(static_cast<size_t>(b) * R + r) * P.tiles + tile] >> (16 * g)) & 0xFFFFu;
                     else see[rt] = (1u << max(0, min(16, r - t0 - 16 * g + 1))) - 1u;         // rows t0 + 16 g .. r
                 }
-                const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g)) & 0xFFFFu;
+                const int one_lift = P.value_lift[bht];
                 half8_t p[RT][2];
-                weigh(s, 1.0f, P.value_scale[bht], in_part, [&](int rt) { return see[rt]; }, [&](int) { return spoilt; }, p);
+                if (one_lift >= 0) weigh(s, 1.0f, pow2(one_lift - kLeast), in_part, [&](int rt) { return see[rt]; }, p);
+                else weigh_rows(s, *reinterpret_cast<const u32x4*>(P.row_lift + bht * kBlock + g * 16), see, p);
                 values(p);
             };
             auto products16 = [&](unsigned at, auto second, float4_t (&s)[RT][4]) {   // second: the keys' second parts, or the first ones again
@@ -1065,8 +1132,9 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
         }
 
         // From this wavefront's products to everyone's weights p.  With `part` only the tokens of kept(rt) count (a bit for each of this
-        // lane's four), and the weights of spoilt are NaN.
-        auto weigh = [&](float4_t (&s)[RT], float ks, float vs, auto part, auto kept, unsigned spoilt, half8_t (&p)[RT][2]) {
+        // lane's four).  `rows`: each token's values are in units of their own (lifts: log2 and kLeast); these lie far apart, so
+        // the sum takes every weight without its own.
+        auto weigh = [&](float4_t (&s)[RT], float ks, float vs, auto part, auto kept, auto rows, unsigned lifts, half8_t (&p)[RT][2]) {
             const float lift = __builtin_amdgcn_logf(vs), inv_vs = __builtin_amdgcn_rcpf(vs) * kPerUnit;   // (exact for powers of two)
             const bool low = vs < most_vs * 0x1p-60f;                   // weights may vanish in binary32
             most_vs = __builtin_fmaxf(most_vs, vs);
@@ -1075,12 +1143,16 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 f[rt] = factor[rt] * ks;
-                if constexpr (part) {
+                if constexpr (rows) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[rt][i] = kept(rt) >> i & 1u ? fmaf(s[rt][i], f[rt], byte_of(lifts, i)) : -__builtin_inff();
+                } else if constexpr (part) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[rt][i] = kept(rt) >> i & 1u ? s[rt][i] : -3.0e38f;
                 }
-                high[rt] = fmaf(__builtin_fmaxf(__builtin_fmaxf(s[rt][0], s[rt][1]), __builtin_fmaxf(s[rt][2], s[rt][3])), f[rt], lift);
-                if constexpr (part) high[rt] = kept(rt) != 0u ? high[rt] : -__builtin_inff();   // (a factor near 0 takes a masked product to a score near 0)
+                high[rt] = __builtin_fmaxf(__builtin_fmaxf(s[rt][0], s[rt][1]), __builtin_fmaxf(s[rt][2], s[rt][3]));
+                high[rt] = rows ? high[rt] - kLeast : fmaf(high[rt], f[rt], lift);
+                if constexpr (part && !rows) high[rt] = kept(rt) != 0u ? high[rt] : -__builtin_inff();   // (a factor near 0 takes a masked product to a score near 0)
                 run |= high[rt] > m[rt] + kLazy;
             }
             float sum[RT];
@@ -1088,18 +1160,29 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
             auto form = [&]() {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    const float from = lift - (m[rt] == -__builtin_inff() ? 0.0f : m[rt]);
+                    const float base = m[rt] == -__builtin_inff() ? 0.0f : m[rt];
                     float w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from));
-                        if constexpr (part) w[i] = kept(rt) >> i & 1u ? (spoilt >> i & 1u ? __builtin_nanf("") : w[i]) : 0.0f;
-                    }
-                    sum[rt] = ((w[0] + w[1]) + (w[2] + w[3])) * inv_vs;
-                    if (low) {
+                    if constexpr (rows) {
                         sum[rt] = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[rt] += !part || (kept(rt) >> i & 1u) ? __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from - lift - kUnit)) : 0.0f;
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = s[rt][i] - (base + kLeast);
+                            w[i] = __builtin_amdgcn_exp2f(x);
+                            sum[rt] += __builtin_amdgcn_exp2f(x - byte_of(lifts, i) + (kLeast - kUnit));
+                        }
+                    } else {
+                        const float from = lift - base;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from));
+                            if constexpr (part) w[i] = kept(rt) >> i & 1u ? w[i] : 0.0f;
+                        }
+                        sum[rt] = ((w[0] + w[1]) + (w[2] + w[3])) * inv_vs;
+                        if (low) {
+                            sum[rt] = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sum[rt] += !part || (kept(rt) >> i & 1u) ? __builtin_amdgcn_exp2f(fmaf(s[rt][i], f[rt], from - lift - kUnit)) : 0.0f;
+                        }
                     }
                     const float2_t lo = {w[0], w[1]}, hi = {w[2], w[3]};
                     uint2 y;
@@ -1197,7 +1280,7 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                     }
                     const int mine = max(0, min(16, left_of(i) - 16 * g));          // of the 16 tokens of this lane's group
                     const unsigned keep = ((1u << mine) - 1u) >> (4 * wave) & 15u;
-                    weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return keep; }, 0u, p);
+                    weigh(s, float_of(my_ks, i), float_of(my_vs, i), part, [&](int) { return keep; }, in_full, 0u, p);
                     wait_fetches<(kStages - 1) * (kI + kV)>();
                     read_some<kV>(at + kI * 1024, w);
 #pragma unroll
@@ -1240,9 +1323,11 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
             }
 #pragma unroll
             for (int k = 0; k < 2 * kV; ++k) v[k] = *reinterpret_cast<const half8_t*>(values + k * 1024);
-            const float4_t ks = *reinterpret_cast<const float4_t*>(P.key_scale + bht * kBlock + g * 16 + 4 * wave);
+            float4_t ks = *reinterpret_cast<const float4_t*>(P.key_scale + bht * kBlock + g * 16 + 4 * wave);
             const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g + 4 * wave)) & 15u;
-            const float vs = P.value_scale[bht];
+            const int one_lift = P.value_lift[bht];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ks[i] = spoilt >> i & 1u ? __builtin_nanf("") : ks[i];   // (of those a row sees every weight is NaN then)
             float4_t s[RT];
             half8_t p[RT][2];
             unsigned see[RT];
@@ -1260,7 +1345,9 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
                 else if (P.parent) see[rt] = static_cast<unsigned>(P.sees[(static_cast<size_t>(b) * R + r) * P.tiles + tile] >> (16 * g + 4 * wave)) & 15u;
                 else see[rt] = (1u << max(0, min(4, r - r0 + 1))) - 1u;
             }
-            weigh(s, 1.0f, vs, in_part, [&](int rt) { return see[rt]; }, spoilt, p);
+            auto seen = [&](int rt) { return see[rt]; };
+            if (one_lift >= 0) weigh(s, 1.0f, pow2(one_lift - kLeast), in_part, seen, in_full, 0u, p);
+            else weigh(s, 1.0f, 1.0f, in_part, seen, in_part, *reinterpret_cast<const unsigned*>(P.row_lift + bht * kBlock + g * 16 + 4 * wave), p);
 #pragma unroll
             for (int t = 0; t < 2 * kV; ++t)
 #pragma unroll

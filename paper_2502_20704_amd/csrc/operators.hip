@@ -166,7 +166,7 @@ bool attend_sizes(int B, int R, int heads, int kv_heads, int head_dim) {
 // Places of the workspace's parts (attend_prepare says what they hold), and its size.
 struct AttendSpace {
     int row_tiles, tiles;
-    size_t pieces, factor, key_scale, value_scale, broken, sees, q16, k16, v16, part, bytes;
+    size_t pieces, factor, key_scale, value_lift, row_lift, broken, sees, q16, k16, v16, part, bytes;
 };
 AttendSpace attend_space(const AttendShape& s, int B, int R, int heads, int H, int D, bool fine) {
     AttendSpace w;
@@ -184,7 +184,8 @@ AttendSpace attend_space(const AttendShape& s, int B, int R, int heads, int H, i
     w.pieces = take(bh * groups * 8);
     w.factor = take(bh * w.row_tiles * 64);
     w.key_scale = take(bht * kBlock * 4);
-    w.value_scale = take(bht * 4);
+    w.value_lift = take(bht * 4);
+    w.row_lift = take(bht * kBlock);
     w.broken = take(bht * 8);
     w.sees = take(static_cast<size_t>(B) * R * w.tiles * 8);
     w.q16 = take(bh * w.row_tiles * 32 * D * parts);
@@ -264,7 +265,8 @@ int attend(const void* q, const void* k, const void* v, int64_t q_stride, int64_
     P.pieces = reinterpret_cast<int2*>(base + w.pieces);
     P.factor = reinterpret_cast<float*>(base + w.factor);
     P.key_scale = reinterpret_cast<float*>(base + w.key_scale);
-    P.value_scale = reinterpret_cast<float*>(base + w.value_scale);
+    P.value_lift = reinterpret_cast<int*>(base + w.value_lift);
+    P.row_lift = reinterpret_cast<unsigned char*>(base + w.row_lift);
     P.broken = reinterpret_cast<unsigned long long*>(base + w.broken);
     P.sees = reinterpret_cast<unsigned long long*>(base + w.sees);
     P.q16 = base + w.q16;

@@ -1103,3 +1103,32 @@ def test_attend_left_out_blocks_lend_no_scale(R, heads, H, D, dtype, theirs, key
     want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), None, np.full(len(some), R), c, 0, [lens[b] for b in some], broken[some], scale, None,
                              True, DT[dtype], left_out=[(i, j) for i, b in enumerate(some) for j in ((0, 2) if b % 2 == 0 else (1,))])
     _within(got["out"][some], want, bound)
+
+
+@pytest.mark.parametrize("B", [2, 150])
+@pytest.mark.parametrize("R,heads,H,D,dtype", [(6, 4, 2, 128, "bf16"), (9, 4, 1, 64, "f16"), (30, 2, 1, 256, "bf16"), (70, 4, 2, 64, "bf16"), (61, 8, 2, 128, "bf16"),
+                                               (50, 4, 1, 128, "f16")])
+@pytest.mark.parametrize("tree", [False, True])
+def test_attend_values_far_larger_in_rows_that_are_not_seen(R, heads, H, D, dtype, tree, B):
+    """A step's rows lie in one tile, and what each sees of it are its own ancestors: the values of the others may be of any size (a padded batch's hold
+    whatever memory held), and those it sees of very different ones."""
+    rng = np.random.default_rng(R + D)
+    lens = [0, 90] * (B // 2)
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, DT[dtype])
+    q, k, v = q.contiguous(), k.contiguous(), v.clone()
+    # sizes that rise along the rows: row r sees none as large as those behind it.  In every third sequence they lie far apart in no order.
+    rise = np.linspace(-12, 14, R).astype(int) if dtype == "f16" else np.linspace(-60, 100, R).astype(int)
+    sizes = np.tile(rise, (B, 1))
+    for b in range(0, B, 3):
+        sizes[b] = rng.permutation(rise)
+    v = (v.float().clamp(-1.0, 1.0) * torch.from_numpy(np.exp2(sizes.astype(np.float64))).float().cuda()[:, :, None, None]).to(DT[dtype])
+    parent = _rand_parents(rng, B, R - 1) if tree else None
+    cache = _to_cache(c, table, lens)
+    got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache) if tree else fsd.fsd_attend_chain(q, k, v, cache)
+    assert (got["row_status"] == 0).all()
+    some = [0, 1] if B == 2 else [0, 1, 2, 75, 77, 149]
+    want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), parent[some] if tree else None, np.full(len(some), R), c, 0, [lens[b] for b in some],
+                             table[some], D ** -0.5, None, True, DT[dtype])
+    if dtype == "f16":
+        bound = bound + 2.0 ** -25                              # half of the distance of binary16's numbers under 2^-14, which results here are
+    _within(got["out"][some], want, bound)
