@@ -1132,3 +1132,92 @@ def test_attend_values_far_larger_in_rows_that_are_not_seen(R, heads, H, D, dtyp
     if dtype == "f16":
         bound = bound + 2.0 ** -25                              # half of the distance of binary16's numbers under 2^-14, which results here are
     _within(got["out"][some], want, bound)
+
+
+# ------------------------------------------------------------------------------------------ conditioning: many rows of a tree to a workgroup
+
+
+def _conditioned_rows(z, tokens, parent, target, c, b):
+    """fsd_condition_tree for one sequence on the GPU, 64 bits, from the definition: (result, error of 32-bit arithmetic allowed for)"""
+    rows, V = z.shape[1:]
+    N = tokens.shape[1]
+    f64 = dict(dtype=torch.float64, device="cuda")
+    said, prompt = torch.zeros(V, **f64), torch.zeros(V, **f64)
+    if c.get("history") is not None:
+        h, n = c["history"][b].long(), int(c["history_len"][b])
+        k = min(int(c["prompt_len"][b]), n)
+        for part, to in ((h[:k], prompt), (h[k:n], said)):
+            part = part[(part >= 0) & (part < V)]
+            to.index_add_(0, part, torch.ones(part.shape, **f64))
+    up = [p if -1 <= p < j else -1 for j, p in enumerate(parent[b].tolist())]
+    last = [r - 1 if target else up[r] for r in range(rows)]
+    on_way = torch.zeros((N + 1, N), dtype=torch.bool)         # of context j + 1
+    for j in range(N):
+        on_way[j + 1] = on_way[up[j] + 1]
+        on_way[j + 1, j] = True
+    on_way = on_way[[i + 1 for i in last]].cuda()
+    count = said.repeat(rows, 1)
+    for j, t in enumerate(tokens[b].tolist()):
+        if 0 <= t < V:
+            count[:, t] += on_way[:, j]
+    y, f, p, r = z[b].double(), float(c["frequency"][b]), float(c["presence"][b]), float(c["repetition"][b])
+    hit = (prompt + count) > 0
+    y = torch.where(hit, torch.where(y > 0, y / r, y * r), y)
+    bias = torch.zeros(V, **f64)
+    if c.get("bias_tokens") is not None:
+        for t, x in zip(c["bias_tokens"][b].tolist(), c["bias_values"][b].tolist()):
+            if 0 <= t < V:
+                bias[t] = x
+    size = y.abs() + abs(f) * count + abs(p) + bias.abs()
+    y = torch.where(count > 0, y - f * count - p, y) + bias
+    err = torch.where(hit | (bias != 0), 5 * 2.0 ** -24 * size, 0.0)
+    if c.get("allowed") is not None:
+        contexts = [i + 1 if c["allowed"].shape[1] > 1 else 0 for i in last]
+        bits = (c["allowed"][b][contexts][..., None] >> torch.arange(32, dtype=torch.int32, device="cuda")) & 1
+        no = bits.flatten(1)[:, :V] == 0
+        y, err = y.masked_fill(no, -float("inf")), err.masked_fill(no, 0.0)
+    return y, err
+
+
+@pytest.mark.parametrize("B,N,V,dtype,target,history,biases,mask,deep", [
+    (64, 66, 128256, "bf16", True, 300, 16, "contexts", False),       # 67 rows a workgroup, whole lines past the caches
+    (64, 70, 128259, "bf16", False, 300, 5, "contexts", True),        # draft rows, rows that begin anywhere
+    (40, 70, 128256, "f32", False, 50, 0, "contexts", False),
+    (40, 66, 128259, "f32", True, 50, 300, "sequence", True),
+    (512, 80, 9001, "bf16", True, 0, 3, None, True),                  # two slices, paths with many tokens in each
+    (300, 90, 4096, "f32", False, 20, 0, None, True),                 # one slice: every candidate is in it
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_condition_trees_with_many_rows_a_workgroup(B, N, V, dtype, target, history, biases, mask, deep, in_place):
+    rng = np.random.default_rng(N + V)
+    rows = N + 1 if target else N
+    g = torch.Generator(device="cuda").manual_seed(N)
+    z = (torch.randn((B, rows, V), generator=g, device="cuda") * 3).to(DT[dtype])
+    tokens = torch.from_numpy(np.where(rng.random((B, N)) < 0.5, rng.integers(0, 40, (B, N)) * (V // 40), rng.integers(-3, V + 3, (B, N))).astype(np.int32)).cuda()
+    parent = np.stack([rng.integers(np.maximum(-1, np.arange(N) - 3) if deep else -1, np.arange(N)) for _ in range(B)]).astype(np.int32)
+    parent[:, 5], parent[0, 7] = 5, -9                                # malformed: children of the root
+    i32 = dict(dtype=torch.int32, device="cuda")
+    c = dict(repetition=torch.rand(B, generator=g, device="cuda") + 0.5, presence=torch.rand(B, generator=g, device="cuda") - 0.3,
+             frequency=torch.rand(B, generator=g, device="cuda"))
+    if history:
+        c.update(history=torch.randint(-1, V + 1, (B, history), generator=g, **i32), history_len=torch.randint(0, history + 1, (B,), generator=g, **i32),
+                 prompt_len=torch.randint(0, history + 1, (B,), generator=g, **i32))
+    if biases:
+        c.update(bias_tokens=torch.randint(-1, V, (B, biases), generator=g, **i32), bias_values=torch.randn((B, biases), generator=g, device="cuda"))
+        c["bias_tokens"][:, 1], c["bias_tokens"][:, 2] = tokens[:, 3], tokens[:, 3]
+    if mask:
+        c["allowed"] = torch.randint(-2 ** 31, 2 ** 31 - 1, (B, N + 1 if mask == "contexts" else 1, (V + 31) // 32), generator=g, device="cuda").int()
+        c["allowed"][1, 0] = 0
+        c["allowed"][2] = -1
+    kept = z.clone() if in_place else z
+    got = fsd.fsd_condition_tree(z, tokens, torch.from_numpy(parent).cuda(), fsd.Conditions(**c), out=dict(out=z) if in_place else None)["out"]
+    half = ref.HALF_STEP[DT[dtype]]
+    for b in range(B):
+        want, err = _conditioned_rows(kept, tokens, parent, target, c, b)
+        y = got[b].double()
+        assert torch.equal(torch.isneginf(y), torch.isneginf(want)), b
+        fine = torch.isfinite(want)
+        off = torch.where(fine, (y - want).abs() - err * (1 + half) - half * want.abs(), -1.0)
+        assert (off <= 2.0 ** -140).all(), b
+        same = (err == 0) & fine
+        assert torch.equal(got[b][same], kept[b][same]), b
