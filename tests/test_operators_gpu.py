@@ -1221,3 +1221,41 @@ def test_condition_trees_with_many_rows_a_workgroup(B, N, V, dtype, target, hist
         assert (off <= 2.0 ** -140).all(), b
         same = (err == 0) & fine
         assert torch.equal(got[b][same], kept[b][same]), b
+
+
+# ------------------------------------------------------------------------------------------ attention: joining pieces of calls with many rows
+
+MANY = [9000, 0, 64, 100, 700, 2000, 3000, 1, 63, 65, 128, 500, 400, 300, 5000]
+JOIN = [
+    # lens, R, heads, kv_heads, D, dtype, rows of the sequences: B R heads over 4096, where a workgroup of the join takes several rows (one case on each side
+    # of that border); items in 2 to 35 pieces beside whole ones, rows that do not fill the last workgroup, sequences without rows
+    ([900], 64, 64, 8, 128, "bf16", None),
+    ([600], 241, 17, 17, 64, "bf16", None),
+    ([3000], 67, 63, 1, 64, "bf16", None),
+    ([2500, 70], 37, 60, 4, 128, "bf16", None),
+    ([1500, 300, 10], 39, 36, 4, 256, "bf16", None),
+    ([4000, 0, 130, 700, 1], 61, 16, 2, 128, "f16", [61, 0, 5, 61, 33]),
+    ([2000, 100, 0], 350, 4, 4, 256, "f16", [350, 0, 99]),
+    (MANY, 9, 32, 8, 128, "bf16", None),
+    (MANY * 2, 5, 28, 4, 64, "f16", [5, 5, 0, 1, 2, 5, 5, 5, 3, 4] * 3),
+    ([64] * 35 + [8000] * 2, 9, 32, 8, 128, "bf16", None),
+    ([10] * 34 + [5000] * 2, 7, 18, 2, 256, "bf16", [7, 6, 5, 0] * 9),
+    ([0, 64] * 15 + [5000] * 2, 61, 16, 2, 64, "bf16", None),
+]
+
+
+@pytest.mark.parametrize("lens,R,heads,H,D,dtype,counts", JOIN)
+def test_attend_joins_pieces_of_many_rows(lens, R, heads, H, D, dtype, counts):
+    rng = np.random.default_rng(R + D)
+    B, dt = len(lens), DT[dtype]
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, dt)
+    rows = np.array(counts if counts is not None else [R] * B, dtype=np.int32)
+    out = dict(out=torch.full((B, R, heads, D), 7.0, dtype=dt, device="cuda"), row_status=torch.full((B,), -1, dtype=torch.int32, device="cuda"))
+    fsd.fsd_attend_chain(q, k, v, _to_cache(c, table, lens), row_count=torch.from_numpy(rows).cuda() if counts is not None else None, out=out)
+    assert (out["row_status"] == 0).all()
+    some = sorted({0, 1, 2, 3, B - 2, B - 1} & set(range(B)))
+    want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), None, rows[some], c, 0, [lens[b] for b in some], table[some], D ** -0.5, None, True, dt)
+    for i, b in enumerate(some):
+        _within(out["out"][b, :rows[b]], want[i, :rows[b]], bound[i, :rows[b]], f"sequence {b}")
+    for b in range(B):
+        assert (out["out"][b, rows[b]:] == 7.0).all() and torch.isfinite(out["out"][b, :rows[b]]).all()
