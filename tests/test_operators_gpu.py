@@ -1259,3 +1259,57 @@ def test_attend_joins_pieces_of_many_rows(lens, R, heads, H, D, dtype, counts):
         _within(out["out"][b, :rows[b]], want[i, :rows[b]], bound[i, :rows[b]], f"sequence {b}")
     for b in range(B):
         assert (out["out"][b, rows[b]:] == 7.0).all() and torch.isfinite(out["out"][b, :rows[b]]).all()
+
+
+# ------------------------------------------------------------------------------------------ ranges, one at a time
+
+
+@pytest.mark.parametrize("R", [9, 40])
+def test_append_each_limit_alone(R):
+    """The blocks' end and the rotation table's end, each the only reason for a refusal, and both just reached: what is refused leaves the cache alone."""
+    rng = np.random.default_rng(R)
+    B, H, D, turns = 3, 2, 64, 110
+    table, P = _tables(rng, B, 3)
+    k = torch.from_numpy(rng.standard_normal((1, B, R, H, D)).astype(np.float32)).cuda()
+    count = torch.tensor([R - 1] * B, dtype=torch.int32, device="cuda")
+    for rotation, lens, bad in ((None, [192 - R, 193 - R, 192], [0, 32, 32]),                       # no table: blocks alone
+                                (turns, [turns - R, turns - R + 1, 0], [0, 32, 0]),                 # blocks to spare
+                                (192, [192 - R, 193 - R, 10], [0, 32, 0]),
+                                (193, [192 - R, 193 - R, 10], [0, 32, 0])):                         # the table reaches further than the blocks
+        c = _random_cache(rng, 1, P, H, D, table, lens)
+        cache = _to_cache(c, table, lens)
+        got = fsd.fsd_cache_append(k, k, cache, count, rotation=_rotation(_turns(rotation, D), True) if rotation else None)
+        assert got["row_status"].tolist() == bad
+        assert got["cache_len"].tolist() == [n if s else n + R for n, s in zip(lens, bad)]
+        left = [int(i) for b in range(B) if bad[b] for i in table[b]] + [i for i in range(P) if i not in table]
+        for n in ("k_codes", "v_codes", "k_scale", "v_scale"):
+            assert np.array_equal(getattr(cache, n)[:, left].cpu().numpy(), c[n][:, left]), n
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_attend_each_report_alone(tree):
+    """A sequence for each thing that is reported, and one beside it where that is just within its range."""
+    rng = np.random.default_rng(17)
+    H, D, R, per = 2, 64, 9, 4
+    lens = [100, 101, 256, 40, 40, 30, 30, 20]
+    B = len(lens)
+    table, c, q, k, v = _case(rng, [per * 64] * B, R, 4, H, D, torch.bfloat16)
+    P = c["k_scale"].shape[1]
+    for n in ("k_codes", "v_codes"):
+        c[n][(c[n] & 0x7F) == 0x7F] = 0x30
+    turns = _turns(per * 64 + R, D)
+    parent = np.tile(np.arange(-1, R - 2, dtype=np.int32), (B, 1))      # chains: row 8 stands 8 behind the cache
+    said, broken, counts = np.array(lens, dtype=np.int32), table.copy(), np.full(B, R, dtype=np.int32)
+    said[3] = per * 64 + 1
+    broken[4, 0], broken[5, 1] = P, P                                   # (sequence 5 holds one block: the second is not its own)
+    counts[6] = R + 1
+    counts[7] = 0
+    reports = [0, 0, 0, 32, 32, 0, 32, 0]
+    for rows, more in ((per * 64 + R, {}), (per * 64 + R - 1, {2: 32, 3: 32}), (109, {1: 32, 2: 32, 3: 32}), (108, {0: 32, 1: 32, 2: 32, 3: 32})):
+        # (row 8 of sequence 0 stands at 108, of sequence 1 at 109, of sequence 2 at 264)
+        rotation = _rotation(turns[:rows].copy(), True)
+        cache = fsd.Cache(*(torch.from_numpy(c[n]).cuda() for n in ("k_codes", "v_codes", "k_scale", "v_scale")), torch.from_numpy(broken).cuda(),
+                          torch.from_numpy(said).cuda())
+        a = dict(rotation=rotation, row_count=torch.from_numpy(counts).cuda())
+        got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, **a) if tree else fsd.fsd_attend_chain(q, k, v, cache, **a)
+        assert got["row_status"].tolist() == [more.get(b, s) for b, s in enumerate(reports)], rows
