@@ -361,6 +361,8 @@ int fsd_condition_chain(const void* logits, const int32_t* cand_tokens, int B, i
  * context, row j+1: the context that ends with node j); rows = N: its draft rows (row j: the
  * context of node j's parent).  A mask per context has N+1 of them, numbered like the target rows.
  * A parent outside [-1, j) is taken as -1 (the verify call flags it).  1 <= N <= 2048.
+ * (Any tree; what takes time is the part of a row's way that the row before does not share: trees of some hundred levels are better numbered
+ * so that neighbours' ways are alike.)
  */
 int fsd_condition_tree(const void* logits, const int32_t* node_tokens, const int32_t* parent, int B, int N, int rows,
                        int V, int dtype, const fsd_conditions* conditions, void* out, void* hip_stream);

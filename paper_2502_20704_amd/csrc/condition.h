@@ -7,12 +7,14 @@
 // history once and counts in LDS the tokens that fall into its slice (integer atomics: the order does not matter), then
 // streams its rows: one bit an entry tells whether the table says anything about it, so that nearly every 16-byte
 // slot is copied (or masked) as it is.  What a row's own way adds is put into the table when the row needs it: along a chain
-// the contexts contain one another and each row adds one candidate; in a tree the few rows whose way has a token in
-// the slice add it and take it away again.  No row keeps another one waiting otherwise: there is no barrier between them.
+// the contexts contain one another and each row adds one candidate; in a tree a row takes away and adds what its way and that of the row before
+// do not share, of tokens in the slice only (most rows: nothing).  No row keeps another one waiting otherwise: there is no barrier between them.
 //
 // What bounds it is memory: 64 x 9 rows of 128256 bfloat16 entries 70 us (4.2 TB/s read and written; a copy of that size 58), 32 trees of 60 rows under
 // a mask each 185 (5.4 TB/s if all were read; slots without an allowed entry are not), 48 x 17 rows of 128259 binary32 entries with histories of 32768
 // 200 (4.2 TB/s).  One row of 32000: 4.5 us, a kernel's start and its two round trips, history and row.
+// Deep trees: one thread walks between two rows' ways, so numbering that keeps neighbours' ways alike is cheap.  8 sequences of 2048 candidates and 32000
+// bfloat16 entries, as a chain 600 us, as a tree that is a chain 820, random parents 620, but two chains whose nodes come in turn 10450.
 #ifndef FSD_CSRC_CONDITION_H_
 #define FSD_CSRC_CONDITION_H_
 
@@ -65,11 +67,11 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
     unsigned* touched = table + P.slice;                     // [slice / 32] its word or its bias says something
     unsigned* side = touched + P.slice / 32;                 // [side][2] of biased tokens: word, 1 + index of the last bias
     unsigned* taken = side + 2 * P.side;                     // how many of them there are
-    unsigned* wayed = taken + 1;                             // trees: [rows_per_wg / 32 + 1] the row's way has a token here
-    short* up = reinterpret_cast<short*>(wayed + (TREE ? P.rows_per_wg / 32 + 1 : 0));   // trees: [N] parent
+    short* up = reinterpret_cast<short*>(taken + 1);         // trees: [N] parent
     short* here = up + (TREE ? P.N : 0);                     // trees: [N] token - v0, or -1
+    short* near = here + (TREE ? P.N : 0);                   // trees: [N] the last node on the way to a node, itself included, with a token here, or -1
 
-    for (int i = tid; i < P.slice + P.slice / 32 + 2 * P.side + 1 + (TREE ? P.rows_per_wg / 32 + 1 : 0); i += kWG) lds[i] = 0;
+    for (int i = tid; i < P.slice + P.slice / 32 + 2 * P.side + 1; i += kWG) lds[i] = 0;
     const int32_t* tokens = P.tokens + static_cast<size_t>(b) * P.N;
     if constexpr (TREE) {
         const int32_t* parent = P.parent + static_cast<size_t>(b) * P.N;
@@ -137,10 +139,13 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
         for (i += tid; i < len; i += kWG) one(i, h[i]);
     }
     if constexpr (TREE) {
-        for (int r = r0 + tid; r < r1; r += kWG) {
-            bool any = false;
-            for (int j = P.target ? r - 1 : up[r]; j >= 0 && !any; j = up[j]) any = here[j] >= 0;
-            if (any) atomicOr(&wayed[(r - r0) >> 5], 1u << ((r - r0) & 31));
+        for (int j0 = 0; j0 < P.N; j0 += kWG) {              // (as many nodes at a time as there are threads: a walk ends where those before know)
+            if (j0 > 0) __syncthreads();
+            if (j0 + tid < P.N) {
+                int j = j0 + tid;
+                while (j >= j0 && here[j] < 0) j = up[j];
+                near[j0 + tid] = static_cast<short>(j < 0 || j >= j0 ? j : near[j]);
+            }
         }
     } else {
         for (int j = tid; j < min(r0, P.N); j += kWG) {      // the candidates on the way to the first row
@@ -154,11 +159,15 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
     const float* bias = P.c.bias_values + static_cast<size_t>(b) * nb;
     const int words = (P.V + 31) / 32;
 
-    // the tokens on the way to a row are taken into the table, or out of it (the bit stays: a zero word says nothing)
-    auto along = [&](int r, unsigned add) {
-        if (tid == 0) {
-            for (int j = P.target ? r - 1 : up[r]; j >= 0; j = up[j])
-                if (here[j] >= 0) say(static_cast<unsigned>(here[j]), add);
+    // From the way that the table holds (its last node with a token here) to another one: of the two ways' ends the one with the larger number is not on
+    // the other way, as a parent's is smaller.  What is taken out leaves its bit (a zero word says nothing).
+    auto move = [&](int from, int to) {
+        while (from != to) {
+            const bool out = from > to;
+            const int end = out ? from : to, above = up[end], next_end = above < 0 ? -1 : near[above];
+            say(static_cast<unsigned>(here[end]), out ? 0xFFFFFFFFu : 1u);   // (-1 or 1)
+            from = out ? next_end : from;
+            to = out ? to : next_end;
         }
     };
     auto adjusted = [&](float z, int at) {
@@ -179,9 +188,11 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
         if (P.c.allowed && r < r1) {
             const int context = P.c.allowed_contexts == 1 ? 0 : TREE && !P.target ? up[r] + 1 : r;
             const uint32_t* mask = P.c.allowed + (static_cast<size_t>(b) * P.c.allowed_contexts + context) * words + v0 / 32;
+            int id = tid;
+            if constexpr (TREE && !BF16) asm volatile("" : "+v"(id));   // (the places worked out anew for every row: kept, they would take registers that are spilled)
 #pragma unroll
             for (int k = 0; k < kConditionSlots; ++k) {
-                const int at = (tid + k * kWG) * VE;
+                const int at = (id + k * kWG) * VE;
                 ok[k] = at < n ? mask[at >> 5] : 0u;
             }
         } else {
@@ -204,16 +215,18 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
     masks(r0, ok);
     masks(r0 + 1, ok1);
     request(r0, ok, now);
+    int held = -1;                                            // trees: the way that the table holds
     for (int r = r0; r < r1; ++r) {
         request(r + 1, ok1, next);
         masks(r + 2, ok2);
-        bool mine = false;
         if constexpr (TREE) {
-            mine = (wayed[(r - r0) >> 5] >> ((r - r0) & 31)) & 1u;
-            if (mine) {
+            const int last = P.target ? r - 1 : __builtin_amdgcn_readfirstlane(up[r]);   // (the same for every thread)
+            const int to = last < 0 ? -1 : __builtin_amdgcn_readfirstlane(near[last]);
+            if (to != held) {
                 meet();
-                along(r, 1u);
+                if (tid == 0) move(held, to);
                 meet();
+                held = to;
             }
         } else if (r > r0) {                                  // (uniform: every thread reads the same token)
             unsigned at;
@@ -268,11 +281,6 @@ __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionPar
             now[k] = next[k];
             ok[k] = ok1[k];
             ok1[k] = ok2[k];
-        }
-        if (TREE && mine) {
-            meet();
-            along(r, 0xFFFFFFFFu);                            // (adds -1)
-            meet();
         }
     }
 }

@@ -87,7 +87,7 @@ int condition(const void* logits, const int32_t* tokens, const int32_t* parent, 
     if (grid > kMaxGroups) return FSD_ERR_SHAPE;
     P.side = c.bias_count < P.slice ? c.bias_count : P.slice;
     size_t lds = lds_of(P.slice);
-    if (tree) lds += (static_cast<size_t>(P.rows_per_wg) / 32 + 1) * 4 + static_cast<size_t>(N) * 4;
+    if (tree) lds += static_cast<size_t>(N) * 6;
     // Past the caches where the logits are more than these hold and lines are written whole: 64 sequences of 9 rows of 128256 bfloat16
     // entries 77 -> 73 us; but 48 of 17 rows of 128259 binary32 entries 203 -> 207, and a small call's reader finds its rows in the caches.
     const bool stream = bytes >= (64u << 20) && V * es % 16 == 0 && aligned16(logits) && aligned16(out);

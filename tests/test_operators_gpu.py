@@ -1313,3 +1313,48 @@ def test_attend_each_report_alone(tree):
         a = dict(rotation=rotation, row_count=torch.from_numpy(counts).cuda())
         got = fsd.fsd_attend_tree(q, k, v, torch.from_numpy(parent).cuda(), cache, **a) if tree else fsd.fsd_attend_chain(q, k, v, cache, **a)
         assert got["row_status"].tolist() == [more.get(b, s) for b, s in enumerate(reports)], rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("few", [3, 9001])
+def test_condition_deep_trees(dtype, few):
+    """More nodes than a workgroup has threads, on paths as long: a chain in tree form, several chains whose nodes come in turn, and the same with the tokens in
+    one slice or spread over all.  Each chain's rows are those of the chain call, bit for bit."""
+    rng = np.random.default_rng(few)
+    B, N, V = 3, 612, 9001
+    z = torch.from_numpy(rng.standard_normal((B, N + 1, V)).astype(np.float32)).to(DT[dtype]).cuda()
+    tokens = torch.from_numpy(rng.integers(0, few, (B, N)).astype(np.int32)).cuda()
+    c = fsd.Conditions(frequency=torch.full((B,), 0.03, device="cuda"), presence=torch.full((B,), 0.25, device="cuda"), repetition=torch.full((B,), 1.5, device="cuda"),
+                       history=torch.from_numpy(rng.integers(0, V, (B, 40)).astype(np.int32)).cuda())
+    for chains in (1, 2, 3, 17):
+        parent = torch.arange(-chains, N - chains, dtype=torch.int32, device="cuda").clamp(min=-1).expand(B, N).contiguous()
+        target = fsd.fsd_condition_tree(z, tokens, parent, c)["out"]
+        draft = fsd.fsd_condition_tree(z[:, 1:].contiguous(), tokens, parent, c)["out"]
+        for i in range(chains):
+            mine = torch.arange(i, N, chains, device="cuda")
+            want = fsd.fsd_condition_chain(torch.cat([z[:, :1], z[:, 1 + mine]], 1), tokens[:, mine].contiguous(), c)["out"]
+            assert torch.equal(target[:, 1 + mine], want[:, 1:]) and torch.equal(target[:, :1], want[:, :1]), (chains, i)
+            want = fsd.fsd_condition_chain(z[:, 1 + mine].contiguous(), tokens[:, mine].contiguous(), c)["out"]
+            assert torch.equal(draft[:, mine], want), (chains, i)
+
+
+def test_condition_a_chain_in_tree_form_costs_like_a_chain():
+    """2048 candidates, all of one token: a row adds what the row before lacks, not its whole way.  (1.6 times the chain call; the whole way each time: 100.)"""
+    B, N, V = 8, 2048, 32000
+    z = torch.randn(B, N + 1, V, device="cuda").to(torch.bfloat16)
+    tokens = torch.full((B, N), 7, dtype=torch.int32, device="cuda")
+    parent = torch.arange(-1, N - 1, dtype=torch.int32, device="cuda").expand(B, N).contiguous()
+    c, out = fsd.Conditions(frequency=torch.full((B,), 0.1, device="cuda")), dict(out=torch.empty_like(z))
+
+    def time_of(run):
+        run()
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(3):
+            run()
+        end.record()
+        torch.cuda.synchronize()
+        return start.elapsed_time(end)
+
+    chain, tree = time_of(lambda: fsd.fsd_condition_chain(z, tokens, c, out=out)), time_of(lambda: fsd.fsd_condition_tree(z, tokens, parent, c, out=out))
+    assert tree < 10 * chain, f"{tree / 3:.2f} ms a call, the chain call {chain / 3:.2f}"
