@@ -97,6 +97,8 @@ class Conditions:
                 _check(t, name, (B, *t.shape[1:]), dtype, dev)
         if bias_tokens is not None and bias_tokens.shape != bias_values.shape:
             raise ValueError("bias_tokens and bias_values differ in shape")
+        if allowed is not None and allowed.shape[1] == 0:
+            raise ValueError("allowed has no context")       # (and no memory: it would count as absent)
         self._held = given
         self.words = allowed.shape[2] if allowed is not None else None
         self.contexts = allowed.shape[1] if allowed is not None else 0

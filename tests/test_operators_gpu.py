@@ -1358,3 +1358,9 @@ def test_condition_a_chain_in_tree_form_costs_like_a_chain():
 
     chain, tree = time_of(lambda: fsd.fsd_condition_chain(z, tokens, c, out=out)), time_of(lambda: fsd.fsd_condition_tree(z, tokens, parent, c, out=out))
     assert tree < 10 * chain, f"{tree / 3:.2f} ms a call, the chain call {chain / 3:.2f}"
+
+
+def test_a_mask_without_contexts_is_refused():
+    """It holds nothing, so its address is none, which means that there is no mask."""
+    with pytest.raises(ValueError):
+        fsd.Conditions(allowed=torch.zeros((2, 0, 4), dtype=torch.int32, device="cuda"))
