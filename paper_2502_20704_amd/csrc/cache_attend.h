@@ -907,6 +907,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attend_rows(AttendParams P) {
                     }
                     l[rt] += column_sum(sum);
                 }
+                most_vs = __builtin_inff();                   // (any unit may have been among them: tiles behind this one are summed without theirs, too)
             };
             // weights and sums of tile `tile`, whose keys lie at `keys` and whose values come when values() is called
             auto one_tile = [&](int tile, auto keys, auto values) {
@@ -1325,7 +1326,7 @@ __global__ __launch_bounds__(kWG, 2) void attend_few(AttendParams P) {
             for (int k = 0; k < 2 * kV; ++k) v[k] = *reinterpret_cast<const half8_t*>(values + k * 1024);
             float4_t ks = *reinterpret_cast<const float4_t*>(P.key_scale + bht * kBlock + g * 16 + 4 * wave);
             const unsigned spoilt = static_cast<unsigned>(P.broken[bht] >> (16 * g + 4 * wave)) & 15u;
-            const int one_lift = P.value_lift[bht];
+            const int one_lift = P.value_lift[bht];                                 // (the same for everyone, and so is the way taken below, with its barriers)
 #pragma unroll
             for (int i = 0; i < 4; ++i) ks[i] = spoilt >> i & 1u ? __builtin_nanf("") : ks[i];   // (of those a row sees every weight is NaN then)
             float4_t s[RT];

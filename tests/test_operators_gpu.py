@@ -1364,3 +1364,26 @@ def test_a_mask_without_contexts_is_refused():
     """It holds nothing, so its address is none, which means that there is no mask."""
     with pytest.raises(ValueError):
         fsd.Conditions(allowed=torch.zeros((2, 0, 4), dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("B", [1, 100])
+@pytest.mark.parametrize("heads,H,D,dtype", [(2, 2, 64, "bf16"), (2, 1, 128, "bf16"), (1, 1, 256, "bf16"), (1, 1, 64, "f16"), (4, 2, 128, "f16")])
+@pytest.mark.parametrize("order", [(0, 1, 2), (1, 0, 2), (2, 1, 0)])
+def test_attend_tiles_of_one_size_behind_tiles_of_many(B, heads, H, D, dtype, order):
+    """Three tiles of rows, one of them with values of very different sizes, the others with small ones: these add little to a row's result, but their weights
+    count like all others."""
+    rng = np.random.default_rng(D + order[0])
+    R, lens = 192, [0] * B
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, DT[dtype])
+    q, k, v = q.contiguous(), k.contiguous(), v.float().clamp(-1.0, 1.0)
+    spread = (-12, 14) if dtype == "f16" else (-60, 60)
+    sizes = np.concatenate([[np.full(64, spread[0]), rng.permutation(np.linspace(*spread, 64).astype(int)), np.full(64, spread[0] + 3)][i] for i in order])
+    v = (v * torch.from_numpy(np.exp2(sizes.astype(np.float64))).float().cuda()[None, :, None, None]).to(DT[dtype])
+    got = fsd.fsd_attend_chain(q, k, v, _to_cache(c, table, lens))["out"]
+    some = [0] if B == 1 else [0, 1, 50, 99]
+    want, bound = ref.attend(_host(q[some]), _host(k[some]), _host(v[some]), None, np.full(len(some), R), c, 0, [lens[b] for b in some], table[some], D ** -0.5, None,
+                             True, DT[dtype])
+    if dtype == "f16":
+        bound = bound + 2.0 ** -25                              # half of the distance of binary16's numbers under 2^-14, which results here are
+    for rows in (slice(0, 64), slice(64, 128), slice(128, 192)):
+        _within(got[some][:, rows], want[:, rows], bound[:, rows], str(rows))
