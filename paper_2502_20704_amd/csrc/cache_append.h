@@ -6,9 +6,10 @@
 //
 // A block of a head is one piece of work: nothing is shared between two of them, so they need not agree on anything.  Its new keys
 // are in registers when their largest magnitude is known, and are then written as codes; so are its new values.
-// Measured: the accepted rows of 64 trees, 8 key heads of 128, 32 layers: 44 us for 140 MB of traffic (the codes of a dimension's 16 tokens
+// Measured: the accepted rows of 64 trees, 8 key heads of 128, 32 layers: 44 us for 148 MB of traffic (the codes of a dimension's 16 tokens
 // lie together, so values are read and written 2 KB at a time; without that, 50 MB), in pieces of 128 bytes to 2 KB all over 1.6 GB: neither more
-// wavefronts a compute unit (6 in place of 4: 49 us) nor a sequence's heads in one XCD (47) change that.  24576 prompt tokens: 55 us for 151 MB.
+// wavefronts a compute unit (6 in place of 4: 49 us) nor a sequence's heads in one XCD (47) change that.  24576 prompt tokens: 56 us for 252 MB, 4.5 TB/s:
+// of the 201 read 100 are keys and values, the rest the rotation's table, as a block's heads lie on all eight XCDs and each fetches its rows.
 //   append_few   a step's accepted rows (at most 16): a wavefront for a head's keys and one for its values, which take the blocks they touch (one, seldom
 //                two) in turn
 //   append_many  a prompt's: a workgroup a block and head

@@ -21,18 +21,22 @@
 // follows only where the maximum is more than 15 above it: a rescaling of O' is rare.  A block whose value scale is far below one before
 // it (values that are all zero have the smallest scale there is) may add nothing to O' and yet much to the sum: there the sum takes exp2(s - m) itself.
 //
+// The rows' own values are held in binary16 in units of that kind: of a tile of 64 rows, or of each row where the rows of a tile differ in size by more
+// than 2^6, as a result must not lose bits beside values that its row does not see.
+//
 // Kernels: attend_prepare turns queries and the rows' keys, brings them and the rows' values into binary16's range by powers of two and lays them
 // out in the workspace as the matrix instruction takes them, so that no piece of the work does this again; it deals out the work, which takes the
 // lengths, and reports the sequences.  attend_few (few rows a key head) or attend_rows is the pass over cache and rows: every workgroup gets the same number of
 // blocks, whichever sequences and heads they belong to.  attend_join puts together what lies across the border of two workgroups.
 //
 // Measured (us; e4m3 cache, head_dim 128, 8 key heads and 32 heads unless said, bfloat16):
-//   1 sequence of 2048 tokens, 1 row             prepare  4.9  few    7  join  3   three kernels' starts and ends, each one chain of requests
-//   64 of up to 8192, 9 rows                             13.5        146        7.5 memory and the barrier a block: 4.2 TB/s of a read's 5.8
-//   2 of up to 131072, 5 rows, 28 on 4, binary16           8.5         62        6   the same, 4.0 TB/s; products twice, in two parts
-//   32 of up to 4096, trees of 61 rows                   18    rows  131       14.5 vector instructions and products, which hardly overlap: 30 and 40 % of
-//                                                                                 the time; with 244 of 256 rows in use, 580 TFLOP/s
-//   3 of up to 7000, 1000 rows, 16 on 16, head_dim 64    11           85        7.5 vector instructions: an exponential for 256 operations of the products
+//   1 sequence of 2048 tokens, 1 row             prepare  5.2  few    8  join  4   three kernels' starts and ends, each one chain of requests
+//   64 of up to 8192, 9 rows                             14          147        7.5 memory and the barrier a block: 4.2 TB/s of a read's 5.8
+//   2 of up to 131072, 5 rows, 28 on 4, binary16           8.7         63        6   the same, 4.0 TB/s; products twice, in two parts
+//   32 of up to 4096, trees of 61 rows                   18.5  rows  132       14.5 a wavefront's chain of products, weights and sums, one block after the other:
+//                                                                                 the matrix unit works 34 % of the time, vector instructions 52 %; with
+//                                                                                 244 of 256 rows in use, 580 TFLOP/s
+//   3 of up to 7000, 1000 rows, 16 on 16, head_dim 64    11.7         81-98     7.5 the same, 25 and 55 %
 #ifndef FSD_CSRC_CACHE_ATTEND_H_
 #define FSD_CSRC_CACHE_ATTEND_H_
 

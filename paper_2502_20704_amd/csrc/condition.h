@@ -10,9 +10,9 @@
 // the contexts contain one another and each row adds one candidate; in a tree a row takes away and adds what its way and that of the row before
 // do not share, of tokens in the slice only (most rows: nothing).  No row keeps another one waiting otherwise: there is no barrier between them.
 //
-// What bounds it is memory: 64 x 9 rows of 128256 bfloat16 entries 70 us (4.2 TB/s read and written; a copy of that size 58), 32 trees of 60 rows under
-// a mask each 185 (5.4 TB/s if all were read; slots without an allowed entry are not), 48 x 17 rows of 128259 binary32 entries with histories of 32768
-// 200 (4.2 TB/s).  One row of 32000: 4.5 us, a kernel's start and its two round trips, history and row.
+// What bounds it is memory: 64 x 9 rows of 128256 bfloat16 entries 71 us (4.2 TB/s read and written; a copy of that size 58), 32 trees of 60 rows under
+// a mask each 186 (of 492 MB 291 are read, as slots without an allowed entry are not: 4.2 TB/s), 48 x 17 rows of 128259 binary32 entries with histories of
+// 32768 201 (4.2 TB/s).  One row of 32000: 4.5 us, a kernel's start and its two round trips, history and row.
 // Deep trees: one thread walks between two rows' ways, so numbering that keeps neighbours' ways alike is cheap.  8 sequences of 2048 candidates and 32000
 // bfloat16 entries, as a chain 600 us, as a tree that is a chain 820, random parents 620, but two chains whose nodes come in turn 10450.
 #ifndef FSD_CSRC_CONDITION_H_
@@ -51,7 +51,8 @@ __device__ __forceinline__ float conditioned(float z, unsigned word, float r, fl
 }
 
 // Wavefronts a SIMD: bfloat16 has LDS for 4 workgroups a compute unit; binary32 tables are half as large, and 6 of them take 48 sequences of
-// 17 rows of 128259 entries 203 us where 5 take 242 (1536 workgroups: one round in place of 1.2).
+// 17 rows of 128259 entries 203 us where 5 take 242 (1536 workgroups: one round in place of 1.2).  That leaves binary32 80 registers, two short: they are
+// spilled before the loop over rows and read again once a row.
 template <bool BF16, bool TREE, bool STREAM>
 __global__ __launch_bounds__(kWG, BF16 ? 4 : 6) void condition_rows(ConditionParams P) {
     constexpr int VE = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;

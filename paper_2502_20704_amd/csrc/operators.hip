@@ -148,14 +148,16 @@ void launch_append_d(hipStream_t st, const AppendParams& P, int tokens) {
 // attend_rows.  Twice the rows an item (8 wavefronts, 256 workgroups): 162 us as well for trees of 244 rows, 115 in place of 110 for a prompt's 1000.
 struct AttendShape { int rt, tile, workers; bool few; };
 constexpr int rows_waves(int head_dim) { return head_dim == 256 ? 8 : 4; }   // of attend_rows: 16 sequences of 256 rows at head_dim 256 62 us with 8, 68 with 4
-constexpr int rows_tiles(int head_dim) { return head_dim == 256 ? 1 : 2; }   // of 16 rows, of each of them
+// Tiles of 16 rows of each of them: at head_dim 128 and 256 what registers hold beside the sums; at 64 they would hold more, which is not measured.
+constexpr int rows_tiles(int head_dim) { return head_dim == 256 ? 1 : 2; }
 AttendShape attend_shape(long rows, int head_dim, int dtype) {
     AttendShape s;
     const long tiles = (rows + 15) / 16;
     s.few = tiles <= (head_dim == 256 ? 2 : 4) - (dtype == FSD_F16 ? 1 : 0);
     s.rt = s.few ? static_cast<int>(tiles) : rows_tiles(head_dim);
     s.tile = 16 * s.rt * (s.few ? 1 : rows_waves(head_dim));
-    // as many workgroups as the 256 compute units hold at once
+    // Two workgroups for each of the 256 compute units, or one of eight wavefronts: what their registers and LDS hold at once at head_dim 128 and 256.  (At
+    // 64 three of most kinds would fit, and four of the smallest; not measured.)
     s.workers = s.few || head_dim != 256 ? 512 : 256;
     return s;
 }
