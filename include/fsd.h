@@ -469,6 +469,7 @@ int fsd_cache_append(const void* k, const void* v, int64_t token_stride, int B, 
  * enter them with the 11 significant bits of binary16 (scaled so that they stay in its range; FSD_F16's queries and keys, which may use
  * all 11, in two parts), the codes exactly; statistics are binary32, the result is rounded once.  Magnitudes of values up to
  * 2^120 and value scales from 2^-100 to 2^111 are in range.  A NaN among the keys or codes a row sees makes its outputs NaN, and so does
+ * an infinite query or key of FSD_F16 (of FSD_BF16 its products' signs decide: a score of -inf is a weight of 0), or
  * a value among the rows that is not finite (all head_dim outputs of the heads that read it); what a row does not see
  * changes its result by a rounding at most, whatever it holds.
  * 1 <= R <= 2049, 1 <= heads / kv_heads <= 64, heads <= 1024, B <= 65535, B * R < 2^24.

@@ -1387,3 +1387,81 @@ def test_attend_tiles_of_one_size_behind_tiles_of_many(B, heads, H, D, dtype, or
         bound = bound + 2.0 ** -25                              # half of the distance of binary16's numbers under 2^-14, which results here are
     for rows in (slice(0, 64), slice(64, 128), slice(128, 192)):
         _within(got[some][:, rows], want[:, rows], bound[:, rows], str(rows))
+
+
+@pytest.mark.parametrize("R,heads", [(6, 4), (80, 4)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attend_infinite_queries_and_keys(R, heads, dtype):
+    """Bfloat16: the sign of a product decides (-inf: no weight; +inf: NaN).  Binary16, in two parts: NaN for rows that see it.  Rows that do not see it are
+    left bit for bit."""
+    rng = np.random.default_rng(R)
+    lens, H, D, at = [100], 2, 128, 3
+    table, c, q, k, v = _case(rng, lens, R, heads, H, D, DT[dtype])
+    q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    q[0, :, :, 7] = torch.where(torch.arange(R, device="cuda")[:, None] % 2 == 0, 1.0, -1.0).to(q.dtype)
+    cache = _to_cache(c, table, lens)
+    clean = fsd.fsd_attend_chain(q, k, v, cache)["out"].clone()
+    for x in (float("inf"), -float("inf")):
+        bad = k.clone()
+        bad[0, at, 1, 7] = x
+        got = fsd.fsd_attend_chain(q, bad, v, cache)["out"]
+        assert torch.equal(got[0, :at], clean[0, :at]) and torch.equal(got[0, :, :2], clean[0, :, :2])
+        for r in range(at, R):
+            if dtype == "f16" or (r % 2 == 0) == (x > 0):
+                assert torch.isnan(got[0, r, 2:]).all(), (x, r)
+        if dtype == "bf16":                                     # those rows as if the token were not there: values of any size in its place
+            gone = k.clone()
+            gone[0, at, 1] = 0
+            gone[0, at, 1, 7] = np.sign(x) * 2.0 ** 100
+            want = fsd.fsd_attend_chain(q, gone, v, cache)["out"]
+            rows = [r for r in range(at, R) if (r % 2 == 0) != (x > 0)]
+            assert torch.isfinite(got[0, rows]).all() and torch.equal(got[0, rows], want[0, rows])
+        bad = q.clone()
+        bad[0, at, 3, 7] = x
+        got = fsd.fsd_attend_chain(bad, k, v, cache)["out"]
+        assert torch.isnan(got[0, at, 3]).all()
+        got[0, at, 3] = clean[0, at, 3]
+        assert torch.equal(got, clean)
+
+
+def test_condition_rows_beyond_32_bits():
+    """4.3 GB of logits, in place: the rows at the end are conditioned like those of a small call."""
+    N, V = 2048, 524288
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("not enough device memory")
+    z = torch.zeros((1, N + 1, V), device="cuda")
+    tail = torch.randn((1, 3, V), device="cuda")
+    z[:, -3:] = tail
+    tokens = torch.zeros((1, N), dtype=torch.int32, device="cuda")
+    tokens[0, -2:] = torch.tensor([V - 1, 77], device="cuda").int()
+    c = fsd.Conditions(frequency=torch.full((1,), 0.5, device="cuda"), history=torch.tensor([[V - 2, 5]], dtype=torch.int32, device="cuda"))
+    fsd.fsd_condition_chain(z, tokens, c, out=dict(out=z))
+    want = tail.clone()
+    want[0, :, 0] -= 0.5 * torch.tensor([N - 2, N - 2, N - 2], device="cuda")
+    want[0, 1:, V - 1] -= 0.5
+    want[0, 2, 77] -= 0.5
+    want[0, :, V - 2] -= 0.5
+    want[0, :, 5] -= 0.5
+    assert torch.equal(z[:, -3:], want)
+
+
+def test_tokens_beyond_32_bits():
+    """Queries, keys and values whose elements lie beyond what 32 bits count: parts of a projection with 2^22 elements a token."""
+    R, step, H, D = 1100, 1 << 22, 2, 64
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("not enough device memory")
+    rng = np.random.default_rng(60)
+    whole = torch.empty((1, R, step), dtype=torch.bfloat16, device="cuda")
+    table, c, *_ = _case(rng, [70], 1, 4, H, D, torch.bfloat16, extra=20)
+    x = torch.from_numpy(rng.standard_normal((1, R, 8, D)) * 0.7).to(torch.bfloat16).cuda()
+    whole[:, :, -8 * D:] = x.flatten(2)
+    far = whole[:, :, -8 * D:].unflatten(2, (8, D))
+    caches = [_to_cache(c, table, [70]) for _ in range(2)]
+    got = [fsd.fsd_attend_chain(t[:, :, :4], t[:, :, 4:6], t[:, :, 6:], cache)["out"] for t, cache in zip((x, far), caches)]
+    assert torch.equal(*got)
+    for count in (9, R):
+        for t, cache in zip((x, far), caches):
+            a = fsd.fsd_cache_append(t[:, -count:, 4:6], t[:, -count:, 6:], cache, torch.tensor([count - 1], dtype=torch.int32, device="cuda"))
+            assert a["row_status"].tolist() == [0]
+        for n in ("k_codes", "v_codes", "k_scale", "v_scale"):
+            assert torch.equal(getattr(caches[0], n), getattr(caches[1], n)), n
