@@ -1465,3 +1465,33 @@ def test_tokens_beyond_32_bits():
             assert a["row_status"].tolist() == [0]
         for n in ("k_codes", "v_codes", "k_scale", "v_scale"):
             assert torch.equal(getattr(caches[0], n), getattr(caches[1], n)), n
+
+
+def test_a_captured_call_on_a_forked_stream():
+    """`stream` during a capture: outputs and workspace come from the graph's memory, and every replay gives the eager result."""
+    rng = np.random.default_rng(70)
+    table, c, q, k, v = _case(rng, [300, 5], 9, 8, 2, 64, torch.bfloat16)
+    cache, z = _to_cache(c, table, [300, 5]), torch.randn(2, 9, 5000, device="cuda")
+    tokens = torch.randint(0, 5000, (2, 8), dtype=torch.int32, device="cuda")
+    conditions = fsd.Conditions(frequency=torch.full((2,), 0.5, device="cuda"))
+
+    def run(stream):
+        return fsd.fsd_attend_chain(q, k, v, cache, stream=stream)["out"], fsd.fsd_condition_chain(z, tokens, conditions, stream=stream)["out"]
+
+    want = [t.clone() for t in run(None)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    run(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        side.wait_stream(torch.cuda.current_stream())
+        got = run(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        for t in got:
+            t.fill_(7.0)
+        junk = torch.randn(1 << 20, device="cuda").sum()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.isfinite(junk) and all(torch.equal(a, b) for a, b in zip(got, want)), i
