@@ -92,7 +92,8 @@ enum {
     FSD_ROW_TOO_DEEP = 4,   /* tree: a node deeper than max_depth */
     FSD_ROW_BAD_TOKEN = 8,  /* strict SD: candidate token id outside [0, V) */
     FSD_ROW_INTERNAL = 16,  /* a bounded device-side wait expired (never expected) */
-    FSD_ROW_BAD_CACHE = 32  /* cache calls: a length, block number, path node or position outside its range */
+    FSD_ROW_BAD_CACHE = 32, /* cache calls: a length, block number, path node or position outside its range */
+    FSD_ROW_NO_BLOCKS = 64  /* fsd_cache_fork: the cache has too few free blocks */
 };
 
 /* Limits: 1 <= V <= fsd_max_vocab(dtype) (524288 for both dtypes); 1 <= K, N,
@@ -489,6 +490,122 @@ int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_strid
                     const int32_t* parent, int B, int R, int heads, int dtype, const int32_t* row_count, float scale,
                     const fsd_rotation* rotation, const fsd_cache* cache, int layer, void* out, int32_t* row_status,
                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Around drafting: the continuations that a drafter proposes, or a beam search
+ * keeps, and what follows them.  A step is fsd_beam_select on the logits of a
+ * sequence's contexts (a tree's level, or a search's beams), then, for states,
+ * fsd_beam_reorder, and for the paged cache fsd_cache_fork with the selection's
+ * parents (as rows of the table).  fsd_cache_fork is also what a serving loop
+ * calls where sequences begin, end, are rolled back or need room.
+ *
+ * The conventions are those of the calls around a verify call; workgroups never
+ * wait for one another.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * The n best continuations of each sequence's beams.  With z the logits of beam w,
+ *
+ *   s(w, v) = scores[w] + z_v - log sum_u exp(z_u)     for v in [0, V) with z_v > -inf
+ *   s(w, -1) = scores[w]                               of a finished beam (done[w] != 0), its only continuation
+ *   ranked by s * weights[w], largest first; of equal ranks the lowest w, then the largest z, then the lowest v
+ *
+ * Normalisers, scores and ranks are held in binary64 (relative error of a row's sum of exponentials under 2^-33); scores_out is rounded once
+ * (a score below binary32's range, to -inf).
+ *
+ *   logits  [B, beams, V]  FSD_F32 or FSD_BF16, row_stride elements from one beam's row to the next (>= V, at most 2^32)
+ *   scores  [B, beams]     -inf: the beam does not count, and its row is not read; NULL: 0
+ *   weights [B, beams]     > 0 and finite, e.g. a power of the length that a continuation has; NULL: 1
+ *   done    [B, beams]     finished beams, whose rows are not read; NULL: none
+ *   scores_out [B, n], parent [B, n], tokens [B, n]   out: s, w and v (-1 for a finished beam); -inf, -1 and -1 behind the last continuation
+ *                          where there are fewer than n
+ *   row_status [B]         out  optional: FSD_ROW_NONFINITE where a row that is read holds NaN or +inf, or a beam that counts has
+ *                          such a score or a weight that is not positive and finite: the sequence has no continuations then.  (A row that is -inf
+ *                          everywhere is none of that: a grammar that has ended a beam.)
+ *   workspace              fsd_beam_workspace_bytes(...) bytes, 256-byte aligned
+ * No output shares a byte with another one, scores, weights, done or the workspace (FSD_ERR_LAYOUT).
+ * 1 <= beams <= 256, 1 <= n <= 128, V <= fsd_max_vocab(dtype), B <= 65535, B * beams * ceil(V / 16384) < 2^24 (FSD_F32: V / 8192).
+ */
+size_t fsd_beam_workspace_bytes(int B, int beams, int V, int n, int dtype);
+int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores, const float* weights, const int32_t* done, int B,
+                    int beams, int V, int dtype, int n, float* scores_out, int32_t* parent, int32_t* tokens, int32_t* row_status,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * States in the order of the continuations: out[l, b, i] = states[l, b, parent[b, i]], zeros where parent is -1.
+ *
+ *   states [layers, B, beams, row_bytes]   bytes of any type, on any address; out [layers, B, n, row_bytes], no overlap with states
+ *   parent [B, n]                          as fsd_beam_select gives it
+ *   row_status [B] out  optional: FSD_ROW_BAD_PARENT where a parent is outside [-1, beams) (its rows are zeros); no overlap with parent or out
+ * 1 <= layers, beams, n, B <= 65535, layers * B * max(beams, n) < 2^31, row_bytes from 1 to 2^40.
+ */
+int fsd_beam_reorder(const void* states, const int32_t* parent, int layers, int B, int beams, int n, size_t row_bytes, void* out,
+                     int32_t* row_status, void* hip_stream);
+
+/*
+ * New sequences that continue old ones: beams that are kept, once or more than once; a prompt that several answers go out from; or the
+ * same sequences with candidates rolled back, room for the next step, some ended and others begun.  The n new sequences take the place of the B
+ * old ones (those of `cache`): what no new one keeps is free again.  A sequence that goes on is its own parent.
+ *
+ *   refs [num_blocks]     for every block the number of places of block tables that name it, these and any others (a stored prompt's, another
+ *                         batch's); 0: free
+ *   parent [n]            the old sequence that new sequence i continues; -1: none, it begins empty
+ *   lengths [n]           tokens of it that are kept, in [0, cache_len[parent]]; NULL: all.  (Without a parent: none.)
+ *   room [n]              tokens that will be appended before the next call: the blocks they need are there; NULL: 0
+ *   block_table_out [n, max_blocks], cache_len_out [n], refs_out [num_blocks]   out: the same of the new sequences.  refs_out may be refs, else no
+ *                         output shares a byte with an input or another output (FSD_ERR_LAYOUT)
+ *   free_blocks [1]       out  optional: blocks free afterwards; negative: how many were lacking
+ *   row_status [n]        out  optional
+ *
+ * A table's entry that is negative names nothing.  With have = lengths[i] tokens, full = have / 64 and need = ceil((have + room[i]) / 64):
+ *   - places < full share the parent's blocks;
+ *   - a place from full to need - 1 keeps its parent's block if no other place will name that: none of other tables (refs less the old sequences' places
+ *     is 0), none of the new sequences' first `full`, and of the other places that want to keep it this is the lowest (sequence, place);
+ *   - all else gets free blocks, the lowest numbers first, in order of (sequence, place).  (A block that only ended sequences held is free.)
+ *     Place `full`, if the sequence has tokens in it (have % 64), is copied there from its parent's, in all layers: the scales, and the groups of 16
+ *     tokens that hold any;
+ *   - places from need on are -1.
+ * Appending to the new sequences then touches no block that another place names.
+ *
+ * FSD_ROW_BAD_PARENT: parent outside [-1, B).  FSD_ROW_BAD_CACHE: cache_len, lengths or room outside its range (have + room at most 64 * max_blocks), or a
+ * place of the parent's that holds some of its first `have` tokens names no block.  Such a sequence comes out empty.  FSD_ROW_NO_BLOCKS, for all of them: there are too few
+ * free blocks; nothing is copied, refs_out is refs and every sequence comes out empty, so that the caller, who still has the old tables, can make room and call again.
+ * Blocks of reserved places may hold anything.  The copied codes' cache is that of `cache` (written in place).
+ * n, B <= 65535, n * max_blocks < 2^31 - 1, num_blocks <= 2^24.
+ */
+size_t fsd_cache_fork_workspace_bytes(int num_blocks, int n);
+int fsd_cache_fork(const fsd_cache* cache, int B, const int32_t* refs, const int32_t* parent, const int32_t* lengths, const int32_t* room, int n,
+                   int32_t* block_table_out, int32_t* cache_len_out, int32_t* refs_out, int32_t* free_blocks, int32_t* row_status,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Pages from one cache to another, or within one: block src_blocks[k] of `src` becomes block dst_blocks[k] of `dst`, in all layers: the scales, and
+ * the groups of 16 tokens that hold any of its first tokens[k] (0 .. 64; NULL: all).  The caches have the same layers, kv_heads and head_dim; they are one cache (all four arrays)
+ * or share none (FSD_ERR_LAYOUT).  Their tables and lengths are not looked at.
+ *
+ *   page_status [n] out  optional: FSD_ROW_BAD_CACHE where a block or tokens is out of range, which copies nothing.  A block of -1 copies nothing either,
+ *                   and is no error
+ * The order of pages is not given: a block that is written twice, or written and read, holds parts of any of them.
+ * n >= 1; n * layers * kv_heads < 2^40.
+ */
+int fsd_cache_copy(const fsd_cache* src, const fsd_cache* dst, const int32_t* src_blocks, const int32_t* dst_blocks, const int32_t* tokens, int n,
+                   int32_t* page_status, void* hip_stream);
+
+/*
+ * A cache's pages moved together: with U blocks in use (refs > 0), those numbered U and up move to the free blocks below U, the lowest to the lowest, in all
+ * layers and whole.  Afterwards blocks 0 .. U-1 are in use and the rest is free.
+ *
+ *   refs [num_blocks]             as in fsd_cache_fork
+ *   block_table_out [B, max_blocks] out: the table with the new numbers; -1 where it names nothing or a free block.  May be the cache's own table
+ *   refs_out [num_blocks]         out  may be refs
+ *   remap [num_blocks]            out  optional: a block's new number, -1 of a free one (for tables of others)
+ *   used_blocks [1]               out  optional: U
+ *   row_status [B]                out  optional: FSD_ROW_BAD_CACHE where a table's row names a free block or one outside [0, num_blocks)
+ * Otherwise no output shares a byte with an input or another output (FSD_ERR_LAYOUT).  num_blocks <= 2^24, B <= 65535.
+ */
+size_t fsd_cache_compact_workspace_bytes(int num_blocks);
+int fsd_cache_compact(const fsd_cache* cache, int B, const int32_t* refs, int32_t* block_table_out, int32_t* refs_out, int32_t* remap,
+                      int32_t* used_blocks, int32_t* row_status, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------------------
  * Everything below is for tests, tuning and benchmarks, not for serving code.

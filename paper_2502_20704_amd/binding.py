@@ -96,6 +96,22 @@ def library() -> ctypes.CDLL:
         L.fsd_attend_chain.restype = i32
         L.fsd_attend_tree.argtypes = [vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, vp, f32, vp, vp, i32, vp, vp, vp, sz, vp]
         L.fsd_attend_tree.restype = i32
+        L.fsd_beam_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.fsd_beam_workspace_bytes.restype = sz
+        L.fsd_beam_select.argtypes = [vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.fsd_beam_select.restype = i32
+        L.fsd_beam_reorder.argtypes = [vp, vp, i32, i32, i32, i32, sz, vp, vp, vp]
+        L.fsd_beam_reorder.restype = i32
+        L.fsd_cache_fork_workspace_bytes.argtypes = [i32, i32]
+        L.fsd_cache_fork_workspace_bytes.restype = sz
+        L.fsd_cache_fork.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.fsd_cache_fork.restype = i32
+        L.fsd_cache_copy.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp]
+        L.fsd_cache_copy.restype = i32
+        L.fsd_cache_compact_workspace_bytes.argtypes = [i32]
+        L.fsd_cache_compact_workspace_bytes.restype = sz
+        L.fsd_cache_compact.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.fsd_cache_compact.restype = i32
         L.fsd_profile_enable.argtypes = [i32]
         L.fsd_profile_enable.restype = i32
         L.fsd_profile_collect.argtypes = [vp, vp]

@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "fsd_kernels.hip")
 SRC_OPERATORS = os.path.join(HERE, "csrc", "operators.hip")   # the operators around a verify call
+SRC_DRAFTING = os.path.join(HERE, "csrc", "drafting.hip")     # the operators around drafting
 LIB = os.path.join(HERE, "libfsd.so")
 
 FLAGS = [
@@ -33,7 +34,7 @@ def build(verbose: bool = False, phase_timing: bool = False) -> str:
     more = ["-DFSD_PHASE_TIMING"] if phase_timing else []
     with tempfile.TemporaryDirectory() as tmp:
         jobs, objects = [], []
-        for src in (SRC, SRC_OPERATORS):   # side by side
+        for src in (SRC, SRC_OPERATORS, SRC_DRAFTING):   # side by side
             objects.append(os.path.join(tmp, os.path.basename(src) + ".o"))
             cmd = ["hipcc", *(f for f in FLAGS if f != "-shared"), *more, "-c", "-o", objects[-1], src]
             if verbose:

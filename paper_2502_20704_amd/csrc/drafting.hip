@@ -1,0 +1,352 @@
+// Host side and C ABI of the operators around drafting: the best continuations of beams and the states that follow them (beam_select.h), and the pages of
+// the 8-bit paged cache (cache_pages.h).  Kernels for gfx950 (MI355X).
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <limits.h>
+
+#include "fsd.h"
+
+#include "operators_common.h"
+#include "operators_host.h"
+#include "beam_select.h"
+#include "cache_pages.h"
+
+namespace {
+
+// parts of a workspace, one behind the other on 256-byte boundaries
+struct Space {
+    size_t bytes = 0;
+    size_t take(size_t n) {
+        const size_t at = bytes;
+        bytes = (bytes + n + 255) / 256 * 256;
+        return at;
+    }
+};
+inline bool workspace_fits(const void* workspace, size_t have, size_t need) {
+    return workspace && reinterpret_cast<uintptr_t>(workspace) % 256 == 0 && have >= need;
+}
+// runs of bytes; whether one of the first n_out meets another of them or one of the rest
+struct Run { const void* at; size_t bytes; };
+bool any_overlap(const Run* runs, int n_out, int n) {
+    for (int i = 0; i < n_out; ++i)
+        for (int k = i + 1; k < n; ++k)
+            if (overlap(runs[i].at, runs[i].bytes, runs[k].at, runs[k].bytes)) return true;
+    return false;
+}
+inline bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; }
+
+// ------------------------------------------------------------------------------------------ selection
+
+// How a row is cut: the larger the slices, the fewer entries their lists have; but a call of few rows wants workgroups on all compute units.
+struct BeamShape { int slots, len, S; };
+constexpr long kBeamWGs = 1024;
+bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
+    if (dtype != FSD_F32 && dtype != FSD_BF16) return false;
+    if (B < 1 || B > kMaxBatch || W < 1 || W > kBeamWidest || n < 1 || n > kBeamMost || V < 1 || V > fsd_max_vocab(dtype)) return false;
+    const int E = dtype == FSD_BF16 ? 8 : 4;
+    const long rows = static_cast<long>(B) * W;
+    s->slots = 8;
+    while (s->slots > 1 && rows * ((V + kWG * E * s->slots - 1) / (kWG * E * s->slots)) < kBeamWGs) s->slots /= 2;
+    const int most = kWG * E * s->slots, S = (V + most - 1) / most;
+    s->len = ((V + S - 1) / S + E - 1) / E * E;              // slices of one length, so that none of them is a remnant
+    s->S = (V + s->len - 1) / s->len;
+    return rows * s->S <= kMaxGroups;
+}
+struct BeamSpace { size_t stat, cand, count, bytes; };
+BeamSpace beam_space(const BeamShape& s, int B, int W, int n) {
+    Space a;
+    BeamSpace w;
+    const size_t lists = static_cast<size_t>(B) * W * s.S;
+    w.stat = a.take(lists * sizeof(double2));
+    w.cand = a.take(lists * n * sizeof(float2));
+    w.count = a.take(lists * sizeof(int));
+    w.bytes = a.bytes;
+    return w;
+}
+template <bool BF16>
+void launch_beam_slices(hipStream_t st, unsigned grid, int slots, const BeamParams& P) {
+    const dim3 g(grid), t(kWG);
+    if (slots == 1) hipLaunchKernelGGL((beam_slices<BF16, 1>), g, t, 0, st, P);
+    else if (slots == 2) hipLaunchKernelGGL((beam_slices<BF16, 2>), g, t, 0, st, P);
+    else if (slots == 4) hipLaunchKernelGGL((beam_slices<BF16, 4>), g, t, 0, st, P);
+    else hipLaunchKernelGGL((beam_slices<BF16, 8>), g, t, 0, st, P);
+}
+
+// ------------------------------------------------------------------------------------------ pages
+
+constexpr int kMostBlocks = 1 << 24;
+constexpr long kCopyWGs = 2048;        // workgroups that share the pages' bytes: 8 a compute unit
+
+PagesPair pages_pair(const fsd_cache& a, const fsd_cache& b) {
+    PagesPair p;
+    p.k_from = static_cast<const char*>(a.k_codes);
+    p.v_from = static_cast<const char*>(a.v_codes);
+    p.k_to = static_cast<char*>(b.k_codes);
+    p.v_to = static_cast<char*>(b.v_codes);
+    p.ks_from = a.k_scale;
+    p.vs_from = a.v_scale;
+    p.ks_to = b.k_scale;
+    p.vs_to = b.v_scale;
+    p.blocks_from = a.num_blocks;
+    p.blocks_to = b.num_blocks;
+    p.layers = a.layers;
+    p.heads = a.kv_heads;
+    p.head_bytes = kBlock * a.head_dim;
+    return p;
+}
+inline int chunks_of(int num_blocks) { return (num_blocks + kPagesChunk - 1) / kPagesChunk; }
+inline unsigned copy_groups(long units) { return static_cast<unsigned>(units < kCopyWGs ? units : kCopyWGs); }
+
+struct ForkSpace { size_t released, shared, claim, free_list, free_count, seq, fresh, copies, at, copy_seq, totals, bytes; };
+ForkSpace fork_space(int P, int n) {
+    Space a;
+    ForkSpace w;
+    const size_t blocks = static_cast<size_t>(P) * 4, seqs = static_cast<size_t>(n);
+    w.released = a.take(blocks);
+    w.shared = a.take(blocks);
+    w.claim = a.take(blocks);
+    w.free_list = a.take(blocks);
+    w.free_count = a.take(static_cast<size_t>(chunks_of(P)) * 4);
+    w.seq = a.take(seqs * sizeof(int4));
+    w.fresh = a.take(seqs * 4);
+    w.copies = a.take(seqs * 4);
+    w.at = a.take(seqs * sizeof(int2));
+    w.copy_seq = a.take(seqs * 4);
+    w.totals = a.take(12);
+    w.bytes = a.bytes;
+    return w;
+}
+struct CompactSpace { size_t used_count, number, from, to, count, totals, bytes; };
+CompactSpace compact_space(int P) {
+    Space a;
+    CompactSpace w;
+    const size_t half = (static_cast<size_t>(P) / 2 + 1) * 4;
+    w.used_count = a.take(static_cast<size_t>(chunks_of(P)) * 4);
+    w.number = a.take(static_cast<size_t>(P) * 4);
+    w.from = a.take(half);
+    w.to = a.take(half);
+    w.count = a.take(half);
+    w.totals = a.take(8);
+    w.bytes = a.bytes;
+    return w;
+}
+bool fork_sizes(int P, int n) { return P >= 1 && P <= kMostBlocks && n >= 1 && n <= kMaxBatch; }
+
+}  // namespace
+
+extern "C" {
+
+size_t fsd_beam_workspace_bytes(int B, int beams, int V, int n, int dtype) {
+    BeamShape s;
+    return beam_shape(B, beams, V, n, dtype, &s) ? beam_space(s, B, beams, n).bytes : 0;
+}
+
+int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores, const float* weights, const int32_t* done, int B, int beams, int V, int dtype,
+                    int n, float* scores_out, int32_t* parent, int32_t* tokens, int32_t* row_status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!logits || !scores_out || !parent || !tokens) return FSD_ERR_NULL;
+    if (dtype != FSD_F32 && dtype != FSD_BF16) return FSD_ERR_DTYPE;
+    BeamShape s;
+    if (!beam_shape(B, beams, V, n, dtype, &s)) return FSD_ERR_SHAPE;
+    const size_t es = dtype == FSD_BF16 ? 2 : 4, in = static_cast<size_t>(B) * beams * 4, out = static_cast<size_t>(B) * n * 4;
+    if (row_stride < V || row_stride > (1L << 32) || reinterpret_cast<uintptr_t>(logits) % es != 0 || misaligned4(scores) || misaligned4(weights) ||
+        misaligned4(done) || misaligned4(scores_out) || misaligned4(parent) || misaligned4(tokens) || misaligned4(row_status))
+        return FSD_ERR_LAYOUT;
+    const BeamSpace w = beam_space(s, B, beams, n);
+    if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return FSD_ERR_WORKSPACE;
+    const size_t read = (static_cast<size_t>(B) * beams - 1) * static_cast<size_t>(row_stride) * es + static_cast<size_t>(V) * es;
+    const Run runs[] = {{scores_out, out}, {parent, out}, {tokens, out}, {row_status, static_cast<size_t>(B) * 4}, {workspace, w.bytes},
+                        {scores, in}, {weights, in}, {done, in}, {logits, read}};
+    if (any_overlap(runs, 5, 9)) return FSD_ERR_LAYOUT;
+    char* base = static_cast<char*>(workspace);
+    BeamParams P;
+    P.logits = static_cast<const char*>(logits);
+    P.row_stride = static_cast<size_t>(row_stride) * es;
+    P.scores = scores;
+    P.weights = weights;
+    P.done = done;
+    P.B = B; P.W = beams; P.V = V; P.n = n;
+    P.len = s.len; P.S = s.S; P.lists = beams * s.S;
+    P.stat = reinterpret_cast<double2*>(base + w.stat);
+    P.cand = reinterpret_cast<float2*>(base + w.cand);
+    P.count = reinterpret_cast<int*>(base + w.count);
+    P.scores_out = scores_out;
+    P.parent = parent;
+    P.tokens = tokens;
+    P.status = row_status;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const unsigned grid = static_cast<unsigned>(static_cast<long>(B) * P.lists);
+    if (dtype == FSD_BF16) launch_beam_slices<true>(st, grid, s.slots, P);
+    else launch_beam_slices<false>(st, grid, s.slots, P);
+    hipLaunchKernelGGL(beam_merge, dim3(static_cast<unsigned>(B)), dim3(kWG), 0, st, P);
+    return launched();
+}
+
+int fsd_beam_reorder(const void* states, const int32_t* parent, int layers, int B, int beams, int n, size_t row_bytes, void* out, int32_t* row_status,
+                     void* hip_stream) {
+    if (!states || !parent || !out) return FSD_ERR_NULL;
+    if (layers < 1 || layers > 65535 || B < 1 || B > kMaxBatch || beams < 1 || beams > 65535 || n < 1 || n > 65535 || row_bytes < 1 || row_bytes > (1ul << 40))
+        return FSD_ERR_SHAPE;
+    const long pairs = static_cast<long>(layers) * B, rows = pairs * n;
+    if (pairs * (beams > n ? beams : n) >= (1L << 31)) return FSD_ERR_SHAPE;
+    if (misaligned4(parent) || misaligned4(row_status)) return FSD_ERR_LAYOUT;
+    ReorderParams P;
+    P.pieces = static_cast<int>((row_bytes + kReorderPiece - 1) / kReorderPiece);
+    // (rows of 2^40 bytes are 2^26 pieces: the product is in range; whether the bytes are is the memory's matter)
+    P.units = rows * P.pieces;
+    const unsigned __int128 in_bytes = static_cast<unsigned __int128>(row_bytes) * pairs * beams, out_bytes = static_cast<unsigned __int128>(row_bytes) * rows;
+    if ((in_bytes >> 62) != 0 || (out_bytes >> 62) != 0) return FSD_ERR_SHAPE;
+    const Run runs[] = {{out, static_cast<size_t>(out_bytes)}, {row_status, static_cast<size_t>(B) * 4}, {states, static_cast<size_t>(in_bytes)},
+                        {parent, static_cast<size_t>(B) * n * 4}};
+    if (any_overlap(runs, 2, 4)) return FSD_ERR_LAYOUT;
+    P.states = static_cast<const char*>(states);
+    P.parent = parent;
+    P.out = static_cast<char*>(out);
+    P.status = row_status;
+    P.row = row_bytes;
+    P.rows = rows;
+    P.B = B; P.W = beams; P.n = n;
+    const long most = 1L << 20;
+    hipLaunchKernelGGL(beam_reorder, dim3(static_cast<unsigned>(P.units < most ? P.units : most)), dim3(kWG), 0, static_cast<hipStream_t>(hip_stream), P);
+    return launched();
+}
+
+size_t fsd_cache_fork_workspace_bytes(int num_blocks, int n) { return fork_sizes(num_blocks, n) ? fork_space(num_blocks, n).bytes : 0; }
+
+int fsd_cache_fork(const fsd_cache* cache, int B, const int32_t* refs, const int32_t* parent, const int32_t* lengths, const int32_t* room, int n,
+                   int32_t* block_table_out, int32_t* cache_len_out, int32_t* refs_out, int32_t* free_blocks, int32_t* row_status, void* workspace,
+                   size_t workspace_bytes, void* hip_stream) {
+    if (!refs || !parent || !block_table_out || !cache_len_out || !refs_out) return FSD_ERR_NULL;
+    const int bad = check_cache(cache);
+    if (bad != FSD_OK) return bad;
+    const fsd_cache& c = *cache;
+    if (B < 1 || B > kMaxBatch || !fork_sizes(c.num_blocks, n) || static_cast<long>(n) * c.max_blocks >= INT_MAX) return FSD_ERR_SHAPE;
+    if (misaligned4(refs) || misaligned4(parent) || misaligned4(lengths) || misaligned4(room) || misaligned4(block_table_out) || misaligned4(cache_len_out) ||
+        misaligned4(refs_out) || misaligned4(free_blocks) || misaligned4(row_status) || misaligned4(c.block_table) || misaligned4(c.cache_len))
+        return FSD_ERR_LAYOUT;
+    const ForkSpace w = fork_space(c.num_blocks, n);
+    if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return FSD_ERR_WORKSPACE;
+    const size_t per = static_cast<size_t>(c.max_blocks) * 4, seqs = static_cast<size_t>(n) * 4, blocks = static_cast<size_t>(c.num_blocks) * 4;
+    const Run runs[] = {{block_table_out, n * per}, {cache_len_out, seqs}, {free_blocks, 4}, {row_status, seqs}, {workspace, w.bytes}, {refs_out, blocks},
+                        {refs_out == refs ? nullptr : refs, blocks}, {parent, seqs}, {lengths, seqs}, {room, seqs}, {c.block_table, B * per},
+                        {c.cache_len, static_cast<size_t>(B) * 4}};
+    if (any_overlap(runs, 6, 12)) return FSD_ERR_LAYOUT;
+    char* base = static_cast<char*>(workspace);
+    auto ints = [base](size_t at) { return reinterpret_cast<int*>(base + at); };
+    ForkParams P;
+    P.table = c.block_table;
+    P.lens = c.cache_len;
+    P.parent = parent;
+    P.keep = lengths;
+    P.room = room;
+    P.refs = refs;
+    P.B = B; P.M = c.max_blocks; P.P = c.num_blocks; P.n = n;
+    P.table_out = block_table_out;
+    P.len_out = cache_len_out;
+    P.refs_out = refs_out;
+    P.free_out = free_blocks;
+    P.status = row_status;
+    P.released = ints(w.released);
+    P.shared = ints(w.shared);
+    P.claim = ints(w.claim);
+    P.free_list = ints(w.free_list);
+    P.free_count = ints(w.free_count);
+    P.seq = reinterpret_cast<int4*>(base + w.seq);
+    P.fresh = ints(w.fresh);
+    P.copies = ints(w.copies);
+    P.at = reinterpret_cast<int2*>(base + w.at);
+    P.copy_seq = ints(w.copy_seq);
+    P.totals = ints(w.totals);
+    P.pair = pages_pair(c, c);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int chunks = chunks_of(P.P);
+    const dim3 t(kWG);
+    const long clear = (static_cast<long>(P.P) + kWG - 1) / kWG;
+    hipLaunchKernelGGL(fork_clear, dim3(static_cast<unsigned>(clear < 2048 ? clear : 2048)), t, 0, st, P);
+    hipLaunchKernelGGL(fork_mark, dim3(static_cast<unsigned>(B + n)), t, 0, st, P);
+    hipLaunchKernelGGL(fork_count, dim3(static_cast<unsigned>(chunks + (n + kWG / 64 - 1) / (kWG / 64))), t, 0, st, P, chunks);
+    hipLaunchKernelGGL(fork_list, dim3(static_cast<unsigned>(chunks + (n + kWG - 1) / kWG)), t, 0, st, P, chunks);
+    const unsigned movers = copy_groups(static_cast<long>(n) * c.layers * c.kv_heads);
+    hipLaunchKernelGGL(fork_apply, dim3(static_cast<unsigned>(chunks + n) + movers), t, 0, st, P, chunks);
+    return launched();
+}
+
+int fsd_cache_copy(const fsd_cache* src, const fsd_cache* dst, const int32_t* src_blocks, const int32_t* dst_blocks, const int32_t* tokens, int n,
+                   int32_t* page_status, void* hip_stream) {
+    if (!src_blocks || !dst_blocks) return FSD_ERR_NULL;
+    int bad = check_cache(src);
+    if (bad == FSD_OK) bad = check_cache(dst);
+    if (bad != FSD_OK) return bad;
+    if (n < 1 || src->layers != dst->layers || src->kv_heads != dst->kv_heads || src->head_dim != dst->head_dim) return FSD_ERR_SHAPE;
+    const long units = static_cast<long>(n) * src->layers;   // (times heads: under 2^31 * 2^31)
+    if (units >= (1L << 40) / src->kv_heads) return FSD_ERR_SHAPE;
+    const size_t list = static_cast<size_t>(n) * 4, codes = static_cast<size_t>(src->layers) * src->kv_heads * kBlock * src->head_dim,
+                 scales = static_cast<size_t>(src->layers) * src->kv_heads * 4;
+    const bool one = src->k_codes == dst->k_codes && src->v_codes == dst->v_codes && src->k_scale == dst->k_scale && src->v_scale == dst->v_scale &&
+                     src->num_blocks == dst->num_blocks;
+    const size_t a = static_cast<size_t>(src->num_blocks), b = static_cast<size_t>(dst->num_blocks);
+    const Run runs[] = {{dst->k_codes, codes * b}, {dst->v_codes, codes * b}, {dst->k_scale, scales * b}, {dst->v_scale, scales * b}, {page_status, list},
+                        {src_blocks, list}, {dst_blocks, list}, {tokens, list},
+                        {one ? nullptr : src->k_codes, codes * a}, {one ? nullptr : src->v_codes, codes * a}, {one ? nullptr : src->k_scale, scales * a},
+                        {one ? nullptr : src->v_scale, scales * a}};
+    if (any_overlap(runs, 5, 12) || misaligned4(src_blocks) || misaligned4(dst_blocks) || misaligned4(tokens) || misaligned4(page_status)) return FSD_ERR_LAYOUT;
+    CopyParams P;
+    P.pair = pages_pair(*src, *dst);
+    P.from = src_blocks;
+    P.to = dst_blocks;
+    P.tokens = tokens;
+    P.status = page_status;
+    P.n = n;
+    P.units = units * src->kv_heads;
+    const long most = 1L << 20;
+    hipLaunchKernelGGL(pages_copy, dim3(static_cast<unsigned>(P.units < most ? P.units : most)), dim3(kWG), 0, static_cast<hipStream_t>(hip_stream), P);
+    return launched();
+}
+
+size_t fsd_cache_compact_workspace_bytes(int num_blocks) { return fork_sizes(num_blocks, 1) ? compact_space(num_blocks).bytes : 0; }
+
+int fsd_cache_compact(const fsd_cache* cache, int B, const int32_t* refs, int32_t* block_table_out, int32_t* refs_out, int32_t* remap, int32_t* used_blocks,
+                      int32_t* row_status, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!refs || !block_table_out || !refs_out) return FSD_ERR_NULL;
+    const int bad = check_cache(cache);
+    if (bad != FSD_OK) return bad;
+    const fsd_cache& c = *cache;
+    if (B < 1 || B > kMaxBatch || !fork_sizes(c.num_blocks, 1)) return FSD_ERR_SHAPE;
+    if (misaligned4(refs) || misaligned4(block_table_out) || misaligned4(refs_out) || misaligned4(remap) || misaligned4(used_blocks) || misaligned4(row_status) ||
+        misaligned4(c.block_table))
+        return FSD_ERR_LAYOUT;
+    const CompactSpace w = compact_space(c.num_blocks);
+    if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return FSD_ERR_WORKSPACE;
+    const size_t table = static_cast<size_t>(B) * c.max_blocks * 4, blocks = static_cast<size_t>(c.num_blocks) * 4;
+    const Run runs[] = {{remap, blocks}, {used_blocks, 4}, {row_status, static_cast<size_t>(B) * 4}, {workspace, w.bytes}, {block_table_out, table}, {refs_out, blocks},
+                        {block_table_out == c.block_table ? nullptr : c.block_table, table}, {refs_out == refs ? nullptr : refs, blocks}};
+    if (any_overlap(runs, 6, 8)) return FSD_ERR_LAYOUT;
+    char* base = static_cast<char*>(workspace);
+    auto ints = [base](size_t at) { return reinterpret_cast<int*>(base + at); };
+    CompactParams P;
+    P.table = c.block_table;
+    P.refs = refs;
+    P.B = B; P.M = c.max_blocks; P.P = c.num_blocks;
+    P.table_out = block_table_out;
+    P.refs_out = refs_out;
+    P.remap = remap;
+    P.used_out = used_blocks;
+    P.status = row_status;
+    P.used_count = ints(w.used_count);
+    P.number = ints(w.number);
+    P.from = ints(w.from);
+    P.to = ints(w.to);
+    P.count = ints(w.count);
+    P.totals = ints(w.totals);
+    P.pair = pages_pair(c, c);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int chunks = chunks_of(P.P);
+    const dim3 t(kWG);
+    hipLaunchKernelGGL(compact_count, dim3(static_cast<unsigned>(chunks)), t, 0, st, P);
+    hipLaunchKernelGGL(compact_list, dim3(static_cast<unsigned>(chunks)), t, 0, st, P, chunks);
+    const unsigned movers = copy_groups(static_cast<long>(c.num_blocks / 2 + 1) * c.layers * c.kv_heads);
+    hipLaunchKernelGGL(compact_apply, dim3(static_cast<unsigned>(chunks + B) + movers), t, 0, st, P, chunks);
+    return launched();
+}
+
+}  // extern "C"

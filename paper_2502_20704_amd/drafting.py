@@ -1,0 +1,185 @@
+"""The operators around drafting: the best continuations of beams, the states that follow them, and the pages of the 8-bit cache.
+
+Argument marshalling only, as in operators.py: tensors are checked and handed to the C ABI (`include/fsd.h` has the definitions).
+"""
+from __future__ import annotations
+
+import math
+
+from . import binding
+from .binding import FsdError, _ptr, _stream, _workspace, library
+from .operators import _check, _new, _on_current, _torch
+
+ROW_NO_BLOCKS = 64
+
+_bytes = {}
+
+
+def _asked_once(call, *key):
+    n = _bytes.get((call, key))
+    if n is None:   # the library's answer for a shape does not change
+        n = _bytes[call, key] = int(getattr(library(), call)(*key))
+    return n
+
+
+def fsd_beam_workspace_bytes(B: int, beams: int, V: int, n: int, dtype: int) -> int:
+    return _asked_once("fsd_beam_workspace_bytes", B, beams, V, n, dtype)
+
+
+def fsd_cache_fork_workspace_bytes(num_blocks: int, n: int) -> int:
+    return _asked_once("fsd_cache_fork_workspace_bytes", num_blocks, n)
+
+
+def fsd_cache_compact_workspace_bytes(num_blocks: int) -> int:
+    return _asked_once("fsd_cache_compact_workspace_bytes", num_blocks)
+
+
+def _space(workspace, need, device, stream):
+    """the workspace to hand over: the caller's, or one out of the stream's memory"""
+    if workspace is None:
+        workspace = _new(stream, device, workspace=((need + 256,), _torch().uint8))["workspace"]
+    elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous() or workspace.dtype != _torch().uint8:
+        raise ValueError(f"workspace: contiguous uint8 on {device} wanted")
+    return _workspace(workspace, 0, device)
+
+
+def _outputs(given, stream, device, optional, /, **tensors):
+    """the caller's outputs, checked, or new ones; optional: those that a caller may leave out"""
+    if given is None:
+        return _new(stream, device, **tensors)
+    for name, (shape, dtype) in tensors.items():
+        if name not in optional or given.get(name) is not None:
+            _check(given[name], name, shape, dtype, device)
+    return given
+
+
+def _row_stride(t, name):
+    """elements between rows of [B, beams, V]: entries lie side by side, and the rows at one distance"""
+    B, W, V = t.shape
+    s = t.stride()
+    step = s[1] if W > 1 else s[0] if B > 1 else V
+    if V > 1 and s[2] != 1 or B > 1 and s[0] != W * step:
+        raise ValueError(f"{name}: entries must lie side by side and rows at one distance from one another")
+    return step
+
+
+def fsd_beam_select(logits, scores, n, *, weights=None, done=None, out=None, workspace=None, stream=None):
+    """logits [B,beams,V] (rows at any one distance: the front of a padded vocabulary will do), scores float32 [B,beams] (None: 0),
+    weights float32 and done int32 [B,beams] -> dict with scores float32, parent and tokens int32 [B,n], best first, and row_status."""
+    torch = _torch()
+    if logits.dim() != 3:
+        raise ValueError("logits have 3 dimensions")
+    if not logits.is_cuda:
+        raise ValueError("logits must live on the GPU")
+    B, W, V = logits.shape
+    dt = binding._dtype_code(logits)
+    dev = logits.device
+    _on_current(dev, stream)
+    step = _row_stride(logits, "logits")
+    for name, t, dtype in (("scores", scores, torch.float32), ("weights", weights, torch.float32), ("done", done, torch.int32)):
+        if t is not None:
+            _check(t, name, (B, W), dtype, dev)
+    out = _outputs(out, stream, dev, ("row_status",), scores=((B, n), torch.float32), parent=((B, n), torch.int32),
+                   tokens=((B, n), torch.int32), row_status=((B,), torch.int32))
+    workspace, base, size = _space(workspace, fsd_beam_workspace_bytes(B, W, V, n, dt), dev, stream)
+    st = library().fsd_beam_select(_ptr(logits), step, _ptr(scores), _ptr(weights), _ptr(done), B, W, V, dt, n, _ptr(out["scores"]),
+                                   _ptr(out["parent"]), _ptr(out["tokens"]), _ptr(out.get("row_status")), base, size, _stream(stream))
+    if st != 0:
+        raise FsdError(st, "fsd_beam_select")
+    out["_workspace"] = workspace
+    return out
+
+
+def fsd_beam_reorder(states, parent, *, batch_dim=0, out=None, stream=None):
+    """states [..., B, beams, ...] of any type with B at batch_dim, parent int32 [B,n] -> dict with out [..., B, n, ...] (zeros where
+    parent is -1) and row_status [B]."""
+    torch = _torch()
+    if not 0 <= batch_dim <= states.dim() - 2:
+        raise ValueError("batch_dim names the sequences' dimension, with the beams' behind it")
+    dev = states.device
+    _check(states, "states")
+    _on_current(dev, stream)
+    if parent.dim() != 2:
+        raise ValueError("parent has 2 dimensions")
+    shape = tuple(states.shape)
+    B, W = shape[batch_dim:batch_dim + 2]
+    n = parent.shape[1]
+    _check(parent, "parent", (B, n), torch.int32, dev)
+    out = _outputs(out, stream, dev, ("row_status",), out=((*shape[:batch_dim + 1], n, *shape[batch_dim + 2:]), states.dtype),
+                   row_status=((B,), torch.int32))
+    st = library().fsd_beam_reorder(_ptr(states), _ptr(parent), math.prod(shape[:batch_dim]), B, W, n,
+                                    math.prod(shape[batch_dim + 2:]) * states.element_size(), _ptr(out["out"]), _ptr(out.get("row_status")),
+                                    _stream(stream))
+    if st != 0:
+        raise FsdError(st, "fsd_beam_reorder")
+    return out
+
+
+def fsd_cache_fork(cache, parent, refs, *, lengths=None, room=None, out=None, workspace=None, stream=None):
+    """parent int32 [n] (rows of the cache's table; -1: none), refs int32 [num_blocks], lengths and room int32 [n] -> dict with block_table
+    [n,max_blocks], cache_len [n], refs [num_blocks], free_blocks [1] and row_status [n].  `cache.with_tables(block_table, cache_len)`
+    is the cache of the new sequences."""
+    torch = _torch()
+    dev = cache.device
+    _on_current(dev, stream)
+    if parent.dim() != 1:
+        raise ValueError("parent has 1 dimension")
+    n, P = parent.shape[0], cache.num_blocks
+    _check(parent, "parent", (n,), torch.int32, dev)
+    _check(refs, "refs", (P,), torch.int32, dev)
+    for name, t in (("lengths", lengths), ("room", room)):
+        if t is not None:
+            _check(t, name, (n,), torch.int32, dev)
+    out = _outputs(out, stream, dev, ("free_blocks", "row_status"), block_table=((n, cache.max_blocks), torch.int32),
+                   cache_len=((n,), torch.int32), refs=((P,), torch.int32), free_blocks=((1,), torch.int32), row_status=((n,), torch.int32))
+    workspace, base, size = _space(workspace, fsd_cache_fork_workspace_bytes(P, n), dev, stream)
+    st = library().fsd_cache_fork(cache._ref, cache.batch, _ptr(refs), _ptr(parent), _ptr(lengths), _ptr(room), n, _ptr(out["block_table"]),
+                                  _ptr(out["cache_len"]), _ptr(out["refs"]), _ptr(out.get("free_blocks")), _ptr(out.get("row_status")), base, size,
+                                  _stream(stream))
+    if st != 0:
+        raise FsdError(st, "fsd_cache_fork")
+    out["_workspace"] = workspace
+    return out
+
+
+def fsd_cache_copy(src, dst, src_blocks, dst_blocks, *, tokens=None, out=None, stream=None):
+    """Blocks src_blocks int32 [n] of the cache src become blocks dst_blocks of dst (which may be src), their first tokens int32 [n] tokens
+    (None: all) -> dict with page_status [n]."""
+    torch = _torch()
+    dev = src.device
+    _on_current(dev, stream)
+    if dst.device != dev:
+        raise ValueError(f"the caches live on {dev} and {dst.device}")
+    if (src.layers, src.kv_heads, src.head_dim) != (dst.layers, dst.kv_heads, dst.head_dim):
+        raise ValueError("the caches differ in layers, kv_heads or head_dim")
+    if src_blocks.dim() != 1:
+        raise ValueError("src_blocks has 1 dimension")
+    n = src_blocks.shape[0]
+    for name, t in (("src_blocks", src_blocks), ("dst_blocks", dst_blocks), ("tokens", tokens)):
+        if t is not None:
+            _check(t, name, (n,), torch.int32, dev)
+    out = _outputs(out, stream, dev, ("page_status",), page_status=((n,), torch.int32))
+    st = library().fsd_cache_copy(src._ref, dst._ref, _ptr(src_blocks), _ptr(dst_blocks), _ptr(tokens), n, _ptr(out.get("page_status")),
+                                  _stream(stream))
+    if st != 0:
+        raise FsdError(st, "fsd_cache_copy")
+    return out
+
+
+def fsd_cache_compact(cache, refs, *, out=None, workspace=None, stream=None):
+    """refs int32 [num_blocks] -> dict with block_table [B,max_blocks], refs and remap [num_blocks], used_blocks [1] and row_status [B].
+    out=dict(block_table=cache.block_table, refs=refs) works in place."""
+    torch = _torch()
+    dev = cache.device
+    _on_current(dev, stream)
+    B, P = cache.batch, cache.num_blocks
+    _check(refs, "refs", (P,), torch.int32, dev)
+    out = _outputs(out, stream, dev, ("remap", "used_blocks", "row_status"), block_table=((B, cache.max_blocks), torch.int32),
+                   refs=((P,), torch.int32), remap=((P,), torch.int32), used_blocks=((1,), torch.int32), row_status=((B,), torch.int32))
+    workspace, base, size = _space(workspace, fsd_cache_compact_workspace_bytes(P), dev, stream)
+    st = library().fsd_cache_compact(cache._ref, B, _ptr(refs), _ptr(out["block_table"]), _ptr(out["refs"]), _ptr(out.get("remap")),
+                                     _ptr(out.get("used_blocks")), _ptr(out.get("row_status")), base, size, _stream(stream))
+    if st != 0:
+        raise FsdError(st, "fsd_cache_compact")
+    out["_workspace"] = workspace
+    return out

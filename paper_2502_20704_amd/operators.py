@@ -143,6 +143,10 @@ class Cache:
                          L, P, H, D, M)
         self._ref = ctypes.byref(self._c)
 
+    def with_tables(self, block_table, cache_len):
+        """The same codes and scales under other tables and lengths (those that fsd_cache_fork gives)."""
+        return Cache(self.k_codes, self.v_codes, self.k_scale, self.v_scale, block_table, cache_len)
+
     @classmethod
     def empty(cls, layers, num_blocks, kv_heads, head_dim, block_table, cache_len):
         """A cache without contents on the device of block_table; scales start at 1."""
