@@ -15,7 +15,8 @@ namespace {
 
 constexpr int kBeamMost = 128;      // n
 constexpr int kBeamWidest = 256;    // beams
-constexpr int kBeamList = 1024;     // entries of a slice that stand in LDS before the n best are taken from them
+constexpr int kWaveList = 256;      // entries of a wavefront's part of a slice that stand in LDS before the n best are taken from all
+constexpr int kAside = 128;         // slots of a wavefront's that stand there until they are taken apart
 constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct BeamParams {
@@ -25,18 +26,18 @@ struct BeamParams {
     const int* done;
     int B, W, V, n;
     int len, S, lists;              // entries of a slice (a multiple of a 16-byte slot's), slices of a row, W * S
-    float2* cand;                   // [B, n, W * S]: logit and token of a list's entry, best first
-    int* count;                     // [B, W * S]
-    double2* stat;                  // [B, W * S]: largest logit, sum of e^(z - largest)
+    unsigned by_S;                  // ceil(2^32 / S), 0 where S is 1
+    float2* cand;                   // [B, n, W * S]: logit and token of a list's entry, best first; -inf behind the last
+    double2* stat;                  // [B, W * S]: a number r and the sum of e^(z - r); -inf and 0 where no entry counts
     float* scores_out;
     int *parent, *tokens, *status;
 };
 
-// e^d for d <= 0, off by 2^-34 of it (under -690: next to nothing, NaN: NaN): d log2 e as a whole number k and a rest of at most 1/2; the rest's power by a
-// polynomial of degree 7 (fitted to the smallest largest relative error on [-1/2, 1/2]), k into its exponent's bits.
-__device__ __forceinline__ double exp_64(double d) {
+// e^x, off by 2^-34 of it, for |x| up to 700: x log2 e as a whole number k and a rest of at most 1/2; the rest's power by a polynomial of degree 7
+// (fitted to the smallest largest relative error on [-1/2, 1/2], 4.0e-11), k added to its exponent.  NaN stays NaN.
+__device__ __forceinline__ double exp_within(double x) {
     constexpr double kWhole = 6755399441055744.0;            // 1.5 * 2^52: what is added to it comes out whole, in the low word
-    const double k = __builtin_fma(d, kLog2e64, kWhole), f = __builtin_fma(d, kLog2e64, kWhole - k);
+    const double k = __builtin_fma(x, kLog2e64, kWhole), f = __builtin_fma(x, kLog2e64, kWhole - k);
     double p = 1.520192135287937e-05;
     p = __builtin_fma(p, f, 0.00015469291148729867);
     p = __builtin_fma(p, f, 0.001333392256490547);
@@ -45,10 +46,12 @@ __device__ __forceinline__ double exp_64(double d) {
     p = __builtin_fma(p, f, 0.24022651198157982);
     p = __builtin_fma(p, f, 0.693147180728448);
     p = __builtin_fma(p, f, 0.9999999999616819);
-    const unsigned long bits = __builtin_bit_cast(unsigned long, p);
-    unsigned hi = static_cast<unsigned>(bits >> 32) + (static_cast<unsigned>(__builtin_bit_cast(unsigned long, k)) << 20);
-    hi = d < -690.0 ? 0u : hi;                               // (the low word alone is less than 2^-1042)
-    return __builtin_bit_cast(double, static_cast<unsigned long>(hi) << 32 | (bits & 0xFFFFFFFFul));
+    return __builtin_amdgcn_ldexp(p, static_cast<int>(__builtin_bit_cast(unsigned long, k)));
+}
+// for any x <= 0: nothing under -700
+__device__ __forceinline__ double exp_below(double x) {
+    const double e = exp_within(x < -700.0 ? -700.0 : x);
+    return x < -700.0 ? 0.0 : e;
 }
 // bits of a number in an order in which larger numbers have larger words (0 and -0 differ: give it neither as -0)
 __device__ __forceinline__ unsigned ordered(float x) {
@@ -58,11 +61,23 @@ __device__ __forceinline__ unsigned ordered(float x) {
 __device__ __forceinline__ float from_ordered(unsigned o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 constexpr unsigned kLeastOrdered = 0x00800000u;   // of the lowest finite number
 
+// the largest of three, without the instructions that make quiet NaNs of others first
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+// x, but no less than -700 (by its word: those of negative numbers grow with the distance from 0; a NaN of this sign is lost, which is looked for elsewhere)
+__device__ __forceinline__ float at_least_700_below(float x) {
+    const unsigned u = __float_as_uint(x), least = 0xC42F0000u;
+    return __uint_as_float(u < least ? u : least);
+}
+
+// entry e of a 16-byte slot
 template <bool BF16>
-__device__ __forceinline__ float slot_entry(const uint4& r, int e) {
-    const unsigned w[4] = {r.x, r.y, r.z, r.w};
-    if constexpr (BF16) return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-    else return __uint_as_float(w[e]);
+__device__ __forceinline__ float slot_entry(const u32x4& r, int e) {
+    if constexpr (BF16) return __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
+    else return __uint_as_float(r[e]);
 }
 
 __device__ __forceinline__ float score_of(const BeamParams& P, long at) { return P.scores ? P.scores[at] : 0.0f; }
@@ -70,12 +85,12 @@ __device__ __forceinline__ bool beam_runs(const BeamParams& P, long at) {   // w
     return score_of(P, at) > -__builtin_inff() && !(P.done && P.done[at]);   // (a score that is NaN is reported without its row)
 }
 
-// A slice's n best entries where more than kBeamList reach the bound that its lanes gave (rows of equal entries, or in order): the n-th largest
-// is found bit by bit, then what is above it and, from the lowest index on, what equals it go into the list.  Returns how many.
-template <bool BF16, int NS>
-__device__ int slice_cut(const uint4 (&r)[NS], int n, unsigned long* list, int* lds, int tid) {
-    constexpr int E = BF16 ? 8 : 4;
-    const int wave = tid / 64, lane = tid % 64;
+// A slice's n best entries where more than kWaveList of a wavefront's reach the bound that its lanes gave (rows of equal entries, or in order): the n-th largest
+// is found bit by bit, then what is above it and, from the lowest index on, what equals it go into the list.  Returns how many.  (It reads the entries
+// again rather than keep the calling kernel's registers in memory; 40 passes over what the caches hold.)
+template <bool BF16>
+__device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, unsigned long* list, int* lds, int tid) {
+    const int wave = tid / 64, lane = tid % 64, len = end - begin;
     auto over_wg = [&](int c) {                              // the sum of all threads' c
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
@@ -84,243 +99,388 @@ __device__ int slice_cut(const uint4 (&r)[NS], int n, unsigned long* list, int* 
         __syncthreads();
         return lds[0] + lds[1] + lds[2] + lds[3];
     };
+    auto word_at = [&](int k) { return ordered(load_logit<BF16>(z, begin + k) + 0.0f); };
     unsigned least = 0;
     for (int bit = 31; bit >= (BF16 ? 16 : 0); --bit) {
         const unsigned c = least | 1u << bit;
         int have = 0;
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) have += ordered(slot_entry<BF16>(r[i], e) + 0.0f) >= c;
+        for (int k = tid; k < len; k += kWG) have += word_at(k) >= c;
         if (over_wg(have) >= n) least = c;
     }
-    // (of bfloat16 entries the low 16 bits: 0 of a positive one, 1 of a negative one, so that this is its lowest word or one that no entry has)
+    // (of bfloat16 entries the low 16 bits: 0 of a positive one, 1 of a negative one; the bits found say which)
     if (BF16 && !(least & 0x80000000u)) least |= 0xFFFFu;
     if (least < kLeastOrdered) least = kLeastOrdered;
     int above = 0;
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) above += ordered(slot_entry<BF16>(r[i], e) + 0.0f) > least;
+    for (int k = tid; k < len; k += kWG) above += word_at(k) > least;
     const int more = over_wg(above);
     if (tid == 0) lds[4] = 0;
-    int before = 0;                                          // entries that equal it, of the slots behind us
+    int before = 0;                                          // entries that equal it, of those behind us
     __syncthreads();
-#pragma unroll 1
-    for (int i = 0; i < NS; ++i) {
-        uint4 slot = r[0];
-#pragma unroll
-        for (int k = 1; k < NS; ++k) slot = i == k ? r[k] : slot;
-        int same = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) same += ordered(slot_entry<BF16>(slot, e) + 0.0f) == least;
-        int upto = same;                                     // of this and the lanes below
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int other = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += other;
-        }
+    for (int k0 = 0; k0 < len; k0 += kWG) {
+        const int k = k0 + tid;
+        const unsigned o = k < len ? word_at(k) : 0u;
+        const unsigned long same = __ballot(o == least);
         __syncthreads();
-        if (lane == 63) lds[wave] = upto;
+        if (lane == 0) lds[wave] = __popcll(same);
         __syncthreads();
-        int at = before + upto - same;
+        int at = before + __popcll(same & ((1ul << lane) - 1));
         for (int w = 0; w < wave; ++w) at += lds[w];
         before += lds[0] + lds[1] + lds[2] + lds[3];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const unsigned o = ordered(slot_entry<BF16>(slot, e) + 0.0f);
-            const bool equal = o == least;
-            if (o > least || (equal && at < n - more)) {
-                const int k = atomicAdd(&lds[4], 1);
-                list[k] = static_cast<unsigned long>(o) << 32 | ~static_cast<unsigned>((i * kWG + tid) * E + e);
-            }
-            at += equal;
-        }
+        if (o > least || (o == least && at < n - more)) list[atomicAdd(&lds[4], 1)] = static_cast<unsigned long>(o) << 32 | ~static_cast<unsigned>(k);
     }
     __syncthreads();
     return lds[4];
 }
 
-// One slice of a row a workgroup, NS slots of 16 bytes a thread.  A wavefront's q-th largest lane maximum, q = n / 4 rounded up, is
-// reached by q entries of its own at least, so the least of the four wavefronts' by n of the slice: what reaches that bound (a few more than n entries
-// where the values lie as those of logits do) is written to LDS and ranked there.
-template <bool BF16, int NS>
-__global__ void __launch_bounds__(kWG) beam_slices(const BeamParams P) {
-    constexpr int E = BF16 ? 8 : 4;
-    __shared__ unsigned long list[kBeamList];
-    __shared__ double wave_sum[4];
-    __shared__ float wave_top[4];
-    __shared__ unsigned wave_bound[4];
-    __shared__ int lds[5];
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-    const long row = blockIdx.x / P.S;
-    const int slice = static_cast<int>(blockIdx.x - row * P.S);
-    if (!beam_runs(P, row)) return;
-    const int begin = slice * P.len, end = begin + P.len < P.V ? begin + P.len : P.V;
-    const char* z = P.logits + static_cast<size_t>(row) * P.row_stride;
-    uint4 r[NS];
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const int at = begin + (i * kWG + tid) * E;
-        if (at + E <= end) r[i] = load_any16(z + static_cast<size_t>(at) * (16 / E));
-        else r[i] = neg_inf_slot<BF16>();
+// Of a wavefront's list (in LDS) those that reach the bound, in their order; how many.
+__device__ __forceinline__ int keep_reaching(unsigned long* list, int count, unsigned bound, int lane) {
+    int kept = 0;
+    for (int k0 = 0; k0 < count; k0 += 64) {
+        const unsigned long x = k0 + lane < count ? list[k0 + lane] : 0;
+        const bool keep = static_cast<unsigned>(x >> 32) >= bound;
+        const unsigned long who = __ballot(keep);
+        if (keep) list[kept + __popcll(who & ((1ul << lane) - 1))] = x;   // (at or before where it was read; a wavefront's LDS instructions are done in order)
+        kept += __popcll(who);
     }
-    // the entries behind the row's last whole slot: its thread takes them one by one
-    const int whole = begin + (end - begin) / E * E;
-    if (whole < end) {
-        const int slot = (end - begin) / E;
-        unsigned w[4];
-        const uint4 none = neg_inf_slot<BF16>();
-        w[0] = none.x; w[1] = none.y; w[2] = none.z; w[3] = none.w;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (whole + e < end) {
-                if constexpr (BF16) {
-                    const unsigned h = reinterpret_cast<const unsigned short*>(z)[whole + e];
-                    w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | h << 16 : (w[e / 2] & 0xFFFF0000u) | h;
-                } else {
-                    w[e] = reinterpret_cast<const unsigned*>(z)[whole + e];
-                }
-            }
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-            if (i * kWG + tid == slot) r[i] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (tid == 0) lds[4] = 0;
+    return kept;
+}
 
-    float mine = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) mine = __builtin_fmaxf(mine, slot_entry<BF16>(r[i], e));
-    const float top = wave_max_all(mine);
-
-    // the wavefront's bound, to the upper 20 bits
-    const unsigned word = ordered(mine + 0.0f);
-    const int q = (P.n + 3) / 4;
+// The wavefront's q-th largest of its lanes' words, to the upper 20 bits
+template <bool BF16>
+__device__ __forceinline__ unsigned wave_bound(unsigned word, int q) {
     unsigned bound = 0;
     for (int bit = 31; bit >= (BF16 ? 16 : 12); --bit) {
         const unsigned c = bound | 1u << bit;
         if (__popcll(__ballot(word >= c)) >= q) bound = c;
     }
+    return bound;
+}
 
-    // the wavefront's sum (NaN stays in it)
-    const double highest = top;
+// One slice of a row a workgroup, in chunks of NS slots of 16 bytes a thread; where a slot has been added up, that of the next chunk is requested in its
+// place.  Of the entries seen so far a wavefront's q-th largest lane maximum, q = n / 4 rounded up, is reached by q of its own at least, so the
+// least of the four wavefronts' by n of the slice: what reaches that bound (few more than n entries where the values lie as those of logits do) is put
+// into LDS and ranked there at the end.  Wavefronts tell one another their bounds without waiting: an older one of another's bounds as well.
+// Exponentials are added up as e^z: binary64 has the range where logits are of the size that models give them.  Where they are not, the slice is gone over again.
+template <bool BF16, int NS>
+__global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
+    constexpr int E = BF16 ? 8 : 4, kChunk = kWG * NS;        // (slots of a chunk)
+    constexpr unsigned kNone = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
+    __shared__ unsigned long list[4 * kWaveList];
+    __shared__ u32x4 aside_slot[4][kAside];
+    __shared__ int aside_at[4][kAside];
+    __shared__ double wave_sum[4], wave_ref[4];
+    __shared__ unsigned bounds[4];
+    __shared__ int lds[5];
+    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+    const unsigned row = blockIdx.x / static_cast<unsigned>(P.S);
+    const int slice = static_cast<int>(blockIdx.x - row * static_cast<unsigned>(P.S));
+    if (!beam_runs(P, row)) return;
+    const int begin = slice * P.len, end = begin + P.len < P.V ? begin + P.len : P.V;
+    const char* const z = P.logits + static_cast<size_t>(row) * P.row_stride;
+    const char* const at_begin = z + static_cast<size_t>(begin) * (16 / E);
+    const int slots = (end - begin) / E, all_slots = (end - begin + E - 1) / E;   // whole ones; and with a last one that is not
+    // (threads without a slot request the last one again: requests without branches go out together)
+    auto request = [&](int slot) {
+        const int from = slot < slots ? slot : slots - 1;
+        return static_cast<u32x4>(*reinterpret_cast<const u32x4_any*>(at_begin + static_cast<unsigned>(from) * 16u));
+    };
+    u32x4 r[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) r[i] = u32x4{kNone, kNone, kNone, kNone};
+    if (slots > 0) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) r[i] = request(i * kWG + tid);
+    }
+    // the entries behind the last whole slot: its thread takes them one by one
+    u32x4 last = {kNone, kNone, kNone, kNone};
+    if (slots < all_slots) {
+        const int whole = begin + slots * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (whole + e < end) {
+                if constexpr (BF16) {
+                    const unsigned h = reinterpret_cast<const unsigned short*>(z)[whole + e];
+                    last[e / 2] = e & 1 ? (last[e / 2] & 0xFFFFu) | h << 16 : (last[e / 2] & 0xFFFF0000u) | h;
+                } else {
+                    last[e] = reinterpret_cast<const unsigned*>(z)[whole + e];
+                }
+            }
+    }
+    auto behind = [&](u32x4& slot, int k) {                   // slots that the slice does not have, or not whole
+#pragma unroll
+        for (int j = 0; j < 4; ++j) slot[j] = k < slots ? slot[j] : k == slots ? last[j] : kNone;
+    };
+
+    unsigned long* const mine_list = list + wave * kWaveList;
+    int count = 0;                                            // of the wavefront's list
+    bool full = false;                                        // whether more were to go into it than it holds
+    int aside = 0;
+    const int q = (P.n + 3) / 4;
+    unsigned least = kLeastOrdered;
+    auto take_apart = [&]() {                                 // the slots that were put aside, 64 entries at a time
+        const float from = from_ordered(least);
+        for (int s0 = 0; s0 < aside; s0 += 64 / E) {
+            const int k = s0 + lane / E;
+            bool is = false;
+            float x = 0.0f;
+            int at = 0;
+            if (k < aside) {
+                const unsigned* words = reinterpret_cast<const unsigned*>(&aside_slot[wave][k]);
+                const int e = lane % E;
+                if constexpr (BF16) x = __uint_as_float(e & 1 ? words[e / 2] & 0xFFFF0000u : words[e / 2] << 16);
+                else x = __uint_as_float(words[e]);
+                at = aside_at[wave][k] * E + e;
+                is = x >= from;
+            }
+            const unsigned long who = __ballot(is);
+            const int n_who = __popcll(who);
+            // make room: what is under the bound by now goes
+            if (count + n_who > kWaveList) count = keep_reaching(mine_list, count, least, lane);
+            const int to = count + __popcll(who & ((1ul << lane) - 1));
+            if (is && to < kWaveList) mine_list[to] = static_cast<unsigned long>(ordered(x + 0.0f)) << 32 | ~static_cast<unsigned>(at);
+            count += n_who;
+            if (count > kWaveList) full = true, count = kWaveList;
+        }
+        aside = 0;
+    };
+    auto all_bounds = [&]() {
+        unsigned bound = 0xFFFFFFFFu;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const unsigned theirs = __hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            bound = theirs < bound ? theirs : bound;
+        }
+        least = bound > least ? bound : least;
+    };
+    auto slot_max = [&](const u32x4& slot) {
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < E; e += 2) m = max3(m, slot_entry<BF16>(slot, e), slot_entry<BF16>(slot, e + 1));
+        return m;
+    };
+
+    // the first chunk's bound
+    float mine = -__builtin_inff();                           // the lane's largest so far
+    if (kChunk > slots) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) behind(r[i], i * kWG + tid);
+    }
+#pragma unroll
+    for (int i = 0; i < NS; ++i) mine = __builtin_fmaxf(mine, slot_max(r[i]));
+    {
+        const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
+        if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    __syncthreads();
+    all_bounds();
+
+    bool broken = false;                                      // an entry is NaN or +inf
     double sum[2] = {0.0, 0.0};
-    if (top > -__builtin_inff()) {
+    int chunk = 0;
+    for (int first = 0; first < all_slots; first += kChunk, ++chunk) {
+        const float from = from_ordered(least);
+        const bool ends = first + 2 * kChunk > slots;         // whether the next chunk is not whole, or none
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
+        for (int i = 0; i < NS; ++i) {
+            const int slot = first + i * kWG + tid;
+            const float top = slot_max(r[i]);
+            mine = __builtin_fmaxf(mine, top);
+            // a slot with an entry that reaches the bound is put aside whole, to be taken apart with others
+            const unsigned long who = __ballot(top >= from);
+            if (who != 0) {
+                if (top >= from) {
+                    const int k = aside + __popcll(who & ((1ul << lane) - 1));
+                    aside_slot[wave][k] = r[i];
+                    aside_at[wave][k] = slot;
+                }
+                aside += __popcll(who);
+                if (aside > kAside - 64) take_apart();
+            }
+            // (what is under -700 counts as -700: nothing beside a largest entry of -600 or more)
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e & 1] += exp_64(static_cast<double>(slot_entry<BF16>(r[i], e)) - highest);
+            for (int e = 0; e < E; e += 2) {
+                const float x = slot_entry<BF16>(r[i], e), y = slot_entry<BF16>(r[i], e + 1);
+                broken |= __builtin_isunordered(x, y);
+                sum[0] += exp_within(static_cast<double>(at_least_700_below(x)));
+                sum[1] += exp_within(static_cast<double>(at_least_700_below(y)));
+            }
+            if (first + kChunk < all_slots) {
+                r[i] = request(slot + kChunk);
+                if (ends) behind(r[i], slot + kChunk);
+            }
+        }
+        // the bound anew where the entries seen have doubled
+        if ((chunk & (chunk + 1)) == 0 && first + kChunk < all_slots && chunk > 0) {
+            const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
+            if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+        all_bounds();
+    }
+    const float top = wave_max_all(mine);
+    double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
+    if (top > 600.0f || (top < -600.0f && top > -__builtin_inff())) {
+        // again, as e^(z - top)
+        ref = top;
+        sum[0] = sum[1] = 0.0;
+        for (int slot = tid; slot < all_slots; slot += kWG)
+            for (int e = 0; e < E && slot * E + e < end - begin; ++e)
+                sum[0] += exp_below(static_cast<double>(load_logit<BF16>(z, begin + slot * E + e)) - ref);
     }
     double s = sum[0] + sum[1];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    // an entry that is NaN or +inf: largest and sum are no numbers then (a wavefront of NaN alone has no largest entry)
-    bool broken = false;
-    if (!(top > -__builtin_inff())) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = slot_entry<BF16>(r[i], e);
-                broken |= x != x;
-            }
-        broken = __ballot(broken) != 0;
-    }
-    if (lane == 0) {
-        wave_top[wave] = top;
-        wave_sum[wave] = broken || !(top < __builtin_inff()) ? __builtin_nan("") : s;
-        wave_bound[wave] = bound;
+    if (!(top > -__builtin_inff())) s = 0.0;
+    const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
+    // the final bound, made of all four wavefronts' entries
+    {
+        const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
+        if (lane == 0) {
+            wave_ref[wave] = ref;
+            wave_sum[wave] = any_broken ? __builtin_nan("") : s;
+            __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
     }
     __syncthreads();
-    unsigned least = wave_bound[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) least = wave_bound[w] < least ? wave_bound[w] : least;
-    if (least < kLeastOrdered) least = kLeastOrdered;
-    const float from = from_ordered(least);
+    all_bounds();
+    take_apart();
+    count = keep_reaching(mine_list, count, least, lane);
+    if (lane == 0) lds[wave] = full ? kWaveList + 1 : count;
+    __syncthreads();
+    const int c0 = lds[0], c1 = lds[1], c2 = lds[2], c3 = lds[3];
+    const int most = c0 > c1 ? c0 : c1, most2 = c2 > c3 ? c2 : c3;
     const size_t at = static_cast<size_t>(row) * P.S + slice;   // of [B, W * S]
-    if (tid == 0) {
+    const int b = static_cast<int>(row / static_cast<unsigned>(P.W));
+    const size_t lists = P.lists, column = at - static_cast<size_t>(b) * lists;
+    float2* const cand = P.cand + static_cast<size_t>(b) * P.n * lists + column;
+    auto put = [&](int rank, unsigned long me) {
+        if (rank < P.n)
+            cand[rank * lists] = make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
+    };
+    int have;
+    if (most <= 64 && most2 <= 64) {
+        // a lane holds an entry of each wavefront's; a wavefront finds the ranks of its own one after the other
+        have = c0 + c1 + c2 + c3;
+        unsigned long other[4];
+        other[0] = lane < c0 ? list[lane] : 0;
+        other[1] = lane < c1 ? list[kWaveList + lane] : 0;
+        other[2] = lane < c2 ? list[2 * kWaveList + lane] : 0;
+        other[3] = lane < c3 ? list[3 * kWaveList + lane] : 0;
+        const unsigned long own = lane < count ? mine_list[lane] : 0;
+        int my_rank = 0;
+        for (int k = 0; k < count; ++k) {
+            const unsigned long me = static_cast<unsigned long>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(own >> 32), k))) << 32 |
+                                     static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(own), k));
+            int rank = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) rank += __popcll(__ballot(other[w] > me));
+            my_rank = lane == k ? rank : my_rank;
+        }
+        if (lane < count) put(my_rank, own);
+    } else {
+        int counts[4] = {c0, c1, c2, c3};
+        if (most > kWaveList || most2 > kWaveList) {
+            __syncthreads();                                  // (all have read the counts)
+            have = slice_cut<BF16>(z, begin, end, P.n, list, lds, tid);
+            counts[0] = have;                                 // (at most n of them)
+            counts[1] = counts[2] = counts[3] = 0;
+        } else {
+            have = c0 + c1 + c2 + c3;
+        }
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            for (int k = tid; k < counts[v]; k += kWG) {
+                const unsigned long me = list[v * kWaveList + k];
+                int rank = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
+                put(rank, me);
+            }
+    }
+    for (int k = have + tid; k < P.n; k += kWG) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
+    if (tid == kWG - 1) {
         double m = -__builtin_inf(), total = 0.0;
-        for (int w = 0; w < 4; ++w) m = wave_top[w] > m ? static_cast<double>(wave_top[w]) : m;
+        for (int w = 0; w < 4; ++w) m = wave_ref[w] > m ? wave_ref[w] : m;
         for (int w = 0; w < 4; ++w) {
-            const double ws = wave_sum[w];
-            if (ws != ws) total = ws;
-            else if (wave_top[w] > -__builtin_inff()) total += ws * exp_64(static_cast<double>(wave_top[w]) - m);
+            const double d = wave_ref[w] - m;                 // (NaN where the slice has no entry)
+            total += d < 0.0 ? (wave_ref[w] > -__builtin_inf() ? wave_sum[w] * exp_below(d) : wave_sum[w]) : wave_sum[w];
         }
         P.stat[at] = make_double2(m, total);
     }
-
-    if (mine >= from) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = slot_entry<BF16>(r[i], e);
-                if (x >= from) {
-                    const int k = atomicAdd(&lds[4], 1);
-                    if (k < kBeamList) list[k] = static_cast<unsigned long>(ordered(x + 0.0f)) << 32 | ~static_cast<unsigned>((i * kWG + tid) * E + e);
-                }
-            }
-    }
-    __syncthreads();
-    int have = lds[4];
-    if (have > kBeamList) have = slice_cut<BF16, NS>(r, P.n, list, lds, tid);
-    const int b = static_cast<int>(row / P.W);
-    const size_t lists = P.lists, column = at - static_cast<size_t>(b) * lists;
-    for (int k = tid; k < have; k += kWG) {
-        const unsigned long me = list[k];
-        int rank = 0;
-        for (int j = 0; j < have; ++j) rank += list[j] > me;
-        if (rank < P.n)
-            P.cand[(static_cast<size_t>(b) * P.n + rank) * lists + column] =
-                make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
-    }
-    if (tid == 0) P.count[at] = have < P.n ? have : P.n;
 }
 
 // ------------------------------------------------------------------------------------------ merging
 
-constexpr int kNoBeam = kBeamWidest;
-
 // A continuation: its rank, (beam, token + 1), its logit.  A rank's rounding may take logits of one beam for equal: then the logits decide.
-struct Ranked { double key; int beam, token1; float z; };
-__device__ __forceinline__ bool before(const Ranked& a, const Ranked& b) {
-    if (a.key != b.key) return a.key > b.key;
-    if (a.beam != b.beam) return a.beam < b.beam;
-    return a.z != b.z ? a.z > b.z : a.token1 < b.token1;
+struct Found { int beam, token1; float z; };
+constexpr int kMergeEach = 16;      // list entries that a thread holds at once
+constexpr int kMergeFew = 256;      // entries that are put into order as they are; of more, the n best are looked for first
+
+// 64-bit order of binary64 numbers, as ordered() is for binary32 ones; the upper word
+__device__ __forceinline__ unsigned ordered_high(double x) {
+    const unsigned u = static_cast<unsigned>(__builtin_bit_cast(unsigned long, x) >> 32);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A sequence a workgroup.  The lists' first entries come first, then their second ones, and so on: after the first few hundred of them
-// the n-th best so far turns nearly all others away, and where as many in a row as there are lists were turned away, so are all behind them.
-__global__ void __launch_bounds__(kWG) beam_merge(const BeamParams P) {
-    __shared__ Ranked found[3 * kWG];
-    __shared__ Ranked best[kBeamMost];
+// A sequence a workgroup of T threads.  All entries of its lists (or 16 a thread at a time) are ranked in registers; a wavefront's q-th largest, q =
+// n / wavefronts rounded up, bounds the n-th largest of all from below as in beam_slices, and the few that reach the least of these are ordered in LDS.
+template <int T>
+__global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
+    constexpr int NW = T / 64, kRoom = T + kBeamMost;
+    __shared__ double key[kRoom];
+    __shared__ Found found[kRoom];
+    __shared__ double best_key[kBeamMost];
+    __shared__ Found best[kBeamMost];
     __shared__ double norm[kBeamWidest];
+    __shared__ float base[kBeamWidest];                       // a beam's score; NaN: its list does not count
+    __shared__ float so_far[kBeamWidest];
+    __shared__ float factor[kBeamWidest];
+    __shared__ unsigned wave_bound[NW];
+    __shared__ int wave_count[2][NW];
     __shared__ int have, bad;
-    const int tid = threadIdx.x, b = blockIdx.x, W = P.W, S = P.S, n = P.n;
-    const long lists = P.lists;
+    const int tid = threadIdx.x, wave = tid / 64, b = blockIdx.x, W = P.W, S = P.S, n = P.n;
+    const int lists = P.lists;
     const long first = static_cast<long>(b) * W;
-    const float* weights = P.weights ? P.weights + first : nullptr;
-    const int* done = P.done ? P.done + first : nullptr;
+    const size_t out = static_cast<size_t>(b) * n;
+    const float2* cand = P.cand + out * lists;
     if (tid == 0) have = 0, bad = 0;
+    const int total = lists * n;                              // (at most 2^21)
+    const int column_step = T % lists;
+    float z[kMergeEach];
+    int token[kMergeEach];
+    // entry k of the lists: the (k / lists)-th of list k % lists
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < kMergeEach; ++i) {
+            const int k = k0 + i * T + tid;
+            const float2 c = k < total ? cand[k] : make_float2(-__builtin_inff(), 0.0f);
+            z[i] = c.x;
+            token[i] = static_cast<int>(__float_as_uint(c.y));
+        }
+    };
+    load(0);                                                  // (on the way while the normalisers are made)
     __syncthreads();
     // normalisers: 16 lanes a beam
-    for (int w0 = 0; w0 < W; w0 += kWG / 16) {
+    for (int w0 = 0; w0 < W; w0 += T / 16) {
         const int w = w0 + tid / 16, part = tid % 16;
         double m = -__builtin_inf(), s = 0.0;
-        bool runs = false, broken = false;
+        float score = 0.0f, by = 1.0f;
+        bool lives = false, ended = false, runs = false, broken = false;
         if (w < W) {
-            const float score = score_of(P, first + w);
-            const bool lives = !(score <= -__builtin_inff());
-            const bool ended = done && done[w];
-            broken = lives && !(score < __builtin_inff());
-            if (lives && weights) broken |= !(weights[w] > 0.0f && weights[w] < __builtin_inff());
+            score = score_of(P, first + w);
+            if (P.weights) by = P.weights[first + w];
+            ended = P.done && P.done[first + w];
+            lives = !(score <= -__builtin_inff());
+            broken = lives && !(score < __builtin_inff() && by > 0.0f && by < __builtin_inff());
             runs = lives && score == score && !ended;
         }
-        const double2* stat = P.stat + static_cast<size_t>(b) * lists + static_cast<size_t>(w) * S;
+        const double2* stat = P.stat + (first + w) * S;
+        double2 own = make_double2(m, 0.0);
+        if (runs && part < S) own = stat[part];
         if (runs) {
-            for (int k = part; k < S; k += 16) {
+            m = own.x;
+            broken |= own.y != own.y;
+            for (int k = part + 16; k < S; k += 16) {
                 const double2 x = stat[k];
                 m = x.x > m ? x.x : m;
                 broken |= x.y != x.y;
@@ -332,22 +492,31 @@ __global__ void __launch_bounds__(kWG) beam_merge(const BeamParams P) {
             m = other > m ? other : m;
         }
         if (runs && m > -__builtin_inf()) {
-            for (int k = part; k < S; k += 16) {
+            if (own.x > -__builtin_inf()) s = own.y * exp_below(own.x - m);
+            for (int k = part + 16; k < S; k += 16) {
                 const double2 x = stat[k];
-                if (x.x > -__builtin_inf()) s += x.y * exp_64(x.x - m);
+                if (x.x > -__builtin_inf()) s += x.y * exp_below(x.x - m);
             }
         }
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o, 16);
         if (broken) bad = 1;                                  // (whoever writes it writes the same)
         if (w < W && part == 0) {
-            norm[w] = runs && m > -__builtin_inf() ? m + log(s) : 0.0;
+            const bool counts = runs && m > -__builtin_inf();
+            norm[w] = counts ? m + log(s) : 0.0;
+            base[w] = counts ? score : __builtin_nanf("");
+            factor[w] = by;
+            so_far[w] = score;
+            if (lives && ended && !broken) {                  // a finished beam, as it stands
+                const int at = atomicAdd(&have, 1);
+                key[at] = static_cast<double>(score) * static_cast<double>(by);
+                found[at] = Found{w, 0, 0.0f};
+            }
         }
     }
     __syncthreads();
-    const size_t out = static_cast<size_t>(b) * n;
     if (bad) {
-        for (int i = tid; i < n; i += kWG) {
+        for (int i = tid; i < n; i += T) {
             P.scores_out[out + i] = -__builtin_inff();
             P.parent[out + i] = -1;
             P.tokens[out + i] = -1;
@@ -355,70 +524,169 @@ __global__ void __launch_bounds__(kWG) beam_merge(const BeamParams P) {
         if (tid == 0 && P.status) P.status[b] = FSD_ROW_NONFINITE;
         return;
     }
-    // finished beams, as they stand
-    if (done && tid < W && done[tid] && score_of(P, first + tid) > -__builtin_inff()) {
-        const float s = score_of(P, first + tid);
-        const double by = weights ? static_cast<double>(weights[tid]) : 1.0;
-        found[atomicAdd(&have, 1)] = Ranked{static_cast<double>(s) * by, tid, 0, 0.0f};
-    }
-    __syncthreads();
-    Ranked last = {-__builtin_inf(), kNoBeam, 0, 0.0f};      // the n-th best of what has been ranked
-    auto rank_found = [&](int count) {                        // the n best of found[0 .. count) to its front, best first
-        for (int k = tid; k < count; k += kWG) {
-            const Ranked me = found[k];
-            int rank = 0;
-            for (int j = 0; j < count; ++j) rank += before(found[j], me);
-            if (rank < n) best[rank] = me;
-        }
-        __syncthreads();
-        const int left = count < n ? count : n;
-        for (int k = tid; k < left; k += kWG) found[k] = best[k];
-        if (left == n) last = best[n - 1];
-        if (tid == 0) have = left;
-        __syncthreads();
+    auto beam_of = [&](int l) { return P.by_S ? static_cast<int>(__umulhi(static_cast<unsigned>(l), P.by_S)) : l; };
+    auto in_front = [](double ka, const Found& a, double kb, const Found& c) {
+        if (ka != kb) return ka > kb;
+        if (a.beam != c.beam) return a.beam < c.beam;
+        return a.z != c.z ? a.z > c.z : a.token1 < c.token1;
     };
-    const long total = lists * n;
-    long quiet = 0;
+    double last_key = -__builtin_inf();                       // the n-th best of what has been ordered
+    Found last = {kBeamWidest, 0, 0.0f};
     int count = have;
     __syncthreads();
-    for (long k0 = 0; k0 < total && quiet < lists; k0 += kWG) {
-        const long k = k0 + tid;
-        bool take = false;
-        Ranked me = {0.0, 0, 0, 0.0f};
-        if (k < total) {
-            const int r = static_cast<int>(k / lists), l = static_cast<int>(k - static_cast<long>(r) * lists), w = l / S;
-            if (beam_runs(P, first + w) && r < P.count[static_cast<size_t>(b) * lists + l]) {
-                const float2 c = P.cand[(out + r) * lists + l];
-                const double s = static_cast<double>(score_of(P, first + w)) + (static_cast<double>(c.x) - norm[w]);
-                me = Ranked{weights ? s * static_cast<double>(weights[w]) : s, w, static_cast<int>(__float_as_uint(c.y)) + 1, c.x};
-                take = before(me, last);
+    // the n best of found[0 .. count) to its front, best first; 16 lanes an entry
+    auto order = [&]() {
+        for (int k0 = 0; k0 < count; k0 += T / 16) {
+            const int k = k0 + tid / 16;
+            int rank = 0;
+            if (k < count) {
+                const double mine = key[k];
+                for (int j = tid % 16; j < count; j += 16) {
+                    const double other = key[j];
+                    if (other > mine) ++rank;
+                    else if (other == mine && j != k) rank += in_front(other, found[j], mine, found[k]);
+                }
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 16);
+            if (k < count && tid % 16 == 0 && rank < n) {
+                best_key[rank] = key[k];
+                best[rank] = found[k];
             }
         }
-        if (take) found[atomicAdd(&have, 1)] = me;
         __syncthreads();
-        const int now = have;
+        count = count < n ? count : n;
+        for (int k = tid; k < count; k += T) {
+            key[k] = best_key[k];
+            found[k] = best[k];
+        }
+        if (count == n) last_key = best_key[n - 1], last = best[n - 1];
+        if (tid == 0) have = count;
         __syncthreads();
-        quiet = now == count ? quiet + kWG : 0;
-        count = now;
-        if (count >= 2 * kWG || (count > n && last.beam == kNoBeam)) {
-            rank_found(count);
-            count = have;
+    };
+    for (int k0 = 0; k0 < total; k0 += T * kMergeEach) {
+        if (k0 > 0) load(k0);
+        double rank[kMergeEach];
+        double most = -__builtin_inf();
+        {
+            int l = (k0 + tid) % lists;
+#pragma unroll
+            for (int i = 0; i < kMergeEach; ++i) {
+                const int w = beam_of(l);
+                const float from = base[w];
+                rank[i] = -__builtin_inf();
+                if (from == from && z[i] > -__builtin_inff())
+                    rank[i] = (static_cast<double>(from) + (static_cast<double>(z[i]) - norm[w])) * static_cast<double>(factor[w]);
+                most = rank[i] > most ? rank[i] : most;
+                l += column_step;
+                l -= l >= lists ? lists : 0;
+            }
+        }
+        const unsigned word = ordered_high(most);
+        const int q = (n + NW - 1) / NW;
+        unsigned bound = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const unsigned c = bound | 1u << bit;
+            if (__popcll(__ballot(word >= c)) >= q) bound = c;
+        }
+        if (tid % 64 == 0) wave_bound[wave] = bound;
+        __syncthreads();
+        for (int i = 0; i < NW; ++i) bound = wave_bound[i] < bound ? wave_bound[i] : bound;
+        // (an entry that is none has the word of -inf; every other one a larger word)
+        const unsigned none = ordered_high(-__builtin_inf());
+        bound = bound > none ? bound : none + 1;
+        int reach, at, all;
+        auto places = [&]() {                                 // of a thread's entries that reach the bound (in any order: they are put into order afterwards)
+            reach = 0;
+#pragma unroll
+            for (int i = 0; i < kMergeEach; ++i) reach += ordered_high(rank[i]) >= bound && rank[i] >= last_key;
+            int upto = reach;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int other = __shfl_up(upto, o, 64);
+                if (tid % 64 >= o) upto += other;
+            }
+            at = 0;
+            if (tid % 64 == 63) at = atomicAdd(&have, upto);
+            at = __shfl(at, 63, 64) + upto - reach;
             __syncthreads();
+            all = have;
+        };
+        places();
+        if (all - count > kMergeFew) {
+            // A bound far under the n-th largest (one beam's lists have most of the best): bit by bit, by all entries
+            bound = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const unsigned c = bound | 1u << bit;
+                int n_c = 0;
+#pragma unroll
+                for (int i = 0; i < kMergeEach; ++i) n_c += __popcll(__ballot(ordered_high(rank[i]) >= c));
+                if (tid % 64 == 0) wave_count[bit & 1][wave] = n_c;
+                __syncthreads();
+                n_c = 0;
+                for (int i = 0; i < NW; ++i) n_c += wave_count[bit & 1][i];
+                if (n_c >= n) bound = c;
+            }
+            bound = bound > none ? bound : none + 1;
+            if (tid == 0) have = count;
+            __syncthreads();
+            places();
+        }
+        if (all <= kRoom) {
+            if (reach != 0) {
+#pragma unroll
+                for (int i = 0; i < kMergeEach; ++i) {
+                    if (ordered_high(rank[i]) >= bound && rank[i] >= last_key) {
+                        key[at] = rank[i];
+                        found[at] = Found{beam_of((k0 + i * T + tid) % lists), token[i] + 1, z[i]};
+                        ++at;
+                    }
+                }
+            }
+            count = all;
+            __syncthreads();
+            order();
+        } else {
+            // more than there is room for (equal ranks, lists of very unequal length): one entry a thread at a time
+            __syncthreads();
+            if (tid == 0) have = count;
+            __syncthreads();
+            if (count > n) order();
+#pragma unroll 1
+            for (int i = 0; i < kMergeEach; ++i) {
+                const int k = k0 + i * T + tid;
+                double mine = rank[0];
+#pragma unroll
+                for (int j = 1; j < kMergeEach; ++j) mine = i == j ? rank[j] : mine;
+                if (mine > -__builtin_inf()) {
+                    const float2 c = cand[k];
+                    const Found me = {beam_of(k % lists), static_cast<int>(__float_as_uint(c.y)) + 1, c.x};
+                    if (in_front(mine, me, last_key, last)) {
+                        const int to = atomicAdd(&have, 1);
+                        key[to] = mine;
+                        found[to] = me;
+                    }
+                }
+                __syncthreads();
+                count = have;
+                __syncthreads();
+                if (count > n) order();
+            }
+            order();
         }
     }
-    rank_found(count);
-    count = have;
-    for (int i = tid; i < n; i += kWG) {
+    for (int i = tid; i < n; i += T) {
         const bool some = i < count;
-        const Ranked me = found[some ? i : 0];
         float s = -__builtin_inff();
+        Found me = {-1, 0, 0.0f};
         if (some) {
-            s = score_of(P, first + me.beam);
+            me = found[i];
+            s = so_far[me.beam];
             if (me.token1 > 0) s = static_cast<float>(static_cast<double>(s) + (static_cast<double>(me.z) - norm[me.beam]));
         }
         P.scores_out[out + i] = s;
-        P.parent[out + i] = some ? me.beam : -1;
-        P.tokens[out + i] = some ? me.token1 - 1 : -1;
+        P.parent[out + i] = me.beam;
+        P.tokens[out + i] = me.token1 - 1;
     }
     if (tid == 0 && P.status) P.status[b] = 0;
 }

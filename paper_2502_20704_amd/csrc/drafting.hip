@@ -38,29 +38,31 @@ inline bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) %
 
 // ------------------------------------------------------------------------------------------ selection
 
-// How a row is cut: the larger the slices, the fewer entries their lists have; but a call of few rows wants workgroups on all compute units.
+// How a row is cut: into as many slices as fill the GPU once (four workgroups a compute unit, what their registers allow), each of several chunks; in a
+// call of few rows into chunks, and these made smaller while compute units are left over.
 struct BeamShape { int slots, len, S; };
-constexpr long kBeamWGs = 1024;
+constexpr long kBeamWGs = 1024, kBeamFew = 512;
 bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
     if (dtype != FSD_F32 && dtype != FSD_BF16) return false;
     if (B < 1 || B > kMaxBatch || W < 1 || W > kBeamWidest || n < 1 || n > kBeamMost || V < 1 || V > fsd_max_vocab(dtype)) return false;
     const int E = dtype == FSD_BF16 ? 8 : 4;
     const long rows = static_cast<long>(B) * W;
-    s->slots = 8;
-    while (s->slots > 1 && rows * ((V + kWG * E * s->slots - 1) / (kWG * E * s->slots)) < kBeamWGs) s->slots /= 2;
-    const int most = kWG * E * s->slots, S = (V + most - 1) / most;
+    auto chunks = [&](int slots) { return (V + kWG * E * slots - 1) / (kWG * E * slots); };
+    s->slots = 4;
+    while (s->slots > 1 && rows * chunks(s->slots) < kBeamFew) s->slots /= 2;
+    int S = chunks(s->slots);
+    if (rows * S > kBeamWGs) S = rows < kBeamWGs ? static_cast<int>(kBeamWGs / rows) : 1;
     s->len = ((V + S - 1) / S + E - 1) / E * E;              // slices of one length, so that none of them is a remnant
     s->S = (V + s->len - 1) / s->len;
     return rows * s->S <= kMaxGroups;
 }
-struct BeamSpace { size_t stat, cand, count, bytes; };
+struct BeamSpace { size_t stat, cand, bytes; };
 BeamSpace beam_space(const BeamShape& s, int B, int W, int n) {
     Space a;
     BeamSpace w;
     const size_t lists = static_cast<size_t>(B) * W * s.S;
     w.stat = a.take(lists * sizeof(double2));
     w.cand = a.take(lists * n * sizeof(float2));
-    w.count = a.take(lists * sizeof(int));
     w.bytes = a.bytes;
     return w;
 }
@@ -69,8 +71,7 @@ void launch_beam_slices(hipStream_t st, unsigned grid, int slots, const BeamPara
     const dim3 g(grid), t(kWG);
     if (slots == 1) hipLaunchKernelGGL((beam_slices<BF16, 1>), g, t, 0, st, P);
     else if (slots == 2) hipLaunchKernelGGL((beam_slices<BF16, 2>), g, t, 0, st, P);
-    else if (slots == 4) hipLaunchKernelGGL((beam_slices<BF16, 4>), g, t, 0, st, P);
-    else hipLaunchKernelGGL((beam_slices<BF16, 8>), g, t, 0, st, P);
+    else hipLaunchKernelGGL((beam_slices<BF16, 4>), g, t, 0, st, P);
 }
 
 // ------------------------------------------------------------------------------------------ pages
@@ -167,9 +168,9 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     P.done = done;
     P.B = B; P.W = beams; P.V = V; P.n = n;
     P.len = s.len; P.S = s.S; P.lists = beams * s.S;
+    P.by_S = s.S == 1 ? 0u : static_cast<unsigned>(((1ul << 32) + s.S - 1) / s.S);
     P.stat = reinterpret_cast<double2*>(base + w.stat);
     P.cand = reinterpret_cast<float2*>(base + w.cand);
-    P.count = reinterpret_cast<int*>(base + w.count);
     P.scores_out = scores_out;
     P.parent = parent;
     P.tokens = tokens;
@@ -178,7 +179,8 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     const unsigned grid = static_cast<unsigned>(static_cast<long>(B) * P.lists);
     if (dtype == FSD_BF16) launch_beam_slices<true>(st, grid, s.slots, P);
     else launch_beam_slices<false>(st, grid, s.slots, P);
-    hipLaunchKernelGGL(beam_merge, dim3(static_cast<unsigned>(B)), dim3(kWG), 0, st, P);
+    if (P.lists * n <= 256 * kMergeEach) hipLaunchKernelGGL((beam_merge<256>), dim3(static_cast<unsigned>(B)), dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((beam_merge<1024>), dim3(static_cast<unsigned>(B)), dim3(1024), 0, st, P);
     return launched();
 }
 
