@@ -412,7 +412,10 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
 // ------------------------------------------------------------------------------------------ merging
 
 // A continuation: its rank, (beam, token + 1), its logit.  A rank's rounding may take logits of one beam for equal: then the logits decide.
-struct Found { int beam, token1; float z; };
+// As a word, the lower of which comes first among equal ranks: 8 bits of the beam, 32 of the logit, the larger the lower, 20 of token + 1.
+__device__ __forceinline__ unsigned long found_word(int beam, float z, int token1) {
+    return static_cast<unsigned long>(beam) << 52 | static_cast<unsigned long>(~ordered(z)) << 20 | static_cast<unsigned>(token1);
+}
 constexpr int kMergeEach = 16;      // list entries that a thread holds at once
 constexpr int kMergeFew = 256;      // entries that are put into order as they are; of more, the n best are looked for first
 
@@ -427,10 +430,10 @@ __device__ __forceinline__ unsigned ordered_high(double x) {
 template <int T>
 __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     constexpr int NW = T / 64, kRoom = T + kBeamMost;
-    __shared__ double key[kRoom];
-    __shared__ Found found[kRoom];
+    __shared__ double key[kRoom + 8];
+    __shared__ unsigned long found[kRoom + 8];
     __shared__ double best_key[kBeamMost];
-    __shared__ Found best[kBeamMost];
+    __shared__ unsigned long best[kBeamMost];
     __shared__ double norm[kBeamWidest];
     __shared__ float base[kBeamWidest];                       // a beam's score; NaN: its list does not count
     __shared__ float so_far[kBeamWidest];
@@ -466,6 +469,9 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         double m = -__builtin_inf(), s = 0.0;
         float score = 0.0f, by = 1.0f;
         bool lives = false, ended = false, runs = false, broken = false;
+        const double2* stat = P.stat + (first + w) * S;
+        double2 own = make_double2(m, 0.0);
+        if (w < W && part < S) own = stat[part];              // (of a beam that does not run, anything: requested together with what says so)
         if (w < W) {
             score = score_of(P, first + w);
             if (P.weights) by = P.weights[first + w];
@@ -474,9 +480,6 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
             broken = lives && !(score < __builtin_inff() && by > 0.0f && by < __builtin_inff());
             runs = lives && score == score && !ended;
         }
-        const double2* stat = P.stat + (first + w) * S;
-        double2 own = make_double2(m, 0.0);
-        if (runs && part < S) own = stat[part];
         if (runs) {
             m = own.x;
             broken |= own.y != own.y;
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
             if (lives && ended && !broken) {                  // a finished beam, as it stands
                 const int at = atomicAdd(&have, 1);
                 key[at] = static_cast<double>(score) * static_cast<double>(by);
-                found[at] = Found{w, 0, 0.0f};
+                found[at] = found_word(w, 0.0f, 0);
             }
         }
     }
@@ -525,33 +528,25 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         return;
     }
     auto beam_of = [&](int l) { return P.by_S ? static_cast<int>(__umulhi(static_cast<unsigned>(l), P.by_S)) : l; };
-    auto in_front = [](double ka, const Found& a, double kb, const Found& c) {
-        if (ka != kb) return ka > kb;
-        if (a.beam != c.beam) return a.beam < c.beam;
-        return a.z != c.z ? a.z > c.z : a.token1 < c.token1;
-    };
     double last_key = -__builtin_inf();                       // the n-th best of what has been ordered
-    Found last = {kBeamWidest, 0, 0.0f};
+    unsigned long last = ~0ul;
     int count = have;
     __syncthreads();
-    // the n best of found[0 .. count) to its front, best first; 16 lanes an entry
+    // the n best of found[0 .. count) to its front, best first: a thread an entry, which all others are compared with (a broadcast each)
     auto order = [&]() {
-        for (int k0 = 0; k0 < count; k0 += T / 16) {
-            const int k = k0 + tid / 16;
+        if (tid < 8) key[count + tid] = -__builtin_inf();
+        __syncthreads();
+        for (int k = tid; k < count; k += T) {
+            const double mine = key[k];
+            const unsigned long me = found[k];
             int rank = 0;
-            if (k < count) {
-                const double mine = key[k];
-                for (int j = tid % 16; j < count; j += 16) {
-                    const double other = key[j];
-                    if (other > mine) ++rank;
-                    else if (other == mine && j != k) rank += in_front(other, found[j], mine, found[k]);
-                }
-            }
+            for (int j = 0; j < count; j += 8) {
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 16);
-            if (k < count && tid % 16 == 0 && rank < n) {
-                best_key[rank] = key[k];
-                best[rank] = found[k];
+                for (int u = 0; u < 8; ++u) rank += (key[j + u] > mine) | ((key[j + u] == mine) & (found[j + u] < me));
+            }
+            if (rank < n) {
+                best_key[rank] = mine;
+                best[rank] = me;
             }
         }
         __syncthreads();
@@ -585,7 +580,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         const unsigned word = ordered_high(most);
         const int q = (n + NW - 1) / NW;
         unsigned bound = 0;
-        for (int bit = 31; bit >= 0; --bit) {
+        for (int bit = 31; bit >= 12; --bit) {                // (the upper 20 bits)
             const unsigned c = bound | 1u << bit;
             if (__popcll(__ballot(word >= c)) >= q) bound = c;
         }
@@ -595,20 +590,14 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         // (an entry that is none has the word of -inf; every other one a larger word)
         const unsigned none = ordered_high(-__builtin_inf());
         bound = bound > none ? bound : none + 1;
-        int reach, at, all;
-        auto places = [&]() {                                 // of a thread's entries that reach the bound (in any order: they are put into order afterwards)
+        int reach, at, all;                                   // of the wavefront; where its first goes; of the workgroup
+        auto places = [&]() {                                 // of the wavefront's entries that reach the bound (in any order: they are put into order afterwards)
             reach = 0;
 #pragma unroll
-            for (int i = 0; i < kMergeEach; ++i) reach += ordered_high(rank[i]) >= bound && rank[i] >= last_key;
-            int upto = reach;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int other = __shfl_up(upto, o, 64);
-                if (tid % 64 >= o) upto += other;
-            }
+            for (int i = 0; i < kMergeEach; ++i) reach += __popcll(__ballot(ordered_high(rank[i]) >= bound && rank[i] >= last_key));
             at = 0;
-            if (tid % 64 == 63) at = atomicAdd(&have, upto);
-            at = __shfl(at, 63, 64) + upto - reach;
+            if (tid % 64 == 0 && reach != 0) at = atomicAdd(&have, reach);
+            at = __builtin_amdgcn_readfirstlane(at);
             __syncthreads();
             all = have;
         };
@@ -636,11 +625,14 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
             if (reach != 0) {
 #pragma unroll
                 for (int i = 0; i < kMergeEach; ++i) {
-                    if (ordered_high(rank[i]) >= bound && rank[i] >= last_key) {
-                        key[at] = rank[i];
-                        found[at] = Found{beam_of((k0 + i * T + tid) % lists), token[i] + 1, z[i]};
-                        ++at;
+                    const bool is = ordered_high(rank[i]) >= bound && rank[i] >= last_key;
+                    const unsigned long who = __ballot(is);
+                    if (is) {
+                        const int to = at + __popcll(who & ((1ul << (tid % 64)) - 1));
+                        key[to] = rank[i];
+                        found[to] = found_word(beam_of((k0 + i * T + tid) % lists), z[i], token[i] + 1);
                     }
+                    at += __popcll(who);
                 }
             }
             count = all;
@@ -660,8 +652,8 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 for (int j = 1; j < kMergeEach; ++j) mine = i == j ? rank[j] : mine;
                 if (mine > -__builtin_inf()) {
                     const float2 c = cand[k];
-                    const Found me = {beam_of(k % lists), static_cast<int>(__float_as_uint(c.y)) + 1, c.x};
-                    if (in_front(mine, me, last_key, last)) {
+                    const unsigned long me = found_word(beam_of(k % lists), c.x, static_cast<int>(__float_as_uint(c.y)) + 1);
+                    if (mine > last_key || (mine == last_key && me < last)) {
                         const int to = atomicAdd(&have, 1);
                         key[to] = mine;
                         found[to] = me;
@@ -678,15 +670,17 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     for (int i = tid; i < n; i += T) {
         const bool some = i < count;
         float s = -__builtin_inff();
-        Found me = {-1, 0, 0.0f};
+        int beam = -1, token1 = 0;
         if (some) {
-            me = found[i];
-            s = so_far[me.beam];
-            if (me.token1 > 0) s = static_cast<float>(static_cast<double>(s) + (static_cast<double>(me.z) - norm[me.beam]));
+            const unsigned long me = found[i];
+            beam = static_cast<int>(me >> 52);
+            token1 = static_cast<int>(me & 0xFFFFFu);
+            s = so_far[beam];
+            if (token1 > 0) s = static_cast<float>(static_cast<double>(s) + (static_cast<double>(from_ordered(~static_cast<unsigned>(me >> 20))) - norm[beam]));
         }
         P.scores_out[out + i] = s;
-        P.parent[out + i] = me.beam;
-        P.tokens[out + i] = me.token1 - 1;
+        P.parent[out + i] = beam;
+        P.tokens[out + i] = token1 - 1;
     }
     if (tid == 0 && P.status) P.status[b] = 0;
 }

@@ -99,13 +99,12 @@ PagesPair pages_pair(const fsd_cache& a, const fsd_cache& b) {
 inline int chunks_of(int num_blocks) { return (num_blocks + kPagesChunk - 1) / kPagesChunk; }
 inline unsigned copy_groups(long units) { return static_cast<unsigned>(units < kCopyWGs ? units : kCopyWGs); }
 
-struct ForkSpace { size_t released, shared, claim, free_list, free_count, seq, fresh, copies, at, copy_seq, totals, bytes; };
+struct ForkSpace { size_t counts, claim, free_list, free_count, seq, fresh, copies, at, copy_seq, totals, bytes; };
 ForkSpace fork_space(int P, int n) {
     Space a;
     ForkSpace w;
     const size_t blocks = static_cast<size_t>(P) * 4, seqs = static_cast<size_t>(n);
-    w.released = a.take(blocks);
-    w.shared = a.take(blocks);
+    w.counts = a.take(2 * blocks);
     w.claim = a.take(blocks);
     w.free_list = a.take(blocks);
     w.free_count = a.take(static_cast<size_t>(chunks_of(P)) * 4);
@@ -180,7 +179,7 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     if (dtype == FSD_BF16) launch_beam_slices<true>(st, grid, s.slots, P);
     else launch_beam_slices<false>(st, grid, s.slots, P);
     if (P.lists * n <= 256 * kMergeEach) hipLaunchKernelGGL((beam_merge<256>), dim3(static_cast<unsigned>(B)), dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((beam_merge<1024>), dim3(static_cast<unsigned>(B)), dim3(1024), 0, st, P);
+    else hipLaunchKernelGGL((beam_merge<512>), dim3(static_cast<unsigned>(B)), dim3(512), 0, st, P);
     return launched();
 }
 
@@ -248,8 +247,7 @@ int fsd_cache_fork(const fsd_cache* cache, int B, const int32_t* refs, const int
     P.refs_out = refs_out;
     P.free_out = free_blocks;
     P.status = row_status;
-    P.released = ints(w.released);
-    P.shared = ints(w.shared);
+    P.counts = reinterpret_cast<unsigned long*>(base + w.counts);
     P.claim = ints(w.claim);
     P.free_list = ints(w.free_list);
     P.free_count = ints(w.free_count);
@@ -263,12 +261,17 @@ int fsd_cache_fork(const fsd_cache* cache, int B, const int32_t* refs, const int
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const int chunks = chunks_of(P.P);
     const dim3 t(kWG);
+    const unsigned movers = copy_groups(static_cast<long>(n) * c.layers * c.kv_heads);
+    if (P.P <= kSmallBlocks && n <= kSmallWG && (static_cast<long>(B) + n) * P.M <= kSmallPlaces) {
+        hipLaunchKernelGGL(fork_small, dim3(1), dim3(kSmallWG), 0, st, P);
+        hipLaunchKernelGGL(fork_move, dim3(movers), t, 0, st, P);
+        return launched();
+    }
     const long clear = (static_cast<long>(P.P) + kWG - 1) / kWG;
     hipLaunchKernelGGL(fork_clear, dim3(static_cast<unsigned>(clear < 2048 ? clear : 2048)), t, 0, st, P);
     hipLaunchKernelGGL(fork_mark, dim3(static_cast<unsigned>(B + n)), t, 0, st, P);
     hipLaunchKernelGGL(fork_count, dim3(static_cast<unsigned>(chunks + (n + kWG / 64 - 1) / (kWG / 64))), t, 0, st, P, chunks);
     hipLaunchKernelGGL(fork_list, dim3(static_cast<unsigned>(chunks + (n + kWG - 1) / kWG)), t, 0, st, P, chunks);
-    const unsigned movers = copy_groups(static_cast<long>(n) * c.layers * c.kv_heads);
     hipLaunchKernelGGL(fork_apply, dim3(static_cast<unsigned>(chunks + n) + movers), t, 0, st, P, chunks);
     return launched();
 }
@@ -344,9 +347,14 @@ int fsd_cache_compact(const fsd_cache* cache, int B, const int32_t* refs, int32_
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const int chunks = chunks_of(P.P);
     const dim3 t(kWG);
+    const unsigned movers = copy_groups(static_cast<long>(c.num_blocks / 2 + 1) * c.layers * c.kv_heads);
+    if (P.P <= kSmallBlocks && B <= kSmallWG && static_cast<long>(B) * P.M <= kSmallPlaces) {
+        hipLaunchKernelGGL(compact_small, dim3(1), dim3(kSmallWG), 0, st, P);
+        hipLaunchKernelGGL(compact_move, dim3(movers), t, 0, st, P);
+        return launched();
+    }
     hipLaunchKernelGGL(compact_count, dim3(static_cast<unsigned>(chunks)), t, 0, st, P);
     hipLaunchKernelGGL(compact_list, dim3(static_cast<unsigned>(chunks)), t, 0, st, P, chunks);
-    const unsigned movers = copy_groups(static_cast<long>(c.num_blocks / 2 + 1) * c.layers * c.kv_heads);
     hipLaunchKernelGGL(compact_apply, dim3(static_cast<unsigned>(chunks + B) + movers), t, 0, st, P, chunks);
     return launched();
 }
