@@ -524,7 +524,7 @@ int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_strid
  *                          everywhere is none of that: a grammar that has ended a beam.)
  *   workspace              fsd_beam_workspace_bytes(...) bytes, 256-byte aligned
  * No output shares a byte with another one, scores, weights, done or the workspace (FSD_ERR_LAYOUT).
- * 1 <= beams <= 256, 1 <= n <= 128, V <= fsd_max_vocab(dtype), B <= 65535, B * beams * ceil(V / 16384) < 2^24 (FSD_F32: V / 8192).
+ * 1 <= beams <= 256, 1 <= n <= 128, 1 <= V <= fsd_max_vocab(dtype), 1 <= B <= 65535.
  */
 size_t fsd_beam_workspace_bytes(int B, int beams, int V, int n, int dtype);
 int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores, const float* weights, const int32_t* done, int B,

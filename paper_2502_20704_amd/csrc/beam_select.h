@@ -13,10 +13,14 @@
 
 namespace {
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kBeamMost = 128;      // n
 constexpr int kBeamWidest = 256;    // beams
 constexpr int kWaveList = 256;      // entries of a wavefront's part of a slice that stand in LDS before the n best are taken from all
-constexpr int kAside = 128;         // slots of a wavefront's that stand there until they are taken apart
+constexpr unsigned short kTableBase = 0x397F;   // bits of the last bfloat16 number under 2^-12
+constexpr unsigned short kTableEnd = 0x4280 - kTableBase + 1;   // entries of either sign: 0, 2^-12 to the last number under 64, 64 and over
+constexpr int kAside = 112;         // slots of a wavefront's that stand there until they are taken apart
 constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct BeamParams {
@@ -26,6 +30,7 @@ struct BeamParams {
     const int* done;
     int B, W, V, n;
     int len, S, lists;              // entries of a slice (a multiple of a 16-byte slot's), slices of a row, W * S
+    unsigned units;                 // B * W * S
     unsigned by_S;                  // ceil(2^32 / S), 0 where S is 1
     float2* cand;                   // [B, n, W * S]: logit and token of a list's entry, best first; -inf behind the last
     double2* stat;                  // [B, W * S]: a number r and the sum of e^(z - r); -inf and 0 where no entry counts
@@ -88,7 +93,7 @@ __device__ __forceinline__ bool beam_runs(const BeamParams& P, long at) {   // w
 // A slice's n best entries where more than kWaveList of a wavefront's reach the bound that its lanes gave (rows of equal entries, or in order): the n-th largest
 // is found bit by bit, then what is above it and, from the lowest index on, what equals it go into the list.  Returns how many.  (It reads the entries
 // again rather than keep the calling kernel's registers in memory; 40 passes over what the caches hold.)
-template <bool BF16>
+template <bool BF16, int NW>
 __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, unsigned long* list, int* lds, int tid) {
     const int wave = tid / 64, lane = tid % 64, len = end - begin;
     auto over_wg = [&](int c) {                              // the sum of all threads' c
@@ -97,26 +102,28 @@ __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, 
         __syncthreads();
         if (lane == 0) lds[wave] = c;
         __syncthreads();
-        return lds[0] + lds[1] + lds[2] + lds[3];
+        int all = 0;
+        for (int w = 0; w < NW; ++w) all += lds[w];
+        return all;
     };
     auto word_at = [&](int k) { return ordered(load_logit<BF16>(z, begin + k) + 0.0f); };
     unsigned least = 0;
     for (int bit = 31; bit >= (BF16 ? 16 : 0); --bit) {
         const unsigned c = least | 1u << bit;
         int have = 0;
-        for (int k = tid; k < len; k += kWG) have += word_at(k) >= c;
+        for (int k = tid; k < len; k += 64 * NW) have += word_at(k) >= c;
         if (over_wg(have) >= n) least = c;
     }
     // (of bfloat16 entries the low 16 bits: 0 of a positive one, 1 of a negative one; the bits found say which)
     if (BF16 && !(least & 0x80000000u)) least |= 0xFFFFu;
     if (least < kLeastOrdered) least = kLeastOrdered;
     int above = 0;
-    for (int k = tid; k < len; k += kWG) above += word_at(k) > least;
+    for (int k = tid; k < len; k += 64 * NW) above += word_at(k) > least;
     const int more = over_wg(above);
-    if (tid == 0) lds[4] = 0;
+    if (tid == 0) lds[NW] = 0;
     int before = 0;                                          // entries that equal it, of those behind us
     __syncthreads();
-    for (int k0 = 0; k0 < len; k0 += kWG) {
+    for (int k0 = 0; k0 < len; k0 += 64 * NW) {
         const int k = k0 + tid;
         const unsigned o = k < len ? word_at(k) : 0u;
         const unsigned long same = __ballot(o == least);
@@ -125,11 +132,11 @@ __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, 
         __syncthreads();
         int at = before + __popcll(same & ((1ul << lane) - 1));
         for (int w = 0; w < wave; ++w) at += lds[w];
-        before += lds[0] + lds[1] + lds[2] + lds[3];
-        if (o > least || (o == least && at < n - more)) list[atomicAdd(&lds[4], 1)] = static_cast<unsigned long>(o) << 32 | ~static_cast<unsigned>(k);
+        for (int w = 0; w < NW; ++w) before += lds[w];
+        if (o > least || (o == least && at < n - more)) list[atomicAdd(&lds[NW], 1)] = static_cast<unsigned long>(o) << 32 | ~static_cast<unsigned>(k);
     }
     __syncthreads();
-    return lds[4];
+    return lds[NW];
 }
 
 // Of a wavefront's list (in LDS) those that reach the bound, in their order; how many.
@@ -143,6 +150,50 @@ __device__ __forceinline__ int keep_reaching(unsigned long* list, int count, uns
         kept += __popcll(who);
     }
     return kept;
+}
+
+// The slots that a wavefront put aside, 64 entries at a time: those that reach the bound go into its list of `count`.  How many it has then; 2^16 more where they
+// are too many for it.
+template <bool BF16>
+__device__ __forceinline__ int slots_apart(const u32x4* slots, const int* places, int aside, unsigned long* list, int count, unsigned least, int lane) {
+    constexpr int E = BF16 ? 8 : 4;
+    const float from = from_ordered(least);
+    bool full = false;
+    for (int s0 = 0; s0 < aside; s0 += 64 / E) {
+        const int k = s0 + lane / E;
+        bool is = false;
+        float x = 0.0f;
+        int at = 0;
+        if (k < aside) {
+            const unsigned* words = reinterpret_cast<const unsigned*>(slots + k);
+            const int e = lane % E;
+            if constexpr (BF16) x = __uint_as_float(e & 1 ? words[e / 2] & 0xFFFF0000u : words[e / 2] << 16);
+            else x = __uint_as_float(words[e]);
+            at = places[k] * E + e;
+            is = x >= from;
+        }
+        const unsigned long who = __ballot(is);
+        const int n_who = __popcll(who);
+        // make room: what is under the bound by now goes
+        if (count + n_who > kWaveList) count = keep_reaching(list, count, least, lane);
+        const int to = count + __popcll(who & ((1ul << lane) - 1));
+        if (is && to < kWaveList) list[to] = static_cast<unsigned long>(ordered(x + 0.0f)) << 32 | ~static_cast<unsigned>(at);
+        count += n_who;
+        if (count > kWaveList) full = true, count = kWaveList;
+    }
+    return count + (full ? 0x10000 : 0);
+}
+
+// Of the entries of a slot that are nearer to 0 than the table goes, and count as 0: what that leaves out
+__device__ __forceinline__ double rest_of_small(u32x4 slot) {
+    double rest = 0.0;
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+        const unsigned w = j == 0 ? slot[0] : j == 1 ? slot[1] : j == 2 ? slot[2] : slot[3];
+        if ((w & 0x7FFFu) - 1u < kTableBase) rest += exp_within(static_cast<double>(__uint_as_float(w << 16))) - 1.0;
+        if ((w >> 16 & 0x7FFFu) - 1u < kTableBase) rest += exp_within(static_cast<double>(__uint_as_float(w & 0xFFFF0000u))) - 1.0;
+    }
+    return rest;
 }
 
 // The wavefront's q-th largest of its lanes' words, to the upper 20 bits
@@ -161,20 +212,33 @@ __device__ __forceinline__ unsigned wave_bound(unsigned word, int q) {
 // least of the four wavefronts' by n of the slice: what reaches that bound (few more than n entries where the values lie as those of logits do) is put
 // into LDS and ranked there at the end.  Wavefronts tell one another their bounds without waiting: an older one of another's bounds as well.
 // Exponentials are added up as e^z: binary64 has the range where logits are of the size that models give them.  Where they are not, the slice is gone over again.
-template <bool BF16, int NS>
-__global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
-    constexpr int E = BF16 ? 8 : 4, kChunk = kWG * NS;        // (slots of a chunk)
+// TABLE: exponentials of bfloat16 numbers are read from a table of all of them from 2^-12 to 64 of either sign (and 0, and those under -64, which
+// count as nothing), which a workgroup makes once and keeps for all of its slices: 7 instructions an entry where the polynomial takes 16.
+template <bool BF16, int NS, bool TABLE>
+__global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamParams P) {
+    constexpr int NW = TABLE ? 8 : 4, T = NW * 64;
+    static_assert(BF16 || !TABLE, "a table of bfloat16 numbers");
+    constexpr int E = BF16 ? 8 : 4, kChunk = T * NS;        // (slots of a chunk)
     constexpr unsigned kNone = BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
-    __shared__ unsigned long list[4 * kWaveList];
-    __shared__ u32x4 aside_slot[4][kAside];
-    __shared__ int aside_at[4][kAside];
-    __shared__ double wave_sum[4], wave_ref[4];
-    __shared__ unsigned bounds[4];
-    __shared__ int lds[5];
+    __shared__ unsigned long list[NW * kWaveList];
+    __shared__ u32x4 aside_slot[NW][kAside];
+    __shared__ int aside_at[NW][kAside];
+    __shared__ double table[TABLE ? 2 * kTableEnd : 1];
+    __shared__ double wave_sum[NW], wave_ref[NW];
+    __shared__ unsigned bounds[NW];
+    __shared__ int lds[NW + 1];
     const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-    const unsigned row = blockIdx.x / static_cast<unsigned>(P.S);
-    const int slice = static_cast<int>(blockIdx.x - row * static_cast<unsigned>(P.S));
-    if (!beam_runs(P, row)) return;
+    if constexpr (TABLE) {
+        for (int k = tid; k < 2 * kTableEnd; k += T) {
+            const int u = k < kTableEnd ? k : k - kTableEnd;
+            const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
+            table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
+        }
+    }
+    for (unsigned unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
+    const unsigned row = unit / static_cast<unsigned>(P.S);
+    const int slice = static_cast<int>(unit - row * static_cast<unsigned>(P.S));
+    if (!beam_runs(P, row)) continue;
     const int begin = slice * P.len, end = begin + P.len < P.V ? begin + P.len : P.V;
     const char* const z = P.logits + static_cast<size_t>(row) * P.row_stride;
     const char* const at_begin = z + static_cast<size_t>(begin) * (16 / E);
@@ -189,7 +253,7 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
     for (int i = 0; i < NS; ++i) r[i] = u32x4{kNone, kNone, kNone, kNone};
     if (slots > 0) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i) r[i] = request(i * kWG + tid);
+        for (int i = 0; i < NS; ++i) r[i] = request(i * T + tid);
     }
     // the entries behind the last whole slot: its thread takes them one by one
     u32x4 last = {kNone, kNone, kNone, kNone};
@@ -215,38 +279,18 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
     int count = 0;                                            // of the wavefront's list
     bool full = false;                                        // whether more were to go into it than it holds
     int aside = 0;
-    const int q = (P.n + 3) / 4;
+    const int q = (P.n + NW - 1) / NW;
     unsigned least = kLeastOrdered;
-    auto take_apart = [&]() {                                 // the slots that were put aside, 64 entries at a time
-        const float from = from_ordered(least);
-        for (int s0 = 0; s0 < aside; s0 += 64 / E) {
-            const int k = s0 + lane / E;
-            bool is = false;
-            float x = 0.0f;
-            int at = 0;
-            if (k < aside) {
-                const unsigned* words = reinterpret_cast<const unsigned*>(&aside_slot[wave][k]);
-                const int e = lane % E;
-                if constexpr (BF16) x = __uint_as_float(e & 1 ? words[e / 2] & 0xFFFF0000u : words[e / 2] << 16);
-                else x = __uint_as_float(words[e]);
-                at = aside_at[wave][k] * E + e;
-                is = x >= from;
-            }
-            const unsigned long who = __ballot(is);
-            const int n_who = __popcll(who);
-            // make room: what is under the bound by now goes
-            if (count + n_who > kWaveList) count = keep_reaching(mine_list, count, least, lane);
-            const int to = count + __popcll(who & ((1ul << lane) - 1));
-            if (is && to < kWaveList) mine_list[to] = static_cast<unsigned long>(ordered(x + 0.0f)) << 32 | ~static_cast<unsigned>(at);
-            count += n_who;
-            if (count > kWaveList) full = true, count = kWaveList;
-        }
+    auto take_apart = [&]() {
+        const int to = slots_apart<BF16>(aside_slot[wave], aside_at[wave], aside, mine_list, count, least, lane);
+        count = to & 0xFFFF;
+        full |= to > 0xFFFF;
         aside = 0;
     };
     auto all_bounds = [&]() {
         unsigned bound = 0xFFFFFFFFu;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const unsigned theirs = __hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             bound = theirs < bound ? theirs : bound;
         }
@@ -263,7 +307,7 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
     float mine = -__builtin_inff();                           // the lane's largest so far
     if (kChunk > slots) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i) behind(r[i], i * kWG + tid);
+        for (int i = 0; i < NS; ++i) behind(r[i], i * T + tid);
     }
 #pragma unroll
     for (int i = 0; i < NS; ++i) mine = __builtin_fmaxf(mine, slot_max(r[i]));
@@ -282,7 +326,7 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
         const bool ends = first + 2 * kChunk > slots;         // whether the next chunk is not whole, or none
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            const int slot = first + i * kWG + tid;
+            const int slot = first + i * T + tid;
             const float top = slot_max(r[i]);
             mine = __builtin_fmaxf(mine, top);
             // a slot with an entry that reaches the bound is put aside whole, to be taken apart with others
@@ -296,13 +340,37 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
                 aside += __popcll(who);
                 if (aside > kAside - 64) take_apart();
             }
-            // (what is under -700 counts as -700: nothing beside a largest entry of -600 or more)
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                const float x = slot_entry<BF16>(r[i], e), y = slot_entry<BF16>(r[i], e + 1);
-                broken |= __builtin_isunordered(x, y);
-                sum[0] += exp_within(static_cast<double>(at_least_700_below(x)));
-                sum[1] += exp_within(static_cast<double>(at_least_700_below(y)));
+            for (int e = 0; e < E; e += 2) broken |= __builtin_isunordered(slot_entry<BF16>(r[i], e), slot_entry<BF16>(r[i], e + 1));
+            if constexpr (TABLE) {                            // (also where it does not hold: then all of it is gone over again)
+                u16x2 least_index = {0xFFFF, 0xFFFF}, index[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned w = r[i][j];
+                    const u16x2 v = __builtin_bit_cast(u16x2, w);
+                    u16x2 u = __builtin_elementwise_sub_sat(v & static_cast<unsigned short>(0x7FFF), u16x2{kTableBase, kTableBase});
+                    u = __builtin_elementwise_min(u, u16x2{kTableEnd - 1, kTableEnd - 1});
+                    least_index = __builtin_elementwise_min(least_index, u);
+                    index[j] = (v >> static_cast<unsigned short>(15)) * static_cast<unsigned short>(kTableEnd) + u;
+                }
+                double e[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    e[2 * j] = table[index[j].x];
+                    e[2 * j + 1] = table[index[j].y];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j & 1] += e[j];
+                if (__ballot(least_index.x == 0 || least_index.y == 0) != 0) {
+                    sum[0] += rest_of_small(r[i]);            // (in a few slots of a hundred)
+                }
+            } else {
+                // (what is under -700 counts as -700: nothing beside a largest entry of -600 or more)
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    sum[0] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e))));
+                    sum[1] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e + 1))));
+                }
             }
             if (first + kChunk < all_slots) {
                 r[i] = request(slot + kChunk);
@@ -318,13 +386,16 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
     }
     const float top = wave_max_all(mine);
     double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
-    if (top > 600.0f || (top < -600.0f && top > -__builtin_inff())) {
+    if ((TABLE ? top >= 64.0f || top < -20.0f : top > 600.0f || top < -600.0f) && top > -__builtin_inff()) {
         // again, as e^(z - top)
         ref = top;
         sum[0] = sum[1] = 0.0;
-        for (int slot = tid; slot < all_slots; slot += kWG)
-            for (int e = 0; e < E && slot * E + e < end - begin; ++e)
-                sum[0] += exp_below(static_cast<double>(load_logit<BF16>(z, begin + slot * E + e)) - ref);
+        for (int slot = tid; slot < all_slots; slot += T) {
+            u32x4 x = slots > 0 ? request(slot) : u32x4{kNone, kNone, kNone, kNone};
+            behind(x, slot);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e & 1] += exp_below(static_cast<double>(slot_entry<BF16>(x, e)) - ref);
+        }
     }
     double s = sum[0] + sum[1];
 #pragma unroll
@@ -346,8 +417,13 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
     count = keep_reaching(mine_list, count, least, lane);
     if (lane == 0) lds[wave] = full ? kWaveList + 1 : count;
     __syncthreads();
-    const int c0 = lds[0], c1 = lds[1], c2 = lds[2], c3 = lds[3];
-    const int most = c0 > c1 ? c0 : c1, most2 = c2 > c3 ? c2 : c3;
+    int counts[NW], have = 0, most = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        counts[w] = lds[w];
+        have += counts[w];
+        most = counts[w] > most ? counts[w] : most;
+    }
     const size_t at = static_cast<size_t>(row) * P.S + slice;   // of [B, W * S]
     const int b = static_cast<int>(row / static_cast<unsigned>(P.W));
     const size_t lists = P.lists, column = at - static_cast<size_t>(b) * lists;
@@ -356,15 +432,11 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
         if (rank < P.n)
             cand[rank * lists] = make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
     };
-    int have;
-    if (most <= 64 && most2 <= 64) {
+    if (most <= 64) {
         // a lane holds an entry of each wavefront's; a wavefront finds the ranks of its own one after the other
-        have = c0 + c1 + c2 + c3;
-        unsigned long other[4];
-        other[0] = lane < c0 ? list[lane] : 0;
-        other[1] = lane < c1 ? list[kWaveList + lane] : 0;
-        other[2] = lane < c2 ? list[2 * kWaveList + lane] : 0;
-        other[3] = lane < c3 ? list[3 * kWaveList + lane] : 0;
+        unsigned long other[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) other[w] = lane < counts[w] ? list[w * kWaveList + lane] : 0;
         const unsigned long own = lane < count ? mine_list[lane] : 0;
         int my_rank = 0;
         for (int k = 0; k < count; ++k) {
@@ -372,40 +444,39 @@ __global__ void __launch_bounds__(kWG, 4) beam_slices(const BeamParams P) {
                                      static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(own), k));
             int rank = 0;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) rank += __popcll(__ballot(other[w] > me));
+            for (int w = 0; w < NW; ++w) rank += __popcll(__ballot(other[w] > me));
             my_rank = lane == k ? rank : my_rank;
         }
         if (lane < count) put(my_rank, own);
     } else {
-        int counts[4] = {c0, c1, c2, c3};
-        if (most > kWaveList || most2 > kWaveList) {
+        if (most > kWaveList) {
             __syncthreads();                                  // (all have read the counts)
-            have = slice_cut<BF16>(z, begin, end, P.n, list, lds, tid);
-            counts[0] = have;                                 // (at most n of them)
-            counts[1] = counts[2] = counts[3] = 0;
-        } else {
-            have = c0 + c1 + c2 + c3;
+            have = slice_cut<BF16, NW>(z, begin, end, P.n, list, lds, tid);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) counts[w] = w == 0 ? have : 0;   // (at most n of them)
         }
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            for (int k = tid; k < counts[v]; k += kWG) {
+        for (int v = 0; v < NW; ++v)
+            for (int k = tid; k < counts[v]; k += T) {
                 const unsigned long me = list[v * kWaveList + k];
                 int rank = 0;
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
+                for (int w = 0; w < NW; ++w)
                     for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
                 put(rank, me);
             }
     }
-    for (int k = have + tid; k < P.n; k += kWG) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
-    if (tid == kWG - 1) {
+    for (int k = have + tid; k < P.n; k += T) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
+    if (tid == T - 1) {
         double m = -__builtin_inf(), total = 0.0;
-        for (int w = 0; w < 4; ++w) m = wave_ref[w] > m ? wave_ref[w] : m;
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) m = wave_ref[w] > m ? wave_ref[w] : m;
+        for (int w = 0; w < NW; ++w) {
             const double d = wave_ref[w] - m;                 // (NaN where the slice has no entry)
             total += d < 0.0 ? (wave_ref[w] > -__builtin_inf() ? wave_sum[w] * exp_below(d) : wave_sum[w]) : wave_sum[w];
         }
         P.stat[at] = make_double2(m, total);
+    }
+    __syncthreads();                                          // (the next slice's bounds and lists go where these were)
     }
 }
 

@@ -38,10 +38,14 @@ inline bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) %
 
 // ------------------------------------------------------------------------------------------ selection
 
-// How a row is cut: into as many slices as fill the GPU once (four workgroups a compute unit, what their registers allow), each of several chunks; in a
-// call of few rows into chunks, and these made smaller while compute units are left over.
-struct BeamShape { int slots, len, S; };
-constexpr long kBeamWGs = 1024, kBeamFew = 512;
+// How a row is cut.  Into as many slices as fill the GPU once (four workgroups of four wavefronts a compute unit, what their registers allow), each of several
+// chunks; in a call of few rows into chunks, and these made smaller while compute units are left over.  Long bfloat16 rows (from 65536 entries and 2^23 in all): by
+// the kernel with the table, two workgroups of eight wavefronts a compute unit, the slices so many that these have about equally many.  Whole calls with and
+// without the table, 16 continuations of 8 beams: 8 sequences of 128256 entries 25 and 31 us, 16 30 and 29, 32 35 and 38, 64 (the first of these two
+// kernels) 38 and 51, 128 75 and 90, 12 of 256000 32 and 37; shorter rows lose by it (128 of 32000 41 and 40, 256 66 and 59), as each pays for its beginning and end.
+struct BeamShape { int slots, len, S; bool table; };
+constexpr long kBeamWGs = 1024, kBeamFew = 512, kTableWGs = 512;
+constexpr int kTableSlots = 2;
 bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
     if (dtype != FSD_F32 && dtype != FSD_BF16) return false;
     if (B < 1 || B > kMaxBatch || W < 1 || W > kBeamWidest || n < 1 || n > kBeamMost || V < 1 || V > fsd_max_vocab(dtype)) return false;
@@ -51,7 +55,16 @@ bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
     s->slots = 4;
     while (s->slots > 1 && rows * chunks(s->slots) < kBeamFew) s->slots /= 2;
     int S = chunks(s->slots);
-    if (rows * S > kBeamWGs) S = rows < kBeamWGs ? static_cast<int>(kBeamWGs / rows) : 1;
+    s->table = dtype == FSD_BF16 && V >= 65536 && rows * V >= 1L << 23;
+    if (s->table) {
+        // (slices of 32768 entries at least; beginning and end of one cost about as much as 6000 entries)
+        double best = 0.0;
+        S = 1;
+        for (int k = 1; k <= 8 && V / k >= 32768 && rows * k <= kMaxGroups; ++k) {
+            const double cost = static_cast<double>((rows * k + kTableWGs - 1) / kTableWGs) * (static_cast<double>(V) / k + 6000.0);
+            if (k == 1 || cost < best) best = cost, S = k;
+        }
+    } else if (rows * S > kBeamWGs) S = rows < kBeamWGs ? static_cast<int>(kBeamWGs / rows) : 1;
     s->len = ((V + S - 1) / S + E - 1) / E * E;              // slices of one length, so that none of them is a remnant
     s->S = (V + s->len - 1) / s->len;
     return rows * s->S <= kMaxGroups;
@@ -67,11 +80,17 @@ BeamSpace beam_space(const BeamShape& s, int B, int W, int n) {
     return w;
 }
 template <bool BF16>
-void launch_beam_slices(hipStream_t st, unsigned grid, int slots, const BeamParams& P) {
-    const dim3 g(grid), t(kWG);
-    if (slots == 1) hipLaunchKernelGGL((beam_slices<BF16, 1>), g, t, 0, st, P);
-    else if (slots == 2) hipLaunchKernelGGL((beam_slices<BF16, 2>), g, t, 0, st, P);
-    else hipLaunchKernelGGL((beam_slices<BF16, 4>), g, t, 0, st, P);
+void launch_beam_slices(hipStream_t st, const BeamShape& s, const BeamParams& P) {
+    const dim3 g(P.units), t(kWG);
+    if constexpr (BF16) {
+        if (s.table) {
+            hipLaunchKernelGGL((beam_slices<true, kTableSlots, true>), dim3(P.units < kTableWGs ? P.units : static_cast<unsigned>(kTableWGs)), dim3(512), 0, st, P);
+            return;
+        }
+    }
+    if (s.slots == 1) hipLaunchKernelGGL((beam_slices<BF16, 1, false>), g, t, 0, st, P);
+    else if (s.slots == 2) hipLaunchKernelGGL((beam_slices<BF16, 2, false>), g, t, 0, st, P);
+    else hipLaunchKernelGGL((beam_slices<BF16, 4, false>), g, t, 0, st, P);
 }
 
 // ------------------------------------------------------------------------------------------ pages
@@ -175,9 +194,9 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     P.tokens = tokens;
     P.status = row_status;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const unsigned grid = static_cast<unsigned>(static_cast<long>(B) * P.lists);
-    if (dtype == FSD_BF16) launch_beam_slices<true>(st, grid, s.slots, P);
-    else launch_beam_slices<false>(st, grid, s.slots, P);
+    P.units = static_cast<unsigned>(static_cast<long>(B) * P.lists);
+    if (dtype == FSD_BF16) launch_beam_slices<true>(st, s, P);
+    else launch_beam_slices<false>(st, s, P);
     if (P.lists * n <= 256 * kMergeEach) hipLaunchKernelGGL((beam_merge<256>), dim3(static_cast<unsigned>(B)), dim3(256), 0, st, P);
     else hipLaunchKernelGGL((beam_merge<512>), dim3(static_cast<unsigned>(B)), dim3(512), 0, st, P);
     return launched();

@@ -263,6 +263,8 @@ FORK = [
     # B, n, M, P, layers, heads, head_dim
     (1, 1, 1, 3, 1, 1, 64), (1, 4, 3, 20, 2, 3, 64), (6, 6, 5, 60, 1, 2, 128), (6, 11, 5, 100, 2, 1, 256), (9, 3, 4, 50, 1, 1, 64),
     (40, 70, 3, 400, 1, 1, 64), (3, 5, 600, 3000, 1, 1, 64), (300, 600, 2, 2500, 1, 1, 64), (5, 5, 2, 5000, 1, 1, 64),
+    # more than one workgroup takes: many blocks, many places, many sequences
+    (12, 30, 5, 4500, 2, 2, 64), (8, 8, 1500, 13000, 1, 1, 64), (300, 600, 20, 6500, 1, 1, 64), (1100, 1200, 2, 4000, 1, 1, 64), (7, 1, 3, 4097, 2, 3, 128),
 ]
 
 
@@ -374,7 +376,8 @@ def test_copy(L, P, Q, H, D, n):
     _same_pages(src, a)
 
 
-@pytest.mark.parametrize("P,share", [(1, 0.0), (1, 1.0), (2, 0.5), (40, 0.0), (40, 1.0), (40, 0.4), (1024, 0.5), (1025, 0.9), (3000, 0.1), (3000, 0.7)])
+@pytest.mark.parametrize("P,share", [(1, 0.0), (1, 1.0), (2, 0.5), (40, 0.0), (40, 1.0), (40, 0.4), (1024, 0.5), (1025, 0.9), (3000, 0.1), (3000, 0.7),
+                                     (4097, 0.5), (5000, 0.0), (5000, 1.0), (9000, 0.3), (6144, 0.8)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_compact(P, share, in_place):
     rng = np.random.default_rng(P)
@@ -399,3 +402,345 @@ def test_compact(P, share, in_place):
         assert (_host(got[name]) == w).all(), name
     ref.move_pages({k: v.copy() for k, v in pages.items()}, pages, want[5])
     _same_pages(cache, pages)
+
+
+# ------------------------------------------------------------------------------------------ larger rows
+
+
+def _long_rows():
+    """bfloat16 rows that go to the kernel with the table of exponentials, and what it does not hold"""
+    rng = np.random.default_rng(12)
+    B, W, V = 12, 8, 100003
+    z = torch.from_numpy(rng.standard_normal((B, W, V)).astype(np.float32) * 3)
+    z[1] *= 30.0                                              # largest beyond 64
+    z[2] -= 100.0                                             # largest under -20
+    z[3] *= 1e-4                                              # nearer to 0 than the table goes
+    z[4] = 0.0
+    z[5] = (torch.arange(V) // 64 / 64.0)                     # in order
+    z[6][torch.from_numpy(rng.random((W, V)) < 0.99)] = -float("inf")
+    z[7, :, :60000] -= 1000.0                                 # nothing like the rest in front
+    z[8, :, 50000:] += 80.0
+    z[9] = -float("inf")
+    z[9, 3, V - 1], z[9, 5, 0] = -3000.0, 7.0
+    z[10] = -70.0 - z[10].abs()                               # under the table's end, every one
+    z[11, :, 1:] = -63.9
+    z[11, :, 0] = 1e-30
+    return z.to(torch.bfloat16), _scores(rng, B, W)
+
+
+@pytest.mark.parametrize("n", [1, 16, 128])
+def test_select_long_rows(n):
+    z, scores = _long_rows()
+    wide = torch.full((12, 8, 100104), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = []
+    for rows in (z.cuda(), wide[:, :, 1:100004].copy_(z)):    # whole, and at odd addresses
+        got.append(fsd.fsd_beam_select(rows, _dev(scores), n))
+    want = ref.select(_host(z), scores, None, None, n)
+    for g in got:
+        _same_selection(g, (*want[:4], np.inf))
+    assert want[4] > 2.0 ** -31
+
+
+def test_select_long_rows_reports():
+    z, scores = _long_rows()
+    z[0, 7, 100002], z[1, 0, 3], z[4, 2, 77], z[6, 6, 50001] = float("nan"), float("inf"), -float("nan"), float("nan")
+    done = np.zeros((12, 8), np.int32)
+    done[6, 6], done[2, 1] = 1, 1
+    got = fsd.fsd_beam_select(z.cuda(), _dev(scores), 5, done=_dev(done))
+    want = ref.select(_host(z), scores, None, done, 5)
+    assert [b for b in range(12) if want[3][b]] == [0, 1, 4]
+    _same_selection(got, (*want[:4], np.inf))
+
+
+@pytest.mark.parametrize("spread", [3.0, 300.0])
+def test_select_long_binary32_rows(spread):
+    """slices of several chunks"""
+    rng = np.random.default_rng(9)
+    z = _logits(rng, 11, 8, 100003, "f32", spread)
+    z[3, :, 40000:60000] = -float("inf")
+    z[4] = 1.25
+    z[5] = torch.arange(100003) / 1000.0
+    scores = _scores(rng, 11, 8)
+    want = ref.select(_host(z), scores, None, None, 37)
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), 37), (*want[:4], np.inf))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_select_one_beam_has_all_of_the_best(dtype):
+    """most of the best entries in the lists of one beam, and of one slice"""
+    rng = np.random.default_rng(10)
+    z = _logits(rng, 3, 60, 6000, dtype, 0.5)
+    z[0, 17] *= 8
+    z[1, 59, 4000:4500] += 9.0
+    scores = np.zeros((3, 60), np.float32)
+    scores[0, 17] = 12.0
+    scores[2] = -np.arange(60) * 3.0
+    want = ref.select(_host(z), scores, None, None, 128)
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), 128), (*want[:4], np.inf))
+
+
+# ------------------------------------------------------------------------------------------ calls beside one another
+
+
+def _select_args(rng, B=5, W=6, V=40009, dtype="bf16"):
+    z, s = _logits(rng, B, W, V, dtype), _scores(rng, B, W)
+    return z, s
+
+
+def test_workspaces_may_hold_anything():
+    rng = np.random.default_rng(21)
+    z, s = _select_args(rng)
+    want = ref.select(_host(z), s, None, None, 9)
+    ws = torch.full((fsd.fsd_beam_workspace_bytes(40, 8, 128256, 60, fsd.F32) + 256,), 255, dtype=torch.uint8, device="cuda")
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(s), 9, workspace=ws), want)
+    fsd.fsd_beam_select(torch.randn((30, 8, 90000), device="cuda"), None, 60, workspace=ws)
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(s), 9, workspace=ws), want)
+    table, lens, refs = _sequences(rng, 9, 4, 60)
+    for fill in (255, 0, 127):
+        ws = torch.full((fsd.fsd_cache_fork_workspace_bytes(60, 20) + 256,), fill, dtype=torch.uint8, device="cuda")
+        _fork(rng, table, lens, refs, rng.integers(-1, 9, 20).astype(np.int32), None, None, workspace=ws)
+
+
+def test_smallest_workspaces():
+    """the sizes that the library asks for are enough, to the byte"""
+    rng = np.random.default_rng(22)
+    z, s = _select_args(rng, 3, 4, 5000)
+    need = fsd.fsd_beam_workspace_bytes(3, 4, 5000, 7, fsd.BF16)
+    arena = torch.full((need + 512,), 99, dtype=torch.uint8, device="cuda")
+    at = (-arena.data_ptr()) % 256
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(s), 7, workspace=arena[at:at + need]), ref.select(_host(z), s, None, None, 7))
+    assert (arena[at + need:] == 99).all() and (arena[:at] == 99).all()
+    with pytest.raises(fsd.FsdError):
+        fsd.fsd_beam_select(z.cuda(), _dev(s), 7, workspace=arena[at:at + need - 1])
+    for P, n, M in ((50, 9, 4), (5000, 9, 4), (2000, 30, 400)):
+        table, lens, refs = _sequences(rng, 4, M, P)
+        need = fsd.fsd_cache_fork_workspace_bytes(P, n)
+        arena = torch.full((need + 512,), 99, dtype=torch.uint8, device="cuda")
+        at = (-arena.data_ptr()) % 256
+        _fork(rng, table, lens, refs, rng.integers(-1, 4, n).astype(np.int32), None, None, workspace=arena[at:at + need])
+        assert (arena[at + need:] == 99).all() and (arena[:at] == 99).all()
+        need = fsd.fsd_cache_compact_workspace_bytes(P)
+        arena = torch.full((need + 512,), 99, dtype=torch.uint8, device="cuda")
+        at = (-arena.data_ptr()) % 256
+        cache = _cache(_pages(rng, 1, P, 1, 64), table, lens)
+        got = fsd.fsd_cache_compact(cache, _dev(refs), workspace=arena[at:at + need])
+        want = ref.compact(table, refs)
+        torch.cuda.synchronize()
+        assert (_host(got["remap"]) == want[2]).all() and (_host(got["block_table"]) == want[0]).all()
+        assert (arena[at + need:] == 99).all() and (arena[:at] == 99).all()
+
+
+def test_reports_may_be_left_out():
+    rng = np.random.default_rng(23)
+    z, s = _select_args(rng, 2, 3, 700, "f32")
+    new = lambda shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+    out = dict(scores=new((2, 5), torch.float32), parent=new((2, 5)), tokens=new((2, 5)))
+    got = dict(fsd.fsd_beam_select(z.cuda(), _dev(s), 5, out=out), row_status=torch.zeros(2))
+    _same_selection(got, ref.select(_host(z), s, None, None, 5))
+    parent = out["parent"]
+    fsd.fsd_beam_reorder(z.cuda(), parent, out=dict(out=torch.empty((2, 5, 700), device="cuda")))
+    for P, M in ((40, 4), (6000, 4)):
+        table, lens, refs = _sequences(rng, 3, M, P)
+        cache = _cache(_pages(rng, 1, P, 1, 64), table, lens)
+        got = fsd.fsd_cache_fork(cache, _dev(np.array([0, 2], np.int32)), _dev(refs), out=dict(block_table=new((2, M)), cache_len=new(2), refs=new(P)))
+        torch.cuda.synchronize()
+        want = ref.fork(table, lens, refs, np.array([0, 2]), None, None)
+        assert (_host(got["block_table"]) == want[0]).all() and (_host(got["refs"]) == want[2]).all()
+        got = fsd.fsd_cache_compact(cache, _dev(refs), out=dict(block_table=new((3, M)), refs=new(P)))
+        torch.cuda.synchronize()
+        assert (_host(got["refs"]) == ref.compact(table, refs)[1]).all()
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(24)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    calls = [_select_args(rng, 6, 7, 90001) for _ in streams]
+    on = [(z.cuda(), _dev(s)) for z, s in calls]
+    tables = [_sequences(rng, 20, 5, 300) for _ in streams]
+    parents = [rng.integers(-1, 20, 33).astype(np.int32) for _ in streams]
+    pages = [_pages(rng, 2, 300, 1, 64) for _ in streams]
+    caches = [_cache(p, t[0], t[1]) for p, t in zip(pages, tables)]
+    refs, par = [_dev(t[2]) for t in tables], [_dev(p) for p in parents]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, st in enumerate(streams):
+            got[i].append((fsd.fsd_beam_select(*on[i], 30, stream=st), fsd.fsd_cache_fork(caches[i], par[i], refs[i], stream=st),
+                           fsd.fsd_beam_reorder(on[i][0], par[i][:6].view(6, 1).clamp(0, 6), stream=st)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        want, forked = ref.select(_host(calls[i][0]), calls[i][1], None, None, 30), ref.fork(*tables[i], parents[i], None, None)
+        ref.move_pages({k: v.copy() for k, v in pages[i].items()}, pages[i], forked[5])
+        _same_pages(caches[i], pages[i])
+        for s, f, r in got[i]:
+            _same_selection(s, want)
+            assert (_host(f["block_table"]) == forked[0]).all() and (_host(f["refs"]) == forked[2]).all()
+            assert torch.equal(r["out"][:, 0], on[i][0][torch.arange(6, device="cuda"), par[i][:6].clamp(0, 6).long()])
+
+
+@pytest.mark.parametrize("P,M", [(200, 5), (6000, 5), (200, 900)])
+def test_replays_from_a_graph(P, M):
+    """A captured step, replayed with other contents of the same tensors, and eager work in between."""
+    rng = np.random.default_rng(P + M)
+    B, W, V, n = 4, 3, 70001, 3
+    z, s = torch.empty((B, W, V), dtype=torch.bfloat16, device="cuda"), torch.empty((B, W), device="cuda")
+    state = torch.randn((2, B, W, 50), device="cuda")
+    offset = (torch.arange(B, dtype=torch.int32, device="cuda") * W)[:, None]
+    pages = _pages(rng, 1, P, 1, 64)
+    cache = _cache(pages, np.full((B * W, M), -1, np.int32), np.zeros(B * W, np.int32))
+    refs, room = torch.zeros(P, dtype=torch.int32, device="cuda"), torch.full((B * n,), 9, dtype=torch.int32, device="cuda")
+
+    def step():
+        best = fsd.fsd_beam_select(z, s, n)
+        states = fsd.fsd_beam_reorder(state, best["parent"], batch_dim=1)
+        rows = torch.where(best["parent"] < 0, -1, best["parent"] + offset).view(-1)
+        forked = fsd.fsd_cache_fork(cache, rows, refs, room=room)
+        packed = fsd.fsd_cache_compact(cache.with_tables(forked["block_table"], forked["cache_len"]), forked["refs"])
+        return best, states, forked, packed
+
+    def fill(k):
+        g = np.random.default_rng(100 + k)
+        z.copy_(_logits(g, B, W, V, "bf16"))
+        s.copy_(torch.from_numpy(_scores(g, B, W)))
+        table, lens, r = _sequences(g, B * W, M, P, most=min(64 * M - 9, 300))
+        cache.block_table.copy_(torch.from_numpy(table))
+        cache.cache_len.copy_(torch.from_numpy(lens))
+        refs.copy_(torch.from_numpy(r))
+        for name, v in pages.items():
+            getattr(cache, name).copy_(torch.from_numpy(v))
+
+    fill(0)
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = step()
+    for k in (1, 2, 3, 1):
+        fill(k)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [{name: t.clone() for name, t in part.items() if name != "_workspace"} for part in captured]
+        after = {name: getattr(cache, name).clone() for name in pages}
+        fill(k)
+        eager = step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, eager):
+            for name, t in a.items():
+                assert torch.equal(t, b[name]), (k, name)
+        for name in pages:
+            assert torch.equal(after[name].view(torch.uint8), getattr(cache, name).view(torch.uint8)), (k, name)
+        _same_selection(eager[0], ref.select(_host(z), _host(s), None, None, n))
+
+
+def test_streams_of_their_own_memory():
+    """`stream`: what the binding allocates stays allocated until that stream has used it"""
+    rng = np.random.default_rng(26)
+    side = torch.cuda.Stream()
+    z, s = _select_args(rng, 3, 4, 20000)
+    zd, sd = z.cuda(), _dev(s)
+    torch.cuda.synchronize()
+    got = fsd.fsd_beam_select(zd, sd, 8, stream=side)
+    for _ in range(8):
+        torch.full((got["_workspace"].numel(),), 255, dtype=torch.uint8, device="cuda")
+    side.synchronize()
+    _same_selection(got, ref.select(_host(z), s, None, None, 8))
+
+
+# ------------------------------------------------------------------------------------------ together
+
+
+def test_beam_search_over_the_cache():
+    """Prompts appended, each continued by beams: attention over the forked cache, the best continuations, histories and pages that follow
+    them.  Every beam's pages in the end are those of a sequence that was never forked."""
+    rng = np.random.default_rng(30)
+    B, W, V, H, G, D, L, P, M = 3, 4, 600, 2, 2, 64, 1, 120, 6
+    emb = {k: torch.from_numpy(rng.standard_normal((V, h, D)).astype(np.float32) * 0.7).to(torch.bfloat16).cuda() for k, h in (("q", H * G), ("k", H), ("v", H))}
+    head = torch.from_numpy(rng.standard_normal((H * G * D, V)).astype(np.float32) * 0.4).cuda()
+    prompts = [rng.integers(0, V, k) for k in (70, 1, 130)]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def append(cache, tokens, counts):                        # tokens [S, R]: the first counts[s] of them
+        t = torch.as_tensor(tokens, dtype=torch.long, device="cuda")
+        out = fsd.fsd_cache_append(emb["k"][t].contiguous(), emb["v"][t].contiguous(), cache, ints(counts) - 1)
+        assert not out["row_status"].any()
+        cache.cache_len.copy_(out["cache_len"])
+
+    def prompt_into(cache, rows):                             # all but a prompt's last token
+        R = max(len(p) for p in rows)
+        append(cache, [list(p) + [0] * (R - len(p)) for p in rows], [len(p) - 1 for p in rows])
+
+    refs = torch.zeros(P, dtype=torch.int32, device="cuda")
+    cache = fsd.Cache.empty(L, P, H, D, torch.full((1, M), -1, dtype=torch.int32, device="cuda"), ints([0]))
+
+    def fork(cache, refs, parent, room):
+        out = fsd.fsd_cache_fork(cache, ints(parent) if isinstance(parent, list) else parent, refs, room=ints(room))
+        assert not out["row_status"].any()
+        table = out["block_table"]
+        count = torch.bincount(table[table >= 0].long(), minlength=P).int()
+        assert torch.equal(out["refs"], count) and int(out["free_blocks"]) == int((count == 0).sum())
+        return cache.with_tables(table, out["cache_len"]), out["refs"]
+
+    cache, refs = fork(cache, refs, [-1] * B, [len(p) for p in prompts])
+    prompt_into(cache, prompts)
+    cache, refs = fork(cache, refs, [b for b in range(B) for _ in range(W)], [1] * (B * W))
+    scores = torch.full((B, W), -float("inf"), device="cuda")
+    scores[:, 0] = 0.0                                        # the first step has one beam
+    history = torch.zeros((B, W, 200), dtype=torch.int32, device="cuda")
+    for b, p in enumerate(prompts):
+        history[b, :, :len(p)] = ints(p.tolist())
+    length = torch.tensor([len(p) for p in prompts], device="cuda")
+    last = torch.stack([history[b, :, len(p) - 1] for b, p in enumerate(prompts)])
+    offset = (torch.arange(B, dtype=torch.int32, device="cuda") * W)[:, None]
+    for _ in range(70):
+        t = last.long().view(B * W, 1)
+        x = fsd.fsd_attend_chain(emb["q"][t].contiguous(), emb["k"][t].contiguous(), emb["v"][t].contiguous(), cache)
+        assert not x["row_status"].any()
+        logits = (x["out"].float().view(B, W, -1) @ head).contiguous()
+        best = fsd.fsd_beam_select(logits, scores, W)
+        want = ref.select(_host(logits), _host(scores), None, None, W)
+        _same_selection(best, (*want[:4], max(want[4], 2.0 ** -30)))
+        append(cache, last.long().view(B * W, 1), [1] * (B * W))
+        cache, refs = fork(cache, refs, (best["parent"] + offset).view(-1).contiguous(), [1] * (B * W))
+        scores, last = best["scores"].clone(), best["tokens"].clone()
+        history = fsd.fsd_beam_reorder(history, best["parent"])["out"]
+        history.scatter_(2, length.view(B, 1, 1).expand(B, W, 1), last[:, :, None])
+        length = length + 1
+    # put together, and each beam again by itself
+    packed = fsd.fsd_cache_compact(cache, refs)
+    assert int(packed["used_blocks"]) == int((refs > 0).sum()) and int(packed["block_table"].max()) < int(packed["used_blocks"])
+    cache = cache.with_tables(packed["block_table"], cache.cache_len)
+    lens = cache.cache_len.tolist()
+    for b in range(B):
+        for w in range(W):
+            tokens = history[b, w, :int(length[b])].tolist()
+            n = len(tokens) - 1
+            assert lens[b * W + w] == n
+            alone = fsd.Cache.empty(L, M, H, D, torch.arange(M, dtype=torch.int32, device="cuda")[None], ints([0]))
+            prompt_into(alone, [np.array(tokens[:len(prompts[b])])])
+            for x in tokens[len(prompts[b]) - 1:-1]:
+                append(alone, [[x]], [1])
+            for j in range(-(-n // 64)):
+                blk, held = int(cache.block_table[b * W + w, j]), min(64, n - 64 * j)
+                assert torch.equal(cache.k_codes[:, blk, :, :held], alone.k_codes[:, j, :, :held])
+                v = [c.v_codes[:, e].transpose(-1, -2).reshape(L, H, 64, D)[:, :, :held] for c, e in ((cache, blk), (alone, j))]
+                assert torch.equal(*v)
+                assert torch.equal(cache.k_scale[:, blk], alone.k_scale[:, j]) and torch.equal(cache.v_scale[:, blk], alone.v_scale[:, j])
+
+
+def test_a_tree_from_the_selection_is_verified():
+    """two levels of a token tree by the selection, verified against the same model: the divergences are 0 and a path of two is accepted"""
+    rng = np.random.default_rng(31)
+    B, V, first, second = 5, 3000, 4, 7
+    root = _logits(rng, B, 1, V, "bf16").cuda()
+    level1 = fsd.fsd_beam_select(root, None, first)
+    below = _logits(rng, B, first, V, "bf16").cuda()          # the model's rows behind the nodes of the first level
+    level2 = fsd.fsd_beam_select(below, level1["scores"], second)
+    behind = _logits(rng, B, second, V, "bf16").cuda()
+    tokens = torch.cat([level1["tokens"], level2["tokens"]], 1).contiguous()
+    parent = torch.cat([torch.full_like(level1["parent"], -1), level2["parent"]], 1).contiguous()
+    target = torch.cat([root, below, behind], 1).contiguous()
+    draft = torch.cat([fsd.fsd_beam_reorder(root, level1["parent"])["out"], fsd.fsd_beam_reorder(below, level2["parent"])["out"]], 1).contiguous()
+    got = fsd.fsd_verify_tree(target, draft, tokens, parent, 3, 0.0, fsd.DIV_JS, fsd.GREEDY)
+    torch.cuda.synchronize()
+    assert not got["row_status"].any() and (got["divergences"] == 0).all() and (got["path_len"] == 2).all()
+    assert torch.equal(got["path_nodes"][:, 1], torch.full_like(got["path_nodes"][:, 1], first))   # the best node of the second level
