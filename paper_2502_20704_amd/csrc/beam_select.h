@@ -58,6 +58,55 @@ __device__ __forceinline__ double exp_below(double x) {
     const double e = exp_within(x < -700.0 ? -700.0 : x);
     return x < -700.0 ? 0.0 : e;
 }
+// what all lanes have alike, as a scalar
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ unsigned uniform(unsigned x) { return static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(x))); }
+
+// Over 16 lanes by rotations within them (no round trip through LDS), over the wavefront's four rows of 16 by scalars.  The sums' order is fixed.
+template <int N>
+__device__ __forceinline__ int rotated(int x) { return __builtin_amdgcn_update_dpp(x, x, 0x120 | N, 0xF, 0xF, false); }
+template <int N>
+__device__ __forceinline__ double rotated(double x) {
+    const unsigned long u = __builtin_bit_cast(unsigned long, x);
+    const unsigned lo = static_cast<unsigned>(rotated<N>(static_cast<int>(u))), hi = static_cast<unsigned>(rotated<N>(static_cast<int>(u >> 32)));
+    return __builtin_bit_cast(double, static_cast<unsigned long>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double row_sum(double x) {          // of 16 lanes: exact in none but the order
+    x += rotated<8>(x);
+    x += rotated<4>(x);
+    x += rotated<2>(x);
+    x += rotated<1>(x);
+    return x;
+}
+__device__ __forceinline__ double row_max(double x) {
+    double y;
+    y = rotated<8>(x), x = y > x ? y : x;
+    y = rotated<4>(x), x = y > x ? y : x;
+    y = rotated<2>(x), x = y > x ? y : x;
+    y = rotated<1>(x), x = y > x ? y : x;
+    return x;
+}
+__device__ __forceinline__ unsigned long lane_word(unsigned long u, int lane) {
+    return static_cast<unsigned long>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane))) << 32 |
+           static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(u), lane));
+}
+__device__ __forceinline__ double lane_value(double x, int lane) { return __builtin_bit_cast(double, lane_word(__builtin_bit_cast(unsigned long, x), lane)); }
+__device__ __forceinline__ double wave_sum_64(double x) {
+    x = row_sum(x);
+    return (lane_value(x, 0) + lane_value(x, 16)) + (lane_value(x, 32) + lane_value(x, 48));
+}
+__device__ __forceinline__ float wave_largest(float x) {
+    auto larger = [](float a, int b) { return __builtin_fmaxf(a, __int_as_float(b)); };
+    x = larger(x, rotated<8>(__float_as_int(x)));
+    x = larger(x, rotated<4>(__float_as_int(x)));
+    x = larger(x, rotated<2>(__float_as_int(x)));
+    x = larger(x, rotated<1>(__float_as_int(x)));
+    const int u = __float_as_int(x);
+    const float a = __int_as_float(__builtin_amdgcn_readlane(u, 0)), b = __int_as_float(__builtin_amdgcn_readlane(u, 16)),
+                c = __int_as_float(__builtin_amdgcn_readlane(u, 32)), d = __int_as_float(__builtin_amdgcn_readlane(u, 48));
+    return __builtin_fmaxf(__builtin_fmaxf(a, b), __builtin_fmaxf(c, d));
+}
+
 // bits of a number in an order in which larger numbers have larger words (0 and -0 differ: give it neither as -0)
 __device__ __forceinline__ unsigned ordered(float x) {
     const unsigned u = __float_as_uint(x);
@@ -227,7 +276,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     __shared__ double wave_sum[NW], wave_ref[NW];
     __shared__ unsigned bounds[NW];
     __shared__ int lds[NW + 1];
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+    const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64;
     if constexpr (TABLE) {
         for (int k = tid; k < 2 * kTableEnd; k += T) {
             const int u = k < kTableEnd ? k : k - kTableEnd;
@@ -291,7 +340,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         unsigned bound = 0xFFFFFFFFu;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const unsigned theirs = __hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            const unsigned theirs = uniform(__hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
             bound = theirs < bound ? theirs : bound;
         }
         least = bound > least ? bound : least;
@@ -384,7 +433,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         }
         all_bounds();
     }
-    const float top = wave_max_all(mine);
+    const float top = wave_largest(mine);
     double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
     if ((TABLE ? top >= 64.0f || top < -20.0f : top > 600.0f || top < -600.0f) && top > -__builtin_inff()) {
         // again, as e^(z - top)
@@ -397,9 +446,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
             for (int e = 0; e < E; ++e) sum[e & 1] += exp_below(static_cast<double>(slot_entry<BF16>(x, e)) - ref);
         }
     }
-    double s = sum[0] + sum[1];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    double s = wave_sum_64(sum[0] + sum[1]);
     if (!(top > -__builtin_inff())) s = 0.0;
     const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
     // the final bound, made of all four wavefronts' entries
@@ -420,7 +467,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     int counts[NW], have = 0, most = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-        counts[w] = lds[w];
+        counts[w] = uniform(lds[w]);
         have += counts[w];
         most = counts[w] > most ? counts[w] : most;
     }
@@ -439,9 +486,9 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         for (int w = 0; w < NW; ++w) other[w] = lane < counts[w] ? list[w * kWaveList + lane] : 0;
         const unsigned long own = lane < count ? mine_list[lane] : 0;
         int my_rank = 0;
+#pragma unroll 4
         for (int k = 0; k < count; ++k) {
-            const unsigned long me = static_cast<unsigned long>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(own >> 32), k))) << 32 |
-                                     static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(own), k));
+            const unsigned long me = lane_word(own, k);
             int rank = 0;
 #pragma unroll
             for (int w = 0; w < NW; ++w) rank += __popcll(__ballot(other[w] > me));
@@ -487,7 +534,6 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
 __device__ __forceinline__ unsigned long found_word(int beam, float z, int token1) {
     return static_cast<unsigned long>(beam) << 52 | static_cast<unsigned long>(~ordered(z)) << 20 | static_cast<unsigned>(token1);
 }
-constexpr int kMergeEach = 16;      // list entries that a thread holds at once
 constexpr int kMergeFew = 256;      // entries that are put into order as they are; of more, the n best are looked for first
 
 // 64-bit order of binary64 numbers, as ordered() is for binary32 ones; the upper word
@@ -496,9 +542,9 @@ __device__ __forceinline__ unsigned ordered_high(double x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A sequence a workgroup of T threads.  All entries of its lists (or 16 a thread at a time) are ranked in registers; a wavefront's q-th largest, q =
+// A sequence a workgroup of T threads.  All entries of its lists (or EACH a thread at a time) are ranked in registers; a wavefront's q-th largest, q =
 // n / wavefronts rounded up, bounds the n-th largest of all from below as in beam_slices, and the few that reach the least of these are ordered in LDS.
-template <int T>
+template <int T, int EACH>
 __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     constexpr int NW = T / 64, kRoom = T + kBeamMost;
     __shared__ double key[kRoom + 8];
@@ -512,7 +558,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     __shared__ unsigned wave_bound[NW];
     __shared__ int wave_count[2][NW];
     __shared__ int have, bad;
-    const int tid = threadIdx.x, wave = tid / 64, b = blockIdx.x, W = P.W, S = P.S, n = P.n;
+    const int tid = threadIdx.x, wave = uniform(tid / 64), b = blockIdx.x, W = P.W, S = P.S, n = P.n;
     const int lists = P.lists;
     const long first = static_cast<long>(b) * W;
     const size_t out = static_cast<size_t>(b) * n;
@@ -520,12 +566,12 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     if (tid == 0) have = 0, bad = 0;
     const int total = lists * n;                              // (at most 2^21)
     const int column_step = T % lists;
-    float z[kMergeEach];
-    int token[kMergeEach];
+    float z[EACH];
+    int token[EACH];
     // entry k of the lists: the (k / lists)-th of list k % lists
     auto load = [&](int k0) {
 #pragma unroll
-        for (int i = 0; i < kMergeEach; ++i) {
+        for (int i = 0; i < EACH; ++i) {
             const int k = k0 + i * T + tid;
             const float2 c = k < total ? cand[k] : make_float2(-__builtin_inff(), 0.0f);
             z[i] = c.x;
@@ -560,11 +606,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 broken |= x.y != x.y;
             }
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-            const double other = __shfl_xor(m, o, 16);
-            m = other > m ? other : m;
-        }
+        m = row_max(m);
         if (runs && m > -__builtin_inf()) {
             if (own.x > -__builtin_inf()) s = own.y * exp_below(own.x - m);
             for (int k = part + 16; k < S; k += 16) {
@@ -572,8 +614,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 if (x.x > -__builtin_inf()) s += x.y * exp_below(x.x - m);
             }
         }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o, 16);
+        s = row_sum(s);
         if (broken) bad = 1;                                  // (whoever writes it writes the same)
         if (w < W && part == 0) {
             const bool counts = runs && m > -__builtin_inf();
@@ -601,23 +642,46 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     auto beam_of = [&](int l) { return P.by_S ? static_cast<int>(__umulhi(static_cast<unsigned>(l), P.by_S)) : l; };
     double last_key = -__builtin_inf();                       // the n-th best of what has been ordered
     unsigned long last = ~0ul;
-    int count = have;
+    int count = uniform(have);
     __syncthreads();
-    // the n best of found[0 .. count) to its front, best first: a thread an entry, which all others are compared with (a broadcast each)
+    // the n best of found[0 .. count) to its front, best first
     auto order = [&]() {
         if (tid < 8) key[count + tid] = -__builtin_inf();
         __syncthreads();
-        for (int k = tid; k < count; k += T) {
-            const double mine = key[k];
-            const unsigned long me = found[k];
-            int rank = 0;
-            for (int j = 0; j < count; j += 8) {
-#pragma unroll
-                for (int u = 0; u < 8; ++u) rank += (key[j + u] > mine) | ((key[j + u] == mine) & (found[j + u] < me));
+        if (count <= 128) {                                   // a lane holds two of them; a wavefront finds the ranks of its share one after the other
+            const int lane = tid % 64;
+            const double k0 = lane < count ? key[lane] : -__builtin_inf(), k1 = lane + 64 < count ? key[lane + 64] : -__builtin_inf();
+            const unsigned long f0 = lane < count ? found[lane] : ~0ul, f1 = lane + 64 < count ? found[lane + 64] : ~0ul;
+            int rank0 = 0, rank1 = 0;
+            auto rank_of = [&](double mine, unsigned long me) {
+                return __popcll(__ballot((k0 > mine) | ((k0 == mine) & (f0 < me)))) + __popcll(__ballot((k1 > mine) | ((k1 == mine) & (f1 < me))));
+            };
+            const int in_first = count < 64 ? count : 64;
+#pragma unroll 4
+            for (int k = wave; k < in_first; k += NW) {
+                const int rank = rank_of(lane_value(k0, k), lane_word(f0, k));
+                rank0 = lane == k ? rank : rank0;
             }
-            if (rank < n) {
-                best_key[rank] = mine;
-                best[rank] = me;
+#pragma unroll 4
+            for (int k = 64 + wave; k < count; k += NW) {
+                const int rank = rank_of(lane_value(k1, k - 64), lane_word(f1, k - 64));
+                rank1 = lane == k - 64 ? rank : rank1;
+            }
+            if (lane < count && lane % NW == wave && rank0 < n) best_key[rank0] = k0, best[rank0] = f0;
+            if (lane + 64 < count && (lane + 64) % NW == wave && rank1 < n) best_key[rank1] = k1, best[rank1] = f1;
+        } else {                                              // a thread an entry, which all others are compared with (a broadcast each)
+            for (int k = tid; k < count; k += T) {
+                const double mine = key[k];
+                const unsigned long me = found[k];
+                int rank = 0;
+                for (int j = 0; j < count; j += 8) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) rank += (key[j + u] > mine) | ((key[j + u] == mine) & (found[j + u] < me));
+                }
+                if (rank < n) {
+                    best_key[rank] = mine;
+                    best[rank] = me;
+                }
             }
         }
         __syncthreads();
@@ -630,14 +694,14 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         if (tid == 0) have = count;
         __syncthreads();
     };
-    for (int k0 = 0; k0 < total; k0 += T * kMergeEach) {
+    for (int k0 = 0; k0 < total; k0 += T * EACH) {
         if (k0 > 0) load(k0);
-        double rank[kMergeEach];
+        double rank[EACH];
         double most = -__builtin_inf();
         {
             int l = (k0 + tid) % lists;
 #pragma unroll
-            for (int i = 0; i < kMergeEach; ++i) {
+            for (int i = 0; i < EACH; ++i) {
                 const int w = beam_of(l);
                 const float from = base[w];
                 rank[i] = -__builtin_inf();
@@ -665,12 +729,12 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         auto places = [&]() {                                 // of the wavefront's entries that reach the bound (in any order: they are put into order afterwards)
             reach = 0;
 #pragma unroll
-            for (int i = 0; i < kMergeEach; ++i) reach += __popcll(__ballot(ordered_high(rank[i]) >= bound && rank[i] >= last_key));
+            for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(ordered_high(rank[i]) >= bound && rank[i] >= last_key));
             at = 0;
             if (tid % 64 == 0 && reach != 0) at = atomicAdd(&have, reach);
             at = __builtin_amdgcn_readfirstlane(at);
             __syncthreads();
-            all = have;
+            all = uniform(have);
         };
         places();
         if (all - count > kMergeFew) {
@@ -680,7 +744,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 const unsigned c = bound | 1u << bit;
                 int n_c = 0;
 #pragma unroll
-                for (int i = 0; i < kMergeEach; ++i) n_c += __popcll(__ballot(ordered_high(rank[i]) >= c));
+                for (int i = 0; i < EACH; ++i) n_c += __popcll(__ballot(ordered_high(rank[i]) >= c));
                 if (tid % 64 == 0) wave_count[bit & 1][wave] = n_c;
                 __syncthreads();
                 n_c = 0;
@@ -695,7 +759,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         if (all <= kRoom) {
             if (reach != 0) {
 #pragma unroll
-                for (int i = 0; i < kMergeEach; ++i) {
+                for (int i = 0; i < EACH; ++i) {
                     const bool is = ordered_high(rank[i]) >= bound && rank[i] >= last_key;
                     const unsigned long who = __ballot(is);
                     if (is) {
@@ -716,11 +780,11 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
             __syncthreads();
             if (count > n) order();
 #pragma unroll 1
-            for (int i = 0; i < kMergeEach; ++i) {
+            for (int i = 0; i < EACH; ++i) {
                 const int k = k0 + i * T + tid;
                 double mine = rank[0];
 #pragma unroll
-                for (int j = 1; j < kMergeEach; ++j) mine = i == j ? rank[j] : mine;
+                for (int j = 1; j < EACH; ++j) mine = i == j ? rank[j] : mine;
                 if (mine > -__builtin_inf()) {
                     const float2 c = cand[k];
                     const unsigned long me = found_word(beam_of(k % lists), c.x, static_cast<int>(__float_as_uint(c.y)) + 1);
@@ -731,7 +795,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                     }
                 }
                 __syncthreads();
-                count = have;
+                count = uniform(have);
                 __syncthreads();
                 if (count > n) order();
             }

@@ -197,8 +197,10 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     P.units = static_cast<unsigned>(static_cast<long>(B) * P.lists);
     if (dtype == FSD_BF16) launch_beam_slices<true>(st, s, P);
     else launch_beam_slices<false>(st, s, P);
-    if (P.lists * n <= 256 * kMergeEach) hipLaunchKernelGGL((beam_merge<256>), dim3(static_cast<unsigned>(B)), dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((beam_merge<512>), dim3(static_cast<unsigned>(B)), dim3(512), 0, st, P);
+    const dim3 sequences(static_cast<unsigned>(B));
+    if (P.lists * n <= 256 * 4) hipLaunchKernelGGL((beam_merge<256, 4>), sequences, dim3(256), 0, st, P);
+    else if (P.lists * n <= 256 * 16) hipLaunchKernelGGL((beam_merge<256, 16>), sequences, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((beam_merge<512, 16>), sequences, dim3(512), 0, st, P);
     return launched();
 }
 
