@@ -34,25 +34,47 @@ def fsd_cache_compact_workspace_bytes(num_blocks: int) -> int:
     return _asked_once("fsd_cache_compact_workspace_bytes", num_blocks)
 
 
-def _space(workspace, need, device, stream):
-    """the workspace to hand over: the caller's, or one out of the stream's memory"""
+_layouts = {}
+_WITH_OUTPUTS = 1 << 16     # bytes of a workspace that is made together with the outputs, and so lives as long as any of them
+
+
+def _parts(stream, device, space, **tensors):
+    """New tensors of 32-bit numbers, of one or two dimensions, and `space` bytes behind them, as parts of one (a new tensor takes the host 1.7 us, a
+    part of one 0.8): them, and where the space begins."""
+    torch = _torch()
+    key = (space, *tensors.items())
+    layout = _layouts.get(key)
+    if layout is None:
+        parts, size = [], 0
+        for name, (shape, dtype) in tensors.items():
+            parts.append((name, dtype == torch.int32, shape, (shape[1], 1) if len(shape) == 2 else (1,), size))
+            size += (math.prod(shape) + 15) // 16 * 16
+        begin = (size * 4 + 255) // 256 * 256
+        if len(_layouts) > 1000:                              # (a program has a few shapes; one that has more pays for them again)
+            _layouts.clear()
+        layout = _layouts[key] = (parts, begin, (begin + space + 256 if space else size * 4) // 4 + 1)
+    parts, begin, words = layout
+    whole = _new(stream, device, whole=((words,), torch.int32))["whole"]
+    floats = whole.view(torch.float32)
+    at = whole.data_ptr()
+    return ({name: torch.as_strided(whole if is_int else floats, shape, stride, offset) for name, is_int, shape, stride, offset in parts}, whole,
+            at + begin + (-at - begin) % 256)
+
+
+def _results(out, optional, workspace, need, device, stream, **tensors):
+    """the caller's outputs (those in `optional` may be missing) and workspace, checked, or new ones -> outputs, workspace, its first address and size"""
+    if out is None:
+        space = need if workspace is None and need <= _WITH_OUTPUTS else 0
+        out, whole, base = _parts(stream, device, space, **tensors)
+        if space:
+            return out, whole, base, need
+    else:
+        _outputs(out, stream, device, optional, None, **tensors)
     if workspace is None:
         workspace = _new(stream, device, workspace=((need + 256,), _torch().uint8))["workspace"]
     elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous() or workspace.dtype != _torch().uint8:
         raise ValueError(f"workspace: contiguous uint8 on {device} wanted")
-    return _workspace(workspace, 0, device)
-
-
-def _parts(stream, device, **tensors):
-    """New tensors of 32-bit numbers, of one or two dimensions, as parts of one (a new tensor takes the host 1.7 us, a part of one 0.8)."""
-    torch = _torch()
-    at, size = [], 0
-    for shape, _ in tensors.values():
-        at.append(size)
-        size += (math.prod(shape) + 15) // 16 * 16
-    whole = _new(stream, device, whole=((size,), torch.int32))["whole"]
-    return {name: torch.as_strided(whole if dtype == torch.int32 else whole.view(dtype), shape, (shape[1], 1) if len(shape) == 2 else (1,), offset)
-            for (name, (shape, dtype)), offset in zip(tensors.items(), at)}
+    return out, *_workspace(workspace, 0, device)
 
 
 def _outputs(given, stream, device, optional, new, /, **tensors):
@@ -91,9 +113,9 @@ def fsd_beam_select(logits, scores, n, *, weights=None, done=None, out=None, wor
     for name, t, dtype in (("scores", scores, torch.float32), ("weights", weights, torch.float32), ("done", done, torch.int32)):
         if t is not None:
             _check(t, name, (B, W), dtype, dev)
-    out = _outputs(out, stream, dev, ("row_status",), _parts, scores=((B, n), torch.float32), parent=((B, n), torch.int32),
-                   tokens=((B, n), torch.int32), row_status=((B,), torch.int32))
-    workspace, base, size = _space(workspace, fsd_beam_workspace_bytes(B, W, V, n, dt), dev, stream)
+    out, workspace, base, size = _results(out, ("row_status",), workspace, fsd_beam_workspace_bytes(B, W, V, n, dt), dev, stream,
+                                          scores=((B, n), torch.float32), parent=((B, n), torch.int32), tokens=((B, n), torch.int32),
+                                          row_status=((B,), torch.int32))
     st = library().fsd_beam_select(_ptr(logits), step, _ptr(scores), _ptr(weights), _ptr(done), B, W, V, dt, n, _ptr(out["scores"]),
                                    _ptr(out["parent"]), _ptr(out["tokens"]), _ptr(out.get("row_status")), base, size, _stream(stream))
     if st != 0:
@@ -142,9 +164,9 @@ def fsd_cache_fork(cache, parent, refs, *, lengths=None, room=None, out=None, wo
     for name, t in (("lengths", lengths), ("room", room)):
         if t is not None:
             _check(t, name, (n,), torch.int32, dev)
-    out = _outputs(out, stream, dev, ("free_blocks", "row_status"), _parts, block_table=((n, cache.max_blocks), torch.int32),
-                   cache_len=((n,), torch.int32), refs=((P,), torch.int32), free_blocks=((1,), torch.int32), row_status=((n,), torch.int32))
-    workspace, base, size = _space(workspace, fsd_cache_fork_workspace_bytes(P, n), dev, stream)
+    out, workspace, base, size = _results(out, ("free_blocks", "row_status"), workspace, fsd_cache_fork_workspace_bytes(P, n), dev, stream,
+                                          block_table=((n, cache.max_blocks), torch.int32), cache_len=((n,), torch.int32), refs=((P,), torch.int32),
+                                          free_blocks=((1,), torch.int32), row_status=((n,), torch.int32))
     st = library().fsd_cache_fork(cache._ref, cache.batch, _ptr(refs), _ptr(parent), _ptr(lengths), _ptr(room), n, _ptr(out["block_table"]),
                                   _ptr(out["cache_len"]), _ptr(out["refs"]), _ptr(out.get("free_blocks")), _ptr(out.get("row_status")), base, size,
                                   _stream(stream))
@@ -186,9 +208,9 @@ def fsd_cache_compact(cache, refs, *, out=None, workspace=None, stream=None):
     _on_current(dev, stream)
     B, P = cache.batch, cache.num_blocks
     _check(refs, "refs", (P,), torch.int32, dev)
-    out = _outputs(out, stream, dev, ("remap", "used_blocks", "row_status"), _parts, block_table=((B, cache.max_blocks), torch.int32),
-                   refs=((P,), torch.int32), remap=((P,), torch.int32), used_blocks=((1,), torch.int32), row_status=((B,), torch.int32))
-    workspace, base, size = _space(workspace, fsd_cache_compact_workspace_bytes(P), dev, stream)
+    out, workspace, base, size = _results(out, ("remap", "used_blocks", "row_status"), workspace, fsd_cache_compact_workspace_bytes(P), dev, stream,
+                                          block_table=((B, cache.max_blocks), torch.int32), refs=((P,), torch.int32), remap=((P,), torch.int32),
+                                          used_blocks=((1,), torch.int32), row_status=((B,), torch.int32))
     st = library().fsd_cache_compact(cache._ref, B, _ptr(refs), _ptr(out["block_table"]), _ptr(out["refs"]), _ptr(out.get("remap")),
                                      _ptr(out.get("used_blocks")), _ptr(out.get("row_status")), base, size, _stream(stream))
     if st != 0:

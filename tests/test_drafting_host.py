@@ -219,7 +219,11 @@ def test_parts_of_one_tensor():
     """outputs that the binding makes are apart, aligned and of the shapes asked for"""
     import torch
 
-    got = drafting._parts(None, torch.device("cpu"), a=((3, 5), torch.float32), b=((7,), torch.int32), c=((1,), torch.int32), d=((2, 2), torch.int32))
+    shapes = dict(a=((3, 5), torch.float32), b=((7,), torch.int32), c=((1,), torch.int32), d=((2, 2), torch.int32))
+    for space in (0, 1, 300, 4096):
+        got, whole, base = drafting._parts(None, torch.device("cpu"), space, **shapes)
+        end = max(t.data_ptr() + 4 * t.numel() for t in got.values())
+        assert base % 256 == 0 and base >= end and (not space or base + space <= whole.data_ptr() + 4 * whole.numel())
     assert got["a"].shape == (3, 5) and got["a"].dtype == torch.float32 and got["a"].is_contiguous() and got["d"].is_contiguous()
     for k, t in enumerate(got.values()):
         t.fill_(k + 1)
