@@ -277,13 +277,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     __shared__ unsigned bounds[NW];
     __shared__ int lds[NW + 1];
     const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64;
-    if constexpr (TABLE) {
-        for (int k = tid; k < 2 * kTableEnd; k += T) {
-            const int u = k < kTableEnd ? k : k - kTableEnd;
-            const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
-            table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
-        }
-    }
+    bool begun = false;                                       // the table is there
     for (unsigned unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
     const unsigned row = unit / static_cast<unsigned>(P.S);
     const int slice = static_cast<int>(unit - row * static_cast<unsigned>(P.S));
@@ -303,6 +297,14 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     if (slots > 0) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) r[i] = request(i * T + tid);
+    }
+    if (TABLE && !begun) {                                    // (while the first requests are on their way; the barrier before its first use comes below)
+        begun = true;
+        for (int k = tid; k < 2 * kTableEnd; k += T) {
+            const int u = k < kTableEnd ? k : k - kTableEnd;
+            const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
+            table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
+        }
     }
     // the entries behind the last whole slot: its thread takes them one by one
     u32x4 last = {kNone, kNone, kNone, kNone};

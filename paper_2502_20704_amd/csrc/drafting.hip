@@ -64,16 +64,29 @@ bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
             const double cost = static_cast<double>((rows * k + kTableWGs - 1) / kTableWGs) * (static_cast<double>(V) / k + 6000.0);
             if (k == 1 || cost < best) best = cost, S = k;
         }
-    } else if (rows * S > kBeamWGs) S = rows < kBeamWGs ? static_cast<int>(kBeamWGs / rows) : 1;
+    } else if (rows * S > kBeamWGs) {
+        // two to four workgroups a compute unit, so many slices that the busiest unit has least to do; beginning and end of one cost about as much as this many
+        // entries (192 binary32 rows of 128259 entries, n = 60: 2 slices 36.6 us, 4 31.8, 5 33.6, 6 35.9)
+        const double ends = 10000.0 + 200.0 * n;
+        const int least = static_cast<int>((kBeamWGs / 2 + rows - 1) / rows), most = static_cast<int>(kBeamWGs / rows);
+        double best = 0.0;
+        S = least;
+        for (int k = least; k <= most; ++k) {
+            const double cost = static_cast<double>((rows * k + 255) / 256) * (static_cast<double>(V) / k + ends);
+            if (k == least || cost < best) best = cost, S = k;
+        }
+    }
     s->len = ((V + S - 1) / S + E - 1) / E * E;              // slices of one length, so that none of them is a remnant
     s->S = (V + s->len - 1) / s->len;
     return rows * s->S <= kMaxGroups;
 }
-struct BeamSpace { size_t stat, cand, bytes; };
-BeamSpace beam_space(const BeamShape& s, int B, int W, int n) {
+struct BeamSpace { size_t lists, stat, cand, bytes; };
+// (as much as any call of these or smaller sizes needs: beam_shape makes at most 1535 slices besides one a row, or of a long row min(8, V / 32768))
+BeamSpace beam_space(int B, int W, int V, int n) {
     Space a;
     BeamSpace w;
-    const size_t lists = static_cast<size_t>(B) * W * s.S;
+    const int of_long_row = V < 65536 ? 1 : V / 32768 < 8 ? V / 32768 : 8;
+    const size_t lists = w.lists = static_cast<size_t>(B) * W * of_long_row + 1536;
     w.stat = a.take(lists * sizeof(double2));
     w.cand = a.take(lists * n * sizeof(float2));
     w.bytes = a.bytes;
@@ -158,7 +171,7 @@ extern "C" {
 
 size_t fsd_beam_workspace_bytes(int B, int beams, int V, int n, int dtype) {
     BeamShape s;
-    return beam_shape(B, beams, V, n, dtype, &s) ? beam_space(s, B, beams, n).bytes : 0;
+    return beam_shape(B, beams, V, n, dtype, &s) ? beam_space(B, beams, V, n).bytes : 0;
 }
 
 int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores, const float* weights, const int32_t* done, int B, int beams, int V, int dtype,
@@ -171,8 +184,9 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     if (row_stride < V || row_stride > (1L << 32) || reinterpret_cast<uintptr_t>(logits) % es != 0 || misaligned4(scores) || misaligned4(weights) ||
         misaligned4(done) || misaligned4(scores_out) || misaligned4(parent) || misaligned4(tokens) || misaligned4(row_status))
         return FSD_ERR_LAYOUT;
-    const BeamSpace w = beam_space(s, B, beams, n);
+    const BeamSpace w = beam_space(B, beams, V, n);
     if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return FSD_ERR_WORKSPACE;
+    if (static_cast<size_t>(B) * beams * s.S > w.lists) return FSD_ERR_SHAPE;   // (never)
     const size_t read = (static_cast<size_t>(B) * beams - 1) * static_cast<size_t>(row_stride) * es + static_cast<size_t>(V) * es;
     const Run runs[] = {{scores_out, out}, {parent, out}, {tokens, out}, {row_status, static_cast<size_t>(B) * 4}, {workspace, w.bytes},
                         {scores, in}, {weights, in}, {done, in}, {logits, read}};

@@ -59,6 +59,8 @@ def test_workspace_sizes():
                 for dtype in (fsd.F32, fsd.BF16):
                     n = fsd.fsd_beam_workspace_bytes(B, W, V, 128, dtype)
                     assert n > 0 and n % 256 == 0
+                    for smaller in ((max(1, B // 2), W, V, 128), (B, max(1, W - 1), V, 128), (B, W, max(1, V - 1000), 128), (B, W, V // 2 + 1, 100)):
+                        assert fsd.fsd_beam_workspace_bytes(*smaller, dtype) <= n
     assert fsd.fsd_cache_fork_workspace_bytes(1, 1) > 0 and fsd.fsd_cache_fork_workspace_bytes(1 << 24, 65535) > 0
     assert fsd.fsd_cache_fork_workspace_bytes(0, 1) == fsd.fsd_cache_fork_workspace_bytes(5, 0) == fsd.fsd_cache_fork_workspace_bytes((1 << 24) + 1, 1) == 0
     assert fsd.fsd_cache_fork_workspace_bytes(5, 65536) == fsd.fsd_cache_compact_workspace_bytes(0) == fsd.fsd_cache_compact_workspace_bytes((1 << 24) + 1) == 0
