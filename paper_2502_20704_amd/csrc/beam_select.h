@@ -1,11 +1,18 @@
 // The best continuations of a sequence's beams (fsd_beam_select) and the states that follow them (fsd_beam_reorder).
 // Part of libfsd (gfx950).
 //
-// beam_slices goes over the logits once: a workgroup has a slice of one beam's row in registers, adds up its exponentials and writes its n
-// best entries, best first.  beam_merge, a workgroup a sequence, makes the normalisers of the beams from the slices' sums and takes the n best of
-// all slices' lists.  Order matters to the last bit (two beams' entries may lie as near to one another as their normalisers' errors), so
-// exponentials, sums and ranks are binary64; on this machine a binary64 fma issues like a binary32 one, and the hardware's binary32
-// exponential takes four times as long, so that this costs what a corrected binary32 exponential would.
+// beam_slices goes over the logits once: a workgroup takes a slice of one beam's row, adds up its exponentials and writes its n best entries, best
+// first.  beam_merge, a workgroup a sequence, makes the normalisers of the beams from the slices' sums and takes the n best of all slices' lists.
+//
+// Whole numbers come out of it, so the order matters to the last bit: two beams' entries may lie as near to one another as their normalisers' errors.
+// Exponentials, sums and ranks are binary64 therefore.  A binary64 fma issues like a binary32 one here (2.0 ns a wavefront and SIMD, as an addition or
+// a conversion), the hardware's binary32 exponential takes 3.8: 16 instructions an entry where binary32 would take 9, and an error of 2^-34 in place of 2^-25.
+//
+// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 38 us; reading them alone 18): vector instructions, 13 an entry, take
+// 27 us of it, the table's reads 15 of the LDS's time; the rest is each row's beginning (a round trip for its score, one for its first entries) and
+// end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us;
+// the list of 60 takes as many instructions as the exponentials.  Merging: 5.5 us for 4 beams, 8 for 64 sequences of 8, 10 at n = 60: a chain of
+// round trips and barriers.
 #ifndef FSD_CSRC_BEAM_SELECT_H_
 #define FSD_CSRC_BEAM_SELECT_H_
 
@@ -71,7 +78,7 @@ __device__ __forceinline__ double rotated(double x) {
     const unsigned lo = static_cast<unsigned>(rotated<N>(static_cast<int>(u))), hi = static_cast<unsigned>(rotated<N>(static_cast<int>(u >> 32)));
     return __builtin_bit_cast(double, static_cast<unsigned long>(hi) << 32 | lo);
 }
-__device__ __forceinline__ double row_sum(double x) {          // of 16 lanes: exact in none but the order
+__device__ __forceinline__ double row_sum(double x) {          // of 16 lanes
     x += rotated<8>(x);
     x += rotated<4>(x);
     x += rotated<2>(x);
@@ -163,7 +170,7 @@ __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, 
         for (int k = tid; k < len; k += 64 * NW) have += word_at(k) >= c;
         if (over_wg(have) >= n) least = c;
     }
-    // (of bfloat16 entries the low 16 bits: 0 of a positive one, 1 of a negative one; the bits found say which)
+    // (an ordered word's low 16 bits are those of a bfloat16 entry's zeros: all 0 of a positive one, all 1 of a negative one)
     if (BF16 && !(least & 0x80000000u)) least |= 0xFFFFu;
     if (least < kLeastOrdered) least = kLeastOrdered;
     int above = 0;
@@ -192,6 +199,7 @@ __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, 
 __device__ __forceinline__ int keep_reaching(unsigned long* list, int count, unsigned bound, int lane) {
     int kept = 0;
     for (int k0 = 0; k0 < count; k0 += 64) {
+        __builtin_amdgcn_wave_barrier();                     // (lanes read what others have written; no instruction, an order for the compiler)
         const unsigned long x = k0 + lane < count ? list[k0 + lane] : 0;
         const bool keep = static_cast<unsigned>(x >> 32) >= bound;
         const unsigned long who = __ballot(keep);
@@ -208,6 +216,7 @@ __device__ __forceinline__ int slots_apart(const u32x4* slots, const int* places
     constexpr int E = BF16 ? 8 : 4;
     const float from = from_ordered(least);
     bool full = false;
+    __builtin_amdgcn_wave_barrier();
     for (int s0 = 0; s0 < aside; s0 += 64 / E) {
         const int k = s0 + lane / E;
         bool is = false;
@@ -256,13 +265,13 @@ __device__ __forceinline__ unsigned wave_bound(unsigned word, int q) {
     return bound;
 }
 
-// One slice of a row a workgroup, in chunks of NS slots of 16 bytes a thread; where a slot has been added up, that of the next chunk is requested in its
-// place.  Of the entries seen so far a wavefront's q-th largest lane maximum, q = n / 4 rounded up, is reached by q of its own at least, so the
-// least of the four wavefronts' by n of the slice: what reaches that bound (few more than n entries where the values lie as those of logits do) is put
+// Slices of rows, one after the other in a workgroup, in chunks of NS slots of 16 bytes a thread; where a slot has been added up, that of the next chunk is requested in its
+// place.  Of the entries seen so far a wavefront's q-th largest lane maximum, q = n / wavefronts rounded up, is reached by q of its own at least, so
+// the least of the wavefronts' by n of the slice: what reaches that bound (few more than n entries where the values lie as those of logits do) is put
 // into LDS and ranked there at the end.  Wavefronts tell one another their bounds without waiting: an older one of another's bounds as well.
 // Exponentials are added up as e^z: binary64 has the range where logits are of the size that models give them.  Where they are not, the slice is gone over again.
 // TABLE: exponentials of bfloat16 numbers are read from a table of all of them from 2^-12 to 64 of either sign (and 0, and those under -64, which
-// count as nothing), which a workgroup makes once and keeps for all of its slices: 7 instructions an entry where the polynomial takes 16.
+// count as nothing), which a workgroup makes once and keeps for all of its slices: 7 instructions an entry where the polynomial takes 16 (51 -> 38 us for the rows above).
 template <bool BF16, int NS, bool TABLE>
 __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamParams P) {
     constexpr int NW = TABLE ? 8 : 4, T = NW * 64;
@@ -279,253 +288,253 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     const int tid = threadIdx.x, wave = uniform(tid / 64), lane = tid % 64;
     bool begun = false;                                       // the table is there
     for (unsigned unit = blockIdx.x; unit < P.units; unit += gridDim.x) {
-    const unsigned row = unit / static_cast<unsigned>(P.S);
-    const int slice = static_cast<int>(unit - row * static_cast<unsigned>(P.S));
-    if (!beam_runs(P, row)) continue;
-    const int begin = slice * P.len, end = begin + P.len < P.V ? begin + P.len : P.V;
-    const char* const z = P.logits + static_cast<size_t>(row) * P.row_stride;
-    const char* const at_begin = z + static_cast<size_t>(begin) * (16 / E);
-    const int slots = (end - begin) / E, all_slots = (end - begin + E - 1) / E;   // whole ones; and with a last one that is not
-    // (threads without a slot request the last one again: requests without branches go out together)
-    auto request = [&](int slot) {
-        const int from = slot < slots ? slot : slots - 1;
-        return static_cast<u32x4>(*reinterpret_cast<const u32x4_any*>(at_begin + static_cast<unsigned>(from) * 16u));
-    };
-    u32x4 r[NS];
+        const unsigned row = unit / static_cast<unsigned>(P.S);
+        const int slice = static_cast<int>(unit - row * static_cast<unsigned>(P.S));
+        if (!beam_runs(P, row)) continue;
+        const int begin = slice * P.len, end = begin + P.len < P.V ? begin + P.len : P.V;
+        const char* const z = P.logits + static_cast<size_t>(row) * P.row_stride;
+        const char* const at_begin = z + static_cast<size_t>(begin) * (16 / E);
+        const int slots = (end - begin) / E, all_slots = (end - begin + E - 1) / E;   // whole ones; and with a last one that is not
+        // (threads without a slot request the last one again: requests without branches go out together)
+        auto request = [&](int slot) {
+            const int from = slot < slots ? slot : slots - 1;
+            return static_cast<u32x4>(*reinterpret_cast<const u32x4_any*>(at_begin + static_cast<unsigned>(from) * 16u));
+        };
+        u32x4 r[NS];
 #pragma unroll
-    for (int i = 0; i < NS; ++i) r[i] = u32x4{kNone, kNone, kNone, kNone};
-    if (slots > 0) {
+        for (int i = 0; i < NS; ++i) r[i] = u32x4{kNone, kNone, kNone, kNone};
+        if (slots > 0) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i) r[i] = request(i * T + tid);
-    }
-    if (TABLE && !begun) {                                    // (while the first requests are on their way; the barrier before its first use comes below)
-        begun = true;
-        for (int k = tid; k < 2 * kTableEnd; k += T) {
-            const int u = k < kTableEnd ? k : k - kTableEnd;
-            const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
-            table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
+            for (int i = 0; i < NS; ++i) r[i] = request(i * T + tid);
         }
-    }
-    // the entries behind the last whole slot: its thread takes them one by one
-    u32x4 last = {kNone, kNone, kNone, kNone};
-    if (slots < all_slots) {
-        const int whole = begin + slots * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (whole + e < end) {
-                if constexpr (BF16) {
-                    const unsigned h = reinterpret_cast<const unsigned short*>(z)[whole + e];
-                    last[e / 2] = e & 1 ? (last[e / 2] & 0xFFFFu) | h << 16 : (last[e / 2] & 0xFFFF0000u) | h;
-                } else {
-                    last[e] = reinterpret_cast<const unsigned*>(z)[whole + e];
-                }
-            }
-    }
-    auto behind = [&](u32x4& slot, int k) {                   // slots that the slice does not have, or not whole
-#pragma unroll
-        for (int j = 0; j < 4; ++j) slot[j] = k < slots ? slot[j] : k == slots ? last[j] : kNone;
-    };
-
-    unsigned long* const mine_list = list + wave * kWaveList;
-    int count = 0;                                            // of the wavefront's list
-    bool full = false;                                        // whether more were to go into it than it holds
-    int aside = 0;
-    const int q = (P.n + NW - 1) / NW;
-    unsigned least = kLeastOrdered;
-    auto take_apart = [&]() {
-        const int to = slots_apart<BF16>(aside_slot[wave], aside_at[wave], aside, mine_list, count, least, lane);
-        count = to & 0xFFFF;
-        full |= to > 0xFFFF;
-        aside = 0;
-    };
-    auto all_bounds = [&]() {
-        unsigned bound = 0xFFFFFFFFu;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const unsigned theirs = uniform(__hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
-            bound = theirs < bound ? theirs : bound;
-        }
-        least = bound > least ? bound : least;
-    };
-    auto slot_max = [&](const u32x4& slot) {
-        float m = -__builtin_inff();
-#pragma unroll
-        for (int e = 0; e < E; e += 2) m = max3(m, slot_entry<BF16>(slot, e), slot_entry<BF16>(slot, e + 1));
-        return m;
-    };
-
-    // the first chunk's bound
-    float mine = -__builtin_inff();                           // the lane's largest so far
-    if (kChunk > slots) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i) behind(r[i], i * T + tid);
-    }
-#pragma unroll
-    for (int i = 0; i < NS; ++i) mine = __builtin_fmaxf(mine, slot_max(r[i]));
-    {
-        const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
-        if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    }
-    __syncthreads();
-    all_bounds();
-
-    bool broken = false;                                      // an entry is NaN or +inf
-    double sum[2] = {0.0, 0.0};
-    int chunk = 0;
-    for (int first = 0; first < all_slots; first += kChunk, ++chunk) {
-        const float from = from_ordered(least);
-        const bool ends = first + 2 * kChunk > slots;         // whether the next chunk is not whole, or none
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            const int slot = first + i * T + tid;
-            const float top = slot_max(r[i]);
-            mine = __builtin_fmaxf(mine, top);
-            // a slot with an entry that reaches the bound is put aside whole, to be taken apart with others
-            const unsigned long who = __ballot(top >= from);
-            if (who != 0) {
-                if (top >= from) {
-                    const int k = aside + __popcll(who & ((1ul << lane) - 1));
-                    aside_slot[wave][k] = r[i];
-                    aside_at[wave][k] = slot;
-                }
-                aside += __popcll(who);
-                if (aside > kAside - 64) take_apart();
-            }
-#pragma unroll
-            for (int e = 0; e < E; e += 2) broken |= __builtin_isunordered(slot_entry<BF16>(r[i], e), slot_entry<BF16>(r[i], e + 1));
-            if constexpr (TABLE) {                            // (also where it does not hold: then all of it is gone over again)
-                u16x2 least_index = {0xFFFF, 0xFFFF}, index[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const unsigned w = r[i][j];
-                    const u16x2 v = __builtin_bit_cast(u16x2, w);
-                    u16x2 u = __builtin_elementwise_sub_sat(v & static_cast<unsigned short>(0x7FFF), u16x2{kTableBase, kTableBase});
-                    u = __builtin_elementwise_min(u, u16x2{kTableEnd - 1, kTableEnd - 1});
-                    least_index = __builtin_elementwise_min(least_index, u);
-                    index[j] = (v >> static_cast<unsigned short>(15)) * static_cast<unsigned short>(kTableEnd) + u;
-                }
-                double e[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    e[2 * j] = table[index[j].x];
-                    e[2 * j + 1] = table[index[j].y];
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j & 1] += e[j];
-                if (__ballot(least_index.x == 0 || least_index.y == 0) != 0) {
-                    sum[0] += rest_of_small(r[i]);            // (in a few slots of a hundred)
-                }
-            } else {
-                // (what is under -700 counts as -700: nothing beside a largest entry of -600 or more)
-#pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    sum[0] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e))));
-                    sum[1] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e + 1))));
-                }
-            }
-            if (first + kChunk < all_slots) {
-                r[i] = request(slot + kChunk);
-                if (ends) behind(r[i], slot + kChunk);
+        if (TABLE && !begun) {                                    // (while the first requests are on their way; the barrier before its first use comes below)
+            begun = true;
+            for (int k = tid; k < 2 * kTableEnd; k += T) {
+                const int u = k < kTableEnd ? k : k - kTableEnd;
+                const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
+                table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
             }
         }
-        // the bound anew where the entries seen have doubled
-        if ((chunk & (chunk + 1)) == 0 && first + kChunk < all_slots && chunk > 0) {
+        // the entries behind the last whole slot: its thread takes them one by one
+        u32x4 last = {kNone, kNone, kNone, kNone};
+        if (slots < all_slots) {
+            const int whole = begin + slots * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (whole + e < end) {
+                    if constexpr (BF16) {
+                        const unsigned h = reinterpret_cast<const unsigned short*>(z)[whole + e];
+                        last[e / 2] = e & 1 ? (last[e / 2] & 0xFFFFu) | h << 16 : (last[e / 2] & 0xFFFF0000u) | h;
+                    } else {
+                        last[e] = reinterpret_cast<const unsigned*>(z)[whole + e];
+                    }
+                }
+        }
+        auto behind = [&](u32x4& slot, int k) {                   // slots that the slice does not have, or not whole
+#pragma unroll
+            for (int j = 0; j < 4; ++j) slot[j] = k < slots ? slot[j] : k == slots ? last[j] : kNone;
+        };
+
+        unsigned long* const mine_list = list + wave * kWaveList;
+        int count = 0;                                            // of the wavefront's list
+        bool full = false;                                        // whether more were to go into it than it holds
+        int aside = 0;
+        const int q = (P.n + NW - 1) / NW;
+        unsigned least = kLeastOrdered;
+        auto take_apart = [&]() {
+            const int to = slots_apart<BF16>(aside_slot[wave], aside_at[wave], aside, mine_list, count, least, lane);
+            count = to & 0xFFFF;
+            full |= to > 0xFFFF;
+            aside = 0;
+        };
+        auto all_bounds = [&]() {
+            unsigned bound = 0xFFFFFFFFu;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const unsigned theirs = uniform(__hip_atomic_load(&bounds[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+                bound = theirs < bound ? theirs : bound;
+            }
+            least = bound > least ? bound : least;
+        };
+        auto slot_max = [&](const u32x4& slot) {
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int e = 0; e < E; e += 2) m = max3(m, slot_entry<BF16>(slot, e), slot_entry<BF16>(slot, e + 1));
+            return m;
+        };
+
+        // the first chunk's bound
+        float mine = -__builtin_inff();                           // the lane's largest so far
+        if (kChunk > slots) {
+#pragma unroll
+            for (int i = 0; i < NS; ++i) behind(r[i], i * T + tid);
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) mine = __builtin_fmaxf(mine, slot_max(r[i]));
+        {
             const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
             if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
+        __syncthreads();
         all_bounds();
-    }
-    const float top = wave_largest(mine);
-    double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
-    if ((TABLE ? top >= 64.0f || top < -20.0f : top > 600.0f || top < -600.0f) && top > -__builtin_inff()) {
-        // again, as e^(z - top)
-        ref = top;
-        sum[0] = sum[1] = 0.0;
-        for (int slot = tid; slot < all_slots; slot += T) {
-            u32x4 x = slots > 0 ? request(slot) : u32x4{kNone, kNone, kNone, kNone};
-            behind(x, slot);
+
+        bool broken = false;                                      // an entry is NaN or +inf
+        double sum[2] = {0.0, 0.0};
+        int chunk = 0;
+        for (int first = 0; first < all_slots; first += kChunk, ++chunk) {
+            const float from = from_ordered(least);
+            const bool ends = first + 2 * kChunk > slots;         // whether the next chunk is not whole, or none
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e & 1] += exp_below(static_cast<double>(slot_entry<BF16>(x, e)) - ref);
+            for (int i = 0; i < NS; ++i) {
+                const int slot = first + i * T + tid;
+                const float top = slot_max(r[i]);
+                mine = __builtin_fmaxf(mine, top);
+                // a slot with an entry that reaches the bound is put aside whole, to be taken apart with others
+                const unsigned long who = __ballot(top >= from);
+                if (who != 0) {
+                    if (top >= from) {
+                        const int k = aside + __popcll(who & ((1ul << lane) - 1));
+                        aside_slot[wave][k] = r[i];
+                        aside_at[wave][k] = slot;
+                    }
+                    aside += __popcll(who);
+                    if (aside > kAside - 64) take_apart();
+                }
+#pragma unroll
+                for (int e = 0; e < E; e += 2) broken |= __builtin_isunordered(slot_entry<BF16>(r[i], e), slot_entry<BF16>(r[i], e + 1));
+                if constexpr (TABLE) {                            // (also where it does not hold: then all of it is gone over again)
+                    u16x2 least_index = {0xFFFF, 0xFFFF}, index[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned w = r[i][j];
+                        const u16x2 v = __builtin_bit_cast(u16x2, w);
+                        u16x2 u = __builtin_elementwise_sub_sat(v & static_cast<unsigned short>(0x7FFF), u16x2{kTableBase, kTableBase});
+                        u = __builtin_elementwise_min(u, u16x2{kTableEnd - 1, kTableEnd - 1});
+                        least_index = __builtin_elementwise_min(least_index, u);
+                        index[j] = (v >> static_cast<unsigned short>(15)) * static_cast<unsigned short>(kTableEnd) + u;
+                    }
+                    double e[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        e[2 * j] = table[index[j].x];
+                        e[2 * j + 1] = table[index[j].y];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j & 1] += e[j];
+                    if (__ballot(least_index.x == 0 || least_index.y == 0) != 0) {
+                        sum[0] += rest_of_small(r[i]);            // (in a few slots of a hundred)
+                    }
+                } else {
+                    // (what is under -700 counts as -700: nothing beside a largest entry of -600 or more)
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) {
+                        sum[0] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e))));
+                        sum[1] += exp_within(static_cast<double>(at_least_700_below(slot_entry<BF16>(r[i], e + 1))));
+                    }
+                }
+                if (first + kChunk < all_slots) {
+                    r[i] = request(slot + kChunk);
+                    if (ends) behind(r[i], slot + kChunk);
+                }
+            }
+            // the bound anew where the entries seen have doubled
+            if ((chunk & (chunk + 1)) == 0 && first + kChunk < all_slots && chunk > 0) {
+                const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
+                if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+            all_bounds();
         }
-    }
-    double s = wave_sum_64(sum[0] + sum[1]);
-    if (!(top > -__builtin_inff())) s = 0.0;
-    const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
-    // the final bound, made of all four wavefronts' entries
-    {
-        const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
-        if (lane == 0) {
-            wave_ref[wave] = ref;
-            wave_sum[wave] = any_broken ? __builtin_nan("") : s;
-            __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        const float top = wave_largest(mine);
+        double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
+        if ((TABLE ? top >= 64.0f || top < -20.0f : top > 600.0f || top < -600.0f) && top > -__builtin_inff()) {
+            // again, as e^(z - top)
+            ref = top;
+            sum[0] = sum[1] = 0.0;
+            for (int slot = tid; slot < all_slots; slot += T) {
+                u32x4 x = slots > 0 ? request(slot) : u32x4{kNone, kNone, kNone, kNone};
+                behind(x, slot);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e & 1] += exp_below(static_cast<double>(slot_entry<BF16>(x, e)) - ref);
+            }
         }
-    }
-    __syncthreads();
-    all_bounds();
-    take_apart();
-    count = keep_reaching(mine_list, count, least, lane);
-    if (lane == 0) lds[wave] = full ? kWaveList + 1 : count;
-    __syncthreads();
-    int counts[NW], have = 0, most = 0;
+        double s = wave_sum_64(sum[0] + sum[1]);
+        if (!(top > -__builtin_inff())) s = 0.0;
+        const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
+        // the final bound, made of all four wavefronts' entries
+        {
+            const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
+            if (lane == 0) {
+                wave_ref[wave] = ref;
+                wave_sum[wave] = any_broken ? __builtin_nan("") : s;
+                __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+        }
+        __syncthreads();
+        all_bounds();
+        take_apart();
+        count = keep_reaching(mine_list, count, least, lane);
+        if (lane == 0) lds[wave] = full ? kWaveList + 1 : count;
+        __syncthreads();
+        int counts[NW], have = 0, most = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        counts[w] = uniform(lds[w]);
-        have += counts[w];
-        most = counts[w] > most ? counts[w] : most;
-    }
-    const size_t at = static_cast<size_t>(row) * P.S + slice;   // of [B, W * S]
-    const int b = static_cast<int>(row / static_cast<unsigned>(P.W));
-    const size_t lists = P.lists, column = at - static_cast<size_t>(b) * lists;
-    float2* const cand = P.cand + static_cast<size_t>(b) * P.n * lists + column;
-    auto put = [&](int rank, unsigned long me) {
-        if (rank < P.n)
-            cand[rank * lists] = make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
-    };
-    if (most <= 64) {
-        // a lane holds an entry of each wavefront's; a wavefront finds the ranks of its own one after the other
-        unsigned long other[NW];
+        for (int w = 0; w < NW; ++w) {
+            counts[w] = uniform(lds[w]);
+            have += counts[w];
+            most = counts[w] > most ? counts[w] : most;
+        }
+        const size_t at = static_cast<size_t>(row) * P.S + slice;   // of [B, W * S]
+        const int b = static_cast<int>(row / static_cast<unsigned>(P.W));
+        const size_t lists = P.lists, column = at - static_cast<size_t>(b) * lists;
+        float2* const cand = P.cand + static_cast<size_t>(b) * P.n * lists + column;
+        auto put = [&](int rank, unsigned long me) {
+            if (rank < P.n)
+                cand[rank * lists] = make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
+        };
+        if (most <= 64) {
+            // a lane holds an entry of each wavefront's; a wavefront finds the ranks of its own one after the other
+            unsigned long other[NW];
 #pragma unroll
-        for (int w = 0; w < NW; ++w) other[w] = lane < counts[w] ? list[w * kWaveList + lane] : 0;
-        const unsigned long own = lane < count ? mine_list[lane] : 0;
-        int my_rank = 0;
+            for (int w = 0; w < NW; ++w) other[w] = lane < counts[w] ? list[w * kWaveList + lane] : 0;
+            const unsigned long own = lane < count ? mine_list[lane] : 0;
+            int my_rank = 0;
 #pragma unroll 4
-        for (int k = 0; k < count; ++k) {
-            const unsigned long me = lane_word(own, k);
-            int rank = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) rank += __popcll(__ballot(other[w] > me));
-            my_rank = lane == k ? rank : my_rank;
-        }
-        if (lane < count) put(my_rank, own);
-    } else {
-        if (most > kWaveList) {
-            __syncthreads();                                  // (all have read the counts)
-            have = slice_cut<BF16, NW>(z, begin, end, P.n, list, lds, tid);
-#pragma unroll
-            for (int w = 0; w < NW; ++w) counts[w] = w == 0 ? have : 0;   // (at most n of them)
-        }
-#pragma unroll
-        for (int v = 0; v < NW; ++v)
-            for (int k = tid; k < counts[v]; k += T) {
-                const unsigned long me = list[v * kWaveList + k];
+            for (int k = 0; k < count; ++k) {
+                const unsigned long me = lane_word(own, k);
                 int rank = 0;
 #pragma unroll
-                for (int w = 0; w < NW; ++w)
-                    for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
-                put(rank, me);
+                for (int w = 0; w < NW; ++w) rank += __popcll(__ballot(other[w] > me));
+                my_rank = lane == k ? rank : my_rank;
             }
-    }
-    for (int k = have + tid; k < P.n; k += T) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
-    if (tid == T - 1) {
-        double m = -__builtin_inf(), total = 0.0;
-        for (int w = 0; w < NW; ++w) m = wave_ref[w] > m ? wave_ref[w] : m;
-        for (int w = 0; w < NW; ++w) {
-            const double d = wave_ref[w] - m;                 // (NaN where the slice has no entry)
-            total += d < 0.0 ? (wave_ref[w] > -__builtin_inf() ? wave_sum[w] * exp_below(d) : wave_sum[w]) : wave_sum[w];
+            if (lane < count) put(my_rank, own);
+        } else {
+            if (most > kWaveList) {
+                __syncthreads();                                  // (all have read the counts)
+                have = slice_cut<BF16, NW>(z, begin, end, P.n, list, lds, tid);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) counts[w] = w == 0 ? have : 0;   // (at most n of them)
+            }
+#pragma unroll
+            for (int v = 0; v < NW; ++v)
+                for (int k = tid; k < counts[v]; k += T) {
+                    const unsigned long me = list[v * kWaveList + k];
+                    int rank = 0;
+#pragma unroll
+                    for (int w = 0; w < NW; ++w)
+                        for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
+                    put(rank, me);
+                }
         }
-        P.stat[at] = make_double2(m, total);
-    }
-    __syncthreads();                                          // (the next slice's bounds and lists go where these were)
+        for (int k = have + tid; k < P.n; k += T) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
+        if (tid == T - 1) {
+            double m = -__builtin_inf(), total = 0.0;
+            for (int w = 0; w < NW; ++w) m = wave_ref[w] > m ? wave_ref[w] : m;
+            for (int w = 0; w < NW; ++w) {
+                const double d = wave_ref[w] - m;                 // (NaN where the slice has no entry)
+                total += d < 0.0 ? (wave_ref[w] > -__builtin_inf() ? wave_sum[w] * exp_below(d) : wave_sum[w]) : wave_sum[w];
+            }
+            P.stat[at] = make_double2(m, total);
+        }
+        __syncthreads();                                          // (the next slice's bounds and lists go where these were)
     }
 }
 

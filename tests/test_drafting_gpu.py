@@ -51,7 +51,7 @@ SELECT = [
     (1, 1, 1, 1, "f32"), (1, 1, 1, 5, "bf16"), (2, 3, 7, 4, "f32"), (2, 2, 3, 128, "bf16"), (3, 4, 1000, 8, "bf16"), (1, 4, 32000, 8, "bf16"),
     (1, 1, 32001, 1, "f32"), (5, 2, 2049, 3, "bf16"), (2, 8, 128257, 16, "bf16"), (2, 3, 128256, 60, "f32"), (1, 1, 262145, 128, "f32"),
     (1, 256, 515, 128, "bf16"), (70, 16, 999, 20, "f32"), (40, 32, 2056, 64, "bf16"), (1, 2, 524288, 33, "bf16"), (300, 1, 515, 2, "bf16"),
-    (130, 9, 16385, 100, "bf16"),
+    (130, 9, 16385, 100, "bf16"), (65535, 1, 5, 3, "bf16"), (1, 256, 70000, 128, "bf16"),
 ]
 
 
@@ -443,12 +443,13 @@ def test_select_long_rows(n):
 
 def test_select_long_rows_reports():
     z, scores = _long_rows()
+    z[3, 4, 99].view(torch.int16).fill_(0x7F81)               # a signalling NaN
     z[0, 7, 100002], z[1, 0, 3], z[4, 2, 77], z[6, 6, 50001] = float("nan"), float("inf"), -float("nan"), float("nan")
     done = np.zeros((12, 8), np.int32)
     done[6, 6], done[2, 1] = 1, 1
     got = fsd.fsd_beam_select(z.cuda(), _dev(scores), 5, done=_dev(done))
     want = ref.select(_host(z), scores, None, done, 5)
-    assert [b for b in range(12) if want[3][b]] == [0, 1, 4]
+    assert [b for b in range(12) if want[3][b]] == [0, 1, 3, 4]
     _same_selection(got, (*want[:4], np.inf))
 
 
