@@ -8,11 +8,12 @@
 // Exponentials, sums and ranks are binary64 therefore.  A binary64 fma issues like a binary32 one here (2.0 ns a wavefront and SIMD, as an addition or
 // a conversion), the hardware's binary32 exponential takes 3.8: 16 instructions an entry where binary32 would take 9, and an error of 2^-34 in place of 2^-25.
 //
-// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 38 us; reading them alone 18): vector instructions, 13 an entry, take
-// 27 us of it, the table's reads 15 of the LDS's time; the rest is each row's beginning (a round trip for its score, one for its first entries) and
-// end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us;
-// the list of 60 takes as many instructions as the exponentials.  Merging: 5.5 us for 4 beams, 8 for 64 sequences of 8, 10 at n = 60: a chain of
-// round trips and barriers.
+// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 37 us; reading them alone 18): vector instructions, 12.6
+// an entry, take 25 us of it, the table's reads 15 of the LDS's time beside them; the rest is each row's beginning (a round trip for its score, one for
+// its first entries) and end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  Without the sums it would
+// take 25 us, without slots put aside 32, without the making of the table 36.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us; the list
+// of 60 takes as many instructions as the exponentials.  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 11 at n = 60: a chain of round trips
+// and barriers.
 #ifndef FSD_CSRC_BEAM_SELECT_H_
 #define FSD_CSRC_BEAM_SELECT_H_
 
@@ -26,7 +27,7 @@ constexpr int kBeamMost = 128;      // n
 constexpr int kBeamWidest = 256;    // beams
 constexpr int kWaveList = 256;      // entries of a wavefront's part of a slice that stand in LDS before the n best are taken from all
 constexpr unsigned short kTableBase = 0x397F;   // bits of the last bfloat16 number under 2^-12
-constexpr unsigned short kTableEnd = 0x4280 - kTableBase + 1;   // entries of either sign: 0, 2^-12 to the last number under 64, 64 and over
+constexpr unsigned short kTableEnd = 2 * (0x4280 - kTableBase);   // entries: 0; 2^-12, -2^-12 and so on to the last numbers under 64; two and the last one for 64 and over
 constexpr int kAside = 112;         // slots of a wavefront's that stand there until they are taken apart
 constexpr double kLog2e64 = 1.4426950408889634074;
 
@@ -143,7 +144,9 @@ __device__ __forceinline__ float slot_entry(const u32x4& r, int e) {
 
 __device__ __forceinline__ float score_of(const BeamParams& P, long at) { return P.scores ? P.scores[at] : 0.0f; }
 __device__ __forceinline__ bool beam_runs(const BeamParams& P, long at) {   // whether a beam's row is read
-    return score_of(P, at) > -__builtin_inff() && !(P.done && P.done[at]);   // (a score that is NaN is reported without its row)
+    const float score = score_of(P, at);
+    const int done = P.done ? P.done[at] : 0;                // (both requested together)
+    return (score > -__builtin_inff()) & (done == 0);        // (a score that is NaN is reported without its row)
 }
 
 // A slice's n best entries where more than kWaveList of a wavefront's reach the bound that its lanes gave (rows of equal entries, or in order): the n-th largest
@@ -242,6 +245,15 @@ __device__ __forceinline__ int slots_apart(const u32x4* slots, const int* places
     return count + (full ? 0x10000 : 0);
 }
 
+// eight times the lower (0) or upper (1) half of a word
+template <int HALF>
+__device__ __forceinline__ unsigned eight_times(unsigned both) {
+    unsigned x;
+    if constexpr (HALF == 0) asm("v_mad_u32_u16 %0, %1, 8, 0" : "=v"(x) : "v"(both));
+    else asm("v_mad_u32_u16 %0, %1, 8, 0 op_sel:[1,0,0,0]" : "=v"(x) : "v"(both));
+    return x;
+}
+
 // Of the entries of a slot that are nearer to 0 than the table goes, and count as 0: what that leaves out
 __device__ __forceinline__ double rest_of_small(u32x4 slot) {
     double rest = 0.0;
@@ -281,7 +293,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
     __shared__ unsigned long list[NW * kWaveList];
     __shared__ u32x4 aside_slot[NW][kAside];
     __shared__ int aside_at[NW][kAside];
-    __shared__ double table[TABLE ? 2 * kTableEnd : 1];
+    __shared__ double table[TABLE ? kTableEnd + 1 : 1];
     __shared__ double wave_sum[NW], wave_ref[NW];
     __shared__ unsigned bounds[NW];
     __shared__ int lds[NW + 1];
@@ -309,10 +321,9 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         }
         if (TABLE && !begun) {                                    // (while the first requests are on their way; the barrier before its first use comes below)
             begun = true;
-            for (int k = tid; k < 2 * kTableEnd; k += T) {
-                const int u = k < kTableEnd ? k : k - kTableEnd;
-                const double x = u == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + u) << 16));
-                table[k] = u == kTableEnd - 1 ? 0.0 : exp_within(k < kTableEnd ? x : -x);
+            for (int k = tid; k <= kTableEnd; k += T) {
+                const double x = k == 0 ? 0.0 : static_cast<double>(__uint_as_float(static_cast<unsigned>(kTableBase + (k + 1) / 2) << 16));
+                table[k] = k >= kTableEnd - 1 ? 0.0 : exp_within(k & 1 ? x : -x);
             }
         }
         // the entries behind the last whole slot: its thread takes them one by one
@@ -406,18 +417,17 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
                     u16x2 least_index = {0xFFFF, 0xFFFF}, index[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const unsigned w = r[i][j];
-                        const u16x2 v = __builtin_bit_cast(u16x2, w);
-                        u16x2 u = __builtin_elementwise_sub_sat(v & static_cast<unsigned short>(0x7FFF), u16x2{kTableBase, kTableBase});
-                        u = __builtin_elementwise_min(u, u16x2{kTableEnd - 1, kTableEnd - 1});
-                        least_index = __builtin_elementwise_min(least_index, u);
-                        index[j] = (v >> static_cast<unsigned short>(15)) * static_cast<unsigned short>(kTableEnd) + u;
+                        const u16x2 v = __builtin_bit_cast(u16x2, static_cast<unsigned>(r[i][j]));
+                        const u16x2 turned = v * static_cast<unsigned short>(2) + (v >> static_cast<unsigned short>(15));   // the sign behind the rest
+                        index[j] = __builtin_elementwise_min(__builtin_elementwise_sub_sat(turned, u16x2{2 * kTableBase + 1, 2 * kTableBase + 1}), u16x2{kTableEnd, kTableEnd});
+                        least_index = __builtin_elementwise_min(least_index, index[j]);
                     }
                     double e[8];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        e[2 * j] = table[index[j].x];
-                        e[2 * j + 1] = table[index[j].y];
+                        const unsigned both = __builtin_bit_cast(unsigned, index[j]);
+                        e[2 * j] = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + eight_times<0>(both));
+                        e[2 * j + 1] = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(table) + eight_times<1>(both));
                     }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[j & 1] += e[j];
@@ -442,7 +452,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
                 const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
                 if (lane == 0) __hip_atomic_store(&bounds[wave], bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             }
-            all_bounds();
+            if ((chunk & (chunk - 1)) == 0) all_bounds();     // (the others' by then)
         }
         const float top = wave_largest(mine);
         double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
@@ -566,7 +576,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     __shared__ float base[kBeamWidest];                       // a beam's score; NaN: its list does not count
     __shared__ float so_far[kBeamWidest];
     __shared__ float factor[kBeamWidest];
-    __shared__ unsigned wave_bound[NW];
+    __shared__ unsigned wave_bound[NW], wave_alone[NW];
     __shared__ int wave_count[2][NW];
     __shared__ int have, bad;
     const int tid = threadIdx.x, wave = uniform(tid / 64), b = blockIdx.x, W = P.W, S = P.S, n = P.n;
@@ -725,14 +735,16 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         }
         const unsigned word = ordered_high(most);
         const int q = (n + NW - 1) / NW;
-        unsigned bound = 0;
+        unsigned bound = 0, alone = 0;                        // its q-th largest, and its n-th: what n of its own reach bounds the n-th of all as well
         for (int bit = 31; bit >= 12; --bit) {                // (the upper 20 bits)
-            const unsigned c = bound | 1u << bit;
+            const unsigned c = bound | 1u << bit, d = alone | 1u << bit;
             if (__popcll(__ballot(word >= c)) >= q) bound = c;
+            if (__popcll(__ballot(word >= d)) >= n) alone = d;
         }
-        if (tid % 64 == 0) wave_bound[wave] = bound;
+        if (tid % 64 == 0) wave_bound[wave] = bound, wave_alone[wave] = alone;
         __syncthreads();
         for (int i = 0; i < NW; ++i) bound = wave_bound[i] < bound ? wave_bound[i] : bound;
+        for (int i = 0; i < NW; ++i) bound = wave_alone[i] > bound ? wave_alone[i] : bound;
         // (an entry that is none has the word of -inf; every other one a larger word)
         const unsigned none = ordered_high(-__builtin_inf());
         bound = bound > none ? bound : none + 1;
