@@ -571,6 +571,7 @@ int fsd_beam_reorder(const void* states, const int32_t* parent, int layers, int 
  * place of the parent's that holds some of its first `have` tokens names no block.  Such a sequence comes out empty.  FSD_ROW_NO_BLOCKS, for all of them: there are too few
  * free blocks; nothing is copied, refs_out is refs and every sequence comes out empty, so that the caller, who still has the old tables, can make room and call again.
  * Blocks of reserved places may hold anything.  The copied codes' cache is that of `cache` (written in place).
+ * Blocks are given out from refs, so calls that give out blocks of one pool go one after another, each with the refs_out of the one before.
  * n, B <= 65535, n * max_blocks < 2^31 - 1, num_blocks <= 2^24.
  */
 size_t fsd_cache_fork_workspace_bytes(int num_blocks, int n);

@@ -245,7 +245,7 @@ __device__ __forceinline__ int slots_apart(const u32x4* slots, const int* places
     return count + (full ? 0x10000 : 0);
 }
 
-// eight times the lower (0) or upper (1) half of a word
+// eight times the lower (0) or upper (1) half of a word, in one instruction
 template <int HALF>
 __device__ __forceinline__ unsigned eight_times(unsigned both) {
     unsigned x;
@@ -845,6 +845,8 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
 
 // ------------------------------------------------------------------------------------------ states
 
+// A piece of a row a workgroup at a time, 16 bytes a thread and step on whatever address (a wavefront's kilobyte is one run, so that the hardware splits
+// few of them).  Bound by the bytes: 163 MB read and written in 30 us, 5.4 TB/s, part of it in the caches; 53 KB in 2.8, a launch.
 struct ReorderParams {
     const char* states;
     const int* parent;

@@ -2,8 +2,12 @@
 // the front (fsd_cache_compact).  Part of libfsd (gfx950).
 //
 // Who gets which block has to come out the same on every run, so nothing hangs on the order in which workgroups come: counts and minima by
-// integer atomics, places of blocks and sequences by sums over what lies in front of them, one kernel behind the other.  What takes time
-// is the pages' bytes; the tables are small beside them.
+// integer atomics, places of blocks and sequences by sums over what lies in front of them, one kernel behind the other.
+//
+// What bounds it: where many pages move, their bytes (1.21 GB read and written by pages_copy in 240 us, 5.05 TB/s; a large copy reaches 4.9 here); where few do, the
+// launches that follow one another, 3 to 5 us each, and in fork_mark the atomics.  256 sequences of some 40000 tokens in one layer: fork_clear 3.0, fork_mark 10.7,
+// fork_count 4.2, fork_list 5.5, fork_apply 4.5 us with the few copies in it; 128 beams in 16 layers, 140 MB of begun pages: fork_small 9.8, fork_move 22 us.
+// Compacting a pool of 1200 blocks, 540 of them in use, 8 layers: compact_small 9, compact_move 136 us for 623 MB (4.6 TB/s).
 #ifndef FSD_CSRC_CACHE_PAGES_H_
 #define FSD_CSRC_CACHE_PAGES_H_
 
@@ -13,8 +17,8 @@ namespace {
 
 constexpr int kPagesChunk = 1024;   // blocks, or places, that a workgroup goes over at once
 constexpr int kNobody = 0x7FFFFFFF;
-// What one workgroup does by itself, its blocks' counts in LDS: four launches behind one another take 14 to 17 us on the device and 10 more on the host than
-// one.  One sequence's 4 beams: 5.2 us; 128 beams of 11 places: 8.5; at the limits here as long as the four kernels.
+// What one workgroup does by itself, its blocks' counts in LDS: the launches behind one another take 14 to 17 us on the device and 10 more on the host than
+// one.  One sequence's 4 beams: 5.2 us; 128 beams of 11 places: 8.5; at the limits here as long as the several kernels.
 constexpr int kSmallWG = 1024, kSmallBlocks = 4096, kSmallPlaces = 8192;
 
 // the sum of all threads' v, and of those below
@@ -57,6 +61,8 @@ struct PagesPair {                  // two caches of one geometry (or one cache 
 };
 // Of block `from` in the one cache to block `to` in the other: a layer's head, its first `groups` groups of 16 tokens.  Keys and values have them at the front of
 // a head's codes alike.
+// (A workgroup has both of a head's runs of 4 to 16 KB on their way at once.  Requests and stores past the caches: 3 % faster at 1.2 GB, and slower where the
+// pages lie in them.)
 __device__ __forceinline__ void move_head(const PagesPair& P, long from, long to, int layer, int head, int groups, int tid) {
     const long src = (static_cast<long>(layer) * P.blocks_from + from) * P.heads + head, dst = (static_cast<long>(layer) * P.blocks_to + to) * P.heads + head;
     const u32x4* k = reinterpret_cast<const u32x4*>(P.k_from + src * P.head_bytes);

@@ -128,6 +128,8 @@ PagesPair pages_pair(const fsd_cache& a, const fsd_cache& b) {
     p.head_bytes = kBlock * a.head_dim;
     return p;
 }
+inline size_t codes_bytes(const fsd_cache& c) { return static_cast<size_t>(c.layers) * c.num_blocks * c.kv_heads * kBlock * c.head_dim; }
+inline size_t scale_bytes(const fsd_cache& c) { return static_cast<size_t>(c.layers) * c.num_blocks * c.kv_heads * 4; }
 inline int chunks_of(int num_blocks) { return (num_blocks + kPagesChunk - 1) / kPagesChunk; }
 inline unsigned copy_groups(long units) { return static_cast<unsigned>(units < kCopyWGs ? units : kCopyWGs); }
 
@@ -265,8 +267,9 @@ int fsd_cache_fork(const fsd_cache* cache, int B, const int32_t* refs, const int
     const size_t per = static_cast<size_t>(c.max_blocks) * 4, seqs = static_cast<size_t>(n) * 4, blocks = static_cast<size_t>(c.num_blocks) * 4;
     const Run runs[] = {{block_table_out, n * per}, {cache_len_out, seqs}, {free_blocks, 4}, {row_status, seqs}, {workspace, w.bytes}, {refs_out, blocks},
                         {refs_out == refs ? nullptr : refs, blocks}, {parent, seqs}, {lengths, seqs}, {room, seqs}, {c.block_table, B * per},
-                        {c.cache_len, static_cast<size_t>(B) * 4}};
-    if (any_overlap(runs, 6, 12)) return FSD_ERR_LAYOUT;
+                        {c.cache_len, static_cast<size_t>(B) * 4}, {c.k_codes, codes_bytes(c)}, {c.v_codes, codes_bytes(c)}, {c.k_scale, scale_bytes(c)},
+                        {c.v_scale, scale_bytes(c)}};
+    if (any_overlap(runs, 6, 16)) return FSD_ERR_LAYOUT;
     char* base = static_cast<char*>(workspace);
     auto ints = [base](size_t at) { return reinterpret_cast<int*>(base + at); };
     ForkParams P;
@@ -320,15 +323,13 @@ int fsd_cache_copy(const fsd_cache* src, const fsd_cache* dst, const int32_t* sr
     if (n < 1 || src->layers != dst->layers || src->kv_heads != dst->kv_heads || src->head_dim != dst->head_dim) return FSD_ERR_SHAPE;
     const long units = static_cast<long>(n) * src->layers;   // (times heads: under 2^31 * 2^31)
     if (units >= (1L << 40) / src->kv_heads) return FSD_ERR_SHAPE;
-    const size_t list = static_cast<size_t>(n) * 4, codes = static_cast<size_t>(src->layers) * src->kv_heads * kBlock * src->head_dim,
-                 scales = static_cast<size_t>(src->layers) * src->kv_heads * 4;
+    const size_t list = static_cast<size_t>(n) * 4;
     const bool one = src->k_codes == dst->k_codes && src->v_codes == dst->v_codes && src->k_scale == dst->k_scale && src->v_scale == dst->v_scale &&
                      src->num_blocks == dst->num_blocks;
-    const size_t a = static_cast<size_t>(src->num_blocks), b = static_cast<size_t>(dst->num_blocks);
-    const Run runs[] = {{dst->k_codes, codes * b}, {dst->v_codes, codes * b}, {dst->k_scale, scales * b}, {dst->v_scale, scales * b}, {page_status, list},
-                        {src_blocks, list}, {dst_blocks, list}, {tokens, list},
-                        {one ? nullptr : src->k_codes, codes * a}, {one ? nullptr : src->v_codes, codes * a}, {one ? nullptr : src->k_scale, scales * a},
-                        {one ? nullptr : src->v_scale, scales * a}};
+    const Run runs[] = {{dst->k_codes, codes_bytes(*dst)}, {dst->v_codes, codes_bytes(*dst)}, {dst->k_scale, scale_bytes(*dst)}, {dst->v_scale, scale_bytes(*dst)},
+                        {page_status, list}, {src_blocks, list}, {dst_blocks, list}, {tokens, list},
+                        {one ? nullptr : src->k_codes, codes_bytes(*src)}, {one ? nullptr : src->v_codes, codes_bytes(*src)},
+                        {one ? nullptr : src->k_scale, scale_bytes(*src)}, {one ? nullptr : src->v_scale, scale_bytes(*src)}};
     if (any_overlap(runs, 5, 12) || misaligned4(src_blocks) || misaligned4(dst_blocks) || misaligned4(tokens) || misaligned4(page_status)) return FSD_ERR_LAYOUT;
     CopyParams P;
     P.pair = pages_pair(*src, *dst);
@@ -359,8 +360,9 @@ int fsd_cache_compact(const fsd_cache* cache, int B, const int32_t* refs, int32_
     if (!workspace_fits(workspace, workspace_bytes, w.bytes)) return FSD_ERR_WORKSPACE;
     const size_t table = static_cast<size_t>(B) * c.max_blocks * 4, blocks = static_cast<size_t>(c.num_blocks) * 4;
     const Run runs[] = {{remap, blocks}, {used_blocks, 4}, {row_status, static_cast<size_t>(B) * 4}, {workspace, w.bytes}, {block_table_out, table}, {refs_out, blocks},
-                        {block_table_out == c.block_table ? nullptr : c.block_table, table}, {refs_out == refs ? nullptr : refs, blocks}};
-    if (any_overlap(runs, 6, 8)) return FSD_ERR_LAYOUT;
+                        {block_table_out == c.block_table ? nullptr : c.block_table, table}, {refs_out == refs ? nullptr : refs, blocks},
+                        {c.k_codes, codes_bytes(c)}, {c.v_codes, codes_bytes(c)}, {c.k_scale, scale_bytes(c)}, {c.v_scale, scale_bytes(c)}};
+    if (any_overlap(runs, 6, 12)) return FSD_ERR_LAYOUT;
     char* base = static_cast<char*>(workspace);
     auto ints = [base](size_t at) { return reinterpret_cast<int*>(base + at); };
     CompactParams P;

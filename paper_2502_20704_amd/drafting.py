@@ -87,6 +87,12 @@ def _outputs(given, stream, device, optional, new, /, **tensors):
     return given
 
 
+def _counts(call, *sizes):
+    """what the library takes as int: a larger one would arrive as another"""
+    if max(sizes) > 0x7FFFFFFF:
+        raise FsdError(-2, call)
+
+
 def _row_stride(t, name):
     """elements between rows of [B, beams, V]: entries lie side by side, and the rows at one distance"""
     B, W, V = t.shape
@@ -113,7 +119,11 @@ def fsd_beam_select(logits, scores, n, *, weights=None, done=None, out=None, wor
     for name, t, dtype in (("scores", scores, torch.float32), ("weights", weights, torch.float32), ("done", done, torch.int32)):
         if t is not None:
             _check(t, name, (B, W), dtype, dev)
-    out, workspace, base, size = _results(out, ("row_status",), workspace, fsd_beam_workspace_bytes(B, W, V, n, dt), dev, stream,
+    _counts("fsd_beam_select", B, W, V, n)
+    need = fsd_beam_workspace_bytes(B, W, V, n, dt)
+    if need == 0:
+        raise FsdError(-2, "fsd_beam_select")                 # (before tensors of such sizes are made)
+    out, workspace, base, size = _results(out, ("row_status",), workspace, need, dev, stream,
                                           scores=((B, n), torch.float32), parent=((B, n), torch.int32), tokens=((B, n), torch.int32),
                                           row_status=((B,), torch.int32))
     st = library().fsd_beam_select(_ptr(logits), step, _ptr(scores), _ptr(weights), _ptr(done), B, W, V, dt, n, _ptr(out["scores"]),
@@ -138,6 +148,7 @@ def fsd_beam_reorder(states, parent, *, batch_dim=0, out=None, stream=None):
     shape = tuple(states.shape)
     B, W = shape[batch_dim:batch_dim + 2]
     n = parent.shape[1]
+    _counts("fsd_beam_reorder", *shape[:batch_dim + 2], math.prod(shape[:batch_dim]), n)
     _check(parent, "parent", (B, n), torch.int32, dev)
     out = _outputs(out, stream, dev, ("row_status",), _new, out=((*shape[:batch_dim + 1], n, *shape[batch_dim + 2:]), states.dtype),
                    row_status=((B,), torch.int32))
@@ -159,6 +170,7 @@ def fsd_cache_fork(cache, parent, refs, *, lengths=None, room=None, out=None, wo
     if parent.dim() != 1:
         raise ValueError("parent has 1 dimension")
     n, P = parent.shape[0], cache.num_blocks
+    _counts("fsd_cache_fork", n)
     _check(parent, "parent", (n,), torch.int32, dev)
     _check(refs, "refs", (P,), torch.int32, dev)
     for name, t in (("lengths", lengths), ("room", room)):
@@ -189,6 +201,7 @@ def fsd_cache_copy(src, dst, src_blocks, dst_blocks, *, tokens=None, out=None, s
     if src_blocks.dim() != 1:
         raise ValueError("src_blocks has 1 dimension")
     n = src_blocks.shape[0]
+    _counts("fsd_cache_copy", n)
     for name, t in (("src_blocks", src_blocks), ("dst_blocks", dst_blocks), ("tokens", tokens)):
         if t is not None:
             _check(t, name, (n,), torch.int32, dev)

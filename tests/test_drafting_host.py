@@ -190,6 +190,17 @@ def test_outputs_that_lie_in_what_a_call_reads():
                     assert _compact(**{name: where}) == -9, (name, what)
 
 
+def test_outputs_that_lie_in_the_pages():
+    codes, scales = 2 * 100 * 2 * 64 * 128, 2 * 100 * 2 * 4
+    for at, m in ((KC, codes), (VC, codes), (KS, scales), (VS, scales)):
+        for where in (at, at + m - 4):
+            for name in ("table", "lens", "refs_out", "free", "status"):
+                assert _fork(**{name: where}) == -9, name
+            for name in ("table", "refs_out", "remap", "used", "status"):
+                assert _compact(**{name: where}) == -9, name
+        assert _fork(ws=at) == -9 and _compact(ws=at + m // 256 * 256 - 256) == -9
+
+
 def test_row_strides():
     import torch
 
@@ -199,6 +210,29 @@ def test_row_strides():
     for bad in (whole[:, :2], whole[:, :, ::2], whole.transpose(0, 1)):
         with pytest.raises(ValueError):
             drafting._row_stride(bad, "z")
+
+
+def test_sizes_are_refused_before_outputs_are_made(monkeypatch):
+    """(the sizes of a call come from the caller's n: outputs of 2^40 numbers are not asked for)"""
+    import torch
+
+    class OnGpu:
+        is_cuda, device, dtype, shape = True, types.SimpleNamespace(index=0), torch.float32, (2, 3, 10)
+
+        def dim(self):
+            return 3
+
+        def stride(self):
+            return 30, 10, 1
+
+    monkeypatch.setattr(drafting, "_on_current", lambda device, stream: None)
+    monkeypatch.setattr(drafting, "_new", lambda *a, **k: pytest.fail("made"))
+    for n in (-1, 0, 129, 1 << 30, 1 << 40, (1 << 32) + 4):
+        with pytest.raises(fsd.FsdError, match="fsd_beam_select"):
+            fsd.fsd_beam_select(OnGpu(), None, n)
+    OnGpu.shape = 2, 3, (1 << 32) + 10
+    with pytest.raises(fsd.FsdError, match="fsd_beam_select"):
+        fsd.fsd_beam_select(OnGpu(), None, 4)
 
 
 def test_binding_refusals():
