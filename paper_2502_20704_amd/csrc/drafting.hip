@@ -214,6 +214,8 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     if (dtype == FSD_BF16) launch_beam_slices<true>(st, s, P);
     else launch_beam_slices<false>(st, s, P);
     const dim3 sequences(static_cast<unsigned>(B));
+    // (threads, and entries a thread holds at once.  256 and 4, 256 and 16, 512 and 16 for 32 entries: 6.0, 8.4, 8.3 us; 64 sequences of 256 entries: 5.6, 7.9, 8.0;
+    // of 2048: 16.4, 14.6, 20.2; of 8192: 50.5, 29.4, 23.0; 4 of 25600: 145, 74, 47)
     if (P.lists * n <= 256 * 4) hipLaunchKernelGGL((beam_merge<256, 4>), sequences, dim3(256), 0, st, P);
     else if (P.lists * n <= 256 * 16) hipLaunchKernelGGL((beam_merge<256, 16>), sequences, dim3(256), 0, st, P);
     else hipLaunchKernelGGL((beam_merge<512, 16>), sequences, dim3(512), 0, st, P);

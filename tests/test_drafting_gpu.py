@@ -480,6 +480,85 @@ def test_select_one_beam_has_all_of_the_best(dtype):
     _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), 128), (*want[:4], np.inf))
 
 
+# ------------------------------------------------------------------------------------------ the largest
+
+
+def test_fork_and_compact_largest_batch():
+    """as many sequences as there may be, before and after"""
+    rng = np.random.default_rng(17)
+    n, P = 65535, 140000
+    table, lens, refs = _sequences(rng, n, 2, P, most=100)
+    parent = rng.integers(-1, n, n).astype(np.int32)
+    codes = lambda: torch.empty((1, P, 1, 64 * 64), dtype=torch.uint8, device="cuda")  # noqa: E731
+    scale = torch.arange(P, dtype=torch.float32, device="cuda").view(1, P, 1)
+    cache = fsd.Cache(codes().view(1, P, 1, 64, 64), codes().view(1, P, 1, 4, 64, 16), scale.clone(), -scale, _dev(table), _dev(lens))
+    want = ref.fork(table, lens, refs, parent, None, None)
+    got = fsd.fsd_cache_fork(cache, _dev(parent), _dev(refs))
+    torch.cuda.synchronize()
+    for name, w in zip(("block_table", "cache_len", "refs", "free_blocks", "row_status"), want):
+        assert (_host(got[name]) == w).all(), name
+    scales = np.arange(P, dtype=np.float32)
+    for a, b, _ in want[5]:
+        scales[b] = a
+    assert len(want[5]) > 10000 and (_host(cache.k_scale).reshape(-1) == scales).all() and (_host(cache.v_scale).reshape(-1) == -scales).all()
+    cache = cache.with_tables(got["block_table"], got["cache_len"])
+    want = ref.compact(want[0], want[2])
+    got = fsd.fsd_cache_compact(cache, got["refs"])
+    torch.cuda.synchronize()
+    for name, w in zip(("block_table", "refs", "remap", "used_blocks", "row_status"), want):
+        assert (_host(got[name]) == w).all(), name
+
+
+def test_pages_beyond_32_bits_of_bytes():
+    """5 GB of codes: pages from behind 2^32 to the front, and back"""
+    L, P, H, D = 1, 40000, 16, 128
+    k, v = (torch.empty((L, P, H * 64 * D), dtype=torch.uint8, device="cuda") for _ in range(2))
+    scale = torch.rand((2, L, P, H), device="cuda")
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = fsd.Cache(k.view(L, P, H, 64, D), v.view(L, P, H, 4, D, 16), scale[0], scale[1], ints(39998, 39999)[None], ints(100))
+    some = [0, 1, 2, 7231, 7232, 32767, 32768, 39997, 39998, 39999]    # (block 7232 is where the low 32 bits of block 40000 would be)
+
+    def fill():
+        for e in some:
+            k[0, e], v[0, e] = (torch.randint(0, 256, (H * 64 * D,), dtype=torch.uint8, device="cuda") for _ in range(2))
+        return {e: (k[0, e].clone(), v[0, e].clone(), scale[:, 0, e].clone()) for e in some}
+
+    def check(was, moved, tokens=None):
+        torch.cuda.synchronize()
+        for e in some:
+            if e in (tokens or {}):                           # the first groups of 16 tokens of each head
+                g = tokens[e]
+                for x, y in ((k[0, e], was[moved[e]][0]), (v[0, e], was[moved[e]][1])):
+                    assert torch.equal(x.view(H, 4, 16 * D)[:, :g], y.view(H, 4, 16 * D)[:, :g]), e
+            else:
+                assert torch.equal(k[0, e], was[moved.get(e, e)][0]) and torch.equal(v[0, e], was[moved.get(e, e)][1]), e
+            assert torch.equal(scale[:, 0, e], was[moved.get(e, e)][2]), e
+
+    was = fill()
+    fsd.fsd_cache_copy(cache, cache, ints(39999, 0), ints(1, 39997))
+    check(was, {1: 39999, 39997: 0})
+    was = fill()
+    refs = torch.ones(P, dtype=torch.int32, device="cuda")
+    refs[[0, 7232]] = 0                                       # a copy of the begun block goes to block 0
+    got = fsd.fsd_cache_fork(cache, ints(0, 0), refs)
+    assert got["block_table"].tolist() == [[39998, 39999], [39998, 0]] and got["refs"][39998] == 2
+    check(was, {0: 39999}, {0: 3})
+    was = fill()
+    refs = torch.zeros(P, dtype=torch.int32, device="cuda")
+    refs[[2, 39998, 39999]] = 1
+    got = fsd.fsd_cache_compact(cache, refs)
+    assert got["block_table"].tolist() == [[0, 1]] and int(got["used_blocks"]) == 3
+    check(was, {0: 39998, 1: 39999})
+
+
+def test_reorder_rows_beyond_32_bits_of_bytes():
+    row = (1 << 30) + 48
+    states = torch.randint(0, 256, (1, 6, row // 8), dtype=torch.int64, device="cuda")
+    got = fsd.fsd_beam_reorder(states, torch.tensor([[5, -1, 0, 4, 5]], dtype=torch.int32, device="cuda"))["out"]
+    for i, w in enumerate((5, None, 0, 4, 5)):
+        assert torch.equal(got[0, i], states[0, w] if w is not None else torch.zeros_like(got[0, i])), i
+
+
 # ------------------------------------------------------------------------------------------ calls beside one another
 
 
