@@ -17,6 +17,8 @@
 #ifndef FSD_CSRC_BEAM_SELECT_H_
 #define FSD_CSRC_BEAM_SELECT_H_
 
+#include <type_traits>
+
 #include "operators_common.h"
 
 namespace {
@@ -500,39 +502,53 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
             if (rank < P.n)
                 cand[rank * lists] = make_float2(from_ordered(static_cast<unsigned>(me >> 32)), __uint_as_float(static_cast<unsigned>(begin) + ~static_cast<unsigned>(me)));
         };
-        if (most <= 64) {
-            // a lane holds an entry of each wavefront's; a wavefront finds the ranks of its own one after the other
-            unsigned long other[NW];
+        // HALVES lanes' worth of each wavefront's entries, one or two a lane; a wavefront finds the ranks of its own one after the other
+        auto by_ballots = [&](auto halves) {
+            constexpr int HALVES = decltype(halves)::value;
+            unsigned long other[HALVES * NW], own[HALVES];
 #pragma unroll
-            for (int w = 0; w < NW; ++w) other[w] = lane < counts[w] ? list[w * kWaveList + lane] : 0;
-            const unsigned long own = lane < count ? mine_list[lane] : 0;
-            int my_rank = 0;
-#pragma unroll 4
-            for (int k = 0; k < count; ++k) {
-                const unsigned long me = lane_word(own, k);
-                int rank = 0;
+            for (int h = 0; h < HALVES; ++h) {
 #pragma unroll
-                for (int w = 0; w < NW; ++w) rank += __popcll(__ballot(other[w] > me));
-                my_rank = lane == k ? rank : my_rank;
+                for (int w = 0; w < NW; ++w) other[h * NW + w] = h * 64 + lane < counts[w] ? list[w * kWaveList + h * 64 + lane] : 0;
+                own[h] = h * 64 + lane < count ? mine_list[h * 64 + lane] : 0;
             }
-            if (lane < count) put(my_rank, own);
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+                int my_rank = 0;
+                const int in_half = count - h * 64 < 64 ? count - h * 64 : 64;
+#pragma unroll 4
+                for (int k = 0; k < in_half; ++k) {
+                    const unsigned long me = lane_word(own[h], k);
+                    int rank = 0;
+#pragma unroll
+                    for (int w = 0; w < HALVES * NW; ++w) rank += __popcll(__ballot(other[w] > me));
+                    my_rank = lane == k ? rank : my_rank;
+                }
+                if (lane < in_half) put(my_rank, own[h]);
+            }
+        };
+        if (most <= 64) {
+            by_ballots(std::integral_constant<int, 1>{});
+        } else if (most <= 128) {
+            by_ballots(std::integral_constant<int, 2>{});
         } else {
             if (most > kWaveList) {
                 __syncthreads();                                  // (all have read the counts)
                 have = slice_cut<BF16, NW>(z, begin, end, P.n, list, lds, tid);
 #pragma unroll
                 for (int w = 0; w < NW; ++w) counts[w] = w == 0 ? have : 0;   // (at most n of them)
+                count = wave == 0 ? have : 0;
             }
+            // a lane an entry of its wavefront's, which all are compared with (a broadcast each)
+            for (int k = lane; k < count; k += 64) {
+                const unsigned long me = mine_list[k];
+                int rank = 0;
 #pragma unroll
-            for (int v = 0; v < NW; ++v)
-                for (int k = tid; k < counts[v]; k += T) {
-                    const unsigned long me = list[v * kWaveList + k];
-                    int rank = 0;
-#pragma unroll
-                    for (int w = 0; w < NW; ++w)
-                        for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
-                    put(rank, me);
-                }
+                for (int w = 0; w < NW; ++w)
+#pragma unroll 8
+                    for (int j = 0; j < counts[w]; ++j) rank += list[w * kWaveList + j] > me;
+                put(rank, me);
+            }
         }
         for (int k = have + tid; k < P.n; k += T) cand[k * lists] = make_float2(-__builtin_inff(), 0.0f);
         if (tid == T - 1) {
@@ -716,7 +732,6 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         __syncthreads();
     };
     for (int k0 = 0; k0 < total; k0 += T * EACH) {
-        if (k0 > 0) load(k0);
         double rank[EACH];
         double most = -__builtin_inf();
         {
@@ -733,6 +748,8 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 l -= l >= lists ? lists : 0;
             }
         }
+        // Lists fall: where no entry of a whole row of them (their r-th ones) reaches the n-th best so far, none behind it does.
+        if (k0 > 0 && count == n && !__syncthreads_or(most >= last_key) && 2 * lists <= T * EACH) break;
         const unsigned word = ordered_high(most);
         const int q = (n + NW - 1) / NW;
         unsigned bound = 0, alone = 0;                        // its q-th largest, and its n-th: what n of its own reach bounds the n-th of all as well
@@ -793,6 +810,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                     at += __popcll(who);
                 }
             }
+            if (k0 + T * EACH < total) load(k0 + T * EACH);       // (on the way meanwhile)
             count = all;
             __syncthreads();
             order();
@@ -822,6 +840,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 __syncthreads();
                 if (count > n) order();
             }
+            if (k0 + T * EACH < total) load(k0 + T * EACH);
             order();
         }
     }
