@@ -214,10 +214,13 @@ int fsd_beam_select(const void* logits, int64_t row_stride, const float* scores,
     if (dtype == FSD_BF16) launch_beam_slices<true>(st, s, P);
     else launch_beam_slices<false>(st, s, P);
     const dim3 sequences(static_cast<unsigned>(B));
-    // (threads, and entries a thread holds at once.  256 and 4, 256 and 16, 512 and 16 for 32 entries: 6.0, 8.4, 8.3 us; 64 sequences of 256 entries: 5.6, 7.9, 8.0;
-    // of 2048: 16.4, 14.6, 20.2; of 8192: 50.5, 29.4, 23.0; 4 of 25600: 145, 74, 47)
-    if (P.lists * n <= 256 * 4) hipLaunchKernelGGL((beam_merge<256, 4>), sequences, dim3(256), 0, st, P);
-    else if (P.lists * n <= 256 * 16) hipLaunchKernelGGL((beam_merge<256, 16>), sequences, dim3(256), 0, st, P);
+    // A round of the merge takes the first entries of all lists, and it is over where a round reaches nothing.  One beam that has all of the best has n / S of them in
+    // each of its lists, so rounds of n * beams entries and a third hold what counts; longer ones cost as many registers and instructions where lists are few.  256 threads of
+    // 4 entries, 512 of 4 and 512 of 16, by n * beams: 32: 5.5, 5.8, 8.1 us; 128: 6.3, 6.5, 9.1; 720: 9.2, 11.6, 13.4; 960: 16.6, 13.9, 23.0; 2376: 23.3, 16.7, 24.0;
+    // 3840: 219, 18.4, 23.5; 8192: 669, 36.0, 25.2; 25600: 57, 35.4, 25.7.
+    const long deep = static_cast<long>(n) * beams;
+    if (P.lists * n <= 256 * 4 || (deep * 4 / 3 <= 256 * 4 && P.lists <= 512)) hipLaunchKernelGGL((beam_merge<256, 4>), sequences, dim3(256), 0, st, P);
+    else if (deep <= 2 * 512 * 4 && P.lists <= 1024) hipLaunchKernelGGL((beam_merge<512, 4>), sequences, dim3(512), 0, st, P);
     else hipLaunchKernelGGL((beam_merge<512, 16>), sequences, dim3(512), 0, st, P);
     return launched();
 }

@@ -480,6 +480,24 @@ def test_select_one_beam_has_all_of_the_best(dtype):
     _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), 128), (*want[:4], np.inf))
 
 
+@pytest.mark.parametrize("far", [0.0, 40.0])
+@pytest.mark.parametrize("B,W,V,n,dtype", [(1, 4, 32000, 128, "bf16"), (2, 4, 15375, 82, "bf16"), (1, 1, 128256, 128, "bf16"), (1, 30, 3000, 128, "f32"), (3, 24, 13697, 99, "f32"),
+                                           (1, 64, 32000, 128, "bf16"), (2, 256, 1500, 128, "f32"), (1, 3, 200001, 100, "f32"), (64, 8, 9000, 128, "bf16")])
+def test_select_one_list_has_most_of_the_best(B, W, V, n, dtype, far):
+    """side by side in one row, and in order, so that one slice's list gives most of the answer, and to its end where the other beams' scores are far below"""
+    rng = np.random.default_rng(W + V + n)
+    z = torch.from_numpy(rng.standard_normal((B, W, V)).astype(np.float32))
+    at = V // 3 // 64 * 64
+    z[:, W - 1, at:at + n] = 9.0 + torch.arange(n) * 0.0625
+    z[-1, 0, 5] = 9.03
+    z = z.to(torch.bfloat16) if dtype == "bf16" else z
+    scores = rng.random((B, W)).astype(np.float32) * 0.01
+    scores[:, :W - 1] -= np.float32(far)
+    want = ref.select(_host(z), scores, None, None, n)
+    _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), n), want)
+    assert far == 0.0 or (want[1][0] == W - 1).all()
+
+
 # ------------------------------------------------------------------------------------------ the largest
 
 
