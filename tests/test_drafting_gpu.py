@@ -498,6 +498,16 @@ def test_select_one_list_has_most_of_the_best(B, W, V, n, dtype, far):
     assert far == 0.0 or (want[1][0] == W - 1).all()
 
 
+@pytest.mark.parametrize("n", [1, 17, 100, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_select_last_slices_of_all_lengths(dtype, n):
+    """rows whose last slice has fewer slots than a workgroup has threads, or than one of its wavefronts"""
+    rng = np.random.default_rng(n)
+    for V in (8, 120, 505, 1000, 1776, 2040, 2055, 2300, 3200, 4100, 6151, 128256):
+        z, scores = _logits(rng, 1, 2, V, dtype), _scores(rng, 1, 2)
+        _same_selection(fsd.fsd_beam_select(z.cuda(), _dev(scores), n), ref.select(_host(z), scores, None, None, n), V)
+
+
 # ------------------------------------------------------------------------------------------ the largest
 
 
