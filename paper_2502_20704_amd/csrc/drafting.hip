@@ -78,6 +78,10 @@ bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
     }
     s->len = ((V + S - 1) / S + E - 1) / E * E;              // slices of one length, so that none of them is a remnant
     s->S = (V + s->len - 1) / s->len;
+    // A slice of one slot a thread has no use for more; one of a few goes in smaller chunks where its registers keep other workgroups waiting (3330 rows of 4032 bfloat16
+    // entries 34.3 and 24.5 us, 3968 of 5120 76 and 67, 528 of 1152 10.8 and 7.9; 144 rows of 13696 binary32 entries 15.2 and 15.4, 64 of 32000 8.7 and 9.0).
+    if (!s->table && s->len <= kWG * E) s->slots = 1;
+    else if (!s->table && s->slots > 2 && s->len <= kWG * E * s->slots && rows * s->S > kBeamWGs) s->slots = 2;
     return rows * s->S <= kMaxGroups;
 }
 struct BeamSpace { size_t lists, stat, cand, bytes; };
