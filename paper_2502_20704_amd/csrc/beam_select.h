@@ -12,8 +12,8 @@
 // an entry, take 25 us of it, the table's reads 15 of the LDS's time beside them; the rest is each row's beginning (a round trip for its score, one for
 // its first entries) and end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  Without the sums it would
 // take 25 us, without slots put aside 32, without the making of the table 36.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us; the list
-// of 60 takes as many instructions as the exponentials.  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 11 at n = 60: a chain of round trips
-// and barriers.
+// of 60 takes as many instructions as the exponentials, and all workgroups begin and end together (exponentials by a table of 512 powers and degree 2, 3 instructions
+// an entry less, change nothing).  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 9 at n = 60: a chain of round trips and barriers.
 #ifndef FSD_CSRC_BEAM_SELECT_H_
 #define FSD_CSRC_BEAM_SELECT_H_
 
