@@ -8,7 +8,7 @@
 // Exponentials, sums and ranks are binary64 therefore.  A binary64 fma issues like a binary32 one here (2.0 ns a wavefront and SIMD, as an addition or
 // a conversion), the hardware's binary32 exponential takes 3.8: 16 instructions an entry where binary32 would take 9, and an error of 2^-34 in place of 2^-25.
 //
-// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 37 us; reading them alone 18): vector instructions, 12.6
+// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 37 us; reading them alone 18): vector instructions, 12.9
 // an entry, take 25 us of it, the table's reads 15 of the LDS's time beside them; the rest is each row's beginning (a round trip for its score, one for
 // its first entries) and end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  Without the sums it would
 // take 25 us, without slots put aside 32, without the making of the table 36.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us; the list

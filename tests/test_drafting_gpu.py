@@ -126,6 +126,25 @@ def test_select_sizes_of_numbers(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,W,V", [(3, 2, 50), (4, 3, 9001), (12, 8, 100003)])
+def test_select_masks_of_the_lowest_number(B, W, V, dtype):
+    """masked places that hold the type's lowest number are entries, behind all others; a row of nothing else has them all equal"""
+    rng = np.random.default_rng(V)
+    z = _logits(rng, B, W, V, dtype)
+    keep = rng.random((B, W, V)) < 12.0 / V
+    z[torch.from_numpy(~keep)] = torch.finfo(DT[dtype]).min
+    z[0] = torch.finfo(DT[dtype]).min
+    z[1, 0] = torch.finfo(DT[dtype]).min
+    scores = _scores(rng, B, W)
+    for n in (5, 40, 128):
+        got, want = fsd.fsd_beam_select(z.cuda(), _dev(scores), n), ref.select(_host(z), scores, None, None, n)
+        _same_selection(got, want)
+    got, want = fsd.fsd_beam_select(z[:1].cuda(), None, 40), ref.select(_host(z[:1]), None, None, None, 40)   # (equal to the last bit)
+    _same_selection(got, (*want[:4], np.inf))
+    assert (want[1] == 0).all() and (want[2] == np.arange(40)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [9, 33333])
 def test_select_reports(V, dtype):
     rng = np.random.default_rng(V)
