@@ -24,12 +24,14 @@
 namespace {
 
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBeamMost = 128;      // n
 constexpr int kBeamWidest = 256;    // beams
 constexpr int kWaveList = 256;      // entries of a wavefront's part of a slice that stand in LDS before the n best are taken from all
 constexpr unsigned short kTableBase = 0x397F;   // bits of the last bfloat16 number under 2^-12
 constexpr unsigned short kTableEnd = 2 * (0x4280 - kTableBase);   // entries: 0; 2^-12, -2^-12 and so on to the last numbers under 64; two and the last one for 64 and over
+constexpr unsigned short kTurnedInf = 0xFF01;   // -inf with its sign behind the rest
 constexpr int kAside = 112;         // slots of a wavefront's that stand there until they are taken apart
 constexpr double kLog2e64 = 1.4426950408889634074;
 
@@ -387,6 +389,15 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
             return m;
         };
 
+        // The same of a bfloat16 slot with an entry over 0; of others, one of their entries.  (As 16-bit numbers those over 0 lie above the others, in their order.)
+        auto slot_max_over_0 = [&](const u32x4& slot) {
+            const i16x2 a = __builtin_elementwise_max(__builtin_bit_cast(i16x2, static_cast<unsigned>(slot[0])), __builtin_bit_cast(i16x2, static_cast<unsigned>(slot[1])));
+            const i16x2 b = __builtin_elementwise_max(__builtin_bit_cast(i16x2, static_cast<unsigned>(slot[2])), __builtin_bit_cast(i16x2, static_cast<unsigned>(slot[3])));
+            const unsigned m = __builtin_bit_cast(unsigned, __builtin_elementwise_max(a, b));
+            const int low = static_cast<int>(m << 16), high = static_cast<int>(m & 0xFFFF0000u);
+            return __int_as_float(low > high ? low : high);
+        };
+
         // the first chunk's bound
         float mine = -__builtin_inff();                           // the lane's largest so far
 #pragma unroll
@@ -402,6 +413,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         all_bounds();
 
         bool broken = false;                                      // an entry is NaN or +inf
+        u16x2 most_turned = {0, 0};                               // (TABLE: tells a NaN, the only ones beyond -inf)
         double sum[2] = {0.0, 0.0};
         // (The last chunk apart from the others: where a branch may or may not request, each slot's wait is one for all requests before it, and 98 MB of binary32 rows
         // take 31.3 us, not 30.)
@@ -411,7 +423,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
             for (int i = 0; i < NS; ++i) {
                 const int slot = first + i * T + tid;
                 if (!decltype(more)::value && first + kChunk > slots) behind(r[i], slot);
-                const float top = slot_max(r[i]);
+                const float top = TABLE && from > 0.0f ? slot_max_over_0(r[i]) : slot_max(r[i]);
                 mine = __builtin_fmaxf(mine, top);
                 // a slot with an entry that reaches the bound is put aside whole, to be taken apart with others
                 const unsigned long who = __ballot(top >= from);
@@ -424,14 +436,17 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
                     aside += __popcll(who);
                     if (aside > kAside - 64) take_apart();
                 }
+                if constexpr (!TABLE) {
 #pragma unroll
-                for (int e = 0; e < E; e += 2) broken |= __builtin_isunordered(slot_entry<BF16>(r[i], e), slot_entry<BF16>(r[i], e + 1));
+                    for (int e = 0; e < E; e += 2) broken |= __builtin_isunordered(slot_entry<BF16>(r[i], e), slot_entry<BF16>(r[i], e + 1));
+                }
                 if constexpr (TABLE) {                            // (also where it does not hold: then all of it is gone over again)
                     u16x2 least_index = {0xFFFF, 0xFFFF}, index[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const u16x2 v = __builtin_bit_cast(u16x2, static_cast<unsigned>(r[i][j]));
                         const u16x2 turned = twice_and(v, v >> static_cast<unsigned short>(15));   // the sign behind the rest
+                        most_turned = __builtin_elementwise_max(most_turned, turned);
                         index[j] = __builtin_elementwise_min(__builtin_elementwise_sub_sat(turned, u16x2{2 * kTableBase + 1, 2 * kTableBase + 1}), u16x2{kTableEnd, kTableEnd});
                         least_index = __builtin_elementwise_min(least_index, index[j]);
                     }
@@ -469,6 +484,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
             if ((chunk & (chunk - 1)) == 0) all_bounds();     // (the others' by then)
         }
         over_chunk(first, std::false_type{});
+        if constexpr (TABLE) broken = most_turned.x > kTurnedInf || most_turned.y > kTurnedInf;
         const float top = wave_largest(mine);
         double ref = top > -__builtin_inff() ? 0.0 : -__builtin_inf();
         if ((TABLE ? top >= 64.0f || top < -20.0f : top > 600.0f || top < -600.0f) && top > -__builtin_inff()) {
