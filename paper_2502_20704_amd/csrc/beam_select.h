@@ -8,10 +8,10 @@
 // Exponentials, sums and ranks are binary64 therefore.  A binary64 fma issues like a binary32 one here (2.0 ns a wavefront and SIMD, as an addition or
 // a conversion), the hardware's binary32 exponential takes 3.8: 16 instructions an entry where binary32 would take 9, and an error of 2^-34 in place of 2^-25.
 //
-// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 37 us; reading them alone 18): vector instructions, 12.9
-// an entry, take 25 us of it, the table's reads 15 of the LDS's time beside them; the rest is each row's beginning (a round trip for its score, one for
-// its first entries) and end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  Without the sums it would
-// take 25 us, without slots put aside 32, without the making of the table 36.  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 31 us; the list
+// What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 36 us; reading them alone 18): vector instructions, 11.9
+// an entry, take 21 us of it, the table's reads 14 of the LDS's time beside them; the rest is what a wavefront waits for within a slot (four of them on a SIMD) and each
+// row's end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  (Without the sums it took 13 us less, without slots put aside 6,
+// without the making of the table 2; the next slice's first requests before this one's end change nothing.)  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 30 us; the list
 // of 60 takes as many instructions as the exponentials, and all workgroups begin and end together (exponentials by a table of 512 powers and degree 2, 3 instructions
 // an entry less, change nothing).  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 9 at n = 60: a chain of round trips and barriers.
 #ifndef FSD_CSRC_BEAM_SELECT_H_
@@ -293,7 +293,7 @@ __device__ __forceinline__ unsigned wave_bound(unsigned word, int q) {
 // into LDS and ranked there at the end.  Wavefronts tell one another their bounds without waiting: an older one of another's bounds as well.
 // Exponentials are added up as e^z: binary64 has the range where logits are of the size that models give them.  Where they are not, the slice is gone over again.
 // TABLE: exponentials of bfloat16 numbers are read from a table of all of them from 2^-12 to 64 of either sign (and 0, and those under -64, which
-// count as nothing), which a workgroup makes once and keeps for all of its slices: 7 instructions an entry where the polynomial takes 16 (51 -> 38 us for the rows above).
+// count as nothing), which a workgroup makes once and keeps for all of its slices: 7 instructions an entry where the polynomial takes 16 (51 -> 38 us for the rows above at that step).
 template <bool BF16, int NS, bool TABLE>
 __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamParams P) {
     constexpr int NW = TABLE ? 8 : 4, T = NW * 64;
