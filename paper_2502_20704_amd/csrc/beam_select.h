@@ -592,6 +592,8 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
 __device__ __forceinline__ unsigned long found_word(int beam, float z, int token1) {
     return static_cast<unsigned long>(beam) << 52 | static_cast<unsigned long>(~ordered(z)) << 20 | static_cast<unsigned>(token1);
 }
+// of a logit, given its row's normaliser
+__device__ __forceinline__ double log_share(float z, double2 norm) { return (static_cast<double>(z) - norm.x) - norm.y; }
 constexpr int kMergeFew = 256;      // entries that are put into order as they are; of more, the n best are looked for first
 
 // 64-bit order of binary64 numbers, as ordered() is for binary32 ones; the upper word
@@ -609,7 +611,9 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
     __shared__ unsigned long found[kRoom + 8];
     __shared__ double best_key[kBeamMost];
     __shared__ unsigned long best[kBeamMost];
-    __shared__ double norm[kBeamWidest];
+    // A row's normaliser in two parts, a number r and log of the sum of e^(z - r): in one, the logarithm would be lost beside an r of 2^53 (a row of the
+    // type's lowest number, from a mask that leaves nothing, would have continuations of probability 1).
+    __shared__ double2 norm[kBeamWidest];
     __shared__ float base[kBeamWidest];                       // a beam's score; NaN: its list does not count
     __shared__ float so_far[kBeamWidest];
     __shared__ float factor[kBeamWidest];
@@ -676,7 +680,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
         if (broken) bad = 1;                                  // (whoever writes it writes the same)
         if (w < W && part == 0) {
             const bool counts = runs && m > -__builtin_inf();
-            norm[w] = counts ? m + log(s) : 0.0;
+            norm[w] = counts ? make_double2(m, log(s)) : make_double2(0.0, 0.0);
             base[w] = counts ? score : __builtin_nanf("");
             factor[w] = by;
             so_far[w] = score;
@@ -763,7 +767,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
                 const float from = base[w];
                 rank[i] = -__builtin_inf();
                 if (from == from && z[i] > -__builtin_inff())
-                    rank[i] = (static_cast<double>(from) + (static_cast<double>(z[i]) - norm[w])) * static_cast<double>(factor[w]);
+                    rank[i] = (static_cast<double>(from) + log_share(z[i], norm[w])) * static_cast<double>(factor[w]);
                 most = rank[i] > most ? rank[i] : most;
                 l += column_step;
                 l -= l >= lists ? lists : 0;
@@ -874,7 +878,7 @@ __global__ void __launch_bounds__(T) beam_merge(const BeamParams P) {
             beam = static_cast<int>(me >> 52);
             token1 = static_cast<int>(me & 0xFFFFFu);
             s = so_far[beam];
-            if (token1 > 0) s = static_cast<float>(static_cast<double>(s) + (static_cast<double>(from_ordered(~static_cast<unsigned>(me >> 20))) - norm[beam]));
+            if (token1 > 0) s = static_cast<float>(static_cast<double>(s) + log_share(from_ordered(~static_cast<unsigned>(me >> 20)), norm[beam]));
         }
         P.scores_out[out + i] = s;
         P.parent[out + i] = beam;

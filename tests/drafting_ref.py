@@ -33,8 +33,9 @@ def select(logits, scores, weights, done, n):
                 continue
             top = z.max()
             with np.errstate(under="ignore"):
-                norm = top + np.log(np.sort(np.exp(z[at] - top)).sum())
-            t = s + (z[at] - norm)
+                rest = np.log(np.sort(np.exp(z[at] - top)).sum())
+            # (top + rest in one number would lose rest's last bits beside a top of 2^20, all of it beside one of 2^53)
+            t = s + (z[at] - (top + rest) if abs(top) < 2.0 ** 20 else (z[at] - top) - rest)
             found.append((t * by, t, w, at, z[at]))
         if bad:
             out[3][b] = NONFINITE

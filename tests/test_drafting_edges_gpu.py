@@ -1,0 +1,36 @@
+"""The operators around drafting on the GPU: numbers at the ends of their ranges."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_20704_amd as fsd
+from tests.test_drafting_gpu import DT, _dev, _host
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------ normalisers
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,times", [(50, 1), (9002, 1), (100002, 10)])   # (30 long rows a number: by the kernel with the table)
+def test_select_rows_of_one_large_number(V, times, dtype):
+    """A row is as likely as it is a number higher up or lower down, however large that number is: where a mask of the type's lowest number leaves a beam
+    nothing, each of its V entries has the score -log V, and does not stand in front of beams that have something."""
+    numbers = [torch.finfo(DT[dtype]).min, -1e30, 2.0 ** 100, -(2.0 ** 60)] * times
+    B, n = len(numbers), 8
+    z = torch.empty((B, 3, V), dtype=DT[dtype])
+    z[:, 0] = torch.tensor(numbers, dtype=DT[dtype])[:, None]
+    z[:, 1], z[:, 1, 5:8] = -math.inf, 0.25
+    z[:, 2], z[:, 2, ::2] = -math.inf, torch.tensor(numbers, dtype=DT[dtype])[:, None]
+    scores = np.array([[-1.0, -1.5, -1.75]] * B, np.float32)
+    got = fsd.fsd_beam_select(z.cuda(), _dev(scores), n)
+    torch.cuda.synchronize()
+    assert not got["row_status"].any()
+    # -1.5 - log 3; then -1.75 - log V + log 2 = -1.057 - log V is behind -1 - log V
+    assert (_host(got["parent"]) == [1, 1, 1, 0, 0, 0, 0, 0]).all() and (_host(got["tokens"]) == [5, 6, 7, 0, 1, 2, 3, 4]).all()
+    want = np.array([-1.5 - math.log(3)] * 3 + [-1.0 - math.log(V)] * 5)
+    # one rounding to binary32, and the normaliser's error
+    assert (np.abs(_host(got["scores"]) - want) <= 2.0 ** -24 * np.abs(want) * (1 + 2.0 ** -20) + 2.0 ** -32).all()
