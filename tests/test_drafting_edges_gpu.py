@@ -34,3 +34,23 @@ def test_select_rows_of_one_large_number(V, times, dtype):
     want = np.array([-1.5 - math.log(3)] * 3 + [-1.0 - math.log(V)] * 5)
     # one rounding to binary32, and the normaliser's error
     assert (np.abs(_host(got["scores"]) - want) <= 2.0 ** -24 * np.abs(want) * (1 + 2.0 ** -20) + 2.0 ** -32).all()
+
+
+def test_select_normaliser_within_its_bound():
+    """The sum of a row's exponentials is off by less than 2^-33 of it, also where every entry's exponential is formed from a wavefront's largest entry, that
+    from the slice's and that from the row's, each at a distance at which the polynomial is off the most.  (Rows beyond the range of e^z; parts of
+    256 entries are the wavefronts' of a call of this size.)"""
+    V, far = 65536, 218 * 2.0 ** -14                          # a multiple of the numbers' distance there
+    z = np.full((V // 1024, 4, 256), 1000.0 - 3 * far)
+    z[:, :, 0] += far                                         # a part's largest
+    z[:, 0] = -np.inf
+    z[:, 0, 0] = 1000.0 - far                                 # a slice's, alone in its part
+    z[0, 0, 0] = 1000.0                                       # the row's
+    z = z.reshape(1, 1, V).astype(np.float32)
+    least = z[0, 0].astype(np.float64) - 1000.0
+    norm = math.log(math.fsum(np.exp(least[least > -np.inf]).tolist()))
+    scores = np.array([[norm]], np.float32)                   # (so that the result is near 0, and its rounding small)
+    got = fsd.fsd_beam_select(_dev(z), _dev(scores), 1)
+    want = float(scores[0, 0]) - norm
+    assert int(got["tokens"][0, 0]) == 0
+    assert abs(float(got["scores"][0, 0]) - want) <= 2.0 ** -33 + 2.0 ** -24 * abs(want) + 2.0 ** -45
