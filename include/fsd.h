@@ -511,7 +511,8 @@ int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_strid
  *   ranked by s * weights[w], largest first; of equal ranks the lowest w, then the largest z, then the lowest v
  *
  * Normalisers, scores and ranks are held in binary64 (relative error of a row's sum of exponentials under 2^-33; z_v's distance from the row's normaliser is formed
- * without a loss where both are large: a row of V times the type's lowest number has V continuations of -log V); scores_out is rounded once
+ * without a loss where both are large: a row of V times the type's lowest number has V continuations of -log V; a row's only
+ * entry has the beam's score itself); scores_out is rounded once
  * (a score below binary32's range, to -inf).
  *
  *   logits  [B, beams, V]  FSD_F32 or FSD_BF16, row_stride elements from one beam's row to the next (>= V, at most 2^32)

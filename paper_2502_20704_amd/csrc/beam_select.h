@@ -501,6 +501,8 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         }
         double s = wave_sum_64(sum[0] + sum[1]);
         if (!(top > -__builtin_inff())) s = 0.0;
+        // One entry (or one beside which the others are nothing) has its sum without an error: what is certain has the beam's score itself, and ties with others that have.
+        if (s == exp_within(static_cast<double>(top) - ref)) ref = top, s = 1.0;   // (NaN where there is no entry)
         const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
         // the final bound, made of all four wavefronts' entries
         {

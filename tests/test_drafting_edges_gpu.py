@@ -54,3 +54,34 @@ def test_select_normaliser_within_its_bound():
     want = float(scores[0, 0]) - norm
     assert int(got["tokens"][0, 0]) == 0
     assert abs(float(got["scores"][0, 0]) - want) <= 2.0 ** -33 + 2.0 ** -24 * abs(want) + 2.0 ** -45
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,B", [(40, 4), (9000, 4), (100003, 14)])
+def test_select_only_continuations_are_certain(V, B, dtype):
+    """A row with one entry gives the beam's score itself, so that it ties with a finished beam of that score and with other such rows: the lowest beam comes
+    first, whatever the logits are."""
+    rng = np.random.default_rng(V)
+    W = 6
+    z = torch.full((B, W, V), -math.inf, dtype=DT[dtype])
+    at = rng.integers(0, V, (B, W))
+    values = rng.standard_normal((B, W)) * 4
+    values[1] = rng.standard_normal(W) * 300                  # beyond the table's range, and e^z's
+    values[2] = rng.uniform(-1e30, 1e30, W)
+    values[3, :3], values[3, 3:] = [0.0, 64.0, -63.5], [1e-30, -2.0 ** -13, 600.0]
+    for b in range(B):
+        for w in range(W):
+            z[b, w, at[b, w]] = float(values[b, w])
+    scores = np.full((B, W), -2.3, np.float32)
+    done = np.zeros((B, W), np.int32)
+    done[0, 2] = done[2, 3] = 1
+    for n in (1, 4, 9):
+        got = fsd.fsd_beam_select(z.cuda(), _dev(scores), n, done=_dev(done))
+        k = min(n, W)
+        assert not got["row_status"].any()
+        assert (_host(got["parent"])[:, :k] == np.arange(k)).all() and (_host(got["parent"])[:, k:] == -1).all()
+        assert (_host(got["tokens"])[:, :k] == np.where(done[:, :k] != 0, -1, at[:, :k])).all()
+        assert (_host(got["scores"])[:, :k] == scores[:, :k]).all()
+    # (0 is no size to measure an error of 2^-33 by: exactly 0)
+    got = fsd.fsd_beam_select(z.cuda(), None, 4)
+    assert (got["scores"] == 0.0).all() and (_host(got["parent"]) == np.arange(4)).all()
