@@ -13,11 +13,14 @@ from .operators import _check, _new, _on_current, _torch
 ROW_NO_BLOCKS = 64
 
 _bytes = {}
+_MOST_KEPT = 1000           # shapes: a program has a few; one that has more pays for them again
 
 
 def _asked_once(call, *key):
     n = _bytes.get((call, key))
     if n is None:   # the library's answer for a shape does not change
+        if len(_bytes) > _MOST_KEPT:
+            _bytes.clear()
         n = _bytes[call, key] = int(getattr(library(), call)(*key))
     return n
 
@@ -69,7 +72,7 @@ def _results(call, sizes, specs, out, optional, workspace, need, device, stream)
         space = need if workspace is None and need <= _WITH_OUTPUTS else 0
         layout = _layouts.get((call, space, sizes))
         if layout is None:
-            if len(_layouts) > 1000:                          # (a program has a few shapes; one that has more pays for them again)
+            if len(_layouts) > _MOST_KEPT:
                 _layouts.clear()
             layout = _layouts[call, space, sizes] = _layout(space, specs(*sizes))
         out, whole, base = _parts(stream, device, space, layout)

@@ -1,0 +1,13 @@
+"""What the binding of the operators around drafting keeps and hands on (no GPU needed)."""
+import paper_2502_20704_amd as fsd
+from paper_2502_20704_amd import drafting
+
+
+def test_answers_for_shapes_do_not_pile_up():
+    """a server sees new batch sizes for as long as it runs"""
+    want = [fsd.fsd_cache_fork_workspace_bytes(50, n) for n in (1, 2, 3)]
+    for n in range(1, 5000):
+        fsd.fsd_cache_fork_workspace_bytes(50, n)
+        fsd.fsd_beam_workspace_bytes(n, 2, 1000, 3, fsd.BF16)
+    assert len(drafting._bytes) <= 1001
+    assert [fsd.fsd_cache_fork_workspace_bytes(50, n) for n in (1, 2, 3)] == want
