@@ -21,7 +21,8 @@ def _asked_once(call, *key):
     if n is None:   # the library's answer for a shape does not change
         if len(_bytes) > _MOST_KEPT:
             _bytes.clear()
-        n = _bytes[call, key] = int(getattr(library(), call)(*key))
+        fits = all(-0x80000000 <= size <= 0x7FFFFFFF for size in key)   # (another size would arrive there in its place)
+        n = _bytes[call, key] = int(getattr(library(), call)(*key)) if fits else 0
     return n
 
 
