@@ -1,6 +1,9 @@
 """The operators around drafting: the best continuations of beams, the states that follow them, and the pages of the 8-bit cache.
 
 Argument marshalling only, as in operators.py: tensors are checked and handed to the C ABI (`include/fsd.h` has the definitions).
+
+The outputs that a call of fsd_beam_select, fsd_cache_fork or fsd_cache_compact makes are parts of one tensor, with its workspace behind them where that is of 64 KB at
+most: whoever keeps one of them keeps all of that.  A program that keeps the parents of every step, for tracing back, clones them or hands in tensors by `out`.
 """
 from __future__ import annotations
 
@@ -131,7 +134,8 @@ def _select_outputs(B, n):
 
 def fsd_beam_select(logits, scores, n, *, weights=None, done=None, out=None, workspace=None, stream=None):
     """logits [B,beams,V] (rows at any one distance: the front of a padded vocabulary will do), scores float32 [B,beams] (None: 0),
-    weights float32 and done int32 [B,beams] -> dict with scores float32, parent and tokens int32 [B,n], best first, and row_status."""
+    weights float32 and done int32 [B,beams] -> dict with scores float32, parent and tokens int32 [B,n], best first, and row_status (new ones: parts
+    of one tensor, see above)."""
     torch = _torch()
     if logits.dim() != 3:
         raise ValueError("logits have 3 dimensions")
@@ -191,7 +195,7 @@ def _fork_outputs(n, M, P):
 def fsd_cache_fork(cache, parent, refs, *, lengths=None, room=None, out=None, workspace=None, stream=None):
     """parent int32 [n] (rows of the cache's table; -1: none), refs int32 [num_blocks], lengths and room int32 [n] -> dict with block_table
     [n,max_blocks], cache_len [n], refs [num_blocks], free_blocks [1] and row_status [n].  `cache.with_tables(block_table, cache_len)`
-    is the cache of the new sequences."""
+    is the cache of the new sequences.  (New outputs: parts of one tensor, see above.)"""
     torch = _torch()
     dev = cache.device
     _on_current(dev, stream)
@@ -245,7 +249,7 @@ def _compact_outputs(B, M, P):
 
 def fsd_cache_compact(cache, refs, *, out=None, workspace=None, stream=None):
     """refs int32 [num_blocks] -> dict with block_table [B,max_blocks], refs and remap [num_blocks], used_blocks [1] and row_status [B].
-    out=dict(block_table=cache.block_table, refs=refs) works in place."""
+    out=dict(block_table=cache.block_table, refs=refs) works in place.  (New outputs: parts of one tensor, see above.)"""
     torch = _torch()
     dev = cache.device
     _on_current(dev, stream)
