@@ -524,8 +524,11 @@ int fsd_attend_tree(const void* q, const void* k, const void* v, int64_t q_strid
  *   row_status [B]         out  optional: FSD_ROW_NONFINITE where a row that is read holds NaN or +inf, or a beam that counts has
  *                          such a score or a weight that is not positive and finite: the sequence has no continuations then.  (A row that is -inf
  *                          everywhere is none of that: a grammar that has ended a beam.)
- *   workspace              fsd_beam_workspace_bytes(...) bytes, 256-byte aligned; those of some sizes are enough for smaller ones as well
- * No output shares a byte with another one, scores, weights, done or the workspace (FSD_ERR_LAYOUT).
+ *   workspace              fsd_beam_workspace_bytes(...) bytes, 256-byte aligned; those of some sizes are enough for smaller ones as well, of either dtype
+ * No output shares a byte with another one, scores, weights, done or the workspace, and neither an output nor the workspace lies between the first and the last byte of the
+ * logits (FSD_ERR_LAYOUT).
+ * Entries of -inf cost nothing.  Where fewer than n entries of a part of a row lie above many equal ones (a mask of a finite number), the part is gone over 18 more times (FSD_F32: 34):
+ * mask by -inf where that can be chosen.
  * 1 <= beams <= 256, 1 <= n <= 128, 1 <= V <= fsd_max_vocab(dtype), 1 <= B <= 65535.
  */
 size_t fsd_beam_workspace_bytes(int B, int beams, int V, int n, int dtype);

@@ -10,10 +10,12 @@
 //
 // What bounds it (64 x 8 rows of 128256 bfloat16 entries, a tenth of the beams finished, 118 MB: 36 us; reading them alone 18): vector instructions, 11.9
 // an entry, take 21 us of it, the table's reads 14 of the LDS's time beside them; the rest is what a wavefront waits for within a slot (four of them on a SIMD) and each
-// row's end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps.  (Without the sums it took 13 us less, without slots put aside 6,
-// without the making of the table 2; the next slice's first requests before this one's end change nothing.)  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 30 us; the list
+// row's end (bound, list, ranks, about 4 us), which only the other workgroup of the compute unit overlaps, and that is in step with it (512 rows are one a workgroup).
+// (Without the sums it took 13 us less, without slots put aside 6, without the making of the table 2; the next slice's first requests before this one's end change
+// nothing.)  16 x 12 rows of 128259 binary32 entries, n = 60, 98 MB: 30 us; the list
 // of 60 takes as many instructions as the exponentials, and all workgroups begin and end together (exponentials by a table of 512 powers and degree 2, 3 instructions
-// an entry less, change nothing).  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 9 at n = 60: a chain of round trips and barriers.
+// an entry less, change nothing).  Merging: 5 us for one sequence of 4 beams, 6 for 64 of 8, 9 at n = 60: a chain of round trips and barriers.  128 x 8 bfloat16 rows of
+// 32000, without the table: 29.5 us, reading 11.
 #ifndef FSD_CSRC_BEAM_SELECT_H_
 #define FSD_CSRC_BEAM_SELECT_H_
 
@@ -156,7 +158,8 @@ __device__ __forceinline__ bool beam_runs(const BeamParams& P, long at) {   // w
 
 // A slice's n best entries where more than kWaveList of a wavefront's reach the bound that its lanes gave (rows of equal entries, or in order): the n-th largest
 // is found bit by bit, then what is above it and, from the lowest index on, what equals it go into the list.  Returns how many.  (It reads the entries
-// again rather than keep the calling kernel's registers in memory; 40 passes over what the caches hold.)
+// again rather than keep the calling kernel's registers in memory: 16 passes, 32 for binary32, and two more, entry by entry, over what the caches hold.  64 x 8 rows
+// of 128256 bfloat16 entries of which a mask of a finite number leaves 5: the kernel takes 1840 us, unmasked 35, masked by -inf 31; 16 x 12 binary32 rows of 128259, n = 60: 1530, 32, 24.)
 template <bool BF16, int NW>
 __device__ __noinline__ int slice_cut(const char* z, int begin, int end, int n, unsigned long* list, int* lds, int tid) {
     const int wave = tid / 64, lane = tid % 64, len = end - begin;
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(TABLE ? 512 : kWG, 4) beam_slices(const BeamPa
         // One entry (or one beside which the others are nothing) has its sum without an error: what is certain has the beam's score itself, and ties with others that have.
         if (s == exp_within(static_cast<double>(top) - ref)) ref = top, s = 1.0;   // (NaN where there is no entry)
         const bool any_broken = __ballot(broken || !(mine < __builtin_inff())) != 0;
-        // the final bound, made of all four wavefronts' entries
+        // the final bound, made of all wavefronts' entries
         {
             const unsigned bound = wave_bound<BF16>(ordered(mine + 0.0f), q);
             if (lane == 0) {

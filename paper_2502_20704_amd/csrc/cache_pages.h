@@ -5,9 +5,10 @@
 // integer atomics, places of blocks and sequences by sums over what lies in front of them, one kernel behind the other.
 //
 // What bounds it: where many pages move, their bytes (1.21 GB read and written by pages_copy in 240 us, 5.05 TB/s; a large copy reaches 4.9 here); where few do, the
-// launches that follow one another, 3 to 5 us each, and in fork_mark the atomics.  256 sequences of some 40000 tokens in one layer: fork_clear 3.0, fork_mark 10.7,
-// fork_count 4.2, fork_list 5.5, fork_apply 4.5 us with the few copies in it; 128 beams in 16 layers, 140 MB of begun pages: fork_small 9.8, fork_move 22 us.
-// Compacting a pool of 1200 blocks, 540 of them in use, 8 layers: compact_small 9, compact_move 136 us for 623 MB (4.6 TB/s).
+// launches that follow one another, 3 to 5 us each, and in fork_mark the atomics.  256 sequences of some 40000 tokens in one layer: fork_clear 3.0, fork_mark 9.9,
+// fork_count 4.2, fork_list 5.9, fork_apply 4.4 us with the few copies in it; 128 beams in 16 layers, 140 MB of begun pages: fork_small 9.4, fork_move 22 us.
+// Compacting a pool of 1200 blocks, 540 of them in use, 8 layers: compact_small 9, compact_move 136 us for 623 MB (4.6 TB/s); one of 6000 blocks, one layer, 390 MB:
+// compact_count 4.9, compact_list 6.2, compact_apply 83.
 #ifndef FSD_CSRC_CACHE_PAGES_H_
 #define FSD_CSRC_CACHE_PAGES_H_
 
@@ -18,7 +19,7 @@ namespace {
 constexpr int kPagesChunk = 1024;   // blocks, or places, that a workgroup goes over at once
 constexpr int kNobody = 0x7FFFFFFF;
 // What one workgroup does by itself, its blocks' counts in LDS: the launches behind one another take 14 to 17 us on the device and 10 more on the host than
-// one.  One sequence's 4 beams: 5.2 us; 128 beams of 11 places: 8.5; at the limits here as long as the several kernels.
+// one.  One sequence's 4 beams: 5.2 us; 128 beams of 11 places: 9.4; at the limits here as long as the several kernels.
 constexpr int kSmallWG = 1024, kSmallBlocks = 4096, kSmallPlaces = 8192;
 
 // the sum of all threads' v, and of those below

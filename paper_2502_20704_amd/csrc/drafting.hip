@@ -41,8 +41,9 @@ inline bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) %
 // How a row is cut.  Into as many slices as fill the GPU once (four workgroups of four wavefronts a compute unit, what their registers allow), each of several
 // chunks; in a call of few rows into chunks, and these made smaller while compute units are left over.  Long bfloat16 rows (from 65536 entries and 2^23 in all): by
 // the kernel with the table, two workgroups of eight wavefronts a compute unit, the slices so many that these have about equally many.  Whole calls with and
-// without the table, 16 continuations of 8 beams: 8 sequences of 128256 entries 25 and 31 us, 16 30 and 29, 32 35 and 38, 64 (the first of these two
-// kernels) 38 and 51, 128 75 and 90, 12 of 256000 32 and 37; shorter rows lose by it (128 of 32000 41 and 40, 256 66 and 59), as each pays for its beginning and end.
+// without the table, 16 continuations of 8 beams: 8 sequences of 128256 entries 23.3 and 22.6 us, 12 27.8 and 22.8, 16 27.8 and 25.2, 32 30.1 and 35.0, 64 39.6 and 52.3,
+// 128 65.3 and 84.2, 12 of 256000 29.0 and 29.6; shorter rows lose by it (64 of 32000 24.8 and 24.9, 128 37.3 and 34.1, 256 62.2 and 54.8), as each pays for its beginning and end.
+// (Of rows of 128256 entries 96 and 128 are taken by the table's kernel and lose by it; the border pays from about 192 on.)
 struct BeamShape { int slots, len, S; bool table; };
 constexpr long kBeamWGs = 1024, kBeamFew = 512, kTableWGs = 512;
 constexpr int kTableSlots = 2;
@@ -85,7 +86,7 @@ bool beam_shape(int B, int W, int V, int n, int dtype, BeamShape* s) {
     return rows * s->S <= kMaxGroups;
 }
 struct BeamSpace { size_t lists, stat, cand, bytes; };
-// (as much as any call of these or smaller sizes needs: beam_shape makes at most 1535 slices besides one a row, or of a long row min(8, V / 32768))
+// (as much as any call of these or smaller sizes needs, of either type: beam_shape makes at most 1535 slices besides one a row, or of a long bfloat16 row min(8, V / 32768))
 BeamSpace beam_space(int B, int W, int V, int n) {
     Space a;
     BeamSpace w;

@@ -23,3 +23,9 @@ def test_sizes_past_an_int_have_no_workspace():
         assert fsd.fsd_cache_fork_workspace_bytes(50 + off, 4) == fsd.fsd_cache_fork_workspace_bytes(50, 4 + off) == 0
         assert fsd.fsd_cache_compact_workspace_bytes(50 + off) == 0
     assert fsd.fsd_beam_workspace_bytes(2, 3, 1000, 4, fsd.BF16) > 0
+
+
+def test_workspaces_serve_either_type():
+    """a workspace of a call's sizes will do for the other type of logits too"""
+    for sizes in ((1, 1, 1, 1), (64, 8, 128256, 16), (3, 256, 524288, 128), (65535, 1, 70000, 2)):
+        assert fsd.fsd_beam_workspace_bytes(*sizes, fsd.F32) == fsd.fsd_beam_workspace_bytes(*sizes, fsd.BF16) > 0
